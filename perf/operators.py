@@ -188,7 +188,6 @@ def prepare(c, seed):
     if c["kind"] == "append":
         st["k_new"], st["v_new"] = (randn((L, S, c["new"], H, d)) for _ in range(2))
         st["k_out"], st["v_out"] = torch.empty_like(st["k_new"]), torch.empty_like(st["v_new"])
-        st["status2"] = torch.zeros(S, **i32)
     if c["kind"] in ("weigh", "observe", "evict"):
         # eviction: weights fall off like 1 / rank, few tokens hold most, one in ten has none;
         # accumulation: the first steps, when what is added shows
@@ -205,7 +204,7 @@ def prepare(c, seed):
         st["freed"], st["n_freed"] = torch.empty((S, table.shape[1]), **i32), torch.empty(S, **i32)
         if c["cache"] == "q4":
             st["k_out"], st["v_out"] = (torch.empty((L, S, c["keep"], H, d), dtype=dt, device=_DEV) for _ in range(2))
-            st["start"], st["status2"] = torch.zeros_like(st["lens"]), torch.zeros(S, **i32)
+            st["start"] = torch.zeros_like(st["lens"])
     st["max_len"] = int(lens.max()) + c.get("new", 0)
     if own:
         _plan(st)
@@ -246,7 +245,7 @@ def _own_append(st):
     from paper_2607_01237_amd import kara
     cache = (st["kp"], st["vp"], st["ksp"], st["vsp"], st["bt"], st["lens"])
     kara.q4_append(st["p"], st["seqs"], st["k_new"], st["v_new"], *cache, st["status"])
-    kara.q4_read(st["p"], st["seqs"], st["lens0"], st["case"]["new"], *cache, st["k_out"], st["v_out"], st["status2"])
+    kara.q4_read(st["p"], st["seqs"], st["lens0"], st["case"]["new"], *cache, st["k_out"], st["v_out"])
     return dict(k=st["k_out"], v=st["v_out"], lens=st["lens"], status=st["status"])
 
 
@@ -280,7 +279,7 @@ def _own_evict(st):
                       n_freed=st["n_freed"], k_scales=st["ksp"], v_scales=st["vsp"])
     if c["cache"] == "q4":
         kara.q4_read(st["p"], st["seqs"], st["start"], c["keep"], st["kp"], st["vp"], st["ksp"], st["vsp"], st["bt"],
-                     st["lens"], st["k_out"], st["v_out"], st["status2"])
+                     st["lens"], st["k_out"], st["v_out"])
     return _evicted(st)
 
 
