@@ -114,6 +114,28 @@ hipError_t launch_rope(const void* qraw, void* q_out, int n_trig, int W, int Hq,
                        const int32_t* trig, const int32_t* rope_pos0, const int32_t* status, hipStream_t stream);
 hipError_t launch_swiglu(void* gate, const void* up, int64_t n, hipStream_t stream);
 
+// Attention of few query rows over the 4-bit cache, keys split over workgroups
+// (kara_q4.hip).
+struct Q4Split {
+  Geom g;
+  int n, n_layers;
+  int T;                      // queries per sequence, its last T positions
+  int n_rt;                   // tiles of 16 query rows per (layer, sequence, KV head)
+  int split_keys, n_splits, max_len;
+  const int32_t *seqs, *bt, *seq_lens;
+  const void* q;              // [n_layers][n][T][Hq][d]
+  PoolPtrs kp, vp, ksp, vsp;  // codes and scales
+  float* ws;                  // records [n_layers][n][T][Hq][n_splits]: m, l, o[d]
+  void* out;                  // [n_layers][n][T][Hq][d]
+  int out_bf16;
+  float* logits;              // [n_layers][n][Hkv][G][ld] q . k, T = 1
+  int64_t ld;
+};
+// Keys per split for so many units (layers x sequences x KV heads x row tiles).
+int q4_split_keys(int64_t units, int max_len);
+// logits: fill a.logits, and leave records (never out) for every sequence.
+hipError_t launch_q4_split(Q4Split a, bool logits, hipStream_t stream);
+
 }  // namespace kara
 
 // Workspace bytes a call with exactly these arguments uses (n_windows = 1:

@@ -1,0 +1,713 @@
+// The cache held in 4 bits (include/kara_q4.h): quantising append, reading
+// back, and attention of few query rows with the keys split over workgroups.
+#include <algorithm>
+
+#include "kara_append.h"
+#include "kara_q4.h"
+#include "kara_q4_device.h"
+
+namespace kara {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegInf = -__builtin_huge_valf();
+// Lower end of a running maximum: finite, so that a logit of -inf weighs 0.
+constexpr float kMaxFloor = -3.402823466e38f;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------- append
+
+// One workgroup per listed sequence: its status and, if it has nothing but
+// KARA_SEQ_OK, its new length.  The rows follow in a second launch, which
+// counts back from that length.
+__global__ __launch_bounds__(kAppendThreads) void q4_commit_kernel(Geom g, int n, const int32_t* __restrict__ seqs,
+                                                                   int n_new, const int32_t* __restrict__ bt,
+                                                                   int32_t* __restrict__ seq_lens,
+                                                                   int32_t* __restrict__ status) {
+  const int j = blockIdx.x;
+  const int st = append_status(g, n, seqs, n_new, bt, seq_lens, j);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    status[j] = st;
+    if (st == KARA_SEQ_OK) seq_lens[seqs[j]] += n_new;
+  }
+}
+
+constexpr int kQuantUnroll = 4;       // octets per thread
+
+// Eight values to eight codes: a lane holds an octet, four lanes a block.
+// Grid as the append of rows: (sequences x token chunks, layer, K|V).
+template <int DT, int D>
+__global__ __launch_bounds__(kAppendThreads) void q4_append_kernel(
+    Geom g, int n, const int32_t* __restrict__ seqs, int n_new, int toks, int chunks, const char* __restrict__ k_new,
+    const char* __restrict__ v_new, PoolPtrs kp, PoolPtrs vp, PoolPtrs ksp, PoolPtrs vsp,
+    const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens, int32_t* __restrict__ status) {
+  constexpr int kOctets = D / 8;                     // of a row
+  constexpr int kOctetBytes = DT == KARA_BF16 ? 16 : 32;
+  const int j = blockIdx.x / chunks;
+  const int tok0 = (blockIdx.x - j * chunks) * toks;
+  const int l = blockIdx.y;
+  const int kv = blockIdx.z;
+  // (other workgroups may have reported a value that is not finite by now)
+  if (status[j] & ~KARA_SEQ_NONFINITE) return;
+  const int s = seqs[j];
+  const int per_tok = g.Hkv * kOctets;
+  const int count = min(toks, n_new - tok0) * per_tok;
+  const int pos0 = seq_lens[s] - n_new + tok0;
+  const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
+  const char* src = (kv ? v_new : k_new) + (((int64_t)l * n + j) * n_new + tok0) * per_tok * kOctetBytes;
+  uint8_t* codes = (uint8_t*)(kv ? vp.p[l] : kp.p[l]);
+  uint8_t* scales = (uint8_t*)(kv ? vsp.p[l] : ksp.p[l]);
+  bool odd = false;
+  // (count is a multiple of a block's four octets, so the four lanes of a block
+  // stay together)
+  for (int i0 = threadIdx.x; i0 < count; i0 += kAppendThreads * kQuantUnroll) {
+    u32x4 v[kQuantUnroll][kOctetBytes / 16];
+#pragma unroll
+    for (int k = 0; k < kQuantUnroll; ++k) {
+      const int i = i0 + k * kAppendThreads;
+      if (i < count)
+#pragma unroll
+        for (int y = 0; y < kOctetBytes / 16; ++y)
+          v[k][y] = __builtin_nontemporal_load((const u32x4*)(src + (int64_t)i * kOctetBytes) + y);
+    }
+#pragma unroll
+    for (int k = 0; k < kQuantUnroll; ++k) {
+      const int i = i0 + k * kAppendThreads;
+      if (i >= count) continue;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (DT == KARA_BF16)
+          x[e] = __uint_as_float((e & 1) ? v[k][0][e >> 1] & 0xffff0000u : v[k][0][e >> 1] << 16);
+        else
+          x[e] = __uint_as_float(v[k][e >> 2][e & 3]);
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+      if (top >= 0x7f800000u) {
+        odd = true;
+        top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t m = __float_as_uint(x[e]) & 0x7fffffffu;
+          if (m > 0x7f800000u) x[e] = 0.f;
+          if (m < 0x7f800000u) top = max(top, m);
+        }
+      }
+      top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+      const uint32_t byte = q4_scale_byte(top);
+      const float scale = q4_scale(byte);
+      uint32_t c = 0;
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], scale, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], scale, 1);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], scale, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], scale, 3);
+      const int tok = i / per_tok, r = i - tok * per_tok;
+      const int h = r / kOctets, o = r - h * kOctets;
+      const int pos = pos0 + tok, b = pos / g.bs;
+      const int64_t row = ((int64_t)row_pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs);
+      *(uint32_t*)(codes + row * (D / 2) + o * 4) = c;
+      if ((o & 3) == 0) scales[row * (D / kQ4Block) + (o >> 2)] = (uint8_t)byte;
+    }
+  }
+  if (__syncthreads_or(odd) && threadIdx.x == 0) atomicOr(&status[j], KARA_SEQ_NONFINITE);
+}
+
+// ---------------------------------------------------------------- read
+
+// The append's mapping the other way round; rows that are not there are zeros.
+template <int DT, int D>
+__global__ __launch_bounds__(kAppendThreads) void q4_read_kernel(
+    Geom g, int n, const int32_t* __restrict__ seqs, const int32_t* __restrict__ start, int n_rows, int toks, int chunks,
+    PoolPtrs kp, PoolPtrs vp, PoolPtrs ksp, PoolPtrs vsp, const int32_t* __restrict__ bt,
+    const int32_t* __restrict__ seq_lens, char* __restrict__ k_out, char* __restrict__ v_out) {
+  constexpr int kOctets = D / 8;
+  constexpr int kOctetBytes = DT == KARA_BF16 ? 16 : 32;
+  const int j = blockIdx.x / chunks;
+  const int tok0 = (blockIdx.x - j * chunks) * toks;
+  const int l = blockIdx.y;
+  const int kv = blockIdx.z;
+  const int s = seqs[j];
+  const bool listed = s >= 0 && s < g.n_seqs;
+  const int len = listed ? (int)min((int64_t)seq_lens[s], (int64_t)g.max_blocks * g.bs) : 0;
+  const int64_t pos0 = (int64_t)(listed ? start[s] : 0) + tok0;
+  const int32_t* row_pages = bt + (int64_t)(listed ? s : 0) * g.max_blocks;
+  const int per_tok = g.Hkv * kOctets;
+  const int count = min(toks, n_rows - tok0) * per_tok;
+  char* dst = (kv ? v_out : k_out) + (((int64_t)l * n + j) * n_rows + tok0) * per_tok * kOctetBytes;
+  const uint8_t* codes = (const uint8_t*)(kv ? vp.p[l] : kp.p[l]);
+  const uint8_t* scales = (const uint8_t*)(kv ? vsp.p[l] : ksp.p[l]);
+  for (int i0 = threadIdx.x; i0 < count; i0 += kAppendThreads * kQuantUnroll) {
+    uint32_t c[kQuantUnroll], byte[kQuantUnroll];
+#pragma unroll
+    for (int k = 0; k < kQuantUnroll; ++k) {
+      const int i = i0 + k * kAppendThreads;
+      c[k] = 0, byte[k] = 127;
+      if (i < count) {
+        const int tok = i / per_tok, r = i - tok * per_tok;
+        const int h = r / kOctets, o = r - h * kOctets;
+        const int64_t pos = pos0 + tok;
+        if (pos >= 0 && pos < len) {
+          const int b = (int)pos / g.bs;
+          const int page = row_pages[b];
+          if (page >= 0 && page < g.num_pages) {
+            const int64_t row = ((int64_t)page * g.Hkv + h) * g.bs + ((int)pos - b * g.bs);
+            c[k] = *(const uint32_t*)(codes + row * (D / 2) + o * 4);
+            byte[k] = scales[row * (D / kQ4Block) + (o >> 2)];
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kQuantUnroll; ++k) {
+      const int i = i0 + k * kAppendThreads;
+      if (i >= count) continue;
+      const float scale = q4_scale(byte[k]);
+      u32x4* to = (u32x4*)(dst + (int64_t)i * kOctetBytes);
+      if constexpr (DT == KARA_BF16) {
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, q4_octet(c[k], scale)), to);
+      } else {
+        const floatx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 0);
+        const floatx2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 1);
+        const floatx2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 2);
+        const floatx2 f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 3);
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, floatx4{a[0], a[1], b[0], b[1]}), to);
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, floatx4{e[0], e[1], f[0], f[1]}), to + 1);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- attention, keys split
+
+constexpr int kSplitThreads = 256;
+constexpr int kSplitWaves = kSplitThreads / 64;
+constexpr int kSplitMin = 256;       // keys per split, at least (the workspace's records are sized for that)
+constexpr int kSplitMax = 1024;
+constexpr int kSplitBlock = 32;      // keys a wave works on at a time
+constexpr int kSplitWgTarget = 4096; // workgroups a launch keeps when its splits grow
+
+// One workgroup of four waves per (layer, sequence, KV head, tile of 16 query
+// rows, split of split_keys keys): for the tile's rows, the split's maximum m,
+// exponential sum l and unnormalised output o, in log2 units and fp32.  Rows of
+// a (layer, sequence, KV head) run over (query, head in group).
+//
+// The pool rows of the split's keys and their scales go to LDS first; the four
+// waves then take the split's 32-key blocks in turn.  A lane's 16 bytes of codes
+// at d = 128 are one block of 32 values with one scale, which the hardware turns
+// into the four bf16 operands of S^T = K Q^T (keys as the M dimension); a lane so
+// holds four keys of one query per tile, and its weights are the B operand of
+// O^T += V^T P^T as they stand.  V is read as rows, d/16 columns of a key per
+// lane, and the pairs of columns that the conversion gives are put together to
+// pairs of keys by byte permutes.
+//
+// NQ: bf16 terms of a query (1: bf16, exact; 3: fp32, 24 bits); NP: bf16 terms of a
+// weight (1 where the output is bf16; 3 where it is fp32).  K and V are exact in one.
+// LOGITS: q . k of every key goes to `logits` too, [unit][G][ld] (one query each).
+template <int NQ, int NP, int D, bool LOGITS>
+__global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
+  constexpr int KS = D / 32;                 // products per dot product
+  constexpr int E = D / 16;                  // output columns per lane
+  constexpr int kRow = D / 2;                // bytes of a row's codes
+  constexpr int kKW = D / 32;                // a lane's words of a key's codes: an eighth of a row's values per word
+  struct Stage {
+    uint32_t row[kSplitMax], ks[kSplitMax], vs[kSplitMax];
+  };
+  __shared__ __attribute__((aligned(16))) union {
+    Stage st;
+    float o[kSplitWaves][16][D];
+  } lds;
+  __shared__ float red_m[kSplitWaves][16], red_l[kSplitWaves][16];
+  Stage& st = lds.st;
+
+  const Geom& g = a.g;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int gq = lane >> 4, li = lane & 15;
+  const int split = blockIdx.x % a.n_splits;
+  int64_t rest = blockIdx.x / a.n_splits;
+  const int rt = (int)(rest % a.n_rt);
+  rest /= a.n_rt;
+  const int h = (int)(rest % g.Hkv);
+  const int j = (int)((rest / g.Hkv) % a.n);
+  const int l = (int)(rest / ((int64_t)g.Hkv * a.n));
+  const int s = a.seqs[j];
+  const int G = g.G, T = a.T, R = G * T;
+  const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
+  const int k0 = split * a.split_keys;
+  // row r of the unit: output row orow + (r / G) * Hq + r % G
+  const int64_t orow = ((int64_t)l * a.n + j) * T * g.Hq + h * G;
+  const int row0 = rt * 16;
+  const int rows = min(16, R - row0);
+  if (len <= 0 || len > a.max_len || k0 >= len) {
+    // no keys: zero rows where no combine kernel follows
+    if (!LOGITS && a.n_splits == 1)
+      for (int i = tid; i < rows * D; i += kSplitThreads) {
+        const int r = row0 + i / D;
+        const int64_t at = (orow + (int64_t)(r / G) * g.Hq + r % G) * D + i % D;
+        if (a.out_bf16) ((__bf16*)a.out)[at] = (__bf16)0.f;
+        else ((float*)a.out)[at] = 0.f;
+      }
+    return;
+  }
+  const int nk = min(len - k0, a.split_keys);                 // keys of this split
+  const float c = g.scale * kLog2e;
+
+  const int npad = (nk + kSplitBlock - 1) / kSplitBlock * kSplitBlock;
+  {
+    const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
+    // (padding keys of the last block repeat its last key, with no weight)
+    for (int i = tid; i < npad; i += kSplitThreads) {
+      const int pos = k0 + min(i, nk - 1);
+      const int b = pos / g.bs;
+      const int page = min(max(row_pages[b], 0), g.num_pages - 1);
+      const uint32_t row = (uint32_t)(((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs));
+      st.row[i] = row;
+      if constexpr (D == 128) {
+        st.ks[i] = ((const uint32_t*)a.ksp.p[l])[row];
+        st.vs[i] = ((const uint32_t*)a.vsp.p[l])[row];
+      } else {
+        st.ks[i] = ((const uint16_t*)a.ksp.p[l])[row];
+        st.vs[i] = ((const uint16_t*)a.vsp.p[l])[row];
+      }
+    }
+  }
+  // lane (gq, li): values gq*D/4 .. of query row li; its limit: keys of the split it sees
+  bf16x8 qa[NQ][KS];
+  int limit = 0;
+  {
+    const bool there = li < rows;
+    const int r = row0 + (there ? li : 0);
+    const int t = r / G;
+    const int64_t at = (orow + (int64_t)t * g.Hq + (r - t * G)) * D + gq * (D / 4);
+    if (there) limit = min(nk, len - T + t + 1 - k0);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      if constexpr (NQ == 1) {
+        const uint4 v = *(const uint4*)((const __bf16*)a.q + at + x * 8);
+        qa[0][x] = __builtin_bit_cast(bf16x8, there ? v : uint4{0, 0, 0, 0});
+      } else {
+        const floatx4* src = (const floatx4*)((const float*)a.q + at + x * 8);
+        const floatx4 u = src[0], v = src[1];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          __bf16 t3[NQ];
+          bf16_terms(there ? (i < 4 ? u[i & 3] : v[i & 3]) : 0.f, t3);
+#pragma unroll
+          for (int y = 0; y < NQ; ++y) qa[y][x][i] = t3[y];
+        }
+      }
+    }
+  }
+  // the first query row of the tile sees the fewest keys
+  const int limit0 = __builtin_amdgcn_readfirstlane(limit);
+  __syncthreads();
+
+  const char* kbase = (const char*)a.kp.p[l] + gq * (kRow / 4);
+  const char* vbase = (const char*)a.vp.p[l] + li * (E / 2);
+  uint32_t kb[2][2][kKW];        // [buffer][tile][words]
+  uint32_t vb[2][8];             // [buffer][key 16t + 4gq + r at 4t + r]
+  auto load = [&](int blk, int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char* src = kbase + (uint64_t)st.row[blk * kSplitBlock + t * 16 + li] * kRow;
+      if constexpr (D == 128) {
+        const uint4 v = *(const uint4*)src;
+        kb[b][t][0] = v.x, kb[b][t][1] = v.y, kb[b][t][2] = v.z, kb[b][t][3] = v.w;
+      } else {
+        const uint2 v = *(const uint2*)src;
+        kb[b][t][0] = v.x, kb[b][t][1] = v.y;
+      }
+      const uint4 rw = *(const uint4*)&st.row[blk * kSplitBlock + t * 16 + 4 * gq];
+      const uint32_t r4[4] = {rw.x, rw.y, rw.z, rw.w};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const char* vsrc = vbase + (uint64_t)r4[r] * kRow;
+        if constexpr (D == 128) vb[b][4 * t + r] = *(const uint32_t*)vsrc;
+        else vb[b][4 * t + r] = *(const uint16_t*)vsrc;
+      }
+    }
+  };
+
+  float m = kMaxFloor, lsum = 0.f;   // query li's reference, and this lane's part of its sum
+  floatx4 o[E];                      // query li, columns (4gq + r) * E + e
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  float* lrow = nullptr;
+  if constexpr (LOGITS)
+    lrow = a.logits + ((((int64_t)l * a.n + j) * g.Hkv + h) * G + min(li, rows - 1)) * a.ld + k0 + 4 * gq;
+
+  const int nblk = npad / kSplitBlock;
+  auto work = [&](int blk, int b) __attribute__((always_inline)) {
+    floatx4 sv[2];
+    const int kbyte = D == 128 ? gq : gq >> 1;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float scale = q4_scale((st.ks[blk * kSplitBlock + t * 16 + li] >> (8 * kbyte)) & 255u);
+      floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        const bf16x8 ka = q4_octet(kb[b][t][x], scale);
+#pragma unroll
+        for (int y = NQ - 1; y >= 0; --y) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qa[y][x], acc, 0, 0, 0);
+      }
+      sv[t] = acc;
+    }
+    // Wait states between the last product and the first read of its result,
+    // which lies past a branch: the compiler does not count across it (see the
+    // decode attention over rows).  12 cycles per block.
+    asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[0]), "+v"(sv[1]));
+    if constexpr (LOGITS) {
+      if (li < rows)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) *(floatx4*)(lrow + blk * kSplitBlock + t * 16) = sv[t];
+    }
+    if (blk * kSplitBlock + kSplitBlock > limit0) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (blk * kSplitBlock + t * 16 + 4 * gq + r >= limit) sv[t][r] = kNegInf;
+    }
+    float mx = sv[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sv[t][r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
+    // the reference m is raised only past a headroom of 2^8
+    if (__ballot(mx > m + 8.f) != 0ull) {
+      const float mn = fmaxf(m, mx);
+      const float f = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      lsum *= f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= f;
+    }
+    bf16x8 pb[NP];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sv[t][r], c, -m));
+        __bf16 pt[NP];
+        bf16_terms(p, pt);
+        // (one term: the sum is of the rounded weights, as the output is)
+        lsum += NP == 1 ? (float)pt[0] : p;
+#pragma unroll
+        for (int y = 0; y < NP; ++y) pb[y][4 * t + r] = pt[y];
+      }
+    // V: pairs of columns of a key to pairs of keys of a column
+    uint32_t pv[8][E / 2];
+    const int vshift = 8 * (D == 128 ? li >> 2 : li >> 3);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint4 sc = *(const uint4*)&st.vs[blk * kSplitBlock + t * 16 + 4 * gq];
+      const uint32_t s4[4] = {sc.x, sc.y, sc.z, sc.w};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float scale = q4_scale((s4[r] >> vshift) & 255u);
+        pv[4 * t + r][0] = q4_pair<0>(vb[b][4 * t + r], scale);
+        pv[4 * t + r][1] = q4_pair<1>(vb[b][4 * t + r], scale);
+        if constexpr (E == 8) {
+          pv[4 * t + r][2] = q4_pair<2>(vb[b][4 * t + r], scale);
+          pv[4 * t + r][3] = q4_pair<3>(vb[b][4 * t + r], scale);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+      const uint4 va = {__builtin_amdgcn_perm(pv[1][e >> 1], pv[0][e >> 1], sel),
+                        __builtin_amdgcn_perm(pv[3][e >> 1], pv[2][e >> 1], sel),
+                        __builtin_amdgcn_perm(pv[5][e >> 1], pv[4][e >> 1], sel),
+                        __builtin_amdgcn_perm(pv[7][e >> 1], pv[6][e >> 1], sel)};
+#pragma unroll
+      for (int y = NP - 1; y >= 0; --y)
+        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[y], o[e], 0, 0, 0);
+    }
+  };
+  if (wave < nblk) {
+    load(wave, 0);
+    int blk = wave;
+    for (;;) {
+      const int n1 = blk + kSplitWaves;
+      if (n1 < nblk) load(n1, 1);
+      work(blk, 0);
+      if (n1 >= nblk) break;
+      blk = n1 + kSplitWaves;
+      if (blk < nblk) load(blk, 0);
+      work(n1, 1);
+      if (blk >= nblk) break;
+    }
+  }
+
+  // ---- the four waves' sums ----
+  asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[E - 1]));   // (as above, past the loop's branch)
+  lsum += __shfl_xor(lsum, 16, 64);
+  lsum += __shfl_xor(lsum, 32, 64);
+  if (gq == 0) {
+    red_m[wave][li] = m;
+    red_l[wave][li] = lsum;
+  }
+  __syncthreads();   // the staged rows and scales are no longer read
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+      *(floatx4*)&lds.o[wave][li][(4 * gq + r) * E + e] = floatx4{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]};
+  __syncthreads();
+  const int nw = min(nblk, kSplitWaves);   // waves that had keys
+  const bool direct = !LOGITS && len <= a.split_keys;
+  for (int x = tid; x < rows * D; x += kSplitThreads) {
+    const int i = x / D, e = x - i * D;
+    float M = red_m[0][i];
+    for (int w = 1; w < nw; ++w) M = fmaxf(M, red_m[w][i]);
+    float L = 0.f, O = 0.f;
+    for (int w = 0; w < nw; ++w) {
+      const float f = __builtin_amdgcn_exp2f(red_m[w][i] - M);
+      L += red_l[w][i] * f;
+      O += lds.o[w][i][e] * f;
+    }
+    const int r = row0 + i;
+    const int64_t at = orow + (int64_t)(r / G) * g.Hq + r % G;
+    if (direct) {
+      const float v = L == 0.f ? 0.f : O / L;   // (a row that sees no key)
+      if (a.out_bf16) ((__bf16*)a.out)[at * D + e] = (__bf16)v;
+      else ((float*)a.out)[at * D + e] = v;
+    } else {
+      float* rec = a.ws + (at * a.n_splits + split) * (D + 2);
+      if (e == 0) rec[0] = M, rec[1] = L;
+      rec[2 + e] = O;
+    }
+  }
+}
+
+// One wave per output row of a sequence longer than one split: its splits'
+// records joined.
+template <int D>
+__global__ __launch_bounds__(256) void q4_combine_kernel(Geom g, int n, int T, const int32_t* __restrict__ seqs,
+                                                         const int32_t* __restrict__ seq_lens, int max_len,
+                                                         int split_keys, int n_splits, int64_t n_rows,
+                                                         const float* __restrict__ ws, void* __restrict__ out,
+                                                         int out_bf16) {
+  constexpr int kDPerLane = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);   // (l, j, t, hq)
+  if (row >= n_rows) return;
+  const int s = seqs[(row / ((int64_t)g.Hq * T)) % n];
+  const int len = s >= 0 && s < g.n_seqs ? seq_lens[s] : 0;
+  const bool none = len <= 0 || len > max_len;
+  if (!none && len <= split_keys) return;   // the split kernel wrote it
+  float L = 0.f, acc[kDPerLane] = {};
+  if (!none) {
+    const int ns = (len + split_keys - 1) / split_keys;
+    constexpr int rec = D + 2;
+    const float* w = ws + row * n_splits * rec;
+    float M = kMaxFloor;
+    for (int sp = lane; sp < ns; sp += 64) M = fmaxf(M, w[sp * rec]);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+    for (int sp = 0; sp < ns; ++sp) {
+      const float f = __builtin_amdgcn_exp2f(w[sp * rec] - M);
+      L += w[sp * rec + 1] * f;
+#pragma unroll
+      for (int e = 0; e < kDPerLane; ++e) acc[e] += w[sp * rec + 2 + lane * kDPerLane + e] * f;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kDPerLane; ++e) {
+    const float v = L == 0.f ? 0.f : acc[e] / L;   // (a row that sees no key)
+    if (out_bf16) ((__bf16*)out)[row * D + lane * kDPerLane + e] = (__bf16)v;
+    else ((float*)out)[row * D + lane * kDPerLane + e] = v;
+  }
+}
+
+// Keys per split: 256 while the launch has few workgroups, up to 1024 where 16
+// per CU remain: fewer records and prologues.
+int split_keys_of(int64_t units, int max_len) {
+  int keys = kSplitMin;
+  while (keys < kSplitMax && units * ((max_len + 2 * keys - 1) / (2 * keys)) >= kSplitWgTarget) keys *= 2;
+  return keys;
+}
+
+// a grid of one dimension: HIP counts its threads in 32 bits
+bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
+
+bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && n_layers <= kMaxLayersPerLaunch; }
+
+PoolPtrs ptrs(const void* const* pools, int n_layers) {
+  PoolPtrs x{};
+  for (int i = 0; i < n_layers; ++i) x.p[i] = const_cast<void*>(pools[i]);
+  return x;
+}
+
+}  // namespace
+
+hipError_t launch_q4_split(Q4Split a, bool logits, hipStream_t stream) {
+  const Geom& g = a.g;
+  const int64_t blocks = (int64_t)a.n_layers * a.n * g.Hkv * a.n_rt * a.n_splits;
+  const dim3 grid((unsigned)blocks), block(kSplitThreads);
+  const bool f32 = g.dtype == KARA_F32;
+#define KARA_Q4_SPLIT(NQ, NP, LG)                                                                   \
+  do {                                                                                              \
+    if (g.d == 128) hipLaunchKernelGGL((q4_split_kernel<NQ, NP, 128, LG>), grid, block, 0, stream, a); \
+    else hipLaunchKernelGGL((q4_split_kernel<NQ, NP, 64, LG>), grid, block, 0, stream, a);          \
+  } while (0)
+  if (logits) {
+    if (f32) KARA_Q4_SPLIT(3, 3, true);
+    else KARA_Q4_SPLIT(1, 3, true);
+  } else {
+    if (f32) KARA_Q4_SPLIT(3, 3, false);
+    else KARA_Q4_SPLIT(1, 1, false);
+  }
+#undef KARA_Q4_SPLIT
+  return hipGetLastError();
+}
+
+int q4_split_keys(int64_t units, int max_len) { return split_keys_of(units, max_len); }
+
+}  // namespace kara
+
+using namespace kara;
+
+extern "C" {
+
+kara_status_t kara_q4_append(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_new, int32_t n_layers,
+                             const void* k_new, const void* v_new, void* const* k_pools, void* const* v_pools,
+                             void* const* k_scales, void* const* v_scales, const int32_t* block_table,
+                             int32_t* seq_lens, int32_t* status, void* stream) {
+  Geom g;
+  const kara_status_t st = make_geom(p, n, &g);
+  if (st != KARA_OK) return st;
+  if (!layers_ok(n, n_layers) || n_new < 0) return KARA_ERR_INVALID_ARG;
+  if (n == 0 || n_new == 0) return KARA_OK;
+  if (!seqs || !k_new || !v_new || !block_table || !seq_lens || !status || !pools_ok(k_pools, n_layers) ||
+      !pools_ok(v_pools, n_layers) || !pools_ok(k_scales, n_layers) || !pools_ok(v_scales, n_layers))
+    return KARA_ERR_INVALID_ARG;
+  hipStream_t s = (hipStream_t)stream;
+  const int per_tok = g.Hkv * (g.d / 8);
+  const int toks = std::min(n_new, std::max(1, 2 * kAppendThreads * kQuantUnroll / per_tok));
+  const int64_t chunks = ((int64_t)n_new + toks - 1) / toks;
+  if (!grid_ok(n * chunks) || (int64_t)toks * per_tok > INT32_MAX / 2) return KARA_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)(n * chunks), (unsigned)n_layers, 2), block(kAppendThreads);
+  hipLaunchKernelGGL(q4_commit_kernel, dim3((unsigned)n), block, 0, s, g, n, seqs, n_new, block_table, seq_lens, status);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_status(e);
+#define KARA_Q4_APPEND(DT, D)                                                                                       \
+  hipLaunchKernelGGL((q4_append_kernel<DT, D>), grid, block, 0, s, g, n, seqs, n_new, toks, (int)chunks,            \
+                     (const char*)k_new, (const char*)v_new, ptrs(k_pools, n_layers), ptrs(v_pools, n_layers),      \
+                     ptrs(k_scales, n_layers), ptrs(v_scales, n_layers), block_table, (const int32_t*)seq_lens, status)
+  if (g.dtype == KARA_BF16) {
+    if (g.d == 128) KARA_Q4_APPEND(KARA_BF16, 128);
+    else KARA_Q4_APPEND(KARA_BF16, 64);
+  } else {
+    if (g.d == 128) KARA_Q4_APPEND(KARA_F32, 128);
+    else KARA_Q4_APPEND(KARA_F32, 64);
+  }
+#undef KARA_Q4_APPEND
+  return hip_status(hipGetLastError());
+}
+
+kara_status_t kara_q4_read(const kara_params_t* p, int32_t n, const int32_t* seqs, const int32_t* start, int32_t n_rows,
+                           int32_t n_layers, const void* const* k_pools, const void* const* v_pools,
+                           const void* const* k_scales, const void* const* v_scales, const int32_t* block_table,
+                           const int32_t* seq_lens, void* k_out, void* v_out, void* stream) {
+  Geom g;
+  const kara_status_t st = make_geom(p, n, &g);
+  if (st != KARA_OK) return st;
+  if (!layers_ok(n, n_layers) || n_rows < 0) return KARA_ERR_INVALID_ARG;
+  if (n == 0 || n_rows == 0) return KARA_OK;
+  if (!seqs || !start || !k_out || !v_out || !block_table || !seq_lens || !pools_ok(k_pools, n_layers) ||
+      !pools_ok(v_pools, n_layers) || !pools_ok(k_scales, n_layers) || !pools_ok(v_scales, n_layers))
+    return KARA_ERR_INVALID_ARG;
+  const int per_tok = g.Hkv * (g.d / 8);
+  const int toks = std::min(n_rows, std::max(1, 2 * kAppendThreads * kQuantUnroll / per_tok));
+  const int64_t chunks = ((int64_t)n_rows + toks - 1) / toks;
+  if (!grid_ok(n * chunks) || (int64_t)toks * per_tok > INT32_MAX / 2) return KARA_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)(n * chunks), (unsigned)n_layers, 2), block(kAppendThreads);
+#define KARA_Q4_READ(DT, D)                                                                                        \
+  hipLaunchKernelGGL((q4_read_kernel<DT, D>), grid, block, 0, (hipStream_t)stream, g, n, seqs, start, n_rows, toks, \
+                     (int)chunks, ptrs(k_pools, n_layers), ptrs(v_pools, n_layers), ptrs(k_scales, n_layers),      \
+                     ptrs(v_scales, n_layers), block_table, seq_lens, (char*)k_out, (char*)v_out)
+  if (g.dtype == KARA_BF16) {
+    if (g.d == 128) KARA_Q4_READ(KARA_BF16, 128);
+    else KARA_Q4_READ(KARA_BF16, 64);
+  } else {
+    if (g.d == 128) KARA_Q4_READ(KARA_F32, 128);
+    else KARA_Q4_READ(KARA_F32, 64);
+  }
+#undef KARA_Q4_READ
+  return hip_status(hipGetLastError());
+}
+
+kara_status_t kara_q4_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers, int32_t n_query,
+                                               int32_t max_len, size_t* bytes) {
+  Geom g;
+  const kara_status_t st = make_geom(p, n, &g);
+  if (st != KARA_OK) return st;
+  if (!bytes || !layers_ok(n, n_layers) || n_query < 1 || max_len < 1 || (int64_t)max_len > (int64_t)g.max_blocks * g.bs ||
+      (int64_t)n_query * g.Hq > INT32_MAX / 4)
+    return KARA_ERR_INVALID_ARG;
+  const int64_t n_splits = (max_len + kSplitMin - 1) / kSplitMin;
+  *bytes = n_splits == 1 ? 0 : (size_t)n_layers * n * n_query * g.Hq * n_splits * (g.d + 2) * sizeof(float);
+  return KARA_OK;
+}
+
+kara_status_t kara_q4_attention(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,
+                                int32_t n_query, const void* q, const void* const* k_pools, const void* const* v_pools,
+                                const void* const* k_scales, const void* const* v_scales, const int32_t* block_table,
+                                const int32_t* seq_lens, int32_t max_len, void* out, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  kara_status_t st = kara_q4_attention_workspace_size(p, n, n_layers, n_query, max_len, &need);
+  if (st != KARA_OK) return st;
+  if (n == 0) return KARA_OK;
+  if (!seqs || !q || !block_table || !seq_lens || !out || !pools_ok(k_pools, n_layers) || !pools_ok(v_pools, n_layers) ||
+      !pools_ok(k_scales, n_layers) || !pools_ok(v_scales, n_layers))
+    return KARA_ERR_INVALID_ARG;
+  if (need && (!workspace || workspace_bytes < need)) return KARA_ERR_WORKSPACE;
+  Q4Split a{};
+  st = make_geom(p, n, &a.g);
+  if (st != KARA_OK) return st;
+  const Geom& g = a.g;
+  a.n = n;
+  a.n_layers = n_layers;
+  a.T = n_query;
+  a.n_rt = (int)(((int64_t)g.G * n_query + 15) / 16);
+  const int64_t units = (int64_t)n_layers * n * g.Hkv * a.n_rt;
+  a.split_keys = split_keys_of(units, max_len);
+  a.n_splits = (max_len + a.split_keys - 1) / a.split_keys;
+  const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
+  if (!grid_ok(units * a.n_splits) || !grid_ok((rows + 3) / 4)) return KARA_ERR_UNSUPPORTED;
+  a.max_len = max_len;
+  a.seqs = seqs;
+  a.bt = block_table;
+  a.seq_lens = seq_lens;
+  a.q = q;
+  a.kp = ptrs(k_pools, n_layers);
+  a.vp = ptrs(v_pools, n_layers);
+  a.ksp = ptrs(k_scales, n_layers);
+  a.vsp = ptrs(v_scales, n_layers);
+  a.ws = (float*)workspace;
+  a.out = out;
+  a.out_bf16 = g.dtype == KARA_BF16;
+  hipError_t e = launch_q4_split(a, false, (hipStream_t)stream);
+  if (e != hipSuccess || a.n_splits == 1) return hip_status(e);
+  const dim3 grid((unsigned)((rows + 3) / 4));
+  if (g.d == 128)
+    hipLaunchKernelGGL((q4_combine_kernel<128>), grid, dim3(256), 0, (hipStream_t)stream, g, n, n_query, seqs, seq_lens,
+                       max_len, a.split_keys, a.n_splits, rows, (const float*)a.ws, out, (int)a.out_bf16);
+  else
+    hipLaunchKernelGGL((q4_combine_kernel<64>), grid, dim3(256), 0, (hipStream_t)stream, g, n, n_query, seqs, seq_lens,
+                       max_len, a.split_keys, a.n_splits, rows, (const float*)a.ws, out, (int)a.out_bf16);
+  return hip_status(hipGetLastError());
+}
+
+}  // extern "C"

@@ -1,0 +1,53 @@
+// Device side of the 4-bit cache's format (include/kara_q4.h): blocks of 32
+// e2m1 codes with one power-of-two scale, which gfx950 converts in hardware.
+#pragma once
+
+#include "kara_internal.h"
+
+namespace kara {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+constexpr int kQ4Block = 32;
+
+// 2^(byte - 127), the factor that scale byte 1..254 stands for
+__device__ __forceinline__ float q4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Scale byte of a block whose largest magnitude has the fp32 bits `top`
+// (finite): adding 0x1fffff carries into the exponent past a mantissa of 1.75,
+// that is past 7 units of the scale two binades below.
+__device__ __forceinline__ uint32_t q4_scale_byte(uint32_t top) {
+  const int e = (int)((top + 0x1fffffu) >> 23) - 129;
+  return (uint32_t)(min(max(e, -125), 125) + 127);
+}
+
+// The pair of values in byte B of `codes`, as two bf16 (exact)
+template <int B>
+__device__ __forceinline__ uint32_t q4_pair(uint32_t codes, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, B));
+}
+
+// The eight values of `codes`, in order
+__device__ __forceinline__ bf16x8 q4_octet(uint32_t codes, float scale) {
+  const uint4 v = {q4_pair<0>(codes, scale), q4_pair<1>(codes, scale), q4_pair<2>(codes, scale),
+                   q4_pair<3>(codes, scale)};
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// x as the sum of NT bf16 values, each the rounding of what the ones before
+// leave: 8, 16 or 24 bits of x
+template <int NT>
+__device__ __forceinline__ void bf16_terms(float x, __bf16 (&t)[NT]) {
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    t[i] = (__bf16)x;
+    x -= (float)t[i];
+  }
+}
+
+}  // namespace
+}  // namespace kara

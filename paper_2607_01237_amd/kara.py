@@ -19,12 +19,16 @@ LIB_PATH = os.environ.get("KARA_LIBRARY") or os.path.join(_PKG, "libkara.so")
 HEADERS = [os.path.join(os.path.dirname(_PKG), "include", h)
            for h in ("kara.h", "kara_harness.h", "kara_sched.h", "kara_recompute.h")]
 
+# the operators beside the step: the cache in 4 bits, eviction by accumulated weight
+OPERATOR_HEADERS = [os.path.join(os.path.dirname(_PKG), "include", h) for h in ("kara_q4.h", "kara_evict.h")]
+
 BF16, F32 = 0, 1
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_SCHED_MISMATCH, ERR_SCHED_NOMEM = 0, -1, -2, -3, -4, -5, -6
 ERR_SCRATCH_LIMIT = -7
 NOALLOC_SCRATCH_BYTES = 64 << 20      # KARA_NOALLOC_SCRATCH_BYTES
 SEQ_OK, SEQ_BAD_WINDOW, SEQ_BAD_PAGE, SEQ_DUP_TRIGGER, SEQ_BAD_INDEX, SEQ_BAD_KEPT, SEQ_DUP_PAGE = \
     0, 1, 2, 4, 8, 16, 32
+SEQ_NONFINITE = 64                    # kara_q4_append: a report, the sequence was appended
 MAX_COMPRESSIBLE = 4096
 REQ_WAITING, REQ_RUNNING, REQ_FINISHED = 0, 1, 2
 
@@ -140,6 +144,11 @@ _SIGS = {
                                              ctypes.POINTER(ctypes.c_size_t)]),
     "kara_recompute_queries": (_I32, [_PAR, ctypes.POINTER(KaraModel), _I32, _VP, _I32, ctypes.POINTER(LayerWeights),
                                       _VP, _VP, _PP, _PP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]),
+    "kara_q4_append": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _VP, _PP, _PP, _PP, _PP, _VP, _VP, _VP, _VP]),
+    "kara_q4_read": (_I32, [_PAR, _I32, _VP, _VP, _I32, _I32, _PP, _PP, _PP, _PP, _VP, _VP, _VP, _VP, _VP]),
+    "kara_q4_attention_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
+    "kara_q4_attention": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _PP, _PP, _PP, _PP, _VP, _VP, _I32, _VP, _VP,
+                                 ctypes.c_size_t, _VP]),
     "kara_sched_create": (_I32, [ctypes.POINTER(SchedConfig), _P32, ctypes.POINTER(ctypes.c_void_p)]),
     "kara_sched_destroy": (_I32, [_VP]),
     "kara_sched_submit": (_I32, [_VP, _I32, _I32, _P64]),
@@ -154,10 +163,10 @@ _SIGS = {
 _lib = None
 
 
-def header_functions() -> list[str]:
-    """Names of the functions include/kara.h and include/kara_harness.h declare."""
+def header_functions(headers=None) -> list[str]:
+    """Names of the functions that HEADERS (or the given headers) declare."""
     names = set()
-    for h in HEADERS:
+    for h in headers or HEADERS:
         names |= set(re.findall(r"^\S.*?\b(kara_\w+)\s*\(", open(h).read(), flags=re.M))
     return sorted(names)
 
@@ -500,6 +509,111 @@ def recompute_queries(p, m: KaraModel, trig, weights, hidden_in, hidden_out, k_p
         _ptr_array(k_pools), _ptr_array(v_pools), _ptr(block_table), _ptr(seq_lens), _ptr(win_start),
         _ptr(rope_pos0), _ptr(q_out), _ptr(status), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+# ---- the cache held in 4 bits (include/kara_q4.h)
+
+def _launch(stream):
+    """Current device and the stream's handle, which must be of that device:
+    the library launches where the process stands."""
+    import torch
+    dev = torch._C._cuda_getDevice()
+    if stream is None:
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise KaraError("marshal", ERR_INVALID_ARG, f"stream of device {stream.device_index}, current device {dev}")
+    return dev, stream.cuda_stream
+
+
+def _on(dev, t):
+    """Pointer of a contiguous tensor on the current device (None: NULL)."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise KaraError("marshal", ERR_INVALID_ARG, f"tensor on {t.device}, current device cuda:{dev}")
+    if not t.is_contiguous():
+        raise KaraError("marshal", ERR_INVALID_ARG, "tensor is not contiguous")
+    return t.data_ptr()
+
+
+def _array_on(dev, tensors):
+    return (ctypes.c_void_p * len(tensors))(*[_on(dev, t) for t in tensors]) if tensors is not None else None
+
+
+def _q4_pools(p, L, **pools):
+    """Codes (k_pools, v_pools) and scales (k_scales, v_scales) of L layers."""
+    import torch
+    rows = p.num_pages * p.n_kv_heads * p.block_size
+    for name, ts in pools.items():
+        n = rows * p.head_dim // (32 if name.endswith("scales") else 2)
+        if len(ts) != L:
+            raise KaraError("marshal", ERR_INVALID_ARG, f"{name}: {len(ts)} layers, expected {L}")
+        for i, t in enumerate(ts):
+            if t is None or t.dtype != torch.uint8 or t.numel() < n:
+                if t is None:
+                    raise KaraError("marshal", ERR_INVALID_ARG, f"{name}[{i}]: missing")
+                _need(f"{name}[{i}]", t, n, torch.uint8)
+
+
+def _nbytes(workspace):
+    return workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def q4_append(p, seqs, k_new, v_new, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, status, stream=None):
+    """Quantises k_new / v_new [n_layers][n][n_new][Hkv][d] and appends them after each listed sequence's tokens."""
+    n, L = seqs.numel(), len(k_pools)
+    n_new = k_new.shape[2]
+    _need("seqs", seqs, 0, _i32())
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        _need(name, t, L * n * n_new * p.n_kv_heads * p.head_dim, _dt(p))
+    _q4_pools(p, L, k_pools=k_pools, v_pools=v_pools, k_scales=k_scales, v_scales=v_scales)
+    _tables(p, block_table, seq_lens)
+    _need("status", status, n, _i32())
+    dev, s = _launch(stream)
+    _check("kara_q4_append", load().kara_q4_append(
+        ctypes.byref(p), n, _on(dev, seqs), n_new, L, _on(dev, k_new), _on(dev, v_new), _array_on(dev, k_pools),
+        _array_on(dev, v_pools), _array_on(dev, k_scales), _array_on(dev, v_scales), _on(dev, block_table),
+        _on(dev, seq_lens), _on(dev, status), s))
+
+
+def q4_read(p, seqs, start, n_rows, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, k_out, v_out,
+            stream=None):
+    """Rows [start[s], start[s] + n_rows) of each listed sequence into k_out / v_out [n_layers][n][n_rows][Hkv][d]."""
+    n, L, n_rows = seqs.numel(), len(k_pools), int(n_rows)
+    _need("seqs", seqs, 0, _i32())
+    _need("start", start, p.n_seqs, _i32())
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        _need(name, t, L * n * n_rows * p.n_kv_heads * p.head_dim, _dt(p))
+    _q4_pools(p, L, k_pools=k_pools, v_pools=v_pools, k_scales=k_scales, v_scales=v_scales)
+    _tables(p, block_table, seq_lens)
+    dev, s = _launch(stream)
+    _check("kara_q4_read", load().kara_q4_read(
+        ctypes.byref(p), n, _on(dev, seqs), _on(dev, start), n_rows, L, _array_on(dev, k_pools),
+        _array_on(dev, v_pools), _array_on(dev, k_scales), _array_on(dev, v_scales), _on(dev, block_table),
+        _on(dev, seq_lens), _on(dev, k_out), _on(dev, v_out), s))
+
+
+def q4_attention_workspace_size(p, n, n_layers, n_query, max_len) -> int:
+    out = ctypes.c_size_t(0)
+    _check("kara_q4_attention_workspace_size", load().kara_q4_attention_workspace_size(
+        ctypes.byref(p), n, n_layers, n_query, max_len, ctypes.byref(out)))
+    return int(out.value)
+
+
+def q4_attention(p, seqs, n_query, q, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, max_len, out,
+                 workspace, stream=None):
+    """Causal attention of each listed sequence's last n_query tokens; q, out [n_layers][n][n_query][Hq][d]."""
+    n, L, n_query = seqs.numel(), len(k_pools), int(n_query)
+    _need("seqs", seqs, 0, _i32())
+    for name, t in (("q", q), ("out", out)):
+        _need(name, t, L * n * n_query * p.n_q_heads * p.head_dim, _dt(p))
+    _q4_pools(p, L, k_pools=k_pools, v_pools=v_pools, k_scales=k_scales, v_scales=v_scales)
+    _tables(p, block_table, seq_lens)
+    dev, s = _launch(stream)
+    _check("kara_q4_attention", load().kara_q4_attention(
+        ctypes.byref(p), n, _on(dev, seqs), L, n_query, _on(dev, q), _array_on(dev, k_pools), _array_on(dev, v_pools),
+        _array_on(dev, k_scales), _array_on(dev, v_scales), _on(dev, block_table), _on(dev, seq_lens), int(max_len),
+        _on(dev, out), _on(dev, workspace), _nbytes(workspace), s))
 
 
 # ---- periodic compression policy (include/kara_sched.h): host runtime
