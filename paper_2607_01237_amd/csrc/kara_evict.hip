@@ -1,0 +1,574 @@
+// Eviction by accumulated attention weight (include/kara_evict.h): decoding
+// attention that counts each key's weight, selection by those counts, and the
+// cut of the cache in place.
+#include <algorithm>
+
+#include "kara_evict.h"
+#include "kara_harness.h"
+#include "kara_internal.h"
+#include "kara_page_check.h"
+
+namespace kara {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kMaxFloor = -3.402823466e38f;
+constexpr int kMaxGroup = KARA_HARNESS_MAX_GROUP;
+
+bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
+size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+struct WeightPtrs {
+  float* p[kMaxLayersPerLaunch];
+};
+
+// ---------------------------------------------------------------- attention that counts
+
+constexpr int kFinThreads = 256;
+constexpr int kFinKeys = 4 * kFinThreads;   // keys per workgroup
+
+// Second half of a counting decoding step: the splits' records joined to the
+// output, and every key's weight -- exp2(logit - M) / L over the group's query
+// heads -- added to its accumulator.  One workgroup per (layer, sequence, KV
+// head, 1024 keys); a sequence's workgroups share out its query heads' outputs.
+template <int D>
+__global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
+    Geom g, int n, const int32_t* __restrict__ seqs, const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens,
+    int n_new, int max_len, int split_keys, int n_splits, int chunks, const float* __restrict__ records,
+    const float* __restrict__ logits, int64_t ld, WeightPtrs wp, float* __restrict__ out) {
+  __shared__ float red_m[kMaxGroup], red_i[kMaxGroup];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int chunk = blockIdx.x % chunks;
+  const int64_t rest = blockIdx.x / chunks;
+  const int h = (int)(rest % g.Hkv);
+  const int j = (int)((rest / g.Hkv) % n);
+  const int l = (int)(rest / ((int64_t)g.Hkv * n));
+  const int s = seqs[j], G = g.G;
+  const int64_t orow = ((int64_t)l * n + j) * g.Hq + h * G;
+  const int len = s >= 0 && s < g.n_seqs ? seq_lens[s] : 0;
+  if (len <= 0 || len > max_len) {
+    if (chunk == 0)
+      for (int i = tid; i < G * D; i += kFinThreads) out[orow * D + i] = 0.f;
+    return;
+  }
+  const int k0 = chunk * kFinKeys;
+  if (k0 >= len) return;
+  constexpr int rec = D + 2;
+  const int ns = (len + split_keys - 1) / split_keys;
+  const int nc = (len + kFinKeys - 1) / kFinKeys;      // this sequence's workgroups
+  int dup = 0;
+  for (int o = tid; o < j; o += kFinThreads) dup |= seqs[o] == s;
+  for (int i = wave; i < G; i += kFinThreads / 64) {
+    const float* w = records + (orow + i) * n_splits * rec;
+    float M = kMaxFloor, L = 0.f;
+    for (int sp = lane; sp < ns; sp += 64) M = fmaxf(M, w[(int64_t)sp * rec]);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+    for (int sp = lane; sp < ns; sp += 64) L += w[(int64_t)sp * rec + 1] * __builtin_amdgcn_exp2f(w[(int64_t)sp * rec] - M);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) L += __shfl_xor(L, x, 64);
+    if (lane == 0) red_m[i] = M, red_i[i] = 1.f / L;
+  }
+  dup = __syncthreads_or(dup);
+  for (int i = chunk; i < G; i += nc) {
+    const float* w = records + (orow + i) * n_splits * rec;
+    for (int e = tid; e < D; e += kFinThreads) {
+      float acc = 0.f;
+      for (int sp = 0; sp < ns; ++sp)
+        acc += w[(int64_t)sp * rec + 2 + e] * __builtin_amdgcn_exp2f(w[(int64_t)sp * rec] - red_m[i]);
+      out[(orow + i) * D + e] = acc * red_i[i];
+    }
+  }
+  if (dup) return;        // an earlier listing counts
+  const float c = g.scale * kLog2e;
+  const int k = k0 + 4 * tid;
+  if (k >= len) return;
+  float add[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < G; ++i) {
+    const floatx4 x = *(const floatx4*)(logits + (orow + i) * ld + k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) add[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[e], c, -red_m[i])), red_i[i], add[e]);
+  }
+  const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int pos = k + e;
+    if (pos >= len) break;
+    const int b = pos / g.bs;
+    const int page = row_pages[b];
+    if (page < 0 || page >= g.num_pages) continue;
+    float* to = wp.p[l] + ((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs);
+    *to = pos >= len - n_new ? add[e] : *to + add[e];
+  }
+}
+
+// ---------------------------------------------------------------- the cut
+
+struct EvictArgs {
+  Geom g;
+  int n, n_layers, keep, n_sink, n_recent, max_len;
+  const int32_t* seqs;
+  int32_t *bt, *seq_lens, *kept, *status;
+  PoolPtrs k, v, ks, vs;      // rows or codes; scales (null: rows)
+  WeightPtrs w;
+  int row_bytes;              // of k and v
+  int scale_bytes;            // of ks and vs; 0: none
+};
+
+__global__ __launch_bounds__(kValidateThreads) void evict_validate_kernel(EvictArgs a) {
+  __shared__ uint32_t lds[kValidateLds];
+  const Geom& g = a.g;
+  const int j = blockIdx.x, tid = threadIdx.x;
+  const int s = a.seqs[j];
+  if (s < 0 || s >= g.n_seqs) {
+    if (tid == 0) a.status[j] = KARA_SEQ_BAD_INDEX;
+    return;
+  }
+  int dup = 0;
+  for (int o = tid; o < a.n; o += kValidateThreads) dup |= o != j && a.seqs[o] == s;
+  int st = __syncthreads_or(dup) ? KARA_SEQ_DUP_TRIGGER : 0;
+  const int len = a.seq_lens[s];
+  if (len < 0 || len > a.max_len || (int64_t)len > (int64_t)g.max_blocks * g.bs)
+    st |= KARA_SEQ_BAD_WINDOW;
+  else
+    st |= pages_status(a.bt + (int64_t)s * g.max_blocks, 0, (len + g.bs - 1) / g.bs, g.num_pages, lds);
+  if (tid == 0) a.status[j] = st;
+}
+
+constexpr int kPickThreads = 256;
+constexpr int kPickWaves = kPickThreads / 64;
+constexpr int kPickLds = 16384;      // keys held in LDS; a longer row is read again in each pass
+
+// Order-preserving: a larger weight has the larger key, -0 ranks as 0, NaN below all.
+__device__ __forceinline__ uint32_t weight_key(float f) {
+  uint32_t u = __float_as_uint(f);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
+  if ((u & 0x7fffffffu) == 0) u = 0;
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// One workgroup per (layer, sequence, KV head): the positions that stay.  A
+// radix selection over the accumulators between the first n_sink and the last
+// n_recent positions finds the weight of the last one taken and how many equal
+// ones are (8 bits a pass); then every wave writes its quarter of the sequence
+// in order.
+__global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
+  extern __shared__ uint32_t keys[];
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t found[3];                        // digit, items wanted in its bin, items in it
+  __shared__ uint32_t wave_gt[kPickWaves], wave_eq[kPickWaves];
+  const Geom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t u = blockIdx.x;
+  const int h = (int)(u % g.Hkv);
+  const int j = (int)((u / g.Hkv) % a.n);
+  const int l = (int)(u / ((int64_t)g.Hkv * a.n));
+  int32_t* kept = a.kept + u * a.keep;
+  const int s = a.seqs[j];
+  const int len = a.status[j] == 0 ? a.seq_lens[s] : 0;
+  if (len <= a.keep) {
+    for (int i = tid; i < a.keep; i += kPickThreads) kept[i] = i < len ? i : -1;
+    return;
+  }
+  const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
+  const float* w = a.w.p[l];
+  const int lo = a.n_sink, hi = len - a.n_recent;      // candidates
+  const uint32_t want = (uint32_t)(a.keep - a.n_sink - a.n_recent);
+  auto fetch = [&](int pos) __attribute__((always_inline)) {
+    const int b = pos / g.bs;
+    return weight_key(w[((int64_t)row_pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs)]);
+  };
+  const bool in_lds = hi - lo <= kPickLds;
+  if (in_lds) {
+    for (int i = lo + tid; i < hi; i += kPickThreads) keys[i - lo] = fetch(i);
+    __syncthreads();
+  }
+  auto key = [&](int pos) __attribute__((always_inline)) { return in_lds ? keys[pos - lo] : fetch(pos); };
+
+  // key of the last one taken: `prefix` (with the digits below `shift` open where
+  // its bin is taken whole), `need` of the equal ones
+  uint32_t prefix = 0, need = want;
+  int shift = 32;
+  while (shift > 0 && need > 0) {
+    shift -= 8;
+    hist[tid] = 0;
+    __syncthreads();
+    for (int i = lo + tid; i < hi; i += kPickThreads) {
+      const uint32_t k = key(i);
+      if (shift == 24 || ((k ^ prefix) >> (shift + 8)) == 0) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    }
+    __syncthreads();
+    // (one wave, bins from the largest: lane i holds 255 - 4i .. 252 - 4i)
+    if (wave == 0) {
+      uint32_t c[4], tot = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tot += c[e] = hist[255 - 4 * lane - e];
+      uint32_t above = tot;
+#pragma unroll
+      for (int x = 1; x < 64; x <<= 1) {
+        const uint32_t up = (uint32_t)__shfl_up((int)above, x, 64);
+        if (lane >= x) above += up;
+      }
+      above -= tot;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (above < need && need <= above + c[e]) found[0] = 255 - 4 * lane - e, found[1] = need - above, found[2] = c[e];
+        above += c[e];
+      }
+    }
+    __syncthreads();
+    prefix |= found[0] << shift;
+    need = found[1];
+    if (found[1] == found[2]) break;
+    __syncthreads();
+  }
+  // taken: keys above the prefix, and of those equal to it (in the digits that were
+  // looked at) the first `need`
+  const uint32_t edge = prefix >> (shift & 31);
+  const bool any = want > 0;
+  const int per = ((len + kPickWaves * 64 - 1) / (kPickWaves * 64)) * 64;     // positions per wave
+  const int w0 = min(wave * per, len), w1 = min(w0 + per, len);
+  auto rank = [&](int pos) __attribute__((always_inline)) {                   // 2: stays, 1: stays if among the first
+    if (pos >= w1) return 0;
+    if (pos < lo || pos >= hi) return 2;
+    if (!any) return 0;
+    const uint32_t k = key(pos) >> (shift & 31);
+    return k > edge ? 2 : k == edge ? 1 : 0;
+  };
+  uint32_t gt = 0, eq = 0;
+  for (int i = w0; i < w1; i += 64) {
+    const int r = rank(i + lane);
+    gt += (uint32_t)__popcll(__ballot(r == 2));
+    eq += (uint32_t)__popcll(__ballot(r == 1));
+  }
+  if (lane == 0) wave_gt[wave] = gt, wave_eq[wave] = eq;
+  __syncthreads();
+  uint32_t at = 0, eq_at = 0;          // taken, and equal ones, before this wave's part
+  for (int x = 0; x < wave; ++x) {
+    at += wave_gt[x];
+    eq_at += wave_eq[x];
+  }
+  at += min(eq_at, need);
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int i = w0; i < w1; i += 64) {
+    const int r = rank(i + lane);
+    const uint64_t e = __ballot(r == 1);
+    const bool stays = r == 2 || (r == 1 && eq_at + (uint32_t)__popcll(e & below) < need);
+    const uint64_t b = __ballot(stays);
+    if (stays) kept[at + (uint32_t)__popcll(b & below)] = i + lane;
+    at += (uint32_t)__popcll(b);
+    eq_at += (uint32_t)__popcll(e);
+  }
+}
+
+constexpr int kMoveThreads = 256;
+constexpr int kMoveUnroll = 8;
+constexpr int kMoveStage = 32768 / 4;     // kept positions and table entries held in LDS, at most
+
+// One workgroup per (layer, sequence, KV head, part): K rows, V rows, and the small
+// arrays (scales, accumulators).  Row i takes row kept[i] >= i, so working up in
+// tiles -- a tile's rows all loaded before any of it is stored -- never overwrites
+// a row still to be read.
+template <bool STAGED>
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
+  extern __shared__ int32_t stage[];
+  const Geom& g = a.g;
+  const int tid = threadIdx.x;
+  const int part = blockIdx.x % 3;
+  const int64_t u = blockIdx.x / 3;
+  const int h = (int)(u % g.Hkv);
+  const int j = (int)((u / g.Hkv) % a.n);
+  const int l = (int)(u / ((int64_t)g.Hkv * a.n));
+  if (a.status[j] != 0) return;
+  const int s = a.seqs[j];
+  const int len = a.seq_lens[s];
+  if (len <= a.keep) return;
+  const int32_t* kept = a.kept + u * a.keep;
+  const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
+  if constexpr (STAGED) {
+    for (int i = tid; i < a.keep; i += kMoveThreads) stage[i] = kept[i];
+    const int nb = (len + g.bs - 1) / g.bs;
+    for (int b = tid; b < nb; b += kMoveThreads) stage[a.keep + b] = row_pages[b];
+    __syncthreads();
+  }
+  auto source = [&](int i) __attribute__((always_inline)) { return STAGED ? stage[i] : kept[i]; };
+  auto row = [&](int pos) __attribute__((always_inline)) {
+    const int b = pos / g.bs;
+    const int64_t page = STAGED ? stage[a.keep + b] : row_pages[b];
+    return (page * g.Hkv + h) * g.bs + (pos - b * g.bs);
+  };
+  if (part < 2) {
+    char* base = (char*)(part ? a.v.p[l] : a.k.p[l]);
+    const int cpr = a.row_bytes >> 4, rpp = kMoveThreads / cpr, tile = rpp * kMoveUnroll;
+    const int c = tid % cpr, r = tid / cpr;
+    for (int x0 = 0; x0 < a.keep; x0 += tile) {
+      u32x4 v[kMoveUnroll];
+      int dst[kMoveUnroll];
+#pragma unroll
+      for (int k = 0; k < kMoveUnroll; ++k) {
+        const int i = x0 + k * rpp + r;
+        dst[k] = -1;
+        if (i < a.keep) {
+          const int src = source(i);
+          if (src != i) {
+            dst[k] = i;
+            v[k] = __builtin_nontemporal_load((const u32x4*)(base + row(src) * a.row_bytes + c * 16));
+          }
+        }
+      }
+      // all of this tile's loads have landed before any thread stores
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kMoveUnroll; ++k)
+        if (dst[k] >= 0) __builtin_nontemporal_store(v[k], (u32x4*)(base + row(dst[k]) * a.row_bytes + c * 16));
+    }
+    return;
+  }
+  for (int x0 = 0; x0 < a.keep; x0 += kMoveThreads) {
+    const int i = x0 + tid;
+    const int src = i < a.keep ? source(i) : i;
+    float w = 0.f;
+    uint32_t sk = 0, sv = 0;
+    const int64_t from = src != i ? row(src) : 0, to = src != i ? row(i) : 0;
+    if (src != i) {
+      w = a.w.p[l][from];
+      if (a.scale_bytes == 4) {
+        sk = ((const uint32_t*)a.ks.p[l])[from];
+        sv = ((const uint32_t*)a.vs.p[l])[from];
+      } else if (a.scale_bytes == 2) {
+        sk = ((const uint16_t*)a.ks.p[l])[from];
+        sv = ((const uint16_t*)a.vs.p[l])[from];
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (src != i) {
+      a.w.p[l][to] = w;
+      if (a.scale_bytes == 4) {
+        ((uint32_t*)a.ks.p[l])[to] = sk;
+        ((uint32_t*)a.vs.p[l])[to] = sv;
+      } else if (a.scale_bytes == 2) {
+        ((uint16_t*)a.ks.p[l])[to] = (uint16_t)sk;
+        ((uint16_t*)a.vs.p[l])[to] = (uint16_t)sv;
+      }
+    }
+  }
+}
+
+constexpr int kCutThreads = 256;
+
+__global__ __launch_bounds__(kCutThreads) void evict_commit_kernel(EvictArgs a, int32_t* __restrict__ freed,
+                                                                   int32_t* __restrict__ n_freed) {
+  const Geom& g = a.g;
+  const int j = blockIdx.x, tid = threadIdx.x;
+  int32_t* fr = freed + (int64_t)j * g.max_blocks;
+  const int s = a.seqs[j];
+  const int len = a.status[j] == 0 ? a.seq_lens[s] : 0;
+  __syncthreads();                       // every thread has read the length before it changes
+  const int new_len = min(len, a.keep);
+  const int old_b = (len + g.bs - 1) / g.bs, new_b = (new_len + g.bs - 1) / g.bs;
+  int32_t* row = a.bt + (int64_t)(a.status[j] == 0 ? s : 0) * g.max_blocks;
+  for (int c = tid; c < g.max_blocks; c += kCutThreads) {
+    const bool gone = c < old_b - new_b;
+    fr[c] = gone ? row[new_b + c] : -1;
+    if (gone) row[new_b + c] = -1;
+  }
+  if (tid == 0) {
+    n_freed[j] = old_b - new_b;
+    if (new_len < len) a.seq_lens[s] = new_len;
+  }
+}
+
+bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && n_layers <= kMaxLayersPerLaunch; }
+
+PoolPtrs ptrs(const void* const* pools, int n_layers) {
+  PoolPtrs x{};
+  if (pools)
+    for (int i = 0; i < n_layers; ++i) x.p[i] = const_cast<void*>(pools[i]);
+  return x;
+}
+
+WeightPtrs weight_ptrs(float* const* w, int n_layers) {
+  WeightPtrs x{};
+  for (int i = 0; i < n_layers; ++i) x.p[i] = w[i];
+  return x;
+}
+
+// both scale arrays or neither
+bool scales_ok(const void* const* ks, const void* const* vs, int n_layers) {
+  return (!ks && !vs) || (pools_ok(ks, n_layers) && pools_ok(vs, n_layers));
+}
+
+struct CountWs {
+  size_t records, logits, total;
+  int64_t ld;
+};
+
+CountWs count_ws(const Geom& g, int n, int n_layers, int max_len) {
+  const int64_t rows = (int64_t)n_layers * n * g.Hq;
+  const int64_t splits = (max_len + KARA_HARNESS_SPLIT_KEYS - 1) / KARA_HARNESS_SPLIT_KEYS;
+  CountWs w{};
+  w.ld = (max_len + 31) / 32 * 32;       // (the splits write whole blocks of up to 32 keys)
+  w.logits = align256((size_t)(rows * splits * (g.d + 2)) * sizeof(float));
+  w.total = align256(w.logits + (size_t)(rows * w.ld) * sizeof(float));
+  return w;
+}
+
+}  // namespace
+}  // namespace kara
+
+using namespace kara;
+
+extern "C" {
+
+kara_status_t kara_evict_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers, int32_t max_len,
+                                                  size_t* bytes) {
+  Geom g;
+  const kara_status_t st = make_geom(p, n, &g);
+  if (st != KARA_OK) return st;
+  if (g.G > kMaxGroup) return KARA_ERR_UNSUPPORTED;
+  if (!bytes || !layers_ok(n, n_layers) || max_len < 1 || (int64_t)max_len > (int64_t)g.max_blocks * g.bs)
+    return KARA_ERR_INVALID_ARG;
+  *bytes = count_ws(g, n, n_layers, max_len).total;
+  return KARA_OK;
+}
+
+kara_status_t kara_evict_attention(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,
+                                   const void* q, const void* const* k_pools, const void* const* v_pools,
+                                   const void* const* k_scales, const void* const* v_scales, float* const* weights,
+                                   const int32_t* block_table, const int32_t* seq_lens, int32_t n_new, int32_t max_len,
+                                   float* out, void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  kara_status_t st = kara_evict_attention_workspace_size(p, n, n_layers, max_len, &need);
+  if (st != KARA_OK) return st;
+  if (n_new < 0) return KARA_ERR_INVALID_ARG;
+  if (n == 0) return KARA_OK;
+  if (!seqs || !q || !block_table || !seq_lens || !out || !pools_ok(k_pools, n_layers) || !pools_ok(v_pools, n_layers) ||
+      !scales_ok(k_scales, v_scales, n_layers) || !pools_ok((const void* const*)weights, n_layers))
+    return KARA_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < need) return KARA_ERR_WORKSPACE;
+  Geom g;
+  st = make_geom(p, n, &g);
+  if (st != KARA_OK) return st;
+  const CountWs w = count_ws(g, n, n_layers, max_len);
+  float* records = (float*)workspace;
+  float* logits = (float*)((char*)workspace + w.logits);
+  const int64_t units = (int64_t)n_layers * n * g.Hkv;
+  const int chunks = (max_len + kFinKeys - 1) / kFinKeys;
+  if (!grid_ok(units * ((max_len + KARA_HARNESS_SPLIT_KEYS - 1) / KARA_HARNESS_SPLIT_KEYS))) return KARA_ERR_UNSUPPORTED;
+  hipStream_t s = (hipStream_t)stream;
+  const PoolPtrs kp = ptrs(k_pools, n_layers), vp = ptrs(v_pools, n_layers);
+  int keys = 0;
+  hipError_t e;
+  if (k_scales) {
+    Q4Split a{};
+    a.g = g;
+    a.n = n;
+    a.n_layers = n_layers;
+    a.T = 1;
+    a.n_rt = 1;
+    a.split_keys = keys = q4_split_keys(units, max_len);
+    a.n_splits = (max_len + keys - 1) / keys;
+    a.max_len = max_len;
+    a.seqs = seqs;
+    a.bt = block_table;
+    a.seq_lens = seq_lens;
+    a.q = q;
+    a.kp = kp;
+    a.vp = vp;
+    a.ksp = ptrs(k_scales, n_layers);
+    a.vsp = ptrs(v_scales, n_layers);
+    a.ws = records;
+    a.logits = logits;
+    a.ld = w.ld;
+    e = launch_q4_split(a, true, s);
+  } else {
+    e = launch_decode_logits(g, n, seqs, n_layers, q, kp, vp, block_table, seq_lens, max_len, records, logits, w.ld, &keys, s);
+  }
+  if (e != hipSuccess) return hip_status(e);
+  const int n_splits = (max_len + keys - 1) / keys;
+  const dim3 grid((unsigned)(units * chunks)), block(kFinThreads);
+  if (g.d == 128)
+    hipLaunchKernelGGL((evict_finish_kernel<128>), grid, block, 0, s, g, n, seqs, block_table, seq_lens, n_new, max_len, keys,
+                       n_splits, chunks, (const float*)records, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
+  else
+    hipLaunchKernelGGL((evict_finish_kernel<64>), grid, block, 0, s, g, n, seqs, block_table, seq_lens, n_new, max_len, keys,
+                       n_splits, chunks, (const float*)records, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
+  return hip_status(hipGetLastError());
+}
+
+kara_status_t kara_evict_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers, int32_t keep, size_t* bytes) {
+  Geom g;
+  const kara_status_t st = make_geom(p, n, &g);
+  if (st != KARA_OK) return st;
+  if (!bytes || !layers_ok(n, n_layers) || keep < 1) return KARA_ERR_INVALID_ARG;
+  *bytes = (size_t)n_layers * n * g.Hkv * keep * sizeof(int32_t);
+  return KARA_OK;
+}
+
+kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers, int32_t keep,
+                                int32_t n_sink, int32_t n_recent, void* const* k_pools, void* const* v_pools,
+                                void* const* k_scales, void* const* v_scales, float* const* weights,
+                                int32_t* block_table, int32_t* seq_lens, int32_t max_len, int32_t commit, int32_t* kept,
+                                int32_t* freed, int32_t* n_freed, int32_t* status, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  kara_status_t st = kara_evict_workspace_size(p, n, n_layers, keep, &need);
+  if (st != KARA_OK) return st;
+  EvictArgs a{};
+  st = make_geom(p, n, &a.g);
+  if (st != KARA_OK) return st;
+  const Geom& g = a.g;
+  if (n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > keep || max_len < 1 ||
+      (int64_t)max_len > (int64_t)g.max_blocks * g.bs)
+    return KARA_ERR_INVALID_ARG;
+  if (n == 0) return KARA_OK;
+  if (!seqs || !block_table || !seq_lens || !status || !pools_ok(k_pools, n_layers) || !pools_ok(v_pools, n_layers) ||
+      !scales_ok(k_scales, v_scales, n_layers) || !pools_ok((const void* const*)weights, n_layers) ||
+      (commit && (!freed || !n_freed)))
+    return KARA_ERR_INVALID_ARG;
+  if (!kept && (!workspace || workspace_bytes < need)) return KARA_ERR_WORKSPACE;
+  const int64_t units = (int64_t)n_layers * n * g.Hkv;
+  if (!grid_ok(units * 3)) return KARA_ERR_UNSUPPORTED;
+  a.n = n;
+  a.n_layers = n_layers;
+  a.keep = keep;
+  a.n_sink = n_sink;
+  a.n_recent = n_recent;
+  a.max_len = max_len;
+  a.seqs = seqs;
+  a.bt = block_table;
+  a.seq_lens = seq_lens;
+  a.kept = kept ? kept : (int32_t*)workspace;
+  a.status = status;
+  a.k = ptrs(k_pools, n_layers);
+  a.v = ptrs(v_pools, n_layers);
+  a.ks = ptrs(k_scales, n_layers);
+  a.vs = ptrs(v_scales, n_layers);
+  a.w = weight_ptrs(weights, n_layers);
+  a.row_bytes = k_scales ? g.d / 2 : g.d * g.esize;
+  a.scale_bytes = k_scales ? g.d / 32 : 0;
+  hipStream_t s = (hipStream_t)stream;
+  hipLaunchKernelGGL(evict_validate_kernel, dim3((unsigned)n), dim3(kValidateThreads), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_status(e);
+  const size_t pick_lds = (size_t)std::min(max_len, kPickLds) * sizeof(uint32_t);
+  hipLaunchKernelGGL(evict_pick_kernel, dim3((unsigned)units), dim3(kPickThreads), pick_lds, s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return hip_status(e);
+  const int64_t staged = (int64_t)keep + (max_len + g.bs - 1) / g.bs;
+  if (staged <= kMoveStage)
+    hipLaunchKernelGGL((evict_move_kernel<true>), dim3((unsigned)(units * 3)), dim3(kMoveThreads), (size_t)staged * 4, s, a);
+  else
+    hipLaunchKernelGGL((evict_move_kernel<false>), dim3((unsigned)(units * 3)), dim3(kMoveThreads), 0, s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || !commit) return hip_status(e);
+  hipLaunchKernelGGL(evict_commit_kernel, dim3((unsigned)n), dim3(kCutThreads), 0, s, a, freed, n_freed);
+  return hip_status(hipGetLastError());
+}
+
+}  // extern "C"

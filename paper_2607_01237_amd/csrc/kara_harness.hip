@@ -187,11 +187,14 @@ __device__ __forceinline__ float swap16_add(float a, float b) {
 // One split in the launch, or a sequence that ends inside its first: out
 // is written here.  Otherwise a record per (layer, j, query head, split) in
 // ws, strided as n_splits: m, l, o[d].
-template <int DT, int D, int GP>
+//
+// LOGITS: every split leaves a record, and q . k of every key goes to
+// logits [layer][j][query head][ld] for the caller's own second kernel.
+template <int DT, int D, int GP, bool LOGITS>
 __global__ __launch_bounds__(kDecThreads, 2) void decode_split_kernel(
     Geom g, int n, const int32_t* __restrict__ seqs, const char* __restrict__ q, PoolPtrs kp, PoolPtrs vp,
     const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens, int max_len, int split_keys, int n_splits,
-    float* __restrict__ ws, float* __restrict__ out) {
+    float* __restrict__ ws, float* __restrict__ out, float* __restrict__ logits, int64_t ld) {
   using C = DCfg<DT, D, GP>;
   constexpr int TB = C::kTB, KC = C::kKC, E = C::kE, VW = C::kVW;
   __shared__ __attribute__((aligned(16))) uint32_t row_of[kDecMaxSplit];   // pool row of the split's keys
@@ -214,7 +217,7 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_kernel(
   const int k0 = split * split_keys;
   if (len <= 0 || len > max_len || k0 >= len) {
     // no keys: zero rows where no combine kernel follows
-    if (n_splits == 1)
+    if (!LOGITS && n_splits == 1)
       for (int i = tid; i < G * D; i += kDecThreads) out[orow * D + i] = 0.f;
     return;
   }
@@ -228,7 +231,9 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_kernel(
     for (int i = tid; i < npad; i += kDecThreads) {
       const int pos = k0 + min(i, nk - 1);
       const int b = pos / g.bs;
-      row_of[i] = (uint32_t)(((int64_t)row_pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs));
+      int page = row_pages[b];
+      if constexpr (LOGITS) page = min(max(page, 0), g.num_pages - 1);
+      row_of[i] = (uint32_t)(((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs));
     }
   }
   // lane (gq, li): 16-byte chunks gq + 4x of row li (any assignment of chunks
@@ -308,6 +313,13 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_kernel(
     // (bf16) or 10 (fp32) are needed, so with three waves per SIMD the maximum
     // read what the registers held before.  12 cycles per block.
     asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[TB - 1]));
+    if constexpr (LOGITS) {
+      if (li < G) {
+        float* to = logits + (orow + li) * ld + k0 + blk * C::kBlock + 4 * gq;
+#pragma unroll
+        for (int t = 0; t < TB; ++t) *(floatx4*)(to + t * 16) = sv[t];
+      }
+    }
     const int left = nk - blk * C::kBlock;
     if (left < C::kBlock) {
 #pragma unroll
@@ -407,7 +419,7 @@ __global__ __launch_bounds__(kDecThreads, 2) void decode_split_kernel(
     }
   __syncthreads();
   const int nw = min(nblk, kDecWaves);   // waves that had keys
-  const bool direct = len <= split_keys;
+  const bool direct = !LOGITS && len <= split_keys;
   float* rec = ws + (orow * n_splits + split) * (D + 2);
   for (int x = tid; x < G * D; x += kDecThreads) {
     const int i = x / D, e = x - i * D;
@@ -486,37 +498,53 @@ int decode_split_keys(const Geom& g, int n, int n_layers, int max_len) {
   return keys;
 }
 
+struct DecodeCall {
+  int n, n_layers, max_len;
+  const int32_t *seqs, *bt, *seq_lens;
+  const void* q;
+  const PoolPtrs *kp, *vp;
+  float *out, *ws;
+  float* logits;     // null: out alone
+  int64_t ld;
+};
+
 template <int DT, int D, int GP>
-hipError_t launch_decode_g(const Geom& g, int n, const int32_t* seqs, int n_layers, const void* q, const PoolPtrs& kp,
-                           const PoolPtrs& vp, const int32_t* bt, const int32_t* seq_lens, int max_len, float* out,
-                           float* ws, hipStream_t stream) {
-  const int keys = decode_split_keys(g, n, n_layers, max_len);
-  const int n_splits = (max_len + keys - 1) / keys;
-  const int64_t blocks = (int64_t)n_layers * n * g.Hkv * n_splits;
-  hipLaunchKernelGGL((decode_split_kernel<DT, D, GP>), dim3((unsigned)blocks), dim3(kDecThreads), 0, stream, g, n, seqs,
-                     (const char*)q, kp, vp, bt, seq_lens, max_len, keys, n_splits, ws, out);
+hipError_t launch_decode_g(const Geom& g, const DecodeCall& c, hipStream_t stream) {
+  const int keys = decode_split_keys(g, c.n, c.n_layers, c.max_len);
+  const int n_splits = (c.max_len + keys - 1) / keys;
+  const int64_t blocks = (int64_t)c.n_layers * c.n * g.Hkv * n_splits;
+  if (c.logits) {
+    hipLaunchKernelGGL((decode_split_kernel<DT, D, GP, true>), dim3((unsigned)blocks), dim3(kDecThreads), 0, stream, g,
+                       c.n, c.seqs, (const char*)c.q, *c.kp, *c.vp, c.bt, c.seq_lens, c.max_len, keys, n_splits, c.ws,
+                       c.out, c.logits, c.ld);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((decode_split_kernel<DT, D, GP, false>), dim3((unsigned)blocks), dim3(kDecThreads), 0, stream, g,
+                     c.n, c.seqs, (const char*)c.q, *c.kp, *c.vp, c.bt, c.seq_lens, c.max_len, keys, n_splits, c.ws,
+                     c.out, nullptr, 0);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || n_splits == 1) return e;
-  const int64_t rows = (int64_t)n_layers * n * g.Hq;
-  hipLaunchKernelGGL((decode_combine_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, g, n, seqs,
-                     seq_lens, max_len, keys, n_splits, rows, (const float*)ws, out);
+  const int64_t rows = (int64_t)c.n_layers * c.n * g.Hq;
+  hipLaunchKernelGGL((decode_combine_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, g, c.n, c.seqs,
+                     c.seq_lens, c.max_len, keys, n_splits, rows, (const float*)c.ws, c.out);
   return hipGetLastError();
 }
 
 // query heads per KV head, rounded up to an instance's accumulators
 template <int DT, int D>
-hipError_t launch_decode(const Geom& g, int n, const int32_t* seqs, int n_layers, const void* q, const PoolPtrs& kp,
-                         const PoolPtrs& vp, const int32_t* bt, const int32_t* seq_lens, int max_len, float* out,
-                         float* ws, hipStream_t stream) {
-#define KARA_DECODE_G(GP) \
-  return launch_decode_g<DT, D, GP>(g, n, seqs, n_layers, q, kp, vp, bt, seq_lens, max_len, out, ws, stream)
-  if (g.G == 1) KARA_DECODE_G(1);
-  if (g.G == 2) KARA_DECODE_G(2);
-  if (g.G <= 4) KARA_DECODE_G(4);
-  if (g.G == 5) KARA_DECODE_G(5);
-  if (g.G <= 8) KARA_DECODE_G(8);
-  KARA_DECODE_G(16);
-#undef KARA_DECODE_G
+hipError_t launch_decode(const Geom& g, const DecodeCall& c, hipStream_t stream) {
+  if (g.G == 1) return launch_decode_g<DT, D, 1>(g, c, stream);
+  if (g.G == 2) return launch_decode_g<DT, D, 2>(g, c, stream);
+  if (g.G <= 4) return launch_decode_g<DT, D, 4>(g, c, stream);
+  if (g.G == 5) return launch_decode_g<DT, D, 5>(g, c, stream);
+  if (g.G <= 8) return launch_decode_g<DT, D, 8>(g, c, stream);
+  return launch_decode_g<DT, D, 16>(g, c, stream);
+}
+
+hipError_t launch_decode_any(const Geom& g, const DecodeCall& c, hipStream_t stream) {
+  if (g.dtype == KARA_BF16)
+    return g.d == 128 ? launch_decode<KARA_BF16, 128>(g, c, stream) : launch_decode<KARA_BF16, 64>(g, c, stream);
+  return g.d == 128 ? launch_decode<KARA_F32, 128>(g, c, stream) : launch_decode<KARA_F32, 64>(g, c, stream);
 }
 
 // the step's window fields are irrelevant here; validate the rest
@@ -527,6 +555,16 @@ kara_status_t harness_geom(const kara_params_t* p, int32_t n, Geom* g) {
 }
 
 }  // namespace
+
+hipError_t launch_decode_logits(const Geom& g, int n, const int32_t* seqs, int n_layers, const void* q,
+                                const PoolPtrs& kp, const PoolPtrs& vp, const int32_t* bt, const int32_t* seq_lens,
+                                int max_len, float* records, float* logits, int64_t ld, int* split_keys,
+                                hipStream_t stream) {
+  *split_keys = decode_split_keys(g, n, n_layers, max_len);
+  return launch_decode_any(g, DecodeCall{n, n_layers, max_len, seqs, bt, seq_lens, q, &kp, &vp, nullptr, records, logits, ld},
+                           stream);
+}
+
 }  // namespace kara
 
 using namespace kara;
@@ -613,20 +651,8 @@ kara_status_t kara_harness_decode_attention(const kara_params_t* p, int32_t n, c
     kp.p[i] = const_cast<void*>(k_pools[i]);
     vp.p[i] = const_cast<void*>(v_pools[i]);
   }
-  hipStream_t s = (hipStream_t)stream;
-  float* ws = (float*)workspace;
-  hipError_t e;
-  if (g.dtype == KARA_BF16)
-    e = g.d == 128 ? launch_decode<KARA_BF16, 128>(g, n, seqs, n_layers, q, kp, vp, block_table, seq_lens, max_len,
-                                                  out, ws, s)
-                   : launch_decode<KARA_BF16, 64>(g, n, seqs, n_layers, q, kp, vp, block_table, seq_lens, max_len,
-                                                 out, ws, s);
-  else
-    e = g.d == 128 ? launch_decode<KARA_F32, 128>(g, n, seqs, n_layers, q, kp, vp, block_table, seq_lens, max_len,
-                                                 out, ws, s)
-                   : launch_decode<KARA_F32, 64>(g, n, seqs, n_layers, q, kp, vp, block_table, seq_lens, max_len,
-                                                out, ws, s);
-  return hip_status(e);
+  const DecodeCall c{n, n_layers, max_len, seqs, block_table, seq_lens, q, &kp, &vp, out, (float*)workspace, nullptr, 0};
+  return hip_status(launch_decode_any(g, c, (hipStream_t)stream));
 }
 
 }  // extern "C"

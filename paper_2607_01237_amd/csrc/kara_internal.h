@@ -131,6 +131,12 @@ struct Q4Split {
   float* logits;              // [n_layers][n][Hkv][G][ld] q . k, T = 1
   int64_t ld;
 };
+// Decode attention over rows (kara_harness.hip) up to its splits: records
+// [n_layers][n][Hq][n_splits]: m, l, o[d] and logits q . k [n_layers][n][Hq][ld].
+hipError_t launch_decode_logits(const Geom& g, int n, const int32_t* seqs, int n_layers, const void* q,
+                                const PoolPtrs& kp, const PoolPtrs& vp, const int32_t* bt, const int32_t* seq_lens,
+                                int max_len, float* records, float* logits, int64_t ld, int* split_keys,
+                                hipStream_t stream);
 // Keys per split for so many units (layers x sequences x KV heads x row tiles).
 int q4_split_keys(int64_t units, int max_len);
 // logits: fill a.logits, and leave records (never out) for every sequence.

@@ -2,6 +2,7 @@
 // of Eq. (9) (Algorithm 1's MemoryCompaction) and the metadata update
 // (UpdateMetadata: trailing blocks released, table and length rewritten).
 #include "kara_internal.h"
+#include "kara_page_check.h"
 
 namespace kara {
 namespace {
@@ -12,13 +13,6 @@ namespace {
 // moves rows in place, and a page mapped twice would be read and written by
 // two workgroups at once.  keep_kept: a KARA_SEQ_BAD_KEPT bit already in
 // status[t] survives (the staged per-layer calls of one event).
-constexpr int kValidateThreads = 256;
-// One buffer of LDS words, used as a bitmap of the pool's pages when it has
-// that many bits (a duplicate is a bit already set: one pass over the row;
-// 1,100 blocks 42 -> 6 us against the pairwise scan), else as a copy of the
-// table row for the pairwise scan when the row fits, else not at all.
-constexpr int kValidateLds = 8192;
-
 __global__ __launch_bounds__(kValidateThreads) void validate_kernel(
     Geom g, const int32_t* __restrict__ trig, const int32_t* __restrict__ bt,
     const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ win_start,
@@ -49,41 +43,7 @@ __global__ __launch_bounds__(kValidateThreads) void validate_kernel(
   const int b0 = p0 / g.bs;
   const int b1 = (len + g.bs - 1) / g.bs;
   __shared__ uint32_t lds[kValidateLds];
-  int bad = 0, twice = 0;
-  const int n_words = (g.num_pages + 31) / 32;
-  if (n_words <= kValidateLds) {
-    for (int i = tid; i < n_words; i += kValidateThreads) lds[i] = 0;
-    __syncthreads();
-    for (int b = tid; b < b0; b += kValidateThreads) {
-      const int pg = row[b];
-      if (pg >= 0 && pg < g.num_pages) atomicOr(&lds[pg >> 5], 1u << (pg & 31));
-    }
-    __syncthreads();
-    for (int b = b0 + tid; b < b1; b += kValidateThreads) {
-      const int pg = row[b];
-      if (pg < 0 || pg >= g.num_pages) bad = 1;
-      else twice |= (atomicOr(&lds[pg >> 5], 1u << (pg & 31)) >> (pg & 31)) & 1;
-    }
-  } else {
-    const bool in_lds = b1 <= kValidateLds;
-    if (in_lds)
-      for (int b = tid; b < b1; b += kValidateThreads) lds[b] = (uint32_t)row[b];
-    __syncthreads();
-    for (int b = b0 + tid; b < b1; b += kValidateThreads) {
-      const int pg = in_lds ? (int)lds[b] : row[b];
-      if (pg < 0 || pg >= g.num_pages) {
-        bad = 1;
-        continue;
-      }
-      if (in_lds) {
-        for (int c = 0; c < b; ++c) twice |= (int)lds[c] == pg;
-      } else {
-        for (int c = 0; c < b; ++c) twice |= row[c] == pg;
-      }
-    }
-  }
-  const int st = st0 | (__syncthreads_or(bad) ? KARA_SEQ_BAD_PAGE : 0) |
-                 (__syncthreads_or(twice) ? KARA_SEQ_DUP_PAGE : 0);
+  const int st = st0 | pages_status(row, b0, b1, g.num_pages, lds);
   if (tid == 0) status[t] = st;
 }
 

@@ -149,6 +149,15 @@ _SIGS = {
     "kara_q4_attention_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
     "kara_q4_attention": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _PP, _PP, _PP, _PP, _VP, _VP, _I32, _VP, _VP,
                                  ctypes.c_size_t, _VP]),
+    "kara_evict_attention_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
+    "kara_evict_attention": (_I32, [_PAR, _I32, _VP, _I32, _VP, _PP, _PP, _PP, _PP, _PP, _VP, _VP, _I32, _I32, _VP, _VP,
+                                    ctypes.c_size_t, _VP]),
+    "kara_evict_observe_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
+    "kara_evict_observe": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _PP, _PP, _PP, _VP, _VP, _I32, _I32, _VP,
+                                  ctypes.c_size_t, _VP]),
+    "kara_evict_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
+    "kara_evict_tokens": (_I32, [_PAR, _I32, _VP, _I32, _I32, _I32, _I32, _PP, _PP, _PP, _PP, _PP, _VP, _VP, _I32, _I32,
+                                 _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]),
     "kara_sched_create": (_I32, [ctypes.POINTER(SchedConfig), _P32, ctypes.POINTER(ctypes.c_void_p)]),
     "kara_sched_destroy": (_I32, [_VP]),
     "kara_sched_submit": (_I32, [_VP, _I32, _I32, _P64]),
@@ -614,6 +623,104 @@ def q4_attention(p, seqs, n_query, q, k_pools, v_pools, k_scales, v_scales, bloc
         ctypes.byref(p), n, _on(dev, seqs), L, n_query, _on(dev, q), _array_on(dev, k_pools), _array_on(dev, v_pools),
         _array_on(dev, k_scales), _array_on(dev, v_scales), _on(dev, block_table), _on(dev, seq_lens), int(max_len),
         _on(dev, out), _on(dev, workspace), _nbytes(workspace), s))
+
+
+# ---- eviction by accumulated attention weight (include/kara_evict.h)
+
+def _either_cache(p, L, k_pools, v_pools, k_scales, v_scales, weights):
+    """Pools of rows (no scales) or of 4-bit codes, and the accumulators; v_pools may be left out."""
+    if (k_scales is None) != (v_scales is None) and v_pools is not None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales and v_scales: both or neither")
+    given = {"k_pools": k_pools, "v_pools": v_pools} if v_pools is not None else {"k_pools": k_pools}
+    if k_scales is not None:
+        if v_pools is not None:
+            _q4_pools(p, L, k_scales=k_scales, v_scales=v_scales, **given)
+        else:
+            _q4_pools(p, L, k_scales=k_scales, **given)
+    else:
+        for name, ts in given.items():
+            if len(ts) != L:
+                raise KaraError("marshal", ERR_INVALID_ARG, f"{name}: {len(ts)} layers, expected {L}")
+            _pools(p, ts, name)
+    n = p.num_pages * p.n_kv_heads * p.block_size
+    if len(weights) != L:
+        raise KaraError("marshal", ERR_INVALID_ARG, f"weights: {len(weights)} layers, expected {L}")
+    for i, t in enumerate(weights):
+        _need(f"weights[{i}]", t, n, _f32())
+
+
+def evict_attention_workspace_size(p, n, n_layers, max_len) -> int:
+    out = ctypes.c_size_t(0)
+    _check("kara_evict_attention_workspace_size", load().kara_evict_attention_workspace_size(
+        ctypes.byref(p), n, n_layers, max_len, ctypes.byref(out)))
+    return int(out.value)
+
+
+def evict_attention(p, seqs, q, k_pools, v_pools, weights, block_table, seq_lens, n_new, max_len, out, workspace,
+                    k_scales=None, v_scales=None, stream=None):
+    """decode_attention that adds every key's weight to its accumulator (weights:
+    fp32 [num_pages][Hkv][block_size] per layer); fp32 out of q's shape."""
+    n, L = seqs.numel(), len(k_pools)
+    _need("seqs", seqs, 0, _i32())
+    _need("q", q, L * n * p.n_q_heads * p.head_dim, _dt(p))
+    _need("out", out, L * n * p.n_q_heads * p.head_dim, _f32())
+    _either_cache(p, L, k_pools, v_pools, k_scales, v_scales, weights)
+    _tables(p, block_table, seq_lens)
+    dev, s = _launch(stream)
+    _check("kara_evict_attention", load().kara_evict_attention(
+        ctypes.byref(p), n, _on(dev, seqs), L, _on(dev, q), _array_on(dev, k_pools), _array_on(dev, v_pools),
+        _array_on(dev, k_scales), _array_on(dev, v_scales), _array_on(dev, weights), _on(dev, block_table),
+        _on(dev, seq_lens), int(n_new), int(max_len), _on(dev, out), _on(dev, workspace), _nbytes(workspace), s))
+
+
+def evict_observe_workspace_size(p, n, n_layers, n_query, max_len) -> int:
+    out = ctypes.c_size_t(0)
+    _check("kara_evict_observe_workspace_size", load().kara_evict_observe_workspace_size(
+        ctypes.byref(p), n, n_layers, n_query, max_len, ctypes.byref(out)))
+    return int(out.value)
+
+
+def evict_observe(p, seqs, n_query, q, k_pools, weights, block_table, seq_lens, n_new, max_len, workspace, k_scales=None,
+                  stream=None):
+    """Adds the weights that each listed sequence's last n_query tokens give
+    (q [n_layers][n][n_query][Hq][d]) to the accumulators."""
+    n, L, n_query = seqs.numel(), len(k_pools), int(n_query)
+    _need("seqs", seqs, 0, _i32())
+    _need("q", q, L * n * n_query * p.n_q_heads * p.head_dim, _dt(p))
+    _either_cache(p, L, k_pools, None, k_scales, None, weights)
+    _tables(p, block_table, seq_lens)
+    dev, s = _launch(stream)
+    _check("kara_evict_observe", load().kara_evict_observe(
+        ctypes.byref(p), n, _on(dev, seqs), L, n_query, _on(dev, q), _array_on(dev, k_pools), _array_on(dev, k_scales),
+        _array_on(dev, weights), _on(dev, block_table), _on(dev, seq_lens), int(n_new), int(max_len),
+        _on(dev, workspace), _nbytes(workspace), s))
+
+
+def evict_workspace_size(p, n, n_layers, keep) -> int:
+    out = ctypes.c_size_t(0)
+    _check("kara_evict_workspace_size", load().kara_evict_workspace_size(
+        ctypes.byref(p), n, n_layers, keep, ctypes.byref(out)))
+    return int(out.value)
+
+
+def evict_tokens(p, seqs, keep, n_sink, n_recent, k_pools, v_pools, weights, block_table, seq_lens, max_len, commit,
+                 status, workspace, kept=None, freed=None, n_freed=None, k_scales=None, v_scales=None, stream=None):
+    """Cuts every listed sequence longer than `keep` to that many tokens: the first
+    n_sink, the last n_recent and the largest accumulators between."""
+    n, L, keep = seqs.numel(), len(k_pools), int(keep)
+    _need("seqs", seqs, 0, _i32())
+    _either_cache(p, L, k_pools, v_pools, k_scales, v_scales, weights)
+    _tables(p, block_table, seq_lens)
+    _need("kept", kept, L * n * p.n_kv_heads * keep, _i32())
+    _need("freed", freed, n * p.max_blocks_per_seq, _i32())
+    _need("n_freed", n_freed, n, _i32())
+    _need("status", status, n, _i32())
+    dev, s = _launch(stream)
+    _check("kara_evict_tokens", load().kara_evict_tokens(
+        ctypes.byref(p), n, _on(dev, seqs), L, keep, int(n_sink), int(n_recent), _array_on(dev, k_pools),
+        _array_on(dev, v_pools), _array_on(dev, k_scales), _array_on(dev, v_scales), _array_on(dev, weights),
+        _on(dev, block_table), _on(dev, seq_lens), int(max_len), int(bool(commit)), _on(dev, kept), _on(dev, freed),
+        _on(dev, n_freed), _on(dev, status), _on(dev, workspace), _nbytes(workspace), s))
 
 
 # ---- periodic compression policy (include/kara_sched.h): host runtime

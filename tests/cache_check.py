@@ -48,13 +48,14 @@ def rows_of(pool, table, s, n, bs):
 
 
 def logit_error(q, k, scale, terms=1):
-    """How far an fp32 logit may be off, relative to its exponential: products of
-    d terms summed in fp32 in any order (d EPS of the sum of magnitudes), scaled
+    """How far an fp32 logit may be off, relative to its exponential, for queries q
+    [.., Hq, d] over keys k [n, Hkv, d]: products of d terms summed in fp32 in any order (d EPS of the sum of magnitudes), scaled
     by a rounded constant (3 EPS of the logit: constant, product, subtraction of
     the maximum), exponentiated within 2 EPS.  `terms`: bf16 terms a factor is
     held in, 24 bits of it in three (another EPS of the magnitudes each)."""
     d = q.shape[-1]
-    mags = scale * float((np.abs(q).max(axis=tuple(range(q.ndim - 1))) * np.abs(k).reshape(-1, d).max(axis=0)).sum())
+    Hq, Hkv = q.shape[-2], k.shape[-2]
+    mags = scale * max(float((np.abs(q[..., h, :]).reshape(-1, d) @ np.abs(k[:, h * Hkv // Hq]).T).max()) for h in range(Hq))
     return (d + 3 + 2 * terms) * EPS * mags + 3 * EPS
 
 
