@@ -471,7 +471,7 @@ kara_status_t kara_evict_attention(const kara_params_t* p, int32_t n, const int3
     a.n_layers = n_layers;
     a.T = 1;
     a.n_rt = 1;
-    a.split_keys = keys = q4_split_keys(units, max_len);
+    a.split_keys = keys = q4_split_keys(g, units, max_len);
     a.n_splits = (max_len + keys - 1) / keys;
     a.max_len = max_len;
     a.seqs = seqs;

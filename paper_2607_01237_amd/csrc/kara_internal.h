@@ -122,6 +122,7 @@ struct Q4Split {
   int T;                      // queries per sequence, its last T positions
   int n_rt;                   // tiles of 16 query rows per (layer, sequence, KV head)
   int split_keys, n_splits, max_len;
+  int run;                    // set by the launch
   const int32_t *seqs, *bt, *seq_lens;
   const void* q;              // [n_layers][n][T][Hq][d]
   PoolPtrs kp, vp, ksp, vsp;  // codes and scales
@@ -138,7 +139,7 @@ hipError_t launch_decode_logits(const Geom& g, int n, const int32_t* seqs, int n
                                 int max_len, float* records, float* logits, int64_t ld, int* split_keys,
                                 hipStream_t stream);
 // Keys per split for so many units (layers x sequences x KV heads x row tiles).
-int q4_split_keys(int64_t units, int max_len);
+int q4_split_keys(const Geom& g, int64_t units, int max_len);
 // logits: fill a.logits, and leave records (never out) for every sequence.
 hipError_t launch_q4_split(Q4Split a, bool logits, hipStream_t stream);
 

@@ -31,6 +31,25 @@ __device__ inline void copy16(const void* g, char* lds_wave_base) {
       : "memory");
 }
 
+// The same copy of 4 bytes per lane, and of 2 that land zero-extended in 4.
+#define KARA_COPY_LDS(NAME, INS)                                                              \
+  __device__ inline void NAME(const void* g, char* lds_wave_base) {                           \
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(                                      \
+        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_wave_base);         \
+    uint32_t saved;                                                                           \
+    asm volatile(                                                                             \
+        "s_mov_b32 %0, m0\n\t"                                                                \
+        "s_mov_b32 m0, %2\n\t"                                                                \
+        "s_nop 0\n\t" INS " %1, off\n\t"                                                     \
+        "s_mov_b32 m0, %0"                                                                    \
+        : "=&s"(saved)                                                                        \
+        : "v"(g), "s"(lds)                                                                    \
+        : "memory");                                                                          \
+  }
+KARA_COPY_LDS(copy4, "global_load_lds_dword")
+KARA_COPY_LDS(copy2, "global_load_lds_ushort")
+#undef KARA_COPY_LDS
+
 // Workgroup barrier for LDS traffic only.  __syncthreads() would also drain
 // every outstanding global->LDS copy (its release fence waits on vmcnt),
 // defeating a prefetch ring; the copies this barrier must cover are waited

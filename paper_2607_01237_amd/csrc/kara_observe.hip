@@ -61,13 +61,12 @@ struct Octet {
       static_assert(NT == 1, "bf16 rows");
       t[0] = __builtin_bit_cast(bf16x8, v[0]);
     } else {
+      uint32_t w[4][NT];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        __bf16 x[NT];
-        bf16_terms(__uint_as_float(v[i >> 2][i & 3]), x);
+      for (int i = 0; i < 4; ++i)
+        bf16_term_pairs(__uint_as_float(v[i >> 1][2 * i & 3]), __uint_as_float(v[i >> 1][(2 * i & 3) + 1]), w[i]);
 #pragma unroll
-        for (int y = 0; y < NT; ++y) t[y][i] = x[y];
-      }
+      for (int y = 0; y < NT; ++y) t[y] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
     }
   }
 };

@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "kara_append.h"
+#include "kara_lds.h"
 #include "kara_q4.h"
 #include "kara_q4_device.h"
 
@@ -187,8 +188,10 @@ __global__ __launch_bounds__(kAppendThreads) void q4_read_kernel(
 constexpr int kSplitThreads = 256;
 constexpr int kSplitWaves = kSplitThreads / 64;
 constexpr int kSplitMin = 256;       // keys per split, at least (the workspace's records are sized for that)
-constexpr int kSplitMax = 1024;
+constexpr int kSplitMax = 2048;
+constexpr int kSplitRows = 1024;     // runs of keys a split's LDS table holds
 constexpr int kSplitBlock = 32;      // keys a wave works on at a time
+constexpr int kSplitStages = 2;      // blocks of a wave's LDS ring, all on their way while it works
 constexpr int kSplitWgTarget = 4096; // workgroups a launch keeps when its splits grow
 
 // One workgroup of four waves per (layer, sequence, KV head, tile of 16 query
@@ -196,14 +199,14 @@ constexpr int kSplitWgTarget = 4096; // workgroups a launch keeps when its split
 // exponential sum l and unnormalised output o, in log2 units and fp32.  Rows of
 // a (layer, sequence, KV head) run over (query, head in group).
 //
-// The pool rows of the split's keys and their scales go to LDS first; the four
-// waves then take the split's 32-key blocks in turn.  A lane's 16 bytes of codes
-// at d = 128 are one block of 32 values with one scale, which the hardware turns
-// into the four bf16 operands of S^T = K Q^T (keys as the M dimension); a lane so
-// holds four keys of one query per tile, and its weights are the B operand of
-// O^T += V^T P^T as they stand.  V is read as rows, d/16 columns of a key per
-// lane, and the pairs of columns that the conversion gives are put together to
-// pairs of keys by byte permutes.
+// The pool rows of the split's keys go to LDS first; the four waves then take the
+// split's 32-key blocks in turn, each through a ring of its own in LDS that direct
+// copies fill two blocks ahead (4.3 KB a block at d = 128; no barrier in the loop).  A lane's 16 bytes of codes at d = 128 are one block of 32
+// values with one scale, which the hardware turns into the four bf16 operands of
+// S^T = K Q^T (keys as the M dimension); a lane so holds four keys of one query per
+// tile, and its weights are the B operand of O^T += V^T P^T as they stand.  V is
+// read as rows, d/16 columns of a key per lane, and the pairs of columns that the
+// conversion gives are put together to pairs of keys by byte permutes.
 //
 // NQ: bf16 terms of a query (1: bf16, exact; 3: fp32, 24 bits); NP: bf16 terms of a
 // weight (1 where the output is bf16; 3 where it is fp32).  K and V are exact in one.
@@ -214,28 +217,34 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
   constexpr int E = D / 16;                  // output columns per lane
   constexpr int kRow = D / 2;                // bytes of a row's codes
   constexpr int kKW = D / 32;                // a lane's words of a key's codes: an eighth of a row's values per word
-  struct Stage {
-    uint32_t row[kSplitMax], ks[kSplitMax], vs[kSplitMax];
+  constexpr int kCodes = kSplitBlock * kRow;           // a block's codes of K, or of V
+  constexpr int kStage = 2 * kCodes + 64 * 4;          // and a word of scales per key and K|V
+  constexpr int kCopies = 2 * (kCodes / 1024) + 1;     // copies per block
+  struct Ring {
+    uint32_t row[kSplitRows];                          // pool rows of runs of keys, in 16 bytes of codes
+    __attribute__((aligned(16))) char b[kSplitWaves][kSplitStages][kStage];
   };
   __shared__ __attribute__((aligned(16))) union {
-    Stage st;
+    Ring st;
     float o[kSplitWaves][16][D];
   } lds;
   __shared__ float red_m[kSplitWaves][16], red_l[kSplitWaves][16];
-  Stage& st = lds.st;
+  Ring& st = lds.st;
 
   const Geom& g = a.g;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
-  const int split = blockIdx.x % a.n_splits;
-  int64_t rest = blockIdx.x / a.n_splits;
-  const int rt = (int)(rest % a.n_rt);
-  rest /= a.n_rt;
-  const int h = (int)(rest % g.Hkv);
-  const int j = (int)((rest / g.Hkv) % a.n);
-  const int l = (int)(rest / ((int64_t)g.Hkv * a.n));
+  uint32_t rest = blockIdx.x;                // (a 64-bit division is 140 scalar instructions)
+  const int split = rest % (uint32_t)a.n_splits;
+  rest /= (uint32_t)a.n_splits;
+  const int rt = rest % (uint32_t)a.n_rt;
+  rest /= (uint32_t)a.n_rt;
+  const int h = rest % (uint32_t)g.Hkv;
+  rest /= (uint32_t)g.Hkv;
+  const int j = rest % (uint32_t)a.n;
+  const int l = rest / (uint32_t)a.n;
   const int s = a.seqs[j];
   const int G = g.G, T = a.T, R = G * T;
   const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
@@ -259,100 +268,145 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
   const float c = g.scale * kLog2e;
 
   const int npad = (nk + kSplitBlock - 1) / kSplitBlock * kSplitBlock;
-  {
-    const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
-    // (padding keys of the last block repeat its last key, with no weight)
-    for (int i = tid; i < npad; i += kSplitThreads) {
-      const int pos = k0 + min(i, nk - 1);
-      const int b = pos / g.bs;
-      const int page = min(max(row_pages[b], 0), g.num_pages - 1);
-      const uint32_t row = (uint32_t)(((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs));
-      st.row[i] = row;
-      if constexpr (D == 128) {
-        st.ks[i] = ((const uint32_t*)a.ksp.p[l])[row];
-        st.vs[i] = ((const uint32_t*)a.vsp.p[l])[row];
-      } else {
-        st.ks[i] = ((const uint16_t*)a.ksp.p[l])[row];
-        st.vs[i] = ((const uint16_t*)a.vsp.p[l])[row];
-      }
-    }
-  }
   // lane (gq, li): values gq*D/4 .. of query row li; its limit: keys of the split it sees
-  bf16x8 qa[NQ][KS];
+  uint4 qraw[KS * (NQ == 1 ? 1 : 2)];
   int limit = 0;
+  const bool there = li < rows;
   {
-    const bool there = li < rows;
     const int r = row0 + (there ? li : 0);
-    const int t = r / G;
+    const int t = T == 1 ? 0 : r / G;
     const int64_t at = (orow + (int64_t)t * g.Hq + (r - t * G)) * D + gq * (D / 4);
     if (there) limit = min(nk, len - T + t + 1 - k0);
+    const uint4* src = (const uint4*)((const char*)a.q + at * (NQ == 1 ? 2 : 4));
 #pragma unroll
-    for (int x = 0; x < KS; ++x) {
-      if constexpr (NQ == 1) {
-        const uint4 v = *(const uint4*)((const __bf16*)a.q + at + x * 8);
-        qa[0][x] = __builtin_bit_cast(bf16x8, there ? v : uint4{0, 0, 0, 0});
-      } else {
-        const floatx4* src = (const floatx4*)((const float*)a.q + at + x * 8);
-        const floatx4 u = src[0], v = src[1];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          __bf16 t3[NQ];
-          bf16_terms(there ? (i < 4 ? u[i & 3] : v[i & 3]) : 0.f, t3);
-#pragma unroll
-          for (int y = 0; y < NQ; ++y) qa[y][x][i] = t3[y];
-        }
-      }
+    for (int x = 0; x < KS * (NQ == 1 ? 1 : 2); ++x) qraw[x] = src[x];
+  }
+  // Pool rows of the split's keys, in 16 bytes of codes.  Runs of 2^run keys (the
+  // power of two in the block size, 16 at most; k0 is a multiple of it) lie in one
+  // page: an entry each.  (An entry per key, 8 table reads and divisions a thread,
+  // took 18 of a workgroup's 73 thousand cycles.)
+  const int run = a.run;
+  {
+    const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
+    for (int i = tid; i < npad >> run; i += kSplitThreads) {
+      const int pos = k0 + min(i << run, (nk - 1) >> run << run);
+      const int b = pos / g.bs;
+      const int page = min(max(row_pages[b], 0), g.num_pages - 1);
+      st.row[i] = (uint32_t)((page * g.Hkv + h) * g.bs + (pos - b * g.bs)) * (kRow / 16);
     }
   }
+  bf16x8 qa[NQ][KS];
+#pragma unroll
+  for (int x = 0; x < KS; ++x) {
+    if constexpr (NQ == 1) {
+      qa[0][x] = __builtin_bit_cast(bf16x8, there ? qraw[x] : uint4{0, 0, 0, 0});
+    } else {
+      const floatx4 u = __builtin_bit_cast(floatx4, qraw[2 * x]), v = __builtin_bit_cast(floatx4, qraw[2 * x + 1]);
+      uint32_t w[4][NQ];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x0 = i < 2 ? u[2 * i] : v[2 * i - 4], x1 = i < 2 ? u[2 * i + 1] : v[2 * i - 3];
+        bf16_term_pairs(there ? x0 : 0.f, there ? x1 : 0.f, w[i]);
+      }
+#pragma unroll
+      for (int y = 0; y < NQ; ++y) qa[y][x] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
+    }
+  }
+  // (the query loads are waited for here, not in the loop behind the copies)
+#pragma unroll
+  for (int y = 0; y < NQ; ++y)
+#pragma unroll
+    for (int x = 0; x < KS; ++x) asm volatile("" : "+v"(qa[y][x]));
   // the first query row of the tile sees the fewest keys
   const int limit0 = __builtin_amdgcn_readfirstlane(limit);
   __syncthreads();
 
-  const char* kbase = (const char*)a.kp.p[l] + gq * (kRow / 4);
-  const char* vbase = (const char*)a.vp.p[l] + li * (E / 2);
-  uint32_t kb[2][2][kKW];        // [buffer][tile][words]
-  uint32_t vb[2][8];             // [buffer][key 16t + 4gq + r at 4t + r]
-  auto load = [&](int blk, int b) __attribute__((always_inline)) {
+  const int nblk = npad / kSplitBlock;
+  // Block blk into stage b.  K rows lie in key order, their 16-byte chunks XOR-swizzled
+  // (d = 128: by row / 4, d = 64: by row / 8) so that 16 rows read at one chunk hit
+  // different banks; V rows 4q + r of a tile at slot 4r + q, so that a read of rows
+  // 4gq + r takes consecutive ones.  Then the scales: a word per key, K's, V's.
+  constexpr int kCPR = kRow / 16;                      // chunks per row
+  constexpr int kRows = 64 / kCPR;                     // rows per copy
+  const int crow = lane / kCPR, cchunk = lane % kCPR;
+  const int kchunk = cchunk ^ (D == 128 ? (crow >> 2) & 3 : (crow >> 3) & 1);
+  const int vrow = (crow & 16) | ((crow & 3) << 2) | ((crow >> 2) & 3);
+  const char* kbase = (const char*)a.kp.p[l] + kchunk * 16;
+  const char* vbase = (const char*)a.vp.p[l] + cchunk * 16;
+  const char* sbase = (const char*)(lane < 32 ? a.ksp.p[l] : a.vsp.p[l]);
+  // (waited for here: left to its first use, in the loop, the wait would be for the
+  // copies too)
+  asm volatile("" : "+v"(sbase));
+  const int run_mask = (1 << run) - 1;
+  auto issue = [&](int blk, int b) __attribute__((always_inline)) {
+    char* to = st.b[wave][b];
+    constexpr int kTimes = kSplitBlock / kRows;
+    // (a padding key is the last one: its page may end before it)
+    auto at = [&](int key) __attribute__((always_inline)) {
+      key = min(blk * kSplitBlock + key, nk - 1);
+      return (uint64_t)(st.row[key >> run] + (key & run_mask) * (kRow / 16));
+    };
+    uint64_t kat[kTimes], vat[kTimes], sat = at(lane & 31);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const char* src = kbase + (uint64_t)st.row[blk * kSplitBlock + t * 16 + li] * kRow;
-      if constexpr (D == 128) {
-        const uint4 v = *(const uint4*)src;
-        kb[b][t][0] = v.x, kb[b][t][1] = v.y, kb[b][t][2] = v.z, kb[b][t][3] = v.w;
-      } else {
-        const uint2 v = *(const uint2*)src;
-        kb[b][t][0] = v.x, kb[b][t][1] = v.y;
-      }
-      const uint4 rw = *(const uint4*)&st.row[blk * kSplitBlock + t * 16 + 4 * gq];
-      const uint32_t r4[4] = {rw.x, rw.y, rw.z, rw.w};
+    for (int t = 0; t < kTimes; ++t) kat[t] = at(t * kRows + crow), vat[t] = at(t * kRows + vrow);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const char* vsrc = vbase + (uint64_t)r4[r] * kRow;
-        if constexpr (D == 128) vb[b][4 * t + r] = *(const uint32_t*)vsrc;
-        else vb[b][4 * t + r] = *(const uint16_t*)vsrc;
-      }
+    for (int t = 0; t < kTimes; ++t) {
+      copy16(kbase + (kat[t] << 4), to + t * 1024);
+      copy16(vbase + (vat[t] << 4), to + kCodes + t * 1024);
     }
+    // (a row has as many bytes of scales as 16-byte chunks of codes)
+    if constexpr (D == 128) copy4(sbase + sat, to + 2 * kCodes);
+    else copy2(sbase + sat, to + 2 * kCodes);
+  };
+#pragma unroll
+  for (int i = 0; i < kSplitStages; ++i)
+    if (wave + i * kSplitWaves < nblk) issue(wave + i * kSplitWaves, i);
+  // byte b of a row's scales, turned right by 8b + 9, lies on an fp32 exponent
+  const uint32_t kturn = 8 * (D == 128 ? gq : gq >> 1) + 9, vturn = 8 * (D == 128 ? li >> 2 : li >> 3) + 9;
+  auto scale_of = [](uint32_t word, uint32_t turn) __attribute__((always_inline)) {
+    return __uint_as_float(__builtin_amdgcn_alignbit(word, word, turn) & 0x7f800000u);
   };
 
   float m = kMaxFloor, lsum = 0.f;   // query li's reference, and this lane's part of its sum
+  floatx4 lones = {0.f, 0.f, 0.f, 0.f};   // NP = 1: the sum, in every element
   floatx4 o[E];                      // query li, columns (4gq + r) * E + e
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  bf16x8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
   float* lrow = nullptr;
   if constexpr (LOGITS)
     lrow = a.logits + ((((int64_t)l * a.n + j) * g.Hkv + h) * G + min(li, rows - 1)) * a.ld + k0 + 4 * gq;
 
-  const int nblk = npad / kSplitBlock;
-  auto work = [&](int blk, int b) __attribute__((always_inline)) {
-    floatx4 sv[2];
-    const int kbyte = D == 128 ? gq : gq >> 1;
+  const int koff = D == 128 ? li * kRow + ((gq ^ (li >> 2)) * 16) : li * kRow + (((gq >> 1) ^ (li >> 3)) * 16) + (gq & 1) * 8;
+  const int voff = kCodes + gq * kRow + li * (E / 2);
+  // a block as the lane holds it: K words and scale words of key 16t + li, V words
+  // and scale words of keys 16t + 4gq + r
+  uint32_t kw[2][kKW], kscale[2], vw[8];
+  uint4 vscale[2];
+  auto take = [&](const char* b) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const float scale = q4_scale((st.ks[blk * kSplitBlock + t * 16 + li] >> (8 * kbyte)) & 255u);
+      __builtin_memcpy(kw[t], b + t * 16 * kRow + koff, kKW * 4);
+      kscale[t] = *(const uint32_t*)(b + 2 * kCodes + (t * 16 + li) * 4);
+      vscale[t] = *(const uint4*)(b + 2 * kCodes + 128 + (t * 16 + 4 * gq) * 4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const char* vp = b + voff + (t * 16 + 4 * r) * kRow;
+        vw[4 * t + r] = D == 128 ? *(const uint32_t*)vp : *(const uint16_t*)vp;
+      }
+    }
+  };
+  auto work = [&](int blk) __attribute__((always_inline)) {
+    floatx4 sv[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float scale = scale_of(kscale[t], kturn);
       floatx4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < KS; ++x) {
-        const bf16x8 ka = q4_octet(kb[b][t][x], scale);
+        const bf16x8 ka = q4_octet(kw[t][x], scale);
 #pragma unroll
         for (int y = NQ - 1; y >= 0; --y) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qa[y][x], acc, 0, 0, 0);
       }
@@ -379,45 +433,51 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sv[t][r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
-    // the reference m is raised only past a headroom of 2^8
-    if (__ballot(mx > m + 8.f) != 0ull) {
+    // The reference m, one for the four lanes of a query, is raised only where a
+    // logit passes it by more than 2^8: no exchange between lanes before that.
+    if (__ballot(mx * c > m + 8.f) != 0ull) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
       const float mn = fmaxf(m, mx);
       const float f = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       lsum *= f;
+      if constexpr (NP == 1) lones *= f;
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] *= f;
     }
-    bf16x8 pb[NP];
+    uint32_t pw[NP][4];                  // terms of the lane's eight weights, in pairs
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sv[t][r], c, -m));
-        __bf16 pt[NP];
-        bf16_terms(p, pt);
-        // (one term: the sum is of the rounded weights, as the output is)
-        lsum += NP == 1 ? (float)pt[0] : p;
+      for (int r = 0; r < 4; r += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sv[t][r], c, -m));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sv[t][r + 1], c, -m));
+        if constexpr (NP > 1) lsum += p0 + p1;
+        uint32_t w[NP];
+        bf16_term_pairs(p0, p1, w);
 #pragma unroll
-        for (int y = 0; y < NP; ++y) pb[y][4 * t + r] = pt[y];
+        for (int y = 0; y < NP; ++y) pw[y][2 * t + (r >> 1)] = w[y];
       }
+    bf16x8 pb[NP];
+#pragma unroll
+    for (int y = 0; y < NP; ++y) pb[y] = __builtin_bit_cast(bf16x8, uint4{pw[y][0], pw[y][1], pw[y][2], pw[y][3]});
+    // (one term: the sum is of the rounded weights, as the output is, and formed as
+    // one more product, with ones)
+    if constexpr (NP == 1) lones = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[0], lones, 0, 0, 0);
     // V: pairs of columns of a key to pairs of keys of a column
     uint32_t pv[8][E / 2];
-    const int vshift = 8 * (D == 128 ? li >> 2 : li >> 3);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const uint4 sc = *(const uint4*)&st.vs[blk * kSplitBlock + t * 16 + 4 * gq];
-      const uint32_t s4[4] = {sc.x, sc.y, sc.z, sc.w};
+      const uint32_t s4[4] = {vscale[t].x, vscale[t].y, vscale[t].z, vscale[t].w};
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float scale = q4_scale((s4[r] >> vshift) & 255u);
-        pv[4 * t + r][0] = q4_pair<0>(vb[b][4 * t + r], scale);
-        pv[4 * t + r][1] = q4_pair<1>(vb[b][4 * t + r], scale);
+        const float scale = scale_of(s4[r], vturn);
+        pv[4 * t + r][0] = q4_pair<0>(vw[4 * t + r], scale);
+        pv[4 * t + r][1] = q4_pair<1>(vw[4 * t + r], scale);
         if constexpr (E == 8) {
-          pv[4 * t + r][2] = q4_pair<2>(vb[b][4 * t + r], scale);
-          pv[4 * t + r][3] = q4_pair<3>(vb[b][4 * t + r], scale);
+          pv[4 * t + r][2] = q4_pair<2>(vw[4 * t + r], scale);
+          pv[4 * t + r][3] = q4_pair<3>(vw[4 * t + r], scale);
         }
       }
     }
@@ -433,25 +493,28 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
         o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[y], o[e], 0, 0, 0);
     }
   };
-  if (wave < nblk) {
-    load(wave, 0);
-    int blk = wave;
-    for (;;) {
-      const int n1 = blk + kSplitWaves;
-      if (n1 < nblk) load(n1, 1);
-      work(blk, 0);
-      if (n1 >= nblk) break;
-      blk = n1 + kSplitWaves;
-      if (blk < nblk) load(blk, 0);
-      work(n1, 1);
-      if (blk >= nblk) break;
-    }
+  // The wave's i-th block passes through stage i mod kSplitStages: once it is in
+  // registers, the stage takes the copies of block i + kSplitStages.
+  int stage = 0;
+  for (int blk = wave; blk < nblk; blk += kSplitWaves) {
+    static_assert(kSplitStages == 2, "one newer block may be outstanding");
+    if (blk + kSplitWaves < nblk) wait_vm<kCopies>();
+    else wait_vm<0>();
+    take(st.b[wave][stage]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // taken before the stage is written again
+    if (blk + kSplitStages * kSplitWaves < nblk) issue(blk + kSplitStages * kSplitWaves, stage);
+    work(blk);
+    stage ^= 1;
   }
 
   // ---- the four waves' sums ----
   asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[E - 1]));   // (as above, past the loop's branch)
-  lsum += __shfl_xor(lsum, 16, 64);
-  lsum += __shfl_xor(lsum, 32, 64);
+  if constexpr (NP == 1) {
+    lsum = lones[0];
+  } else {
+    lsum += __shfl_xor(lsum, 16, 64);
+    lsum += __shfl_xor(lsum, 32, 64);
+  }
   if (gq == 0) {
     red_m[wave][li] = m;
     red_l[wave][li] = lsum;
@@ -475,8 +538,8 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
       L += red_l[w][i] * f;
       O += lds.o[w][i][e] * f;
     }
-    const int r = row0 + i;
-    const int64_t at = orow + (int64_t)(r / G) * g.Hq + r % G;
+    const int r = row0 + i, t = T == 1 ? 0 : r / G;
+    const int64_t at = orow + (int64_t)t * g.Hq + (r - t * G);
     if (direct) {
       const float v = L == 0.f ? 0.f : O / L;   // (a row that sees no key)
       if (a.out_bf16) ((__bf16*)a.out)[at * D + e] = (__bf16)v;
@@ -529,11 +592,16 @@ __global__ __launch_bounds__(256) void q4_combine_kernel(Geom g, int n, int T, c
   }
 }
 
-// Keys per split: 256 while the launch has few workgroups, up to 1024 where 16
-// per CU remain: fewer records and prologues.
-int split_keys_of(int64_t units, int max_len) {
+// log2 of the keys that lie in one page whatever run of them a split starts at
+int run_of(int bs) { return std::min(4, __builtin_ctz((unsigned)bs)); }
+
+// Keys per split: 256 while the launch has few workgroups, up to 2048 (1024 where
+// pages give runs of one key) where 16 workgroups per CU remain: fewer records and
+// prologues.
+int split_keys_of(int bs, int64_t units, int max_len) {
+  const int most = std::min(kSplitMax, kSplitRows << run_of(bs));
   int keys = kSplitMin;
-  while (keys < kSplitMax && units * ((max_len + 2 * keys - 1) / (2 * keys)) >= kSplitWgTarget) keys *= 2;
+  while (keys < most && units * ((max_len + 2 * keys - 1) / (2 * keys)) >= kSplitWgTarget) keys *= 2;
   return keys;
 }
 
@@ -551,6 +619,7 @@ PoolPtrs ptrs(const void* const* pools, int n_layers) {
 }  // namespace
 
 hipError_t launch_q4_split(Q4Split a, bool logits, hipStream_t stream) {
+  a.run = run_of(a.g.bs);
   const Geom& g = a.g;
   const int64_t blocks = (int64_t)a.n_layers * a.n * g.Hkv * a.n_rt * a.n_splits;
   const dim3 grid((unsigned)blocks), block(kSplitThreads);
@@ -571,7 +640,7 @@ hipError_t launch_q4_split(Q4Split a, bool logits, hipStream_t stream) {
   return hipGetLastError();
 }
 
-int q4_split_keys(int64_t units, int max_len) { return split_keys_of(units, max_len); }
+int q4_split_keys(const Geom& g, int64_t units, int max_len) { return split_keys_of(g.bs, units, max_len); }
 
 }  // namespace kara
 
@@ -682,7 +751,7 @@ kara_status_t kara_q4_attention(const kara_params_t* p, int32_t n, const int32_t
   a.T = n_query;
   a.n_rt = (int)(((int64_t)g.G * n_query + 15) / 16);
   const int64_t units = (int64_t)n_layers * n * g.Hkv * a.n_rt;
-  a.split_keys = split_keys_of(units, max_len);
+  a.split_keys = split_keys_of(g.bs, units, max_len);
   a.n_splits = (max_len + a.split_keys - 1) / a.split_keys;
   const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
   if (!grid_ok(units * a.n_splits) || !grid_ok((rows + 3) / 4)) return KARA_ERR_UNSUPPORTED;
