@@ -237,7 +237,10 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
   uint32_t rest = blockIdx.x;                // (a 64-bit division is 140 scalar instructions)
-  const int split = rest % (uint32_t)a.n_splits;
+  // (blocks go round the 8 XCDs: split x of eight units in a row falls to the same
+  // ones, the next eight are shifted, so that no XCD gets all the short last splits)
+  const uint32_t unit8 = rest / ((uint32_t)a.n_splits * 8);
+  const int split = (rest + unit8) % (uint32_t)a.n_splits;
   rest /= (uint32_t)a.n_splits;
   const int rt = rest % (uint32_t)a.n_rt;
   rest /= (uint32_t)a.n_rt;
