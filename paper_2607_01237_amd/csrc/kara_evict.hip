@@ -41,11 +41,13 @@ __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
     const float* __restrict__ logits, int64_t ld, WeightPtrs wp, float* __restrict__ out) {
   __shared__ float red_m[kMaxGroup], red_i[kMaxGroup];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int chunk = blockIdx.x % chunks;
-  const int64_t rest = blockIdx.x / chunks;
-  const int h = (int)(rest % g.Hkv);
-  const int j = (int)((rest / g.Hkv) % n);
-  const int l = (int)(rest / ((int64_t)g.Hkv * n));
+  uint32_t rest = blockIdx.x;
+  const int chunk = rest % (uint32_t)chunks;
+  rest /= (uint32_t)chunks;
+  const int h = rest % (uint32_t)g.Hkv;
+  rest /= (uint32_t)g.Hkv;
+  const int j = rest % (uint32_t)n;
+  const int l = rest / (uint32_t)n;
   const int s = seqs[j], G = g.G;
   const int64_t orow = ((int64_t)l * n + j) * g.Hq + h * G;
   const int len = s >= 0 && s < g.n_seqs ? seq_lens[s] : 0;
@@ -93,6 +95,19 @@ __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
     for (int e = 0; e < 4; ++e) add[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[e], c, -red_m[i])), red_i[i], add[e]);
   }
   const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
+  if ((g.bs & 3) == 0) {
+    // the four keys lie in one page, on 16 bytes
+    const int b = k / g.bs;
+    const int page = row_pages[b];
+    if (page < 0 || page >= g.num_pages) return;
+    floatx4* to = (floatx4*)(wp.p[l] + ((int64_t)page * g.Hkv + h) * g.bs + (k - b * g.bs));
+    const floatx4 was = *to;
+    floatx4 now;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) now[e] = k + e >= len ? was[e] : k + e >= len - n_new ? add[e] : was[e] + add[e];
+    *to = now;
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int pos = k + e;

@@ -529,17 +529,18 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
     for (int e = 0; e < E; e += 4)
       *(floatx4*)&lds.o[wave][li][(4 * gq + r) * E + e] = floatx4{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]};
   __syncthreads();
-  const int nw = min(nblk, kSplitWaves);   // waves that had keys
   const bool direct = !LOGITS && len <= a.split_keys;
   for (int x = tid; x < rows * D; x += kSplitThreads) {
     const int i = x / D, e = x - i * D;
-    float M = red_m[0][i];
-    for (int w = 1; w < nw; ++w) M = fmaxf(M, red_m[w][i]);
-    float L = 0.f, O = 0.f;
-    for (int w = 0; w < nw; ++w) {
-      const float f = __builtin_amdgcn_exp2f(red_m[w][i] - M);
-      L += red_l[w][i] * f;
-      O += lds.o[w][i][e] * f;
+    // (a wave without keys left its start: a maximum below all, sums of 0)
+    float wm[kSplitWaves], M = kMaxFloor, L = 0.f, O = 0.f;
+#pragma unroll
+    for (int w = 0; w < kSplitWaves; ++w) M = fmaxf(M, wm[w] = red_m[w][i]);
+#pragma unroll
+    for (int w = 0; w < kSplitWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(wm[w] - M);
+      L = fmaf(red_l[w][i], f, L);
+      O = fmaf(lds.o[w][i][e], f, O);
     }
     const int r = row0 + i, t = T == 1 ? 0 : r / G;
     const int64_t at = orow + (int64_t)t * g.Hq + (r - t * G);
@@ -576,15 +577,39 @@ __global__ __launch_bounds__(256) void q4_combine_kernel(Geom g, int n, int T, c
     const int ns = (len + split_keys - 1) / split_keys;
     constexpr int rec = D + 2;
     const float* w = ws + row * n_splits * rec;
-    float M = kMaxFloor;
-    for (int sp = lane; sp < ns; sp += 64) M = fmaxf(M, w[sp * rec]);
+    // lane i: split i's maximum and sum, 64 at a time, the first kept
+    const float m0 = lane < ns ? w[lane * rec] : kMaxFloor, l0 = lane < ns ? w[lane * rec + 1] : 0.f;
+    float M = m0;
+    for (int sp = lane + 64; sp < ns; sp += 64) M = fmaxf(M, w[sp * rec]);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
-    for (int sp = 0; sp < ns; ++sp) {
-      const float f = __builtin_amdgcn_exp2f(w[sp * rec] - M);
-      L += w[sp * rec + 1] * f;
+    for (int sp0 = 0; sp0 < ns; sp0 += 64) {
+      float f, lf;
+      if (sp0 == 0) {
+        f = __builtin_amdgcn_exp2f(m0 - M);
+        lf = l0 * f;
+      } else {
+        f = sp0 + lane < ns ? __builtin_amdgcn_exp2f(w[(sp0 + lane) * rec] - M) : 0.f;
+        lf = sp0 + lane < ns ? w[(sp0 + lane) * rec + 1] * f : 0.f;
+      }
+      const int cnt = min(64, ns - sp0);
+      const float* v = w + (int64_t)sp0 * rec + 2 + lane * kDPerLane;
+      // (four records at once; past the last a record of weight 0 is read again)
+      for (int i = 0; i < cnt; i += 4) {
+        float x[4][kDPerLane];
 #pragma unroll
-      for (int e = 0; e < kDPerLane; ++e) acc[e] += w[sp * rec + 2 + lane * kDPerLane + e] * f;
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < kDPerLane; ++e) x[y][e] = v[min(i + y, cnt - 1) * rec + e];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const bool in = i + y < cnt;
+          const float fi = in ? __shfl(f, i + y, 64) : 0.f;
+          L += in ? __shfl(lf, i + y, 64) : 0.f;
+#pragma unroll
+          for (int e = 0; e < kDPerLane; ++e) acc[e] = fmaf(x[y][e], fi, acc[e]);
+        }
+      }
     }
   }
 #pragma unroll
