@@ -8,6 +8,7 @@ falls back to the CPU.  A missing or unloadable library raises KaraError.
 
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import re
@@ -144,19 +145,19 @@ _SIGS = {
                                              ctypes.POINTER(ctypes.c_size_t)]),
     "kara_recompute_queries": (_I32, [_PAR, ctypes.POINTER(KaraModel), _I32, _VP, _I32, ctypes.POINTER(LayerWeights),
                                       _VP, _VP, _PP, _PP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]),
-    "kara_q4_append": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _VP, _PP, _PP, _PP, _PP, _VP, _VP, _VP, _VP]),
-    "kara_q4_read": (_I32, [_PAR, _I32, _VP, _VP, _I32, _I32, _PP, _PP, _PP, _PP, _VP, _VP, _VP, _VP, _VP]),
+    "kara_q4_append": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "kara_q4_read": (_I32, [_PAR, _I32, _VP, _VP, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
     "kara_q4_attention_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
-    "kara_q4_attention": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _PP, _PP, _PP, _PP, _VP, _VP, _I32, _VP, _VP,
+    "kara_q4_attention": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _VP, _VP,
                                  ctypes.c_size_t, _VP]),
     "kara_evict_attention_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
-    "kara_evict_attention": (_I32, [_PAR, _I32, _VP, _I32, _VP, _PP, _PP, _PP, _PP, _PP, _VP, _VP, _I32, _I32, _VP, _VP,
+    "kara_evict_attention": (_I32, [_PAR, _I32, _VP, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _I32, _VP, _VP,
                                     ctypes.c_size_t, _VP]),
     "kara_evict_observe_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
-    "kara_evict_observe": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _PP, _PP, _PP, _VP, _VP, _I32, _I32, _VP,
+    "kara_evict_observe": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _I32, _VP,
                                   ctypes.c_size_t, _VP]),
     "kara_evict_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
-    "kara_evict_tokens": (_I32, [_PAR, _I32, _VP, _I32, _I32, _I32, _I32, _PP, _PP, _PP, _PP, _PP, _VP, _VP, _I32, _I32,
+    "kara_evict_tokens": (_I32, [_PAR, _I32, _VP, _I32, _I32, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _I32,
                                  _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]),
     "kara_sched_create": (_I32, [ctypes.POINTER(SchedConfig), _P32, ctypes.POINTER(ctypes.c_void_p)]),
     "kara_sched_destroy": (_I32, [_VP]),
@@ -520,207 +521,220 @@ def recompute_queries(p, m: KaraModel, trig, weights, hidden_in, hidden_out, k_p
         workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
-# ---- the cache held in 4 bits (include/kara_q4.h)
+# ---- the operators of include/kara_q4.h and include/kara_evict.h.  Their calls are
+# made once per layer group and step, from a few microseconds on: each tensor is
+# looked at once, and a call's pool pointers share one array.
 
 def _launch(stream):
-    """Current device and the stream's handle, which must be of that device:
-    the library launches where the process stands."""
+    """(torch, current device, the stream's handle); the stream must be of that
+    device, as the library launches where the process stands."""
     import torch
     dev = torch._C._cuda_getDevice()
     if stream is None:
-        return dev, torch._C._cuda_getCurrentRawStream(dev)
+        return torch, dev, torch._C._cuda_getCurrentRawStream(dev)
     if stream.device_index != dev:
         raise KaraError("marshal", ERR_INVALID_ARG, f"stream of device {stream.device_index}, current device {dev}")
-    return dev, stream.cuda_stream
+    return torch, dev, stream.cuda_stream
 
 
-def _on(dev, t):
-    """Pointer of a contiguous tensor on the current device (None: NULL)."""
+def _reject(dev, name, t, n, dtype):
+    """Says what is wrong with an argument that _arg would not take."""
     if t is None:
-        return None
+        raise KaraError("marshal", ERR_INVALID_ARG, f"{name}: missing")
+    _need(name, t, n, dtype)
     if t.get_device() != dev:
-        raise KaraError("marshal", ERR_INVALID_ARG, f"tensor on {t.device}, current device cuda:{dev}")
-    if not t.is_contiguous():
-        raise KaraError("marshal", ERR_INVALID_ARG, "tensor is not contiguous")
+        raise KaraError("marshal", ERR_INVALID_ARG, f"{name}: tensor on {t.device}, current device cuda:{dev}")
+    raise KaraError("marshal", ERR_INVALID_ARG, f"{name}: tensor is not contiguous")
+
+
+def _arg(dev, name, t, n, dtype):
+    """Pointer of a contiguous tensor of at least n elements on the current device."""
+    if t is None or t.dtype is not dtype or t.numel() < n or t.get_device() != dev or not t.is_contiguous():
+        _reject(dev, name, t, n, dtype)
     return t.data_ptr()
 
 
-def _array_on(dev, tensors):
-    return (ctypes.c_void_p * len(tensors))(*[_on(dev, t) for t in tensors]) if tensors is not None else None
-
-
-def _q4_pools(p, L, **pools):
-    """Codes (k_pools, v_pools) and scales (k_scales, v_scales) of L layers."""
-    import torch
-    rows = p.num_pages * p.n_kv_heads * p.block_size
-    for name, ts in pools.items():
-        n = rows * p.head_dim // (32 if name.endswith("scales") else 2)
+def _pool_args(dev, L, pools):
+    """pools: (name, one tensor per layer or None, elements, dtype).  Returns the
+    array of their pointers, to be kept until the call is made, and the address
+    of each pool's part (None: NULL)."""
+    ptrs, at = array.array("Q"), []
+    for name, ts, n, dtype in pools:
+        if ts is None:
+            at.append(None)
+            continue
         if len(ts) != L:
             raise KaraError("marshal", ERR_INVALID_ARG, f"{name}: {len(ts)} layers, expected {L}")
+        at.append(8 * len(ptrs))
         for i, t in enumerate(ts):
-            if t is None or t.dtype != torch.uint8 or t.numel() < n:
-                if t is None:
-                    raise KaraError("marshal", ERR_INVALID_ARG, f"{name}[{i}]: missing")
-                _need(f"{name}[{i}]", t, n, torch.uint8)
+            if t is None or t.dtype is not dtype or t.numel() < n or t.get_device() != dev or not t.is_contiguous():
+                _reject(dev, f"{name}[{i}]", t, n, dtype)
+            ptrs.append(t.data_ptr())
+    base = ptrs.buffer_info()[0]
+    return ptrs, [None if x is None else base + x for x in at]
 
 
-def _nbytes(workspace):
-    return workspace.numel() * workspace.element_size() if workspace is not None else 0
+def _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights=None, values=True):
+    """Pool arguments of a cache of rows (no scales) or of 4-bit codes."""
+    rows = p.num_pages * p.n_kv_heads * p.block_size
+    d = p.head_dim
+    if values and (k_scales is None) != (v_scales is None):
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales and v_scales: both or neither")
+    if k_scales is None:
+        n, dt = rows * d, torch.bfloat16 if p.dtype == BF16 else torch.float32
+    else:
+        n, dt = rows * d // 2, torch.uint8
+    pools = [("k_pools", k_pools, n, dt)]
+    if values:
+        pools.append(("v_pools", v_pools, n, dt))
+    pools.append(("k_scales", k_scales, rows * d // 32, torch.uint8))
+    if values:
+        pools.append(("v_scales", v_scales, rows * d // 32, torch.uint8))
+    if weights is not None:
+        pools.append(("weights", weights, rows, torch.float32))
+    return _pool_args(dev, L, pools)
 
+
+def _table_args(torch, dev, p, seqs, block_table, seq_lens):
+    n = p.n_seqs
+    return (_arg(dev, "seqs", seqs, 0, torch.int32),
+            _arg(dev, "block_table", block_table, n * p.max_blocks_per_seq, torch.int32),
+            _arg(dev, "seq_lens", seq_lens, n, torch.int32))
+
+
+def _workspace_arg(dev, workspace):
+    if workspace is None:
+        return None, 0
+    return _arg(dev, "workspace", workspace, 0, workspace.dtype), workspace.numel() * workspace.element_size()
+
+
+def _size(fn, *args) -> int:
+    out = ctypes.c_size_t(0)
+    _check(fn, getattr(load(), fn)(*args, ctypes.byref(out)))
+    return int(out.value)
+
+
+def _dtype(torch, p):
+    return torch.bfloat16 if p.dtype == BF16 else torch.float32
+
+
+# ---- the cache held in 4 bits (include/kara_q4.h)
 
 def q4_append(p, seqs, k_new, v_new, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, status, stream=None):
     """Quantises k_new / v_new [n_layers][n][n_new][Hkv][d] and appends them after each listed sequence's tokens."""
-    n, L = seqs.numel(), len(k_pools)
-    n_new = k_new.shape[2]
-    _need("seqs", seqs, 0, _i32())
-    for name, t in (("k_new", k_new), ("v_new", v_new)):
-        _need(name, t, L * n * n_new * p.n_kv_heads * p.head_dim, _dt(p))
-    _q4_pools(p, L, k_pools=k_pools, v_pools=v_pools, k_scales=k_scales, v_scales=v_scales)
-    _tables(p, block_table, seq_lens)
-    _need("status", status, n, _i32())
-    dev, s = _launch(stream)
-    _check("kara_q4_append", load().kara_q4_append(
-        ctypes.byref(p), n, _on(dev, seqs), n_new, L, _on(dev, k_new), _on(dev, v_new), _array_on(dev, k_pools),
-        _array_on(dev, v_pools), _array_on(dev, k_scales), _array_on(dev, v_scales), _on(dev, block_table),
-        _on(dev, seq_lens), _on(dev, status), s))
+    lib = load()
+    torch, dev, s = _launch(stream)
+    n, L, n_new = seqs.numel(), len(k_pools), k_new.shape[2]
+    size, dt = L * n * n_new * p.n_kv_heads * p.head_dim, _dtype(torch, p)
+    if k_scales is None or v_scales is None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
+    keep, (k, v, ks, vs) = _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    _check("kara_q4_append", lib.kara_q4_append(
+        ctypes.byref(p), n, sq, n_new, L, _arg(dev, "k_new", k_new, size, dt), _arg(dev, "v_new", v_new, size, dt),
+        k, v, ks, vs, bt, sl, _arg(dev, "status", status, n, torch.int32), s))
 
 
 def q4_read(p, seqs, start, n_rows, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, k_out, v_out,
             stream=None):
     """Rows [start[s], start[s] + n_rows) of each listed sequence into k_out / v_out [n_layers][n][n_rows][Hkv][d]."""
+    lib = load()
+    torch, dev, s = _launch(stream)
     n, L, n_rows = seqs.numel(), len(k_pools), int(n_rows)
-    _need("seqs", seqs, 0, _i32())
-    _need("start", start, p.n_seqs, _i32())
-    for name, t in (("k_out", k_out), ("v_out", v_out)):
-        _need(name, t, L * n * n_rows * p.n_kv_heads * p.head_dim, _dt(p))
-    _q4_pools(p, L, k_pools=k_pools, v_pools=v_pools, k_scales=k_scales, v_scales=v_scales)
-    _tables(p, block_table, seq_lens)
-    dev, s = _launch(stream)
-    _check("kara_q4_read", load().kara_q4_read(
-        ctypes.byref(p), n, _on(dev, seqs), _on(dev, start), n_rows, L, _array_on(dev, k_pools),
-        _array_on(dev, v_pools), _array_on(dev, k_scales), _array_on(dev, v_scales), _on(dev, block_table),
-        _on(dev, seq_lens), _on(dev, k_out), _on(dev, v_out), s))
+    size, dt = L * n * n_rows * p.n_kv_heads * p.head_dim, _dtype(torch, p)
+    if k_scales is None or v_scales is None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
+    keep, (k, v, ks, vs) = _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    _check("kara_q4_read", lib.kara_q4_read(
+        ctypes.byref(p), n, sq, _arg(dev, "start", start, p.n_seqs, torch.int32), n_rows, L, k, v, ks, vs, bt, sl,
+        _arg(dev, "k_out", k_out, size, dt), _arg(dev, "v_out", v_out, size, dt), s))
 
 
 def q4_attention_workspace_size(p, n, n_layers, n_query, max_len) -> int:
-    out = ctypes.c_size_t(0)
-    _check("kara_q4_attention_workspace_size", load().kara_q4_attention_workspace_size(
-        ctypes.byref(p), n, n_layers, n_query, max_len, ctypes.byref(out)))
-    return int(out.value)
+    return _size("kara_q4_attention_workspace_size", ctypes.byref(p), n, n_layers, n_query, max_len)
 
 
 def q4_attention(p, seqs, n_query, q, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, max_len, out,
                  workspace, stream=None):
     """Causal attention of each listed sequence's last n_query tokens; q, out [n_layers][n][n_query][Hq][d]."""
+    lib = load()
+    torch, dev, s = _launch(stream)
     n, L, n_query = seqs.numel(), len(k_pools), int(n_query)
-    _need("seqs", seqs, 0, _i32())
-    for name, t in (("q", q), ("out", out)):
-        _need(name, t, L * n * n_query * p.n_q_heads * p.head_dim, _dt(p))
-    _q4_pools(p, L, k_pools=k_pools, v_pools=v_pools, k_scales=k_scales, v_scales=v_scales)
-    _tables(p, block_table, seq_lens)
-    dev, s = _launch(stream)
-    _check("kara_q4_attention", load().kara_q4_attention(
-        ctypes.byref(p), n, _on(dev, seqs), L, n_query, _on(dev, q), _array_on(dev, k_pools), _array_on(dev, v_pools),
-        _array_on(dev, k_scales), _array_on(dev, v_scales), _on(dev, block_table), _on(dev, seq_lens), int(max_len),
-        _on(dev, out), _on(dev, workspace), _nbytes(workspace), s))
+    size, dt = L * n * n_query * p.n_q_heads * p.head_dim, _dtype(torch, p)
+    if k_scales is None or v_scales is None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
+    keep, (k, v, ks, vs) = _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    ws, ws_bytes = _workspace_arg(dev, workspace)
+    _check("kara_q4_attention", lib.kara_q4_attention(
+        ctypes.byref(p), n, sq, L, n_query, _arg(dev, "q", q, size, dt), k, v, ks, vs, bt, sl, int(max_len),
+        _arg(dev, "out", out, size, dt), ws, ws_bytes, s))
 
 
 # ---- eviction by accumulated attention weight (include/kara_evict.h)
 
-def _either_cache(p, L, k_pools, v_pools, k_scales, v_scales, weights):
-    """Pools of rows (no scales) or of 4-bit codes, and the accumulators; v_pools may be left out."""
-    if (k_scales is None) != (v_scales is None) and v_pools is not None:
-        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales and v_scales: both or neither")
-    given = {"k_pools": k_pools, "v_pools": v_pools} if v_pools is not None else {"k_pools": k_pools}
-    if k_scales is not None:
-        if v_pools is not None:
-            _q4_pools(p, L, k_scales=k_scales, v_scales=v_scales, **given)
-        else:
-            _q4_pools(p, L, k_scales=k_scales, **given)
-    else:
-        for name, ts in given.items():
-            if len(ts) != L:
-                raise KaraError("marshal", ERR_INVALID_ARG, f"{name}: {len(ts)} layers, expected {L}")
-            _pools(p, ts, name)
-    n = p.num_pages * p.n_kv_heads * p.block_size
-    if len(weights) != L:
-        raise KaraError("marshal", ERR_INVALID_ARG, f"weights: {len(weights)} layers, expected {L}")
-    for i, t in enumerate(weights):
-        _need(f"weights[{i}]", t, n, _f32())
-
-
 def evict_attention_workspace_size(p, n, n_layers, max_len) -> int:
-    out = ctypes.c_size_t(0)
-    _check("kara_evict_attention_workspace_size", load().kara_evict_attention_workspace_size(
-        ctypes.byref(p), n, n_layers, max_len, ctypes.byref(out)))
-    return int(out.value)
+    return _size("kara_evict_attention_workspace_size", ctypes.byref(p), n, n_layers, max_len)
 
 
 def evict_attention(p, seqs, q, k_pools, v_pools, weights, block_table, seq_lens, n_new, max_len, out, workspace,
                     k_scales=None, v_scales=None, stream=None):
     """decode_attention that adds every key's weight to its accumulator (weights:
     fp32 [num_pages][Hkv][block_size] per layer); fp32 out of q's shape."""
+    lib = load()
+    torch, dev, s = _launch(stream)
     n, L = seqs.numel(), len(k_pools)
-    _need("seqs", seqs, 0, _i32())
-    _need("q", q, L * n * p.n_q_heads * p.head_dim, _dt(p))
-    _need("out", out, L * n * p.n_q_heads * p.head_dim, _f32())
-    _either_cache(p, L, k_pools, v_pools, k_scales, v_scales, weights)
-    _tables(p, block_table, seq_lens)
-    dev, s = _launch(stream)
-    _check("kara_evict_attention", load().kara_evict_attention(
-        ctypes.byref(p), n, _on(dev, seqs), L, _on(dev, q), _array_on(dev, k_pools), _array_on(dev, v_pools),
-        _array_on(dev, k_scales), _array_on(dev, v_scales), _array_on(dev, weights), _on(dev, block_table),
-        _on(dev, seq_lens), int(n_new), int(max_len), _on(dev, out), _on(dev, workspace), _nbytes(workspace), s))
+    size = L * n * p.n_q_heads * p.head_dim
+    keep, (k, v, ks, vs, w) = _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    ws, ws_bytes = _workspace_arg(dev, workspace)
+    _check("kara_evict_attention", lib.kara_evict_attention(
+        ctypes.byref(p), n, sq, L, _arg(dev, "q", q, size, _dtype(torch, p)), k, v, ks, vs, w, bt, sl, int(n_new),
+        int(max_len), _arg(dev, "out", out, size, torch.float32), ws, ws_bytes, s))
 
 
 def evict_observe_workspace_size(p, n, n_layers, n_query, max_len) -> int:
-    out = ctypes.c_size_t(0)
-    _check("kara_evict_observe_workspace_size", load().kara_evict_observe_workspace_size(
-        ctypes.byref(p), n, n_layers, n_query, max_len, ctypes.byref(out)))
-    return int(out.value)
+    return _size("kara_evict_observe_workspace_size", ctypes.byref(p), n, n_layers, n_query, max_len)
 
 
 def evict_observe(p, seqs, n_query, q, k_pools, weights, block_table, seq_lens, n_new, max_len, workspace, k_scales=None,
                   stream=None):
     """Adds the weights that each listed sequence's last n_query tokens give
     (q [n_layers][n][n_query][Hq][d]) to the accumulators."""
+    lib = load()
+    torch, dev, s = _launch(stream)
     n, L, n_query = seqs.numel(), len(k_pools), int(n_query)
-    _need("seqs", seqs, 0, _i32())
-    _need("q", q, L * n * n_query * p.n_q_heads * p.head_dim, _dt(p))
-    _either_cache(p, L, k_pools, None, k_scales, None, weights)
-    _tables(p, block_table, seq_lens)
-    dev, s = _launch(stream)
-    _check("kara_evict_observe", load().kara_evict_observe(
-        ctypes.byref(p), n, _on(dev, seqs), L, n_query, _on(dev, q), _array_on(dev, k_pools), _array_on(dev, k_scales),
-        _array_on(dev, weights), _on(dev, block_table), _on(dev, seq_lens), int(n_new), int(max_len),
-        _on(dev, workspace), _nbytes(workspace), s))
+    size = L * n * n_query * p.n_q_heads * p.head_dim
+    keep, (k, ks, w) = _cache_args(torch, dev, p, L, k_pools, None, k_scales, None, weights, values=False)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    ws, ws_bytes = _workspace_arg(dev, workspace)
+    _check("kara_evict_observe", lib.kara_evict_observe(
+        ctypes.byref(p), n, sq, L, n_query, _arg(dev, "q", q, size, _dtype(torch, p)), k, ks, w, bt, sl, int(n_new),
+        int(max_len), ws, ws_bytes, s))
 
 
 def evict_workspace_size(p, n, n_layers, keep) -> int:
-    out = ctypes.c_size_t(0)
-    _check("kara_evict_workspace_size", load().kara_evict_workspace_size(
-        ctypes.byref(p), n, n_layers, keep, ctypes.byref(out)))
-    return int(out.value)
+    return _size("kara_evict_workspace_size", ctypes.byref(p), n, n_layers, keep)
 
 
 def evict_tokens(p, seqs, keep, n_sink, n_recent, k_pools, v_pools, weights, block_table, seq_lens, max_len, commit,
                  status, workspace, kept=None, freed=None, n_freed=None, k_scales=None, v_scales=None, stream=None):
     """Cuts every listed sequence longer than `keep` to that many tokens: the first
     n_sink, the last n_recent and the largest accumulators between."""
+    lib = load()
+    torch, dev, s = _launch(stream)
     n, L, keep = seqs.numel(), len(k_pools), int(keep)
-    _need("seqs", seqs, 0, _i32())
-    _either_cache(p, L, k_pools, v_pools, k_scales, v_scales, weights)
-    _tables(p, block_table, seq_lens)
-    _need("kept", kept, L * n * p.n_kv_heads * keep, _i32())
-    _need("freed", freed, n * p.max_blocks_per_seq, _i32())
-    _need("n_freed", n_freed, n, _i32())
-    _need("status", status, n, _i32())
-    dev, s = _launch(stream)
-    _check("kara_evict_tokens", load().kara_evict_tokens(
-        ctypes.byref(p), n, _on(dev, seqs), L, keep, int(n_sink), int(n_recent), _array_on(dev, k_pools),
-        _array_on(dev, v_pools), _array_on(dev, k_scales), _array_on(dev, v_scales), _array_on(dev, weights),
-        _on(dev, block_table), _on(dev, seq_lens), int(max_len), int(bool(commit)), _on(dev, kept), _on(dev, freed),
-        _on(dev, n_freed), _on(dev, status), _on(dev, workspace), _nbytes(workspace), s))
+    i32 = torch.int32
+    held, (k, v, ks, vs, w) = _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    ws, ws_bytes = _workspace_arg(dev, workspace)
+    _check("kara_evict_tokens", lib.kara_evict_tokens(
+        ctypes.byref(p), n, sq, L, keep, int(n_sink), int(n_recent), k, v, ks, vs, w, bt, sl, int(max_len),
+        int(bool(commit)), None if kept is None else _arg(dev, "kept", kept, L * n * p.n_kv_heads * keep, i32),
+        None if freed is None else _arg(dev, "freed", freed, n * p.max_blocks_per_seq, i32),
+        None if n_freed is None else _arg(dev, "n_freed", n_freed, n, i32), _arg(dev, "status", status, n, i32),
+        ws, ws_bytes, s))
 
 
 # ---- periodic compression policy (include/kara_sched.h): host runtime
