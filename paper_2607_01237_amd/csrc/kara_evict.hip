@@ -31,14 +31,15 @@ constexpr int kFinThreads = 256;
 constexpr int kFinKeys = 4 * kFinThreads;   // keys per workgroup
 
 // Second half of a counting decoding step: the splits' records joined to the
-// output, and every key's weight -- exp2(logit - M) / L over the group's query
+// output (a record: maximum and sum, ml_step apart, and o, o_step apart), and every
+// key's weight -- exp2(logit - M) / L over the group's query
 // heads -- added to its accumulator.  One workgroup per (layer, sequence, KV
 // head, 1024 keys); a sequence's workgroups share out its query heads' outputs.
 template <int D>
 __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
     Geom g, int n, const int32_t* __restrict__ seqs, const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens,
-    int n_new, int max_len, int split_keys, int n_splits, int chunks, const float* __restrict__ records,
-    const float* __restrict__ logits, int64_t ld, WeightPtrs wp, float* __restrict__ out) {
+    int n_new, int max_len, int split_keys, int n_splits, int chunks, const float* __restrict__ rec_ml, int ml_step,
+    const float* __restrict__ rec_o, int o_step, const float* __restrict__ logits, int64_t ld, WeightPtrs wp, float* __restrict__ out) {
   __shared__ float red_m[kMaxGroup], red_i[kMaxGroup];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t rest = blockIdx.x;
@@ -58,29 +59,30 @@ __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
   }
   const int k0 = chunk * kFinKeys;
   if (k0 >= len) return;
-  constexpr int rec = D + 2;
   const int ns = (len + split_keys - 1) / split_keys;
   const int nc = (len + kFinKeys - 1) / kFinKeys;      // this sequence's workgroups
   int dup = 0;
   for (int o = tid; o < j; o += kFinThreads) dup |= seqs[o] == s;
   for (int i = wave; i < G; i += kFinThreads / 64) {
-    const float* w = records + (orow + i) * n_splits * rec;
+    const float* w = rec_ml + (orow + i) * n_splits * ml_step;
     float M = kMaxFloor, L = 0.f;
-    for (int sp = lane; sp < ns; sp += 64) M = fmaxf(M, w[(int64_t)sp * rec]);
+    for (int sp = lane; sp < ns; sp += 64) M = fmaxf(M, w[(int64_t)sp * ml_step]);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
-    for (int sp = lane; sp < ns; sp += 64) L += w[(int64_t)sp * rec + 1] * __builtin_amdgcn_exp2f(w[(int64_t)sp * rec] - M);
+    for (int sp = lane; sp < ns; sp += 64) 
+      L += w[(int64_t)sp * ml_step + 1] * __builtin_amdgcn_exp2f(w[(int64_t)sp * ml_step] - M);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) L += __shfl_xor(L, x, 64);
     if (lane == 0) red_m[i] = M, red_i[i] = 1.f / L;
   }
   dup = __syncthreads_or(dup);
   for (int i = chunk; i < G; i += nc) {
-    const float* w = records + (orow + i) * n_splits * rec;
+    const float* w = rec_ml + (orow + i) * n_splits * ml_step;
+    const float* o = rec_o + (orow + i) * n_splits * o_step;
     for (int e = tid; e < D; e += kFinThreads) {
       float acc = 0.f;
       for (int sp = 0; sp < ns; ++sp)
-        acc += w[(int64_t)sp * rec + 2 + e] * __builtin_amdgcn_exp2f(w[(int64_t)sp * rec] - red_m[i]);
+        acc += o[(int64_t)sp * o_step + e] * __builtin_amdgcn_exp2f(w[(int64_t)sp * ml_step] - red_m[i]);
       out[(orow + i) * D + e] = acc * red_i[i];
     }
   }
@@ -497,7 +499,8 @@ kara_status_t kara_evict_attention(const kara_params_t* p, int32_t n, const int3
     a.vp = vp;
     a.ksp = ptrs(k_scales, n_layers);
     a.vsp = ptrs(v_scales, n_layers);
-    a.ws = records;
+    a.rec_o = records;
+    a.rec_ml = records + (int64_t)n_layers * n * g.Hq * a.n_splits * g.d;
     a.logits = logits;
     a.ld = w.ld;
     e = launch_q4_split(a, true, s);
@@ -506,13 +509,17 @@ kara_status_t kara_evict_attention(const kara_params_t* p, int32_t n, const int3
   }
   if (e != hipSuccess) return hip_status(e);
   const int n_splits = (max_len + keys - 1) / keys;
+  // rows' records are m, l, o[d]; 4-bit ones hold o and m, l apart
+  const float* rec_o = k_scales ? records : records + 2;
+  const float* rec_ml = k_scales ? records + (int64_t)n_layers * n * g.Hq * n_splits * g.d : records;
+  const int o_step = k_scales ? g.d : g.d + 2, ml_step = k_scales ? 2 : g.d + 2;
   const dim3 grid((unsigned)(units * chunks)), block(kFinThreads);
   if (g.d == 128)
     hipLaunchKernelGGL((evict_finish_kernel<128>), grid, block, 0, s, g, n, seqs, block_table, seq_lens, n_new, max_len, keys,
-                       n_splits, chunks, (const float*)records, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
+                       n_splits, chunks, rec_ml, ml_step, rec_o, o_step, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
   else
     hipLaunchKernelGGL((evict_finish_kernel<64>), grid, block, 0, s, g, n, seqs, block_table, seq_lens, n_new, max_len, keys,
-                       n_splits, chunks, (const float*)records, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
+                       n_splits, chunks, rec_ml, ml_step, rec_o, o_step, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
   return hip_status(hipGetLastError());
 }
 

@@ -126,7 +126,7 @@ struct Q4Split {
   const int32_t *seqs, *bt, *seq_lens;
   const void* q;              // [n_layers][n][T][Hq][d]
   PoolPtrs kp, vp, ksp, vsp;  // codes and scales
-  float* ws;                  // records [n_layers][n][T][Hq][n_splits]: m, l, o[d]
+  float *rec_o, *rec_ml;      // records [n_layers][n][T][Hq][n_splits]: o[d]; m, l
   void* out;                  // [n_layers][n][T][Hq][d]
   int out_bf16;
   float* logits;              // [n_layers][n][Hkv][G][ld] q . k, T = 1
@@ -142,6 +142,16 @@ hipError_t launch_decode_logits(const Geom& g, int n, const int32_t* seqs, int n
 int q4_split_keys(const Geom& g, int64_t units, int max_len);
 // logits: fill a.logits, and leave records (never out) for every sequence.
 hipError_t launch_q4_split(Q4Split a, bool logits, hipStream_t stream);
+
+// The same for many query rows (kara_q4_chunk.hip), which pass a workgroup's rows
+// over converted keys; n_rt counts its row blocks.
+constexpr int kQ4ChunkWgs = 256;   // most workgroups of a launch that splits its keys
+struct Q4ChunkPlan {
+  int rows_wg, n_rb, splits, split_keys;
+  int64_t blocks;
+};
+Q4ChunkPlan q4_chunk_plan(const Geom& g, int n, int n_layers, int T, int max_len);
+hipError_t launch_q4_chunk(const Q4Split& a, const Q4ChunkPlan& x, hipStream_t stream);
 
 }  // namespace kara
 

@@ -549,21 +549,21 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
       if (a.out_bf16) ((__bf16*)a.out)[at * D + e] = (__bf16)v;
       else ((float*)a.out)[at * D + e] = v;
     } else {
-      float* rec = a.ws + (at * a.n_splits + split) * (D + 2);
-      if (e == 0) rec[0] = M, rec[1] = L;
-      rec[2 + e] = O;
+      const int64_t rec = at * a.n_splits + split;
+      if (e == 0) a.rec_ml[2 * rec] = M, a.rec_ml[2 * rec + 1] = L;
+      a.rec_o[rec * D + e] = O;
     }
   }
 }
 
-// One wave per output row of a sequence longer than one split: its splits'
-// records joined.
+// One wave per output row of a sequence longer than one split (all: of every
+// sequence): its splits' records joined.
 template <int D>
 __global__ __launch_bounds__(256) void q4_combine_kernel(Geom g, int n, int T, const int32_t* __restrict__ seqs,
                                                          const int32_t* __restrict__ seq_lens, int max_len,
                                                          int split_keys, int n_splits, int64_t n_rows,
-                                                         const float* __restrict__ ws, void* __restrict__ out,
-                                                         int out_bf16) {
+                                                         const float* __restrict__ rec_ml, const float* __restrict__ rec_o,
+                                                         void* __restrict__ out, int out_bf16, int all) {
   constexpr int kDPerLane = D / 64;
   const int lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);   // (l, j, t, hq)
@@ -571,36 +571,31 @@ __global__ __launch_bounds__(256) void q4_combine_kernel(Geom g, int n, int T, c
   const int s = seqs[(row / ((int64_t)g.Hq * T)) % n];
   const int len = s >= 0 && s < g.n_seqs ? seq_lens[s] : 0;
   const bool none = len <= 0 || len > max_len;
-  if (!none && len <= split_keys) return;   // the split kernel wrote it
+  if (!all && !none && len <= split_keys) return;   // the split kernel wrote it
   float L = 0.f, acc[kDPerLane] = {};
   if (!none) {
     const int ns = (len + split_keys - 1) / split_keys;
-    constexpr int rec = D + 2;
-    const float* w = ws + row * n_splits * rec;
+    const float* ml = rec_ml + row * n_splits * 2;
     // lane i: split i's maximum and sum, 64 at a time, the first kept
-    const float m0 = lane < ns ? w[lane * rec] : kMaxFloor, l0 = lane < ns ? w[lane * rec + 1] : 0.f;
+    const float m0 = lane < ns ? ml[2 * lane] : kMaxFloor, l0 = lane < ns ? ml[2 * lane + 1] : 0.f;
     float M = m0;
-    for (int sp = lane + 64; sp < ns; sp += 64) M = fmaxf(M, w[sp * rec]);
+    for (int sp = lane + 64; sp < ns; sp += 64) M = fmaxf(M, ml[2 * sp]);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
     for (int sp0 = 0; sp0 < ns; sp0 += 64) {
-      float f, lf;
-      if (sp0 == 0) {
-        f = __builtin_amdgcn_exp2f(m0 - M);
-        lf = l0 * f;
-      } else {
-        f = sp0 + lane < ns ? __builtin_amdgcn_exp2f(w[(sp0 + lane) * rec] - M) : 0.f;
-        lf = sp0 + lane < ns ? w[(sp0 + lane) * rec + 1] * f : 0.f;
-      }
+      const int sp = sp0 + lane;
+      const float ms = sp0 == 0 ? m0 : sp < ns ? ml[2 * sp] : kMaxFloor;
+      const float f = __builtin_amdgcn_exp2f(ms - M);
+      const float lf = (sp0 == 0 ? l0 : sp < ns ? ml[2 * sp + 1] : 0.f) * f;
       const int cnt = min(64, ns - sp0);
-      const float* v = w + (int64_t)sp0 * rec + 2 + lane * kDPerLane;
+      const float* v = rec_o + (row * n_splits + sp0) * D + lane * kDPerLane;
       // (four records at once; past the last a record of weight 0 is read again)
       for (int i = 0; i < cnt; i += 4) {
         float x[4][kDPerLane];
 #pragma unroll
         for (int y = 0; y < 4; ++y)
 #pragma unroll
-          for (int e = 0; e < kDPerLane; ++e) x[y][e] = v[min(i + y, cnt - 1) * rec + e];
+          for (int e = 0; e < kDPerLane; ++e) x[y][e] = v[min(i + y, cnt - 1) * D + e];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
           const bool in = i + y < cnt;
@@ -632,6 +627,11 @@ int split_keys_of(int bs, int64_t units, int max_len) {
   while (keys < most && units * ((max_len + 2 * keys - 1) / (2 * keys)) >= kSplitWgTarget) keys *= 2;
   return keys;
 }
+
+// Up to this many query rows per (layer, sequence, KV head) go through the split
+// kernel, 16 a workgroup; more through the chunk kernel.
+constexpr int kFewRows = 64;
+bool few_rows(const Geom& g, int T) { return (int64_t)g.G * T <= kFewRows; }
 
 // a grid of one dimension: HIP counts its threads in 32 bits
 bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
@@ -752,8 +752,16 @@ kara_status_t kara_q4_attention_workspace_size(const kara_params_t* p, int32_t n
   if (!bytes || !layers_ok(n, n_layers) || n_query < 1 || max_len < 1 || (int64_t)max_len > (int64_t)g.max_blocks * g.bs ||
       (int64_t)n_query * g.Hq > INT32_MAX / 4)
     return KARA_ERR_INVALID_ARG;
-  const int64_t n_splits = (max_len + kSplitMin - 1) / kSplitMin;
-  *bytes = n_splits == 1 ? 0 : (size_t)n_layers * n * n_query * g.Hq * n_splits * (g.d + 2) * sizeof(float);
+  const size_t rec = (g.d + 2) * sizeof(float);
+  const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
+  if (few_rows(g, n_query)) {
+    const int64_t n_splits = (max_len + kSplitMin - 1) / kSplitMin;
+    *bytes = n_splits == 1 ? 0 : (size_t)(rows * n_splits) * rec;
+  } else {
+    // (a launch that splits its keys has so many workgroups at most, records and all)
+    const Q4ChunkPlan x = q4_chunk_plan(g, n, n_layers, n_query, max_len);
+    *bytes = (size_t)kQ4ChunkWgs * x.rows_wg * rec;
+  }
   return KARA_OK;
 }
 
@@ -777,12 +785,23 @@ kara_status_t kara_q4_attention(const kara_params_t* p, int32_t n, const int32_t
   a.n = n;
   a.n_layers = n_layers;
   a.T = n_query;
-  a.n_rt = (int)(((int64_t)g.G * n_query + 15) / 16);
-  const int64_t units = (int64_t)n_layers * n * g.Hkv * a.n_rt;
-  a.split_keys = split_keys_of(g.bs, units, max_len);
-  a.n_splits = (max_len + a.split_keys - 1) / a.split_keys;
+  const bool few = few_rows(g, n_query);
   const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
-  if (!grid_ok(units * a.n_splits) || !grid_ok((rows + 3) / 4)) return KARA_ERR_UNSUPPORTED;
+  Q4ChunkPlan plan{};
+  if (few) {
+    a.n_rt = (int)(((int64_t)g.G * n_query + 15) / 16);
+    const int64_t units = (int64_t)n_layers * n * g.Hkv * a.n_rt;
+    a.split_keys = split_keys_of(g.bs, units, max_len);
+    a.n_splits = (max_len + a.split_keys - 1) / a.split_keys;
+    if (!grid_ok(units * a.n_splits)) return KARA_ERR_UNSUPPORTED;
+  } else {
+    plan = q4_chunk_plan(g, n, n_layers, n_query, max_len);
+    a.n_rt = plan.n_rb;
+    a.split_keys = plan.split_keys;
+    a.n_splits = plan.splits;
+    if (!grid_ok(2 * plan.blocks)) return KARA_ERR_UNSUPPORTED;
+  }
+  if (!grid_ok((rows + 3) / 4)) return KARA_ERR_UNSUPPORTED;
   a.max_len = max_len;
   a.seqs = seqs;
   a.bt = block_table;
@@ -792,18 +811,21 @@ kara_status_t kara_q4_attention(const kara_params_t* p, int32_t n, const int32_t
   a.vp = ptrs(v_pools, n_layers);
   a.ksp = ptrs(k_scales, n_layers);
   a.vsp = ptrs(v_scales, n_layers);
-  a.ws = (float*)workspace;
+  a.rec_o = (float*)workspace;
+  a.rec_ml = a.rec_o + rows * a.n_splits * g.d;
   a.out = out;
   a.out_bf16 = g.dtype == KARA_BF16;
-  hipError_t e = launch_q4_split(a, false, (hipStream_t)stream);
+  const hipError_t e = few ? launch_q4_split(a, false, (hipStream_t)stream) : launch_q4_chunk(a, plan, (hipStream_t)stream);
   if (e != hipSuccess || a.n_splits == 1) return hip_status(e);
   const dim3 grid((unsigned)((rows + 3) / 4));
   if (g.d == 128)
     hipLaunchKernelGGL((q4_combine_kernel<128>), grid, dim3(256), 0, (hipStream_t)stream, g, n, n_query, seqs, seq_lens,
-                       max_len, a.split_keys, a.n_splits, rows, (const float*)a.ws, out, (int)a.out_bf16);
+                       max_len, a.split_keys, a.n_splits, rows, (const float*)a.rec_ml, (const float*)a.rec_o, out,
+                       (int)a.out_bf16, (int)!few);
   else
     hipLaunchKernelGGL((q4_combine_kernel<64>), grid, dim3(256), 0, (hipStream_t)stream, g, n, n_query, seqs, seq_lens,
-                       max_len, a.split_keys, a.n_splits, rows, (const float*)a.ws, out, (int)a.out_bf16);
+                       max_len, a.split_keys, a.n_splits, rows, (const float*)a.rec_ml, (const float*)a.rec_o, out,
+                       (int)a.out_bf16, (int)!few);
   return hip_status(hipGetLastError());
 }
 

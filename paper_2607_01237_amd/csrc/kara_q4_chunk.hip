@@ -1,0 +1,372 @@
+// Attention of many query rows over the 4-bit cache (kara_q4_attention): a
+// prompt's chunk over what is cached.  Bound by the matrix products.
+//
+// One workgroup of 8 waves owns 128 QT query rows of one (layer, sequence, KV
+// head), rows ordered (query, head in group), and walks the keys they see 64 at a
+// time.  Its threads fetch a chunk's codes two chunks ahead into registers (16
+// bytes, one block of 32 values with its scale, per thread at d = 128), convert
+// them in hardware to bf16 -- exactly -- and write them to the other of two LDS
+// stages while the products of the present one run: a chunk is converted once for
+// all rows, with one barrier.  From there the products are those of the recompute
+// attention: S^T = K Q^T, weights as they stand the B operand of O^T += V^T P^T with
+// V through the transposed LDS read, the row sums one more product with ones.
+//
+// NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones).
+#include <algorithm>
+#include <type_traits>
+
+#include "kara_q4_device.h"
+
+namespace kara {
+namespace {
+
+constexpr int kChThreads = 512;
+constexpr int kChWaves = kChThreads / 64;
+constexpr int kChKeys = 64;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kMaxFloor = -3.402823466e38f;
+constexpr float kHeadroom = 8.f;
+
+template <int D>
+struct ChCfg {
+  static constexpr int kRow = D * 2;                 // bytes of a row in LDS
+  static constexpr int kChunks = kRow / 16;
+  static constexpr int kKS = D / 32;                 // products per dot product
+  static constexpr int kDT = D / 16;                 // 16-row tiles of O^T
+  static constexpr int kTile = kChKeys * kRow;       // a chunk of K, or of V
+  static constexpr int kParts = D / kQ4Block;        // blocks of a row
+  static constexpr int kStagers = 2 * kChKeys * kParts;   // threads with a block to convert
+  static_assert(kStagers <= kChThreads, "a block per thread");
+  // XOR swizzles of a row's 16-byte chunks: those of the recompute attention
+  static __device__ __forceinline__ int swz_k(int row) {
+    if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    return ((row & 3) << 1) | ((row >> 2) & 1);
+  }
+  static __device__ __forceinline__ int swz_v(int row) { return (2 * (D == 128 ? row : row >> 1)) & (kChunks - 1); }
+};
+
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+__device__ inline v4i16 read_tr(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) v4i16*)(__attribute__((address_space(3))) char*)p);
+}
+
+template <int NT, int D, int QT>
+__global__ __launch_bounds__(kChThreads, 1) void q4_chunk_kernel(Q4Split a) {
+  using C = ChCfg<D>;
+  constexpr int KS = C::kKS, DT = C::kDT;
+  __shared__ __attribute__((aligned(16))) char smem[2][2 * C::kTile];
+  const Geom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int gq = lane >> 4, li = lane & 15;
+
+  // All row blocks and splits of a (layer, sequence, KV head) on one XCD, whose L2
+  // then holds its codes once, where the units divide among the 8.
+  uint32_t u, rest = blockIdx.x;
+  const uint32_t per = (uint32_t)a.n_rt * (uint32_t)a.n_splits;
+  const uint32_t units = (uint32_t)(a.n_layers * a.n * g.Hkv);
+  if (units % 8 == 0) {
+    u = rest / (8 * per) * 8 + rest % 8;
+    rest = rest / 8 % per;
+  } else {
+    u = rest / per;
+    rest = rest % per;
+  }
+  const int split = rest % (uint32_t)a.n_splits;
+  const int rb = a.n_rt - 1 - (int)(rest / (uint32_t)a.n_splits);     // the blocks that see most keys first
+  const int h = u % (uint32_t)g.Hkv;
+  u /= (uint32_t)g.Hkv;
+  const int j = u % (uint32_t)a.n, l = u / (uint32_t)a.n;
+  const int s = a.seqs[j];
+  const int G = g.G, T = a.T, R = G * T;
+  const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
+  const int row0 = rb * kChWaves * 16 * QT;
+  const int64_t orow = ((int64_t)l * a.n + j) * T * g.Hq + h * G;
+  const bool none = len <= 0 || len > a.max_len;
+  const int first = len - T;                               // position of query 0
+  const int last_pos = first + (min(row0 + kChWaves * 16 * QT, R) - 1) / G;
+  const int k_lo = split * a.split_keys;
+  const int k_hi = none ? 0 : min(last_pos + 1, k_lo + a.split_keys);
+  const int n_chunks = k_hi > k_lo ? (k_hi - k_lo + kChKeys - 1) / kChKeys : 0;
+
+  // ---- this wave's queries as B operands (lane: query li of each tile) ----
+  const int wrow0 = row0 + wave * 16 * QT;
+  bf16x8 qop[QT][NT][KS];
+  int qpos[QT];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const int r = min(wrow0 + qt * 16 + li, R - 1);
+    const int t = r / G;
+    qpos[qt] = first + t;
+    const int64_t at = (orow + (int64_t)t * g.Hq + (r - t * G)) * D;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      if constexpr (NT == 1) {
+        qop[qt][0][x] = *(const bf16x8*)((const __bf16*)a.q + at + (gq * KS + x) * 8);
+      } else {
+        const floatx4* src = (const floatx4*)((const float*)a.q + at + (gq * KS + x) * 8);
+        const floatx4 p = src[0], q = src[1];
+        uint32_t w[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bf16_term_pairs(i < 2 ? p[2 * i] : q[2 * i - 4], i < 2 ? p[2 * i + 1] : q[2 * i - 3], w[i]);
+#pragma unroll
+        for (int y = 0; y < NT; ++y) qop[qt][y][x] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
+      }
+    }
+  }
+  const int wave_first_pos = first + min(wrow0, R - 1) / G;
+  const int wave_last_pos = first + min(wrow0 + 16 * QT - 1, R - 1) / G;
+
+  floatx4 o[QT][DT], lsum[QT];
+  float m[QT];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    m[qt] = kMaxFloor;
+    lsum[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[qt][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  bf16x8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
+  const float c = g.scale * kLog2e;
+
+  // ---- staging: thread (K|V, key, block) ----
+  const bool stager = tid < C::kStagers;
+  const bool is_v = tid >= C::kStagers / 2;
+  const int skey = (tid % (C::kStagers / 2)) / C::kParts, sblk = tid % C::kParts;
+  const char* codes = (const char*)(is_v ? a.vp.p[l] : a.kp.p[l]);
+  const uint8_t* scales = (const uint8_t*)(is_v ? a.vsp.p[l] : a.ksp.p[l]);
+  const int32_t* row_pages = a.bt + (int64_t)(none ? 0 : s) * g.max_blocks;
+  // (keys past the last one repeat it, finite and masked for every query)
+  auto pos_of = [&](int ch) __attribute__((always_inline)) { return min(k_lo + ch * kChKeys + skey, k_hi - 1); };
+  auto page_of = [&](int ch) __attribute__((always_inline)) { return row_pages[pos_of(ch) / g.bs]; };
+  uint4 cw;
+  uint32_t cscale = 0;
+  int page = 0;
+  auto fetch = [&](int ch) __attribute__((always_inline)) {
+    const int pos = pos_of(ch), b = pos / g.bs;
+    const int pg = min(max(page, 0), g.num_pages - 1);
+    const uint64_t row = (uint64_t)(((int64_t)pg * g.Hkv + h) * g.bs + (pos - b * g.bs));
+    cw = *(const uint4*)(codes + row * (D / 2) + sblk * 16);
+    cscale = scales[row * C::kParts + sblk];
+  };
+  // A block's four octets go to LDS in an order that differs by row, so that the 16
+  // lanes of four rows write 16 different chunks at a time: octet i ^ (row & 3) at
+  // step i, its words exchanged beforehand.
+  const int turn = skey & 3;
+  char* const to0 = &smem[0][(is_v ? C::kTile : 0) + skey * C::kRow];
+  const int swz = is_v ? C::swz_v(skey) : C::swz_k(skey & 15);
+  auto stage = [&](int st) __attribute__((always_inline)) {
+    const float scale = q4_scale(cscale);
+    uint32_t w0 = cw.x, w1 = cw.y, w2 = cw.z, w3 = cw.w;
+    {
+      const uint32_t a0 = turn & 1 ? w1 : w0, a1 = turn & 1 ? w0 : w1, a2 = turn & 1 ? w3 : w2, a3 = turn & 1 ? w2 : w3;
+      w0 = turn & 2 ? a2 : a0, w1 = turn & 2 ? a3 : a1, w2 = turn & 2 ? a0 : a2, w3 = turn & 2 ? a1 : a3;
+    }
+    const uint32_t w[4] = {w0, w1, w2, w3};
+    char* to = to0 + st * 2 * C::kTile;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bf16x8 v = q4_octet(w[i], scale);
+      *(bf16x8*)(to + (((sblk * 4 + (i ^ turn)) ^ swz) * 16)) = v;
+    }
+  };
+
+  int koff[KS], voff[DT];
+#pragma unroll
+  for (int x = 0; x < KS; ++x) koff[x] = li * C::kRow + (((gq * KS + x) ^ C::swz_k(li)) * 16);
+  {
+    const int vrow = 4 * gq + (li >> 2);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      voff[dt] = C::kTile + vrow * C::kRow + (((dt * 2 + ((li & 3) >> 1)) ^ C::swz_v(vrow)) * 16) + (li & 1) * 8;
+  }
+
+  floatx4 sv[QT][4];
+  auto phase_a = [&](const char* st, int k0, auto masked) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) sv[qt][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        const bf16x8 ka = *(const bf16x8*)(st + koff[x] + kt * 16 * C::kRow);
+#pragma unroll
+        for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            sv[qt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qop[qt][y][x], sv[qt][kt], 0, 0, 0);
+      }
+    }
+    if constexpr (decltype(masked)::value) {
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (k0 + kt * 16 + 4 * gq + r > min(qpos[qt], k_hi - 1)) sv[qt][kt][r] = kNegInf;
+    }
+  };
+  auto phase_b = [&](const char* st) __attribute__((always_inline)) {
+    bf16x8 pb[QT][NT][2];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      float cmax = kNegInf;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) cmax = fmaxf(cmax, sv[qt][kt][r]);
+      // the reference, one for a query's four lanes, is raised only past a headroom
+      if (__ballot(cmax * c > m[qt] + kHeadroom) != 0ull) {
+        cmax = fmaxf(cmax, __shfl_xor(cmax, 16, 64));
+        cmax = fmaxf(cmax, __shfl_xor(cmax, 32, 64)) * c;
+        const float mn = fmaxf(m[qt], cmax);
+        const float f = __builtin_amdgcn_exp2f(m[qt] - mn);
+        m[qt] = mn;
+        lsum[qt] *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[qt][dt] *= f;
+      }
+      const float mr = m[qt];
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        uint32_t w[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const floatx4 x = sv[qt][2 * jj + (i >> 1)];
+          bf16_term_pairs(__builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1)], c, -mr)),
+                          __builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1) + 1], c, -mr)), w[i]);
+        }
+#pragma unroll
+        for (int y = 0; y < NT; ++y) pb[qt][y][jj] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
+      }
+    }
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const v4i16 lo = read_tr(st + voff[dt] + (32 * jj) * C::kRow);
+        const v4i16 hi = read_tr(st + voff[dt] + (32 * jj + 16) * C::kRow);
+        bf16x8 va;
+        __builtin_memcpy(&va, &lo, 8);
+        __builtin_memcpy((char*)&va + 8, &hi, 8);
+#pragma unroll
+        for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qt][y][jj], o[qt][dt], 0, 0, 0);
+      }
+#pragma unroll
+      for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+          lsum[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[qt][y][jj], lsum[qt], 0, 0, 0);
+    }
+  };
+
+  if (n_chunks > 0) {
+    if (stager) {
+      page = page_of(0);
+      fetch(0);
+      stage(0);
+      if (n_chunks > 1) {
+        page = page_of(1);
+        fetch(1);
+      }
+      if (n_chunks > 2) page = page_of(2);
+    }
+    auto step = [&](int ch, auto masked) __attribute__((always_inline)) {
+      // every wave has written its part of chunk ch, and is done with chunk ch - 1,
+      // whose stage takes chunk ch + 1
+      __syncthreads();
+      const int k0 = k_lo + ch * kChKeys;
+      const char* st = smem[ch & 1];
+      const bool work = k0 <= wave_last_pos;
+      if (work) {
+        phase_a(st, k0, masked);
+        // (wait states before the products' results are read past the branches below)
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[qt][3]));
+      }
+      if (stager && ch + 1 < n_chunks) {
+        stage((ch + 1) & 1);
+        if (ch + 2 < n_chunks) fetch(ch + 2);
+        if (ch + 3 < n_chunks) page = page_of(ch + 3);
+      }
+      if (work) phase_b(st);
+    };
+    // chunks in which every key is seen by every row of the wave, then the others
+    const int whole = min(k_hi, wave_first_pos + 1) - k_lo;
+    const int first_masked = min(n_chunks, max(whole, 0) / kChKeys);
+    int ch = 0;
+    for (; ch < first_masked; ++ch) step(ch, std::false_type{});
+    for (; ch < n_chunks; ++ch) step(ch, std::true_type{});
+  }
+
+  // ---- lane holds O^T[dt*16 + 4*gq + r][query li] ----
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][DT - 1]), "+v"(lsum[qt]));   // (as above)
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const int r = wrow0 + qt * 16 + li;
+    if (r >= R) continue;
+    const int t = r / G;
+    const int64_t at = orow + (int64_t)t * g.Hq + (r - t * G);
+    if (a.n_splits == 1) {
+      const float inv = lsum[qt][0] == 0.f ? 0.f : 1.f / lsum[qt][0];    // (a row that sees no key)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const floatx4 v = o[qt][dt] * inv;
+        if (a.out_bf16) {
+          const bf16x2 x = {(__bf16)v[0], (__bf16)v[1]}, y = {(__bf16)v[2], (__bf16)v[3]};
+          *(uint2*)((__bf16*)a.out + at * D + dt * 16 + 4 * gq) =
+              uint2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
+        } else {
+          *(floatx4*)((float*)a.out + at * D + dt * 16 + 4 * gq) = v;
+        }
+      }
+    } else if (!none && k_lo < len) {
+      const int64_t rec = at * a.n_splits + split;
+      if (gq == 0) *(floatx2*)(a.rec_ml + 2 * rec) = floatx2{m[qt], lsum[qt][0]};
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *(floatx4*)(a.rec_o + rec * D + dt * 16 + 4 * gq) = o[qt][dt];
+    }
+  }
+}
+
+template <int NT, int QT>
+hipError_t launch(const Q4Split& a, int64_t blocks, hipStream_t stream) {
+  if (a.g.d == 128) hipLaunchKernelGGL((q4_chunk_kernel<NT, 128, QT>), dim3((unsigned)blocks), dim3(kChThreads), 0, stream, a);
+  else hipLaunchKernelGGL((q4_chunk_kernel<NT, 64, QT>), dim3((unsigned)blocks), dim3(kChThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Rows per workgroup, key splits and blocks of a call.
+Q4ChunkPlan q4_chunk_plan(const Geom& g, int n, int n_layers, int T, int max_len) {
+  Q4ChunkPlan x{};
+  const int64_t units = (int64_t)n_layers * n * g.Hkv, R = (int64_t)g.G * T;
+  const int qt = g.dtype == KARA_F32 || R <= kChWaves * 16 ? 1 : 2;
+  x.rows_wg = kChWaves * 16 * qt;
+  x.n_rb = (int)((R + x.rows_wg - 1) / x.rows_wg);
+  x.splits = 1;
+  // (a workgroup holds a CU: fewer of them than CUs split their keys, down to 512)
+  while (x.splits < 16 && units * x.n_rb * x.splits * 2 <= kQ4ChunkWgs && max_len > 512 * x.splits) x.splits *= 2;
+  x.split_keys = x.splits == 1 ? max_len : ((max_len + x.splits - 1) / x.splits + kChKeys - 1) / kChKeys * kChKeys;
+  x.splits = (max_len + x.split_keys - 1) / x.split_keys;
+  x.blocks = units * x.n_rb * x.splits;
+  return x;
+}
+
+hipError_t launch_q4_chunk(const Q4Split& a, const Q4ChunkPlan& x, hipStream_t stream) {
+  if (a.g.dtype == KARA_F32) return launch<3, 1>(a, x.blocks, stream);
+  if (x.rows_wg == kChWaves * 16) return launch<1, 1>(a, x.blocks, stream);
+  return launch<1, 2>(a, x.blocks, stream);
+}
+
+}  // namespace kara
