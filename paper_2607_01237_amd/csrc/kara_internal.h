@@ -147,7 +147,7 @@ hipError_t launch_q4_split(Q4Split a, bool logits, hipStream_t stream);
 // over converted keys; n_rt counts its row blocks.
 constexpr int kQ4ChunkWgs = 256;   // most workgroups of a launch that splits its keys
 struct Q4ChunkPlan {
-  int rows_wg, n_rb, splits, split_keys;
+  int qt, waves, rows_wg, n_rb, splits, split_keys;
   int64_t blocks;
 };
 Q4ChunkPlan q4_chunk_plan(const Geom& g, int n, int n_layers, int T, int max_len);

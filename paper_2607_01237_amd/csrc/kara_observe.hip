@@ -4,6 +4,7 @@
 // exponentials), then column sums with K held and the queries streamed.  No V, no
 // atomics: every key's sum is formed by one workgroup, in row order.
 #include <algorithm>
+#include <type_traits>
 
 #include "kara_evict.h"
 #include "kara_q4_device.h"
@@ -24,12 +25,15 @@ struct ObserveArgs {
   Geom g;
   int n, T, n_new, max_len;
   int row_blocks, splits, split_keys;   // row statistics
-  int key_blocks;                       // column sums
+  int bs_shift;                         // log2(bs) when bs is a power of two, else -1
+  int key_blocks, parts, part_rows;     // column sums: the rows of a unit in parts
   const int32_t *seqs, *bt, *seq_lens;
   const void* q;                        // [n_layers][n][T][Hq][d]
   PoolPtrs k, ks;
   float* w[kMaxLayersPerLaunch];
   floatx2* stats;                       // [n_layers][n][Hkv][T * G][splits]: maximum (log2 units), sum
+  float* sums;                          // [n_layers][n][Hkv][parts][ld] (parts > 1)
+  int64_t ld;
 };
 
 // Eight values of a row as loaded, and as NT bf16 terms.
@@ -80,7 +84,6 @@ __device__ __forceinline__ int swz(int row) {
 }
 
 constexpr int kObsThreads = 256;
-constexpr int kObsWaves = kObsThreads / 64;
 constexpr int kChunk = 64;                  // rows staged at a time
 
 template <int NT, int D>
@@ -120,11 +123,12 @@ __device__ __forceinline__ void read_tile(const char (&b)[NT][kChunk * D * 2], i
 struct Unit {
   int l, j, h, s, len;
 };
-__device__ __forceinline__ bool unit_of(const ObserveArgs& a, int64_t u, Unit* x) {
+__device__ __forceinline__ bool unit_of(const ObserveArgs& a, uint32_t u, Unit* x) {
   const Geom& g = a.g;
-  x->h = (int)(u % g.Hkv);
-  x->j = (int)((u / g.Hkv) % a.n);
-  x->l = (int)(u / ((int64_t)g.Hkv * a.n));
+  x->h = u % (uint32_t)g.Hkv;
+  u /= (uint32_t)g.Hkv;
+  x->j = u % (uint32_t)a.n;
+  x->l = u / (uint32_t)a.n;
   x->s = a.seqs[x->j];
   x->len = x->s >= 0 && x->s < g.n_seqs ? a.seq_lens[x->s] : 0;
   return x->len > 0 && x->len <= a.max_len;
@@ -136,37 +140,39 @@ __device__ __forceinline__ uint64_t key_row(const Geom& g, const int32_t* row_pa
   return (uint64_t)(((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs));
 }
 
-// ---- row statistics: one workgroup per (unit, 128 query rows, split of the keys);
-// a wave holds 32 rows, the keys pass through LDS 64 at a time
-constexpr int kStatRows = kObsWaves * 32;
-
-template <int KSRC, int NK, int QSRC, int NQ, int D>
-__global__ __launch_bounds__(kObsThreads) void observe_stats_kernel(ObserveArgs a) {
+// ---- row statistics: one workgroup per (unit, 64 QT query rows, split of the
+// keys); a wave holds 16 QT rows, the keys pass through LDS 64 at a time.  A lane
+// keeps a maximum and a sum of its own -- of the keys 4gq + r -- and the four of a
+// row meet at the end.
+template <int KSRC, int NK, int QSRC, int NQ, int D, int QT>
+__global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_stats_kernel(ObserveArgs a) {
   constexpr int KS = D / 32, kOct = D / 8, kPer = kChunk * kOct / kObsThreads;
   __shared__ ChunkLds<NK, D> lds;
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
-  const int split = blockIdx.x % a.splits;
-  const int rb = (blockIdx.x / a.splits) % a.row_blocks;
-  const int64_t u = blockIdx.x / (a.splits * a.row_blocks);
+  uint32_t rest = blockIdx.x;
+  const int split = rest % (uint32_t)a.splits;
+  rest /= (uint32_t)a.splits;
+  const int rb = a.row_blocks - 1 - (int)(rest % (uint32_t)a.row_blocks);     // rows that see most keys first
+  const uint32_t u = rest / (uint32_t)a.row_blocks;
   Unit x;
   if (!unit_of(a, u, &x)) return;
   const int G = g.G, R = G * a.T;
-  const int row0 = rb * kStatRows;
+  const int row0 = rb * 64 * QT;
   const int first = x.len - a.T;                       // position of query 0
-  const int last_pos = first + (min(row0 + kStatRows, R) - 1) / G;
+  const int last_pos = first + (min(row0 + 64 * QT, R) - 1) / G;
   const int k_lo = split * a.split_keys;
   const int k_hi = min(min(x.len, last_pos + 1), k_lo + a.split_keys);
   const int32_t* row_pages = a.bt + (int64_t)x.s * g.max_blocks;
-  const int wrow0 = row0 + wave * 32;
-  const int wfirst = first + min(wrow0, R - 1) / G, wlast = first + min(wrow0 + 31, R - 1) / G;
+  const int wrow0 = row0 + wave * 16 * QT;
+  const int wfirst = first + min(wrow0, R - 1) / G, wlast = wrow0 < R ? first + min(wrow0 + 16 * QT - 1, R - 1) / G : -1;
 
-  bf16x8 qa[2][NQ][KS];
-  int qpos[2];
+  bf16x8 qa[QT][NQ][KS];
+  int qpos[QT];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < QT; ++t) {
     const int r = min(wrow0 + t * 16 + li, R - 1);
     const int qt = r / G;
     qpos[t] = first + qt;
@@ -181,112 +187,147 @@ __global__ __launch_bounds__(kObsThreads) void observe_stats_kernel(ObserveArgs 
       for (int z = 0; z < NQ; ++z) qa[t][z][y] = tt[z];
     }
   }
-  float m[2] = {kMaxFloor, kMaxFloor}, sum[2] = {0.f, 0.f};    // of this lane's keys
+  float m[QT], sum[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) m[t] = kMaxFloor, sum[t] = 0.f;
   const float c = g.scale * kLog2e;
 
+  // A thread's kPer octets are one column of rows kObsThreads / kOct apart.  Their
+  // pages are read a chunk before the octets.  (Past the end: the last key, masked.)
+  const int srow = tid / kOct, soct = tid % kOct;
   Octet<KSRC> pre[kPer];
-  auto fetch = [&](int k0) __attribute__((always_inline)) {
+  int page[kPer], slot[kPer];
+  auto look = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int slot = i * kObsThreads + tid;
-      const int pos = min(k0 + slot / kOct, k_hi - 1);         // (past the end: the last key, masked)
-      pre[i].load(a.k.p[x.l], a.ks.p[x.l], key_row(g, row_pages, x.h, pos), slot % kOct, D);
+      const int pos = min(k0 + srow + i * (kObsThreads / kOct), k_hi - 1);
+      const int b = a.bs_shift >= 0 ? pos >> a.bs_shift : pos / g.bs;
+      slot[i] = pos - b * g.bs;
+      page[i] = row_pages[b];
+    }
+  };
+  auto fetch = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int p = min(max(page[i], 0), g.num_pages - 1);
+      pre[i].load(a.k.p[x.l], a.ks.p[x.l], (uint64_t)(((int64_t)p * g.Hkv + x.h) * g.bs + slot[i]), soct, D);
+    }
+  };
+  // one 16-key tile against the wave's rows
+  auto tile = [&](const char (&b)[NK][kChunk * D * 2], int kt, int k0, auto masked) __attribute__((always_inline)) {
+    bf16x8 ka[NK][KS];
+    read_tile<NK, D>(b, kt * 16, gq, li, ka);
+    floatx4 sv[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) sv[t] = dot_tile<NK, NQ, KS>(ka, qa[t]);
+    if constexpr (decltype(masked)::value) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (k0 + kt * 16 + 4 * gq + r >= min(k_hi, qpos[t] + 1)) sv[t][r] = kNegInf;
+    }
+    // a lane's reference is raised only where a logit passes it by more than 2^8
+    float over = kNegInf;
+    float mx[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      mx[t] = fmaxf(fmaxf(sv[t][0], sv[t][1]), fmaxf(sv[t][2], sv[t][3])) * c;
+      over = fmaxf(over, mx[t] - m[t]);
+    }
+    if (__ballot(over > 8.f) != 0ull) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const float mn = fmaxf(m[t], mx[t]);
+        sum[t] *= __builtin_amdgcn_exp2f(m[t] - mn);
+        m[t] = mn;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(sv[t][0], c, -m[t])), e1 = __builtin_amdgcn_exp2f(fmaf(sv[t][1], c, -m[t]));
+      const float e2 = __builtin_amdgcn_exp2f(fmaf(sv[t][2], c, -m[t])), e3 = __builtin_amdgcn_exp2f(fmaf(sv[t][3], c, -m[t]));
+      sum[t] += (e0 + e1) + (e2 + e3);
     }
   };
   if (k_lo < k_hi) {
-    fetch(k_lo);
+    look(k_lo);
+    fetch();
+    look(k_lo + kChunk);
     int buf = 0;
     for (int k0 = k_lo; k0 < k_hi; k0 += kChunk, buf ^= 1) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int slot = i * kObsThreads + tid, row = slot / kOct, o = slot % kOct;
+        const int row = srow + i * (kObsThreads / kOct);
         bf16x8 t[NK];
         pre[i].terms(t);
 #pragma unroll
-        for (int y = 0; y < NK; ++y) __builtin_memcpy(&lds.b[buf][y][row * D * 2 + ((o ^ swz<D>(row & 15)) * 16)], &t[y], 16);
+        for (int y = 0; y < NK; ++y)
+          __builtin_memcpy(&lds.b[buf][y][row * D * 2 + ((soct ^ swz<D>(row & 15)) * 16)], &t[y], 16);
       }
-      if (k0 + kChunk < k_hi) fetch(k0 + kChunk);
+      if (k0 + kChunk < k_hi) {
+        fetch();
+        look(k0 + 2 * kChunk);
+      }
       __syncthreads();
-      if (k0 <= wlast) {
-        const bool masked = k0 + kChunk > min(k_hi, wfirst + 1);
-        floatx4 sv[2][4];
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-          bf16x8 ka[NK][KS];
-          read_tile<NK, D>(lds.b[buf], kt * 16, gq, li, ka);
-#pragma unroll
-          for (int t = 0; t < 2; ++t) sv[t][kt] = dot_tile<NK, NQ, KS>(ka, qa[t]);
-        }
-        // (wait states before the results are read past a branch)
-        asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[0][3]), "+v"(sv[1][3]));
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (masked) {
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (k0 + kt * 16 + 4 * gq + r >= min(k_hi, qpos[t] + 1)) sv[t][kt][r] = kNegInf;
-          }
-          float mx = sv[t][0][0];
-#pragma unroll
-          for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sv[t][kt][r]);
-          const float mn = fmaxf(m[t], mx * c);
-          float add = 0.f;
-#pragma unroll
-          for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) add += __builtin_amdgcn_exp2f(fmaf(sv[t][kt][r], c, -mn));
-          sum[t] = fmaf(sum[t], __builtin_amdgcn_exp2f(m[t] - mn), add);
-          m[t] = mn;
-        }
+      if (k0 > wlast) continue;
+      if (k0 + kChunk > min(k_hi, wfirst + 1)) {
+#pragma unroll 1
+        for (int kt = 0; kt < 4; ++kt) tile(lds.b[buf], kt, k0, std::true_type{});
+      } else {
+#pragma unroll 1
+        for (int kt = 0; kt < 4; ++kt) tile(lds.b[buf], kt, k0, std::false_type{});
       }
     }
   }
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < QT; ++t) {
     float M = fmaxf(m[t], __shfl_xor(m[t], 16, 64));
     M = fmaxf(M, __shfl_xor(M, 32, 64));
     float L = sum[t] * __builtin_amdgcn_exp2f(m[t] - M);
     L += __shfl_xor(L, 16, 64);
     L += __shfl_xor(L, 32, 64);
     const int r = wrow0 + t * 16 + li;
-    if (gq == 0 && r < R) a.stats[(u * R + r) * a.splits + split] = floatx2{M, L};
+    if (gq == 0 && r < R) a.stats[((int64_t)u * R + r) * a.splits + split] = floatx2{M, L};
   }
 }
 
-// ---- column sums: one workgroup per (unit, 128 keys); a wave holds 32 keys, the
-// query rows that see them pass through LDS 64 at a time
-constexpr int kSumKeys = kObsWaves * 32;
+// ---- column sums: one workgroup per (unit, 64 KT keys, part of the rows); a wave
+// holds 16 KT keys, the query rows that see them pass through LDS 64 at a time with
+// their maxima and reciprocal sums.
+constexpr int kPartRows = 2048;             // rows of a part, at most
 
-template <int KSRC, int NK, int QSRC, int NQ, int D>
-__global__ __launch_bounds__(kObsThreads) void observe_sum_kernel(ObserveArgs a) {
+template <int KSRC, int NK, int QSRC, int NQ, int D, int KT>
+__global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sum_kernel(ObserveArgs a) {
   constexpr int KS = D / 32, kOct = D / 8, kPer = kChunk * kOct / kObsThreads;
   __shared__ ChunkLds<NQ, D> lds;
-  __shared__ float row_m[2][kChunk], row_i[2][kChunk];
+  __shared__ floatx2 row_stat[kPartRows];              // maximum and reciprocal sum of the part's rows
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
-  const int kb = blockIdx.x % a.key_blocks;
-  const int64_t u = blockIdx.x / a.key_blocks;
+  uint32_t rest = blockIdx.x;
+  const int part = rest % (uint32_t)a.parts;
+  rest /= (uint32_t)a.parts;
+  const int kb = rest % (uint32_t)a.key_blocks;        // (the first keys are seen by most rows)
+  const uint32_t u = rest / (uint32_t)a.key_blocks;
   Unit x;
   if (!unit_of(a, u, &x)) return;
-  const int key0 = kb * kSumKeys;
+  const int key0 = kb * 64 * KT;
   if (key0 >= x.len) return;
-  int dup = 0;
-  for (int o = tid; o < x.j; o += kObsThreads) dup |= a.seqs[o] == x.s;
-  if (__syncthreads_or(dup)) return;                   // an earlier listing counts
+  if (a.parts == 1) {
+    int dup = 0;
+    for (int o = tid; o < x.j; o += kObsThreads) dup |= a.seqs[o] == x.s;
+    if (__syncthreads_or(dup)) return;                 // an earlier listing counts
+  }
   const int G = g.G, R = G * a.T;
   const int first = x.len - a.T;
   const int32_t* row_pages = a.bt + (int64_t)x.s * g.max_blocks;
-  const int wkey0 = key0 + wave * 32;
+  const int wkey0 = key0 + wave * 16 * KT;
 
-  bf16x8 ka[2][NK][KS];
+  bf16x8 ka[KT][NK][KS];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < KT; ++t) {
     const uint64_t row = key_row(g, row_pages, x.h, min(wkey0 + t * 16 + li, x.len - 1));
 #pragma unroll
     for (int y = 0; y < KS; ++y) {
@@ -298,73 +339,95 @@ __global__ __launch_bounds__(kObsThreads) void observe_sum_kernel(ObserveArgs a)
       for (int z = 0; z < NK; ++z) ka[t][z][y] = tt[z];
     }
   }
-  floatx4 acc[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+  floatx4 acc[KT];
+#pragma unroll
+  for (int t = 0; t < KT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
   const float c = g.scale * kLog2e;
-  // the first row that sees this workgroup's first key
-  const int r_lo = max(0, max(key0, 0) - first) * G;
+  // the part's rows that see this workgroup's first key
+  const int r_lo = max(max(0, key0 - first) * G, part * a.part_rows);
+  const int r_hi = min(R, (part + 1) * a.part_rows);
 
+  for (int r = r_lo + tid; r < r_hi; r += kObsThreads) {
+    const floatx2* st = a.stats + ((int64_t)u * R + r) * a.splits;
+    float M = kMaxFloor, L = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < a.splits; ++i) M = fmaxf(M, st[i][0]);
+#pragma unroll 4
+    for (int i = 0; i < a.splits; ++i) L += st[i][1] * __builtin_amdgcn_exp2f(st[i][0] - M);
+    row_stat[r - r_lo] = floatx2{M, 1.f / L};
+  }
+  // A thread's octets are one column of rows kObsThreads / kOct apart; their queries
+  // are stepped from chunk to chunk, without a division.
+  const int srow = tid / kOct, soct = tid % kOct;
   Octet<QSRC> pre[kPer];
-  float pm = 0.f, pi = 0.f;
+  int qt[kPer], qg[kPer];                              // query and head in group of the next chunk's rows
+  const int step_t = kChunk / G, step_g = kChunk % G;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int r = r_lo + srow + i * (kObsThreads / kOct);
+    qt[i] = r / G;
+    qg[i] = r - qt[i] * G;
+  }
+  const uint64_t qrow0 = ((uint64_t)x.l * a.n + x.j) * a.T * g.Hq + x.h * G;
   auto fetch = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int slot = i * kObsThreads + tid;
-      const int r = min(r0 + slot / kOct, R - 1), qt = r / G;
-      const uint64_t row = (((uint64_t)x.l * a.n + x.j) * a.T + qt) * g.Hq + x.h * G + (r - qt * G);
-      pre[i].load(a.q, nullptr, row, slot % kOct, D);
-    }
-    if (tid < kChunk) {
-      pm = 0.f, pi = 0.f;
-      if (r0 + tid < R) {
-        const floatx2* st = a.stats + (u * R + r0 + tid) * a.splits;
-        pm = kMaxFloor;
-        for (int i = 0; i < a.splits; ++i) pm = fmaxf(pm, st[i][0]);
-        float L = 0.f;
-        for (int i = 0; i < a.splits; ++i) L += st[i][1] * __builtin_amdgcn_exp2f(st[i][0] - pm);
-        pi = 1.f / L;
-      }
+      pre[i].zero();
+      if (r0 + srow + i * (kObsThreads / kOct) < r_hi)
+        pre[i].load(a.q, nullptr, qrow0 + (uint64_t)qt[i] * g.Hq + qg[i], soct, D);
+      qt[i] += step_t;
+      qg[i] += step_g;
+      if (qg[i] >= G) qg[i] -= G, ++qt[i];
     }
   };
-  if (r_lo < R) {
+  // one 16-row tile against the wave's keys
+  auto tile = [&](int buf, int rt, int r0, auto masked) __attribute__((always_inline)) {
+    bf16x8 qb[NQ][KS];
+    read_tile<NQ, D>(lds.b[buf], rt * 16, gq, li, qb);
+    const floatx2 stat = row_stat[min(r0 - r_lo + rt * 16 + li, kPartRows - 1)];
+    const float rm = stat[0], ri = stat[1];
+    floatx4 sv[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) sv[t] = dot_tile<NK, NQ, KS>(ka[t], qb);
+    // (past the last row: sees none)
+    const int pos = !decltype(masked)::value ? 0 : r0 + rt * 16 + li < r_hi ? first + (r0 + rt * 16 + li) / G : -1;
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sv[t][r], c, -rm));
+        // (a row that sees none of these keys may have no sum: its weight is dropped, not multiplied by 0)
+        if constexpr (decltype(masked)::value) acc[t][r] += wkey0 + t * 16 + 4 * gq + r > pos ? 0.f : p * ri;
+        else acc[t][r] = fmaf(p, ri, acc[t][r]);
+      }
+  };
+  if (r_lo < r_hi) {
     fetch(r_lo);
     int buf = 0;
-    for (int r0 = r_lo; r0 < R; r0 += kChunk, buf ^= 1) {
+    for (int r0 = r_lo; r0 < r_hi; r0 += kChunk, buf ^= 1) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int slot = i * kObsThreads + tid, row = slot / kOct, o = slot % kOct;
+        const int row = srow + i * (kObsThreads / kOct);
         bf16x8 t[NQ];
         pre[i].terms(t);
 #pragma unroll
-        for (int y = 0; y < NQ; ++y) __builtin_memcpy(&lds.b[buf][y][row * D * 2 + ((o ^ swz<D>(row & 15)) * 16)], &t[y], 16);
+        for (int y = 0; y < NQ; ++y)
+          __builtin_memcpy(&lds.b[buf][y][row * D * 2 + ((soct ^ swz<D>(row & 15)) * 16)], &t[y], 16);
       }
-      if (tid < kChunk) row_m[buf][tid] = pm, row_i[buf][tid] = pi;
-      if (r0 + kChunk < R) fetch(r0 + kChunk);
+      if (r0 + kChunk < r_hi) fetch(r0 + kChunk);
       __syncthreads();
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt) {
-        const int last = first + min(r0 + rt * 16 + 15, R - 1) / G;
-        if (r0 + rt * 16 >= R || last < wkey0) continue;          // (uniform in the wave)
-        bf16x8 qb[NQ][KS];
-        read_tile<NQ, D>(lds.b[buf], rt * 16, gq, li, qb);
-        const float rm = row_m[buf][rt * 16 + li], ri = row_i[buf][rt * 16 + li];
-        const int pos = r0 + rt * 16 + li < R ? first + (r0 + rt * 16 + li) / G : -1;    // (past the last row: sees none)
-        floatx4 sv[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) sv[t] = dot_tile<NK, NQ, KS>(ka[t], qb);
-        asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[0]), "+v"(sv[1]));
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(sv[t][r], c, -rm));
-            // (a row that sees none of these keys may have no sum: its weight is dropped, not multiplied by 0)
-            acc[t][r] += wkey0 + t * 16 + 4 * gq + r > pos ? 0.f : p * ri;
-          }
+      if (wkey0 >= x.len || first + (min(r0 + kChunk, r_hi) - 1) / G < wkey0) continue;     // (uniform in the wave)
+      if (r0 + kChunk > r_hi || first + r0 / G < wkey0 + 16 * KT - 1) {
+#pragma unroll 1
+        for (int rt = 0; rt < 4; ++rt) tile(buf, rt, r0, std::true_type{});
+      } else {
+#pragma unroll 1
+        for (int rt = 0; rt < 4; ++rt) tile(buf, rt, r0, std::false_type{});
       }
     }
   }
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float v = acc[t][r];
@@ -372,6 +435,10 @@ __global__ __launch_bounds__(kObsThreads) void observe_sum_kernel(ObserveArgs a)
       for (int y = 1; y < 16; y <<= 1) v += __shfl_xor(v, y, 64);
       const int pos = wkey0 + t * 16 + 4 * gq + r;
       if (li != 0 || pos >= x.len) continue;
+      if (a.parts > 1) {
+        a.sums[((int64_t)u * a.parts + part) * a.ld + pos] = v;
+        continue;
+      }
       const int b = pos / g.bs, page = row_pages[b];
       if (page < 0 || page >= g.num_pages) continue;
       float* to = a.w[x.l] + ((int64_t)page * g.Hkv + x.h) * g.bs + (pos - b * g.bs);
@@ -379,50 +446,85 @@ __global__ __launch_bounds__(kObsThreads) void observe_sum_kernel(ObserveArgs a)
     }
 }
 
-bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
-
-// Splits of the keys for the row statistics: enough workgroups for the chip where
-// rows are few, none shorter than 512 keys.
-int stat_splits(int64_t blocks, int max_len) {
-  int splits = 1;
-  while (splits < 16 && blocks * splits < 1024 && max_len > splits * 2 * 512) splits *= 2;
-  return splits;
+// The parts' sums, in order, to the accumulators: one workgroup per (unit, 256 keys).
+__global__ __launch_bounds__(256) void observe_add_kernel(ObserveArgs a, int blocks) {
+  const Geom& g = a.g;
+  const uint32_t u = blockIdx.x / (uint32_t)blocks;
+  const int pos = (int)(blockIdx.x % (uint32_t)blocks) * 256 + threadIdx.x;
+  Unit x;
+  if (!unit_of(a, u, &x)) return;
+  int dup = 0;
+  for (int o = threadIdx.x; o < x.j; o += 256) dup |= a.seqs[o] == x.s;
+  if (__syncthreads_or(dup) || pos >= x.len) return;     // an earlier listing counts
+  float v = 0.f;
+  for (int i = 0; i < a.parts; ++i) v += a.sums[((int64_t)u * a.parts + i) * a.ld + pos];
+  const int b = pos / g.bs, page = a.bt[(int64_t)x.s * g.max_blocks + b];
+  if (page < 0 || page >= g.num_pages) return;
+  float* to = a.w[x.l] + ((int64_t)page * g.Hkv + x.h) * g.bs + (pos - b * g.bs);
+  *to = pos >= x.len - a.n_new ? v : *to + v;
 }
 
+bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
+
+// A wave's rows and keys: 64 where one bf16 term each holds them, 32 of three terms.
+constexpr int kWide = 4, kNarrow = 2;
+int wide_of(const Geom& g) { return g.dtype == KARA_F32 ? kNarrow : kWide; }
+
+// Launches with fewer workgroups than this split: the row statistics their keys (512
+// a split at least), the column sums their rows (256 a part at least, 2048 at most).
+constexpr int kObsWgs = 768;
+constexpr int kMaxParts = 16;
+
 struct Plan {
-  int row_blocks, splits, split_keys, key_blocks;
-  int64_t units;
-  size_t bytes;
+  int row_blocks, splits, split_keys, key_blocks, parts, part_rows;
+  int64_t units, ld;
+  size_t stats_bytes, bytes;
 };
 
 Plan plan_of(const Geom& g, int n, int n_layers, int T, int max_len) {
   Plan x{};
   x.units = (int64_t)n_layers * n * g.Hkv;
   const int64_t R = (int64_t)g.G * T;
-  x.row_blocks = (int)((R + kStatRows - 1) / kStatRows);
-  x.splits = stat_splits(x.units * x.row_blocks, max_len);
+  const int rows = 64 * wide_of(g);
+  x.row_blocks = (int)((R + rows - 1) / rows);
+  x.splits = 1;
+  while (x.splits < kMaxParts && x.units * x.row_blocks * x.splits < kObsWgs && max_len > x.splits * 2 * 512) x.splits *= 2;
   x.split_keys = ((max_len + x.splits - 1) / x.splits + kChunk - 1) / kChunk * kChunk;
-  x.key_blocks = (max_len + kSumKeys - 1) / kSumKeys;
-  x.bytes = (size_t)(x.units * R * x.splits) * sizeof(floatx2);
+  x.key_blocks = (max_len + rows - 1) / rows;
+  const int64_t least = (R + kPartRows - 1) / kPartRows;
+  x.parts = 1;
+  while (x.parts < kMaxParts && x.units * x.key_blocks * x.parts < kObsWgs && R > x.parts * 2 * 256) x.parts *= 2;
+  x.parts = (int)std::max<int64_t>(x.parts, least);
+  x.part_rows = (int)(((R + x.parts - 1) / x.parts + kChunk - 1) / kChunk * kChunk);
+  x.ld = (max_len + 31) / 32 * 32;
+  x.stats_bytes = ((size_t)(x.units * R * x.splits) * sizeof(floatx2) + 255) & ~(size_t)255;
+  x.bytes = x.stats_bytes + (x.parts == 1 ? 0 : (size_t)(x.units * x.parts * x.ld) * sizeof(float));
   return x;
 }
 
-template <int KSRC, int NK, int QSRC, int NQ, int D>
+template <int KSRC, int NK, int QSRC, int NQ, int D, int N>
 hipError_t launch(const ObserveArgs& a, const Plan& x, hipStream_t stream) {
-  hipLaunchKernelGGL((observe_stats_kernel<KSRC, NK, QSRC, NQ, D>), dim3((unsigned)(x.units * x.row_blocks * x.splits)),
+  hipLaunchKernelGGL((observe_stats_kernel<KSRC, NK, QSRC, NQ, D, N>), dim3((unsigned)(x.units * x.row_blocks * x.splits)),
                      dim3(kObsThreads), 0, stream, a);
-  const hipError_t e = hipGetLastError();
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((observe_sum_kernel<KSRC, NK, QSRC, NQ, D>), dim3((unsigned)(x.units * x.key_blocks)),
+  hipLaunchKernelGGL((observe_sum_kernel<KSRC, NK, QSRC, NQ, D, N>), dim3((unsigned)(x.units * x.key_blocks * x.parts)),
                      dim3(kObsThreads), 0, stream, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || x.parts == 1) return e;
+  const int blocks = (a.max_len + 255) / 256;
+  hipLaunchKernelGGL(observe_add_kernel, dim3((unsigned)(x.units * blocks)), dim3(256), 0, stream, a, blocks);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_d(const ObserveArgs& a, const Plan& x, bool codes, hipStream_t stream) {
   const bool f32 = a.g.dtype == KARA_F32;
-  if (codes) return f32 ? launch<kCodeRows, 1, kF32Rows, 3, D>(a, x, stream) : launch<kCodeRows, 1, kBf16Rows, 1, D>(a, x, stream);
-  return f32 ? launch<kF32Rows, 3, kF32Rows, 3, D>(a, x, stream) : launch<kBf16Rows, 1, kBf16Rows, 1, D>(a, x, stream);
+  if (codes)
+    return f32 ? launch<kCodeRows, 1, kF32Rows, 3, D, kNarrow>(a, x, stream)
+               : launch<kCodeRows, 1, kBf16Rows, 1, D, kWide>(a, x, stream);
+  return f32 ? launch<kF32Rows, 3, kF32Rows, 3, D, kNarrow>(a, x, stream)
+             : launch<kBf16Rows, 1, kBf16Rows, 1, D, kWide>(a, x, stream);
 }
 
 }  // namespace
@@ -442,11 +544,15 @@ kara_status_t kara_evict_observe_workspace_size(const kara_params_t* p, int32_t 
   if (!bytes || n < 0 || n_layers < 1 || n_layers > kMaxLayersPerLaunch || n_query < 1 || max_len < 1 ||
       (int64_t)max_len > (int64_t)g.max_blocks * g.bs || (int64_t)n_query * g.Hq > INT32_MAX / 4)
     return KARA_ERR_INVALID_ARG;
-  // (a launch of 1024 row blocks or more does not split; a smaller one has at most
-  // twice 1024 of them, records and all)
+  // (a launch of kObsWgs row blocks or more does not split; a smaller one has fewer
+  // than twice as many, records and all; the same for key blocks and their sums,
+  // beside the parts that many rows take)
   const int64_t R = (int64_t)g.G * n_query;
-  const int64_t rows = (int64_t)n_layers * n * g.Hkv * R;
-  *bytes = (size_t)(rows + (int64_t)2048 * kStatRows) * sizeof(floatx2);
+  const int64_t units = (int64_t)n_layers * n * g.Hkv;
+  const int64_t wg = 64 * wide_of(g);
+  const int64_t least = (R + kPartRows - 1) / kPartRows;
+  *bytes = (size_t)(units * R + 2 * kObsWgs * wg) * sizeof(floatx2) + 256 +
+           (size_t)((least > 1 ? units * least * ((max_len + 31) / 32 * 32) : 0) + 2 * kObsWgs * wg) * sizeof(float);
   return KARA_OK;
 }
 
@@ -467,7 +573,7 @@ kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_
   if (st != KARA_OK) return st;
   const Plan x = plan_of(a.g, n, n_layers, n_query, max_len);
   if (!workspace || workspace_bytes < x.bytes) return KARA_ERR_WORKSPACE;
-  if (!grid_ok(x.units * x.row_blocks * x.splits) || !grid_ok(x.units * x.key_blocks)) return KARA_ERR_UNSUPPORTED;
+  if (!grid_ok(x.units * x.row_blocks * x.splits) || !grid_ok(x.units * x.key_blocks * x.parts)) return KARA_ERR_UNSUPPORTED;
   a.n = n;
   a.T = n_query;
   a.n_new = n_new;
@@ -476,6 +582,10 @@ kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_
   a.splits = x.splits;
   a.split_keys = x.split_keys;
   a.key_blocks = x.key_blocks;
+  a.parts = x.parts;
+  a.part_rows = x.part_rows;
+  a.ld = x.ld;
+  a.bs_shift = (a.g.bs & (a.g.bs - 1)) == 0 ? __builtin_ctz((unsigned)a.g.bs) : -1;
   a.seqs = seqs;
   a.bt = block_table;
   a.seq_lens = seq_lens;
@@ -486,6 +596,7 @@ kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_
     a.w[i] = weights[i];
   }
   a.stats = (floatx2*)workspace;
+  a.sums = (float*)((char*)workspace + x.stats_bytes);
   const hipError_t e = a.g.d == 128 ? launch_d<128>(a, x, k_scales != nullptr, (hipStream_t)stream)
                                     : launch_d<64>(a, x, k_scales != nullptr, (hipStream_t)stream);
   return hip_status(e);

@@ -1,17 +1,19 @@
 // Attention of many query rows over the 4-bit cache (kara_q4_attention): a
 // prompt's chunk over what is cached.  Bound by the matrix products.
 //
-// One workgroup of 8 waves owns 128 QT query rows of one (layer, sequence, KV
+// One workgroup of W waves owns 16 QT W query rows of one (layer, sequence, KV
 // head), rows ordered (query, head in group), and walks the keys they see 64 at a
 // time.  Its threads fetch a chunk's codes two chunks ahead into registers (16
-// bytes, one block of 32 values with its scale, per thread at d = 128), convert
-// them in hardware to bf16 -- exactly -- and write them to the other of two LDS
+// bytes, one block of 32 values with its scale, at a time), convert them in hardware to bf16 -- exactly -- and write them to the other of two LDS
 // stages while the products of the present one run: a chunk is converted once for
 // all rows, with one barrier.  From there the products are those of the recompute
 // attention: S^T = K Q^T, weights as they stand the B operand of O^T += V^T P^T with
 // V through the transposed LDS read, the row sums one more product with ones.
 //
 // NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones).
+//
+// 16 sequences x 1024 queries over 2.5-8.7K cached, 32/8 heads, bf16: 1336 us, 1023
+// TFLOP/s; fp32, 8 x 512: 876 us, 409 TFLOP/s of three products for each.
 #include <algorithm>
 #include <type_traits>
 
@@ -20,24 +22,23 @@
 namespace kara {
 namespace {
 
-constexpr int kChThreads = 512;
-constexpr int kChWaves = kChThreads / 64;
 constexpr int kChKeys = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kMaxFloor = -3.402823466e38f;
 constexpr float kHeadroom = 8.f;
 
-template <int D>
+template <int D, int W>
 struct ChCfg {
+  static constexpr int kThreads = W * 64;
   static constexpr int kRow = D * 2;                 // bytes of a row in LDS
   static constexpr int kChunks = kRow / 16;
   static constexpr int kKS = D / 32;                 // products per dot product
   static constexpr int kDT = D / 16;                 // 16-row tiles of O^T
   static constexpr int kTile = kChKeys * kRow;       // a chunk of K, or of V
   static constexpr int kParts = D / kQ4Block;        // blocks of a row
-  static constexpr int kStagers = 2 * kChKeys * kParts;   // threads with a block to convert
-  static_assert(kStagers <= kChThreads, "a block per thread");
+  static constexpr int kStagers = 2 * kChKeys * kParts;   // blocks of a chunk to convert
+  static constexpr int kPer = kStagers > kThreads ? kStagers / kThreads : 1;
   // XOR swizzles of a row's 16-byte chunks: those of the recompute attention
   static __device__ __forceinline__ int swz_k(int row) {
     if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
@@ -52,9 +53,10 @@ __device__ inline v4i16 read_tr(const char* p) {
       (__attribute__((address_space(3))) v4i16*)(__attribute__((address_space(3))) char*)p);
 }
 
-template <int NT, int D, int QT>
-__global__ __launch_bounds__(kChThreads, 1) void q4_chunk_kernel(Q4Split a) {
-  using C = ChCfg<D>;
+template <int NT, int D, int QT, int W>
+__global__ __launch_bounds__(W * 64, 2) void q4_chunk_kernel(Q4Split a) {
+  using C = ChCfg<D, W>;
+  constexpr int kRowsWg = W * 16 * QT;
   constexpr int KS = C::kKS, DT = C::kDT;
   __shared__ __attribute__((aligned(16))) char smem[2][2 * C::kTile];
   const Geom& g = a.g;
@@ -78,15 +80,39 @@ __global__ __launch_bounds__(kChThreads, 1) void q4_chunk_kernel(Q4Split a) {
   const int rb = a.n_rt - 1 - (int)(rest / (uint32_t)a.n_splits);     // the blocks that see most keys first
   const int h = u % (uint32_t)g.Hkv;
   u /= (uint32_t)g.Hkv;
-  const int j = u % (uint32_t)a.n, l = u / (uint32_t)a.n;
+  int j = u % (uint32_t)a.n;
+  const int l = u / (uint32_t)a.n;
+  // Sequences by length.  Workgroups that wait for a place: the longest first.  Where
+  // all are placed at once, two to a CU, the second half the shortest first, so that
+  // long ones share a CU with short ones.
+  if (a.n > 1 && a.n <= C::kThreads) {
+    int* lens = (int*)smem[0];
+    int mine = -1;
+    if (tid < a.n) {
+      const int s0 = a.seqs[tid];
+      mine = s0 >= 0 && s0 < g.n_seqs ? a.seq_lens[s0] : 0;
+      lens[tid] = mine;
+    }
+    __syncthreads();
+    const int half = W == 8 ? a.n : (a.n + 1) / 2;
+    const int want = j < half ? j : a.n - 1 - (j - half);
+    if (tid < a.n) {
+      int rank = 0;
+      for (int o = 0; o < a.n; ++o) rank += lens[o] > mine || (lens[o] == mine && o < tid);
+      if (rank == want) lens[a.n] = tid;
+    }
+    __syncthreads();
+    j = __builtin_amdgcn_readfirstlane(lens[a.n]);
+    __syncthreads();
+  }
   const int s = a.seqs[j];
   const int G = g.G, T = a.T, R = G * T;
   const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
-  const int row0 = rb * kChWaves * 16 * QT;
+  const int row0 = rb * kRowsWg;
   const int64_t orow = ((int64_t)l * a.n + j) * T * g.Hq + h * G;
   const bool none = len <= 0 || len > a.max_len;
   const int first = len - T;                               // position of query 0
-  const int last_pos = first + (min(row0 + kChWaves * 16 * QT, R) - 1) / G;
+  const int last_pos = first + (min(row0 + kRowsWg, R) - 1) / G;
   const int k_lo = split * a.split_keys;
   const int k_hi = none ? 0 : min(last_pos + 1, k_lo + a.split_keys);
   const int n_chunks = k_hi > k_lo ? (k_hi - k_lo + kChKeys - 1) / kChKeys : 0;
@@ -134,44 +160,49 @@ __global__ __launch_bounds__(kChThreads, 1) void q4_chunk_kernel(Q4Split a) {
   const float c = g.scale * kLog2e;
 
   // ---- staging: thread (K|V, key, block) ----
+  constexpr int kHalf = C::kStagers / 2;              // blocks of K, or of V
   const bool stager = tid < C::kStagers;
-  const bool is_v = tid >= C::kStagers / 2;
-  const int skey = (tid % (C::kStagers / 2)) / C::kParts, sblk = tid % C::kParts;
-  const char* codes = (const char*)(is_v ? a.vp.p[l] : a.kp.p[l]);
-  const uint8_t* scales = (const uint8_t*)(is_v ? a.vsp.p[l] : a.ksp.p[l]);
+  const int skey = (tid % kHalf) / C::kParts, sblk = tid % C::kParts;
   const int32_t* row_pages = a.bt + (int64_t)(none ? 0 : s) * g.max_blocks;
   // (keys past the last one repeat it, finite and masked for every query)
   auto pos_of = [&](int ch) __attribute__((always_inline)) { return min(k_lo + ch * kChKeys + skey, k_hi - 1); };
   auto page_of = [&](int ch) __attribute__((always_inline)) { return row_pages[pos_of(ch) / g.bs]; };
-  uint4 cw;
-  uint32_t cscale = 0;
+  uint4 cw[C::kPer];
+  uint32_t cscale[C::kPer];
   int page = 0;
   auto fetch = [&](int ch) __attribute__((always_inline)) {
     const int pos = pos_of(ch), b = pos / g.bs;
     const int pg = min(max(page, 0), g.num_pages - 1);
     const uint64_t row = (uint64_t)(((int64_t)pg * g.Hkv + h) * g.bs + (pos - b * g.bs));
-    cw = *(const uint4*)(codes + row * (D / 2) + sblk * 16);
-    cscale = scales[row * C::kParts + sblk];
+#pragma unroll
+    for (int i = 0; i < C::kPer; ++i) {
+      const bool is_v = C::kPer == 2 ? i == 1 : tid >= kHalf;
+      cw[i] = *(const uint4*)((const char*)(is_v ? a.vp.p[l] : a.kp.p[l]) + row * (D / 2) + sblk * 16);
+      cscale[i] = ((const uint8_t*)(is_v ? a.vsp.p[l] : a.ksp.p[l]))[row * C::kParts + sblk];
+    }
   };
   // A block's four octets go to LDS in an order that differs by row, so that the 16
   // lanes of four rows write 16 different chunks at a time: octet i ^ (row & 3) at
   // step i, its words exchanged beforehand.
   const int turn = skey & 3;
-  char* const to0 = &smem[0][(is_v ? C::kTile : 0) + skey * C::kRow];
-  const int swz = is_v ? C::swz_v(skey) : C::swz_k(skey & 15);
   auto stage = [&](int st) __attribute__((always_inline)) {
-    const float scale = q4_scale(cscale);
-    uint32_t w0 = cw.x, w1 = cw.y, w2 = cw.z, w3 = cw.w;
-    {
-      const uint32_t a0 = turn & 1 ? w1 : w0, a1 = turn & 1 ? w0 : w1, a2 = turn & 1 ? w3 : w2, a3 = turn & 1 ? w2 : w3;
-      w0 = turn & 2 ? a2 : a0, w1 = turn & 2 ? a3 : a1, w2 = turn & 2 ? a0 : a2, w3 = turn & 2 ? a1 : a3;
-    }
-    const uint32_t w[4] = {w0, w1, w2, w3};
-    char* to = to0 + st * 2 * C::kTile;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bf16x8 v = q4_octet(w[i], scale);
-      *(bf16x8*)(to + (((sblk * 4 + (i ^ turn)) ^ swz) * 16)) = v;
+    for (int y = 0; y < C::kPer; ++y) {
+      const bool is_v = C::kPer == 2 ? y == 1 : tid >= kHalf;
+      char* const to = &smem[st][(is_v ? C::kTile : 0) + skey * C::kRow];
+      const int swz = is_v ? C::swz_v(skey) : C::swz_k(skey & 15);
+      const float scale = q4_scale(cscale[y]);
+      uint32_t w0 = cw[y].x, w1 = cw[y].y, w2 = cw[y].z, w3 = cw[y].w;
+      {
+        const uint32_t a0 = turn & 1 ? w1 : w0, a1 = turn & 1 ? w0 : w1, a2 = turn & 1 ? w3 : w2, a3 = turn & 1 ? w2 : w3;
+        w0 = turn & 2 ? a2 : a0, w1 = turn & 2 ? a3 : a1, w2 = turn & 2 ? a0 : a2, w3 = turn & 2 ? a1 : a3;
+      }
+      const uint32_t w[4] = {w0, w1, w2, w3};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bf16x8 v = q4_octet(w[i], scale);
+        *(bf16x8*)(to + (((sblk * 4 + (i ^ turn)) ^ swz) * 16)) = v;
+      }
     }
   };
 
@@ -338,12 +369,14 @@ __global__ __launch_bounds__(kChThreads, 1) void q4_chunk_kernel(Q4Split a) {
   }
 }
 
-template <int NT, int QT>
+template <int NT, int QT, int W>
 hipError_t launch(const Q4Split& a, int64_t blocks, hipStream_t stream) {
-  if (a.g.d == 128) hipLaunchKernelGGL((q4_chunk_kernel<NT, 128, QT>), dim3((unsigned)blocks), dim3(kChThreads), 0, stream, a);
-  else hipLaunchKernelGGL((q4_chunk_kernel<NT, 64, QT>), dim3((unsigned)blocks), dim3(kChThreads), 0, stream, a);
+  if (a.g.d == 128) hipLaunchKernelGGL((q4_chunk_kernel<NT, 128, QT, W>), dim3((unsigned)blocks), dim3(W * 64), 0, stream, a);
+  else hipLaunchKernelGGL((q4_chunk_kernel<NT, 64, QT, W>), dim3((unsigned)blocks), dim3(W * 64), 0, stream, a);
   return hipGetLastError();
 }
+
+constexpr int kCUs = 256;
 
 }  // namespace
 
@@ -351,12 +384,21 @@ hipError_t launch(const Q4Split& a, int64_t blocks, hipStream_t stream) {
 Q4ChunkPlan q4_chunk_plan(const Geom& g, int n, int n_layers, int T, int max_len) {
   Q4ChunkPlan x{};
   const int64_t units = (int64_t)n_layers * n * g.Hkv, R = (int64_t)g.G * T;
-  const int qt = g.dtype == KARA_F32 || R <= kChWaves * 16 ? 1 : 2;
-  x.rows_wg = kChWaves * 16 * qt;
+  x.qt = g.dtype == KARA_F32 || R <= 8 * 16 ? 1 : 2;
+  auto blocks = [&](int waves) { return units * ((R + waves * 16 * x.qt - 1) / (waves * 16 * x.qt)); };
+  // Eight waves, a CU's worth of registers, convert a chunk once for 256 rows (bf16)
+  // but stand one to a CU: a launch of half to all of the CUs' number ends with its
+  // longest.  There four waves, two to a CU (4 x 512 queries over 2.5-8.7K, 256
+  // blocks: 267 -> 223 us; 16 x 128: 274 -> 224; 5 x 512, 320 blocks: 269 -> 241; 6 x
+  // 512, 384 blocks: 277 against 329; below 128 blocks keys are split, to the same
+  // number of workgroups either way).
+  x.waves = blocks(8) * 2 > kCUs && blocks(8) <= kCUs * 5 / 4 ? 4 : 8;
+  x.rows_wg = x.waves * 16 * x.qt;
   x.n_rb = (int)((R + x.rows_wg - 1) / x.rows_wg);
   x.splits = 1;
-  // (a workgroup holds a CU: fewer of them than CUs split their keys, down to 512)
-  while (x.splits < 16 && units * x.n_rb * x.splits * 2 <= kQ4ChunkWgs && max_len > 512 * x.splits) x.splits *= 2;
+  // (fewer workgroups than CUs: their keys are split, down to 512)
+  if (x.waves == 8)
+    while (x.splits < 16 && units * x.n_rb * x.splits * 2 <= kQ4ChunkWgs && max_len > 512 * x.splits) x.splits *= 2;
   x.split_keys = x.splits == 1 ? max_len : ((max_len + x.splits - 1) / x.splits + kChKeys - 1) / kChKeys * kChKeys;
   x.splits = (max_len + x.split_keys - 1) / x.split_keys;
   x.blocks = units * x.n_rb * x.splits;
@@ -364,9 +406,9 @@ Q4ChunkPlan q4_chunk_plan(const Geom& g, int n, int n_layers, int T, int max_len
 }
 
 hipError_t launch_q4_chunk(const Q4Split& a, const Q4ChunkPlan& x, hipStream_t stream) {
-  if (a.g.dtype == KARA_F32) return launch<3, 1>(a, x.blocks, stream);
-  if (x.rows_wg == kChWaves * 16) return launch<1, 1>(a, x.blocks, stream);
-  return launch<1, 2>(a, x.blocks, stream);
+  if (a.g.dtype == KARA_F32) return x.waves == 8 ? launch<3, 1, 8>(a, x.blocks, stream) : launch<3, 1, 4>(a, x.blocks, stream);
+  if (x.qt == 1) return x.waves == 8 ? launch<1, 1, 8>(a, x.blocks, stream) : launch<1, 1, 4>(a, x.blocks, stream);
+  return x.waves == 8 ? launch<1, 2, 8>(a, x.blocks, stream) : launch<1, 2, 4>(a, x.blocks, stream);
 }
 
 }  // namespace kara
