@@ -3,7 +3,6 @@
 // weights need the rows' sums first: row statistics (each row's maximum and sum of
 // exponentials), then column sums with K held and the queries streamed.  No V, no
 // atomics: every key's sum is formed by one workgroup, in row order.
-#include <algorithm>
 #include <type_traits>
 
 #include "kara_evict.h"
@@ -83,7 +82,16 @@ __device__ __forceinline__ int swz(int row) {
   return ((row & 3) << 1) | ((row >> 2) & 1);
 }
 
-constexpr int kObsThreads = 256;
+// Piece of a block's item, of `pieces` each.  Blocks go round the 8 XCDs, so the
+// pieces of eight items in a row fall to the same ones; the next eight are shifted,
+// or an XCD would get all the long pieces (2 prompts of 2048 queries: half the CUs'
+// time idle).
+__device__ __forceinline__ int spread(uint32_t block, uint32_t pieces) {
+  return (block + block / (8 * pieces)) % pieces;
+}
+
+constexpr int kObsThreads = 512;
+constexpr int kObsWaves = kObsThreads / 64;
 constexpr int kChunk = 64;                  // rows staged at a time
 
 template <int NT, int D>
@@ -140,12 +148,12 @@ __device__ __forceinline__ uint64_t key_row(const Geom& g, const int32_t* row_pa
   return (uint64_t)(((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs));
 }
 
-// ---- row statistics: one workgroup per (unit, 64 QT query rows, split of the
+// ---- row statistics: one workgroup per (unit, 128 QT query rows, split of the
 // keys); a wave holds 16 QT rows, the keys pass through LDS 64 at a time.  A lane
 // keeps a maximum and a sum of its own -- of the keys 4gq + r -- and the four of a
 // row meet at the end.
 template <int KSRC, int NK, int QSRC, int NQ, int D, int QT>
-__global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_stats_kernel(ObserveArgs a) {
+__global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_stats_kernel(ObserveArgs a) {
   constexpr int KS = D / 32, kOct = D / 8, kPer = kChunk * kOct / kObsThreads;
   __shared__ ChunkLds<NK, D> lds;
   const Geom& g = a.g;
@@ -153,16 +161,16 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sta
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
   uint32_t rest = blockIdx.x;
-  const int split = rest % (uint32_t)a.splits;
+  const int split = spread(rest, (uint32_t)a.splits);
   rest /= (uint32_t)a.splits;
   const int rb = a.row_blocks - 1 - (int)(rest % (uint32_t)a.row_blocks);     // rows that see most keys first
   const uint32_t u = rest / (uint32_t)a.row_blocks;
   Unit x;
   if (!unit_of(a, u, &x)) return;
   const int G = g.G, R = G * a.T;
-  const int row0 = rb * 64 * QT;
+  const int row0 = rb * kObsWaves * 16 * QT;
   const int first = x.len - a.T;                       // position of query 0
-  const int last_pos = first + (min(row0 + 64 * QT, R) - 1) / G;
+  const int last_pos = first + (min(row0 + kObsWaves * 16 * QT, R) - 1) / G;
   const int k_lo = split * a.split_keys;
   const int k_hi = min(min(x.len, last_pos + 1), k_lo + a.split_keys);
   const int32_t* row_pages = a.bt + (int64_t)x.s * g.max_blocks;
@@ -213,42 +221,54 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sta
       pre[i].load(a.k.p[x.l], a.ks.p[x.l], (uint64_t)(((int64_t)p * g.Hkv + x.h) * g.bs + slot[i]), soct, D);
     }
   };
-  // one 16-key tile against the wave's rows
-  auto tile = [&](const char (&b)[NK][kChunk * D * 2], int kt, int k0, auto masked) __attribute__((always_inline)) {
-    bf16x8 ka[NK][KS];
-    read_tile<NK, D>(b, kt * 16, gq, li, ka);
-    floatx4 sv[QT];
+  // two 16-key tiles against the wave's rows
+  auto tiles = [&](const char (&b)[NK][kChunk * D * 2], int kt, int k0, auto masked) __attribute__((always_inline)) {
+    floatx4 sv[2][QT];
 #pragma unroll
-    for (int t = 0; t < QT; ++t) sv[t] = dot_tile<NK, NQ, KS>(ka, qa[t]);
+    for (int y = 0; y < 2; ++y) {
+      bf16x8 ka[NK][KS];
+      read_tile<NK, D>(b, (kt + y) * 16, gq, li, ka);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) sv[y][t] = dot_tile<NK, NQ, KS>(ka, qa[t]);
+    }
     if constexpr (decltype(masked)::value) {
 #pragma unroll
-      for (int t = 0; t < QT; ++t)
+      for (int t = 0; t < QT; ++t) {
+        const int sees = min(k_hi, qpos[t] + 1) - (k0 + kt * 16 + 4 * gq);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (k0 + kt * 16 + 4 * gq + r >= min(k_hi, qpos[t] + 1)) sv[t][r] = kNegInf;
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (y * 16 + r >= sees) sv[y][t][r] = kNegInf;
+      }
     }
     // a lane's reference is raised only where a logit passes it by more than 2^8
-    float over = kNegInf;
-    float mx[QT];
+    float over = kNegInf, mx[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      mx[t] = fmaxf(fmaxf(sv[t][0], sv[t][1]), fmaxf(sv[t][2], sv[t][3])) * c;
-      over = fmaxf(over, mx[t] - m[t]);
+      mx[t] = sv[0][t][0];
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx[t] = fmaxf(mx[t], sv[y][t][r]);
+      over = fmaxf(over, fmaf(mx[t], c, -m[t]));
     }
     if (__ballot(over > 8.f) != 0ull) {
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        const float mn = fmaxf(m[t], mx[t]);
+        const float mn = fmaxf(m[t], mx[t] * c);
         sum[t] *= __builtin_amdgcn_exp2f(m[t] - mn);
         m[t] = mn;
       }
     }
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(sv[t][0], c, -m[t])), e1 = __builtin_amdgcn_exp2f(fmaf(sv[t][1], c, -m[t]));
-      const float e2 = __builtin_amdgcn_exp2f(fmaf(sv[t][2], c, -m[t])), e3 = __builtin_amdgcn_exp2f(fmaf(sv[t][3], c, -m[t]));
-      sum[t] += (e0 + e1) + (e2 + e3);
-    }
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][0], c, -m[t])), e1 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][1], c, -m[t]));
+        const float e2 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][2], c, -m[t])), e3 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][3], c, -m[t]));
+        sum[t] += (e0 + e1) + (e2 + e3);
+      }
   };
   if (k_lo < k_hi) {
     look(k_lo);
@@ -273,10 +293,10 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sta
       if (k0 > wlast) continue;
       if (k0 + kChunk > min(k_hi, wfirst + 1)) {
 #pragma unroll 1
-        for (int kt = 0; kt < 4; ++kt) tile(lds.b[buf], kt, k0, std::true_type{});
+        for (int kt = 0; kt < 4; kt += 2) tiles(lds.b[buf], kt, k0, std::true_type{});
       } else {
 #pragma unroll 1
-        for (int kt = 0; kt < 4; ++kt) tile(lds.b[buf], kt, k0, std::false_type{});
+        for (int kt = 0; kt < 4; kt += 2) tiles(lds.b[buf], kt, k0, std::false_type{});
       }
     }
   }
@@ -292,28 +312,39 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sta
   }
 }
 
-// ---- column sums: one workgroup per (unit, 64 KT keys, part of the rows); a wave
+// A row's splits joined into the first: a thread per row.
+__global__ __launch_bounds__(256) void observe_join_kernel(floatx2* stats, int splits, int64_t rows) {
+  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r >= rows) return;
+  floatx2* st = stats + r * splits;
+  float M = kMaxFloor, L = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < splits; ++i) M = fmaxf(M, st[i][0]);
+#pragma unroll 4
+  for (int i = 0; i < splits; ++i) L += st[i][1] * __builtin_amdgcn_exp2f(st[i][0] - M);
+  st[0] = floatx2{M, L};
+}
+
+// ---- column sums: one workgroup per (unit, 128 KT keys, part of the rows); a wave
 // holds 16 KT keys, the query rows that see them pass through LDS 64 at a time with
 // their maxima and reciprocal sums.
-constexpr int kPartRows = 2048;             // rows of a part, at most
-
 template <int KSRC, int NK, int QSRC, int NQ, int D, int KT>
-__global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sum_kernel(ObserveArgs a) {
+__global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum_kernel(ObserveArgs a) {
   constexpr int KS = D / 32, kOct = D / 8, kPer = kChunk * kOct / kObsThreads;
   __shared__ ChunkLds<NQ, D> lds;
-  __shared__ floatx2 row_stat[kPartRows];              // maximum and reciprocal sum of the part's rows
+  __shared__ floatx2 row_stat[2][kChunk];              // maximum and reciprocal sum
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
   uint32_t rest = blockIdx.x;
-  const int part = rest % (uint32_t)a.parts;
+  const int part = spread(rest, (uint32_t)a.parts);
   rest /= (uint32_t)a.parts;
   const int kb = rest % (uint32_t)a.key_blocks;        // (the first keys are seen by most rows)
   const uint32_t u = rest / (uint32_t)a.key_blocks;
   Unit x;
   if (!unit_of(a, u, &x)) return;
-  const int key0 = kb * 64 * KT;
+  const int key0 = kb * kObsWaves * 16 * KT;
   if (key0 >= x.len) return;
   if (a.parts == 1) {
     int dup = 0;
@@ -347,19 +378,11 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sum
   const int r_lo = max(max(0, key0 - first) * G, part * a.part_rows);
   const int r_hi = min(R, (part + 1) * a.part_rows);
 
-  for (int r = r_lo + tid; r < r_hi; r += kObsThreads) {
-    const floatx2* st = a.stats + ((int64_t)u * R + r) * a.splits;
-    float M = kMaxFloor, L = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < a.splits; ++i) M = fmaxf(M, st[i][0]);
-#pragma unroll 4
-    for (int i = 0; i < a.splits; ++i) L += st[i][1] * __builtin_amdgcn_exp2f(st[i][0] - M);
-    row_stat[r - r_lo] = floatx2{M, 1.f / L};
-  }
   // A thread's octets are one column of rows kObsThreads / kOct apart; their queries
   // are stepped from chunk to chunk, without a division.
   const int srow = tid / kOct, soct = tid % kOct;
   Octet<QSRC> pre[kPer];
+  floatx2 st = {0.f, 1.f};
   int qt[kPer], qg[kPer];                              // query and head in group of the next chunk's rows
   const int step_t = kChunk / G, step_g = kChunk % G;
 #pragma unroll
@@ -379,12 +402,13 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sum
       qg[i] += step_g;
       if (qg[i] >= G) qg[i] -= G, ++qt[i];
     }
+    if (tid < kChunk && r0 + tid < r_hi) st = a.stats[((int64_t)u * R + r0 + tid) * a.splits];
   };
   // one 16-row tile against the wave's keys
   auto tile = [&](int buf, int rt, int r0, auto masked) __attribute__((always_inline)) {
     bf16x8 qb[NQ][KS];
     read_tile<NQ, D>(lds.b[buf], rt * 16, gq, li, qb);
-    const floatx2 stat = row_stat[min(r0 - r_lo + rt * 16 + li, kPartRows - 1)];
+    const floatx2 stat = row_stat[buf][rt * 16 + li];
     const float rm = stat[0], ri = stat[1];
     floatx4 sv[KT];
 #pragma unroll
@@ -414,6 +438,7 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sum
         for (int y = 0; y < NQ; ++y)
           __builtin_memcpy(&lds.b[buf][y][row * D * 2 + ((soct ^ swz<D>(row & 15)) * 16)], &t[y], 16);
       }
+      if (tid < kChunk) row_stat[buf][tid] = floatx2{st[0], 1.f / st[1]};
       if (r0 + kChunk < r_hi) fetch(r0 + kChunk);
       __syncthreads();
       if (wkey0 >= x.len || first + (min(r0 + kChunk, r_hi) - 1) / G < wkey0) continue;     // (uniform in the wave)
@@ -421,7 +446,7 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 3 : 2) void observe_sum
 #pragma unroll 1
         for (int rt = 0; rt < 4; ++rt) tile(buf, rt, r0, std::true_type{});
       } else {
-#pragma unroll 1
+#pragma unroll 2
         for (int rt = 0; rt < 4; ++rt) tile(buf, rt, r0, std::false_type{});
       }
     }
@@ -466,13 +491,14 @@ __global__ __launch_bounds__(256) void observe_add_kernel(ObserveArgs a, int blo
 
 bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
 
-// A wave's rows and keys: 64 where one bf16 term each holds them, 32 of three terms.
-constexpr int kWide = 4, kNarrow = 2;
-int wide_of(const Geom& g) { return g.dtype == KARA_F32 ? kNarrow : kWide; }
+// 16-row tiles of a wave's rows, and of its keys (four of them, which 168 registers
+// and three waves per SIMD hold, took 300 us where two take 255: 2 prompts of 2048).
+constexpr int kHeld = 2;
+constexpr int kHeldWg = kObsWaves * 16 * kHeld;         // of a workgroup
 
 // Launches with fewer workgroups than this split: the row statistics their keys (512
-// a split at least), the column sums their rows (256 a part at least, 2048 at most).
-constexpr int kObsWgs = 768;
+// a split at least), the column sums their rows (256 a part at least).
+constexpr int kObsWgs = 512;
 constexpr int kMaxParts = 16;
 
 struct Plan {
@@ -485,16 +511,13 @@ Plan plan_of(const Geom& g, int n, int n_layers, int T, int max_len) {
   Plan x{};
   x.units = (int64_t)n_layers * n * g.Hkv;
   const int64_t R = (int64_t)g.G * T;
-  const int rows = 64 * wide_of(g);
-  x.row_blocks = (int)((R + rows - 1) / rows);
+  x.row_blocks = (int)((R + kHeldWg - 1) / kHeldWg);
   x.splits = 1;
   while (x.splits < kMaxParts && x.units * x.row_blocks * x.splits < kObsWgs && max_len > x.splits * 2 * 512) x.splits *= 2;
   x.split_keys = ((max_len + x.splits - 1) / x.splits + kChunk - 1) / kChunk * kChunk;
-  x.key_blocks = (max_len + rows - 1) / rows;
-  const int64_t least = (R + kPartRows - 1) / kPartRows;
+  x.key_blocks = (max_len + kHeldWg - 1) / kHeldWg;
   x.parts = 1;
   while (x.parts < kMaxParts && x.units * x.key_blocks * x.parts < kObsWgs && R > x.parts * 2 * 256) x.parts *= 2;
-  x.parts = (int)std::max<int64_t>(x.parts, least);
   x.part_rows = (int)(((R + x.parts - 1) / x.parts + kChunk - 1) / kChunk * kChunk);
   x.ld = (max_len + 31) / 32 * 32;
   x.stats_bytes = ((size_t)(x.units * R * x.splits) * sizeof(floatx2) + 255) & ~(size_t)255;
@@ -502,13 +525,19 @@ Plan plan_of(const Geom& g, int n, int n_layers, int T, int max_len) {
   return x;
 }
 
-template <int KSRC, int NK, int QSRC, int NQ, int D, int N>
+template <int KSRC, int NK, int QSRC, int NQ, int D>
 hipError_t launch(const ObserveArgs& a, const Plan& x, hipStream_t stream) {
-  hipLaunchKernelGGL((observe_stats_kernel<KSRC, NK, QSRC, NQ, D, N>), dim3((unsigned)(x.units * x.row_blocks * x.splits)),
+  hipLaunchKernelGGL((observe_stats_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)(x.units * x.row_blocks * x.splits)),
                      dim3(kObsThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((observe_sum_kernel<KSRC, NK, QSRC, NQ, D, N>), dim3((unsigned)(x.units * x.key_blocks * x.parts)),
+  if (x.splits > 1) {
+    const int64_t rows = x.units * a.g.G * a.T;
+    hipLaunchKernelGGL(observe_join_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, stream, a.stats, x.splits, rows);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((observe_sum_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)(x.units * x.key_blocks * x.parts)),
                      dim3(kObsThreads), 0, stream, a);
   e = hipGetLastError();
   if (e != hipSuccess || x.parts == 1) return e;
@@ -521,10 +550,10 @@ template <int D>
 hipError_t launch_d(const ObserveArgs& a, const Plan& x, bool codes, hipStream_t stream) {
   const bool f32 = a.g.dtype == KARA_F32;
   if (codes)
-    return f32 ? launch<kCodeRows, 1, kF32Rows, 3, D, kNarrow>(a, x, stream)
-               : launch<kCodeRows, 1, kBf16Rows, 1, D, kWide>(a, x, stream);
-  return f32 ? launch<kF32Rows, 3, kF32Rows, 3, D, kNarrow>(a, x, stream)
-             : launch<kBf16Rows, 1, kBf16Rows, 1, D, kWide>(a, x, stream);
+    return f32 ? launch<kCodeRows, 1, kF32Rows, 3, D>(a, x, stream)
+               : launch<kCodeRows, 1, kBf16Rows, 1, D>(a, x, stream);
+  return f32 ? launch<kF32Rows, 3, kF32Rows, 3, D>(a, x, stream)
+             : launch<kBf16Rows, 1, kBf16Rows, 1, D>(a, x, stream);
 }
 
 }  // namespace
@@ -545,14 +574,9 @@ kara_status_t kara_evict_observe_workspace_size(const kara_params_t* p, int32_t 
       (int64_t)max_len > (int64_t)g.max_blocks * g.bs || (int64_t)n_query * g.Hq > INT32_MAX / 4)
     return KARA_ERR_INVALID_ARG;
   // (a launch of kObsWgs row blocks or more does not split; a smaller one has fewer
-  // than twice as many, records and all; the same for key blocks and their sums,
-  // beside the parts that many rows take)
-  const int64_t R = (int64_t)g.G * n_query;
-  const int64_t units = (int64_t)n_layers * n * g.Hkv;
-  const int64_t wg = 64 * wide_of(g);
-  const int64_t least = (R + kPartRows - 1) / kPartRows;
-  *bytes = (size_t)(units * R + 2 * kObsWgs * wg) * sizeof(floatx2) + 256 +
-           (size_t)((least > 1 ? units * least * ((max_len + 31) / 32 * 32) : 0) + 2 * kObsWgs * wg) * sizeof(float);
+  // than twice as many, records and all; the same for key blocks and their sums)
+  const int64_t rows = (int64_t)n_layers * n * g.Hkv * g.G * n_query;
+  *bytes = (size_t)(rows + 2 * kObsWgs * kHeldWg) * sizeof(floatx2) + 256 + (size_t)(2 * kObsWgs * kHeldWg) * sizeof(float);
   return KARA_OK;
 }
 
