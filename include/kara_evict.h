@@ -76,7 +76,7 @@ kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_
                                  size_t workspace_bytes, void* stream);
 
 /* Bytes of device workspace kara_evict_tokens needs (written to *bytes, a HOST
- * pointer): 0 where the caller takes the kept positions. */
+ * pointer); 4 n of them where the caller takes the kept positions. */
 kara_status_t kara_evict_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers, int32_t keep,
                                         size_t* bytes);
 

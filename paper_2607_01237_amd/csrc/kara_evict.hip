@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
     const float* o = rec_o + (orow + i) * n_splits * o_step;
     for (int e = tid; e < D; e += kFinThreads) {
       float acc = 0.f;
+#pragma unroll 8
       for (int sp = 0; sp < ns; ++sp)
         acc += o[(int64_t)sp * o_step + e] * __builtin_amdgcn_exp2f(w[(int64_t)sp * ml_step] - red_m[i]);
       out[(orow + i) * D + e] = acc * red_i[i];
@@ -127,37 +128,75 @@ __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
 struct EvictArgs {
   Geom g;
   int n, n_layers, keep, n_sink, n_recent, max_len;
+  int commit;
   const int32_t* seqs;
   int32_t *bt, *seq_lens, *kept, *status;
+  int32_t *freed, *n_freed;   // commit: pages released (each listing's blocks past the cut)
+  int32_t* old_len;           // [n] lengths before the cut, 0 where there is none
   PoolPtrs k, v, ks, vs;      // rows or codes; scales (null: rows)
   WeightPtrs w;
   int row_bytes;              // of k and v
   int scale_bytes;            // of ks and vs; 0: none
 };
 
+// Pages of a listed sequence as they were before the cut: those that it released
+// are in `freed` by the time rows move.
+struct Pages {
+  const int32_t *row, *tail;
+  int first_tail;
+  __device__ __forceinline__ Pages(const EvictArgs& a, int j, int s)
+      : row(a.bt + (int64_t)s * a.g.max_blocks),
+        tail(a.freed + (int64_t)j * a.g.max_blocks),
+        first_tail(a.commit ? (a.keep + a.g.bs - 1) / a.g.bs : a.g.max_blocks) {}
+  __device__ __forceinline__ int operator[](int b) const { return *(b < first_tail ? row + b : tail + (b - first_tail)); }
+};
+
+// One workgroup per listed sequence: its status and, where the call commits, the
+// release of the blocks past the cut and the new length -- first, in one launch;
+// the rows follow by what this leaves in old_len and freed.
 __global__ __launch_bounds__(kValidateThreads) void evict_validate_kernel(EvictArgs a) {
   __shared__ uint32_t lds[kValidateLds];
   const Geom& g = a.g;
   const int j = blockIdx.x, tid = threadIdx.x;
   const int s = a.seqs[j];
-  if (s < 0 || s >= g.n_seqs) {
-    if (tid == 0) a.status[j] = KARA_SEQ_BAD_INDEX;
-    return;
+  int st = KARA_SEQ_BAD_INDEX, len = 0;
+  if (s >= 0 && s < g.n_seqs) {
+    int dup = 0;
+    for (int o = tid; o < a.n; o += kValidateThreads) dup |= o != j && a.seqs[o] == s;
+    st = __syncthreads_or(dup) ? KARA_SEQ_DUP_TRIGGER : 0;
+    len = a.seq_lens[s];
+    if (len < 0 || len > a.max_len || (int64_t)len > (int64_t)g.max_blocks * g.bs)
+      st |= KARA_SEQ_BAD_WINDOW;
+    else
+      st |= pages_status(a.bt + (int64_t)s * g.max_blocks, 0, (len + g.bs - 1) / g.bs, g.num_pages, lds);
   }
-  int dup = 0;
-  for (int o = tid; o < a.n; o += kValidateThreads) dup |= o != j && a.seqs[o] == s;
-  int st = __syncthreads_or(dup) ? KARA_SEQ_DUP_TRIGGER : 0;
-  const int len = a.seq_lens[s];
-  if (len < 0 || len > a.max_len || (int64_t)len > (int64_t)g.max_blocks * g.bs)
-    st |= KARA_SEQ_BAD_WINDOW;
-  else
-    st |= pages_status(a.bt + (int64_t)s * g.max_blocks, 0, (len + g.bs - 1) / g.bs, g.num_pages, lds);
-  if (tid == 0) a.status[j] = st;
+  if (st != 0) len = 0;
+  if (tid == 0) {
+    a.status[j] = st;
+    a.old_len[j] = len;
+  }
+  if (!a.commit) return;
+  __syncthreads();                       // every thread has read the length before it changes
+  const int new_len = min(len, a.keep);
+  const int old_b = (len + g.bs - 1) / g.bs, new_b = (new_len + g.bs - 1) / g.bs;
+  int32_t* row = a.bt + (int64_t)(st == 0 ? s : 0) * g.max_blocks;
+  int32_t* fr = a.freed + (int64_t)j * g.max_blocks;
+  for (int c = tid; c < g.max_blocks; c += kValidateThreads) {
+    const bool gone = c < old_b - new_b;
+    fr[c] = gone ? row[new_b + c] : -1;
+    if (gone) row[new_b + c] = -1;
+  }
+  if (tid == 0) {
+    a.n_freed[j] = old_b - new_b;
+    if (new_len < len) a.seq_lens[s] = new_len;
+  }
 }
 
-constexpr int kPickThreads = 256;
+constexpr int kPickThreads = 512;
 constexpr int kPickWaves = kPickThreads / 64;
 constexpr int kPickLds = 16384;      // keys held in LDS; a longer row is read again in each pass
+constexpr int kPickBits = 11;        // of a digit
+constexpr int kPickBins = 1 << kPickBits;
 
 // Order-preserving: a larger weight has the larger key, -0 ranks as 0, NaN below all.
 __device__ __forceinline__ uint32_t weight_key(float f) {
@@ -169,82 +208,116 @@ __device__ __forceinline__ uint32_t weight_key(float f) {
 
 // One workgroup per (layer, sequence, KV head): the positions that stay.  A
 // radix selection over the accumulators between the first n_sink and the last
-// n_recent positions finds the weight of the last one taken and how many equal
-// ones are (8 bits a pass); then every wave writes its quarter of the sequence
-// in order.
+// n_recent positions finds the key of the last one taken and how many equal
+// ones are; then every wave writes its part of the sequence in order.  Digits of 11
+// bits are taken from the keys' offset above the smallest, from its highest bit on:
+// accumulated weights share their exponents, and digits cut from the keys
+// themselves would meet in a handful of bins.
 __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
-  extern __shared__ uint32_t keys[];
-  __shared__ uint32_t hist[256];
+  extern __shared__ __attribute__((aligned(16))) uint32_t keys[];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[kPickBins];
   __shared__ uint32_t found[3];                        // digit, items wanted in its bin, items in it
-  __shared__ uint32_t wave_gt[kPickWaves], wave_eq[kPickWaves];
+  __shared__ uint32_t wave_a[kPickWaves], wave_b[kPickWaves];
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t u = blockIdx.x;
-  const int h = (int)(u % g.Hkv);
-  const int j = (int)((u / g.Hkv) % a.n);
-  const int l = (int)(u / ((int64_t)g.Hkv * a.n));
-  int32_t* kept = a.kept + u * a.keep;
-  const int s = a.seqs[j];
-  const int len = a.status[j] == 0 ? a.seq_lens[s] : 0;
+  uint32_t rest = blockIdx.x;
+  const int h = rest % (uint32_t)g.Hkv;
+  rest /= (uint32_t)g.Hkv;
+  const int j = rest % (uint32_t)a.n, l = rest / (uint32_t)a.n;
+  int32_t* kept = a.kept + (int64_t)blockIdx.x * a.keep;
+  const int len = a.old_len[j];
   if (len <= a.keep) {
     for (int i = tid; i < a.keep; i += kPickThreads) kept[i] = i < len ? i : -1;
     return;
   }
-  const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
+  const Pages pages(a, j, a.seqs[j]);
   const float* w = a.w.p[l];
   const int lo = a.n_sink, hi = len - a.n_recent;      // candidates
   const uint32_t want = (uint32_t)(a.keep - a.n_sink - a.n_recent);
   auto fetch = [&](int pos) __attribute__((always_inline)) {
     const int b = pos / g.bs;
-    return weight_key(w[((int64_t)row_pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs)]);
+    return weight_key(w[((int64_t)pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs)]);
   };
-  const bool in_lds = hi - lo <= kPickLds;
-  if (in_lds) {
-    for (int i = lo + tid; i < hi; i += kPickThreads) keys[i - lo] = fetch(i);
-    __syncthreads();
-  }
-  auto key = [&](int pos) __attribute__((always_inline)) { return in_lds ? keys[pos - lo] : fetch(pos); };
-
-  // key of the last one taken: `prefix` (with the digits below `shift` open where
-  // its bin is taken whole), `need` of the equal ones
-  uint32_t prefix = 0, need = want;
-  int shift = 32;
-  while (shift > 0 && need > 0) {
-    shift -= 8;
-    hist[tid] = 0;
-    __syncthreads();
-    for (int i = lo + tid; i < hi; i += kPickThreads) {
-      const uint32_t k = key(i);
-      if (shift == 24 || ((k ^ prefix) >> (shift + 8)) == 0) atomicAdd(&hist[(k >> shift) & 255u], 1u);
-    }
-    __syncthreads();
-    // (one wave, bins from the largest: lane i holds 255 - 4i .. 252 - 4i)
-    if (wave == 0) {
-      uint32_t c[4], tot = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) tot += c[e] = hist[255 - 4 * lane - e];
-      uint32_t above = tot;
-#pragma unroll
-      for (int x = 1; x < 64; x <<= 1) {
-        const uint32_t up = (uint32_t)__shfl_up((int)above, x, 64);
-        if (lane >= x) above += up;
-      }
-      above -= tot;
+  const bool in_lds = len <= kPickLds;
+  uint32_t kmin = ~0u, kmax = 0;
+  if (in_lds && (g.bs & 3) == 0) {
+    // four keys lie in one page, on 16 bytes
+    for (int i = 4 * tid; i < len; i += 4 * kPickThreads) {
+      const int b = i / g.bs;
+      const floatx4 f = *(const floatx4*)(w + ((int64_t)pages[b] * g.Hkv + h) * g.bs + (i - b * g.bs));
+      u32x4 k;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (above < need && need <= above + c[e]) found[0] = 255 - 4 * lane - e, found[1] = need - above, found[2] = c[e];
-        above += c[e];
+        k[e] = weight_key(f[e]);
+        if (i + e >= lo && i + e < hi) kmin = min(kmin, k[e]), kmax = max(kmax, k[e]);
       }
+      *(u32x4*)(keys + i) = k;           // (up to three past the length)
+    }
+  } else {
+    for (int i = tid; i < len; i += kPickThreads) {
+      const uint32_t k = fetch(i);
+      if (i >= lo && i < hi) kmin = min(kmin, k), kmax = max(kmax, k);
+      if (in_lds) keys[i] = k;
+    }
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) {
+    kmin = min(kmin, (uint32_t)__shfl_xor((int)kmin, x, 64));
+    kmax = max(kmax, (uint32_t)__shfl_xor((int)kmax, x, 64));
+  }
+  if (lane == 0) wave_a[wave] = kmin, wave_b[wave] = kmax;
+  *(u32x4*)&hist[4 * tid] = u32x4{0, 0, 0, 0};
+  static_assert(kPickBins == 4 * kPickThreads, "four bins a thread");
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < kPickWaves; ++x) kmin = min(kmin, wave_a[x]), kmax = max(kmax, wave_b[x]);
+  // the key's offset above the smallest of the candidates
+  auto key = [&](int pos) __attribute__((always_inline)) { return (in_lds ? keys[pos] : fetch(pos)) - kmin; };
+
+  // the last one taken is `prefix` above kmin (with the digits below `shift` open
+  // where its bin is taken whole), `need` of the equal ones
+  uint32_t prefix = 0, need = want;
+  int shift = kmax > kmin ? 32 - __builtin_clz(kmax - kmin) : 0;
+  bool first = true;
+  while (shift > 0 && need > 0) {
+    const int above_shift = shift;
+    shift = max(0, shift - kPickBits);
+    const uint32_t mask = (1u << (above_shift - shift)) - 1u;
+    for (int i = lo + tid; i < hi; i += kPickThreads) {
+      const uint32_t k = key(i);
+      if (first || ((k ^ prefix) >> above_shift) == 0) atomicAdd(&hist[(k >> shift) & mask], 1u);
+    }
+    __syncthreads();
+    // bins from the largest: thread i holds kPickBins - 1 - 4i and the three below
+    const u32x4 c4 = *(const u32x4*)&hist[kPickBins - 4 - 4 * tid];
+    const uint32_t c[4] = {c4[3], c4[2], c4[1], c4[0]};
+    const uint32_t tot = c[0] + c[1] + c[2] + c[3];
+    uint32_t above = tot;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const uint32_t up = (uint32_t)__shfl_up((int)above, x, 64);
+      if (lane >= x) above += up;
+    }
+    if (lane == 63) wave_a[wave] = above;
+    above -= tot;
+    __syncthreads();
+    for (int x = 0; x < wave; ++x) above += wave_a[x];
+    *(u32x4*)&hist[kPickBins - 4 - 4 * tid] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (above < need && need <= above + c[e]) found[0] = kPickBins - 1 - 4 * tid - e, found[1] = need - above, found[2] = c[e];
+      above += c[e];
     }
     __syncthreads();
     prefix |= found[0] << shift;
     need = found[1];
+    first = false;
     if (found[1] == found[2]) break;
-    __syncthreads();
+    __syncthreads();                     // (found is read before the next pass writes it)
   }
   // taken: keys above the prefix, and of those equal to it (in the digits that were
   // looked at) the first `need`
-  const uint32_t edge = prefix >> (shift & 31);
+  const uint32_t edge = prefix >> shift;
   const bool any = want > 0;
   const int per = ((len + kPickWaves * 64 - 1) / (kPickWaves * 64)) * 64;     // positions per wave
   const int w0 = min(wave * per, len), w1 = min(w0 + per, len);
@@ -252,7 +325,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
     if (pos >= w1) return 0;
     if (pos < lo || pos >= hi) return 2;
     if (!any) return 0;
-    const uint32_t k = key(pos) >> (shift & 31);
+    const uint32_t k = key(pos) >> shift;
     return k > edge ? 2 : k == edge ? 1 : 0;
   };
   uint32_t gt = 0, eq = 0;
@@ -261,12 +334,13 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
     gt += (uint32_t)__popcll(__ballot(r == 2));
     eq += (uint32_t)__popcll(__ballot(r == 1));
   }
-  if (lane == 0) wave_gt[wave] = gt, wave_eq[wave] = eq;
+  __syncthreads();                       // (wave_a is free)
+  if (lane == 0) wave_a[wave] = gt, wave_b[wave] = eq;
   __syncthreads();
   uint32_t at = 0, eq_at = 0;          // taken, and equal ones, before this wave's part
   for (int x = 0; x < wave; ++x) {
-    at += wave_gt[x];
-    eq_at += wave_eq[x];
+    at += wave_a[x];
+    eq_at += wave_b[x];
   }
   at += min(eq_at, need);
   const uint64_t below = ((uint64_t)1 << lane) - 1;
@@ -281,7 +355,6 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
   }
 }
 
-constexpr int kMoveThreads = 256;
 constexpr int kMoveUnroll = 8;
 constexpr int kMoveStage = 32768 / 4;     // kept positions and table entries held in LDS, at most
 
@@ -289,37 +362,36 @@ constexpr int kMoveStage = 32768 / 4;     // kept positions and table entries he
 // arrays (scales, accumulators).  Row i takes row kept[i] >= i, so working up in
 // tiles -- a tile's rows all loaded before any of it is stored -- never overwrites
 // a row still to be read.
-template <bool STAGED>
-__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
+template <bool STAGED, int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a) {
   extern __shared__ int32_t stage[];
   const Geom& g = a.g;
   const int tid = threadIdx.x;
   const int part = blockIdx.x % 3;
-  const int64_t u = blockIdx.x / 3;
-  const int h = (int)(u % g.Hkv);
-  const int j = (int)((u / g.Hkv) % a.n);
-  const int l = (int)(u / ((int64_t)g.Hkv * a.n));
-  if (a.status[j] != 0) return;
-  const int s = a.seqs[j];
-  const int len = a.seq_lens[s];
+  const uint32_t u = blockIdx.x / 3;
+  uint32_t rest = u;
+  const int h = rest % (uint32_t)g.Hkv;
+  rest /= (uint32_t)g.Hkv;
+  const int j = rest % (uint32_t)a.n, l = rest / (uint32_t)a.n;
+  const int len = a.old_len[j];
   if (len <= a.keep) return;
-  const int32_t* kept = a.kept + u * a.keep;
-  const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
+  const int32_t* kept = a.kept + (int64_t)u * a.keep;
+  const Pages pages(a, j, a.seqs[j]);
   if constexpr (STAGED) {
-    for (int i = tid; i < a.keep; i += kMoveThreads) stage[i] = kept[i];
+    for (int i = tid; i < a.keep; i += THREADS) stage[i] = kept[i];
     const int nb = (len + g.bs - 1) / g.bs;
-    for (int b = tid; b < nb; b += kMoveThreads) stage[a.keep + b] = row_pages[b];
+    for (int b = tid; b < nb; b += THREADS) stage[a.keep + b] = pages[b];
     __syncthreads();
   }
   auto source = [&](int i) __attribute__((always_inline)) { return STAGED ? stage[i] : kept[i]; };
   auto row = [&](int pos) __attribute__((always_inline)) {
     const int b = pos / g.bs;
-    const int64_t page = STAGED ? stage[a.keep + b] : row_pages[b];
+    const int64_t page = STAGED ? stage[a.keep + b] : pages[b];
     return (page * g.Hkv + h) * g.bs + (pos - b * g.bs);
   };
   if (part < 2) {
     char* base = (char*)(part ? a.v.p[l] : a.k.p[l]);
-    const int cpr = a.row_bytes >> 4, rpp = kMoveThreads / cpr, tile = rpp * kMoveUnroll;
+    const int cpr = a.row_bytes >> 4, rpp = THREADS / cpr, tile = rpp * kMoveUnroll;
     const int c = tid % cpr, r = tid / cpr;
     for (int x0 = 0; x0 < a.keep; x0 += tile) {
       u32x4 v[kMoveUnroll];
@@ -345,59 +417,56 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
     }
     return;
   }
-  for (int x0 = 0; x0 < a.keep; x0 += kMoveThreads) {
-    const int i = x0 + tid;
-    const int src = i < a.keep ? source(i) : i;
-    float w = 0.f;
-    uint32_t sk = 0, sv = 0;
-    const int64_t from = src != i ? row(src) : 0, to = src != i ? row(i) : 0;
-    if (src != i) {
-      w = a.w.p[l][from];
+  constexpr int kRows = 4;               // of a thread and tile
+  for (int x0 = 0; x0 < a.keep; x0 += THREADS * kRows) {
+    float w[kRows];
+    uint32_t sk[kRows], sv[kRows];
+    bool moves[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int i = x0 + k * THREADS + tid;
+      const int src = i < a.keep ? source(i) : i;
+      moves[k] = src != i;
+      if (!moves[k]) continue;
+      const int64_t from = row(src);
+      w[k] = a.w.p[l][from];
       if (a.scale_bytes == 4) {
-        sk = ((const uint32_t*)a.ks.p[l])[from];
-        sv = ((const uint32_t*)a.vs.p[l])[from];
+        sk[k] = ((const uint32_t*)a.ks.p[l])[from];
+        sv[k] = ((const uint32_t*)a.vs.p[l])[from];
       } else if (a.scale_bytes == 2) {
-        sk = ((const uint16_t*)a.ks.p[l])[from];
-        sv = ((const uint16_t*)a.vs.p[l])[from];
+        sk[k] = ((const uint16_t*)a.ks.p[l])[from];
+        sv[k] = ((const uint16_t*)a.vs.p[l])[from];
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (src != i) {
-      a.w.p[l][to] = w;
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      if (!moves[k]) continue;
+      const int64_t to = row(x0 + k * THREADS + tid);
+      a.w.p[l][to] = w[k];
       if (a.scale_bytes == 4) {
-        ((uint32_t*)a.ks.p[l])[to] = sk;
-        ((uint32_t*)a.vs.p[l])[to] = sv;
+        ((uint32_t*)a.ks.p[l])[to] = sk[k];
+        ((uint32_t*)a.vs.p[l])[to] = sv[k];
       } else if (a.scale_bytes == 2) {
-        ((uint16_t*)a.ks.p[l])[to] = (uint16_t)sk;
-        ((uint16_t*)a.vs.p[l])[to] = (uint16_t)sv;
+        ((uint16_t*)a.ks.p[l])[to] = (uint16_t)sk[k];
+        ((uint16_t*)a.vs.p[l])[to] = (uint16_t)sv[k];
       }
     }
   }
 }
 
-constexpr int kCutThreads = 256;
+// Launches of up to this many workgroups take 1024 threads each: a quarter of the
+// tiles, whose latency is all that such a launch spends (8 x 8 units of 1024 rows
+// of 256 bytes: 36 us with 256).
+constexpr int kMoveWide = 512;
 
-__global__ __launch_bounds__(kCutThreads) void evict_commit_kernel(EvictArgs a, int32_t* __restrict__ freed,
-                                                                   int32_t* __restrict__ n_freed) {
-  const Geom& g = a.g;
-  const int j = blockIdx.x, tid = threadIdx.x;
-  int32_t* fr = freed + (int64_t)j * g.max_blocks;
-  const int s = a.seqs[j];
-  const int len = a.status[j] == 0 ? a.seq_lens[s] : 0;
-  __syncthreads();                       // every thread has read the length before it changes
-  const int new_len = min(len, a.keep);
-  const int old_b = (len + g.bs - 1) / g.bs, new_b = (new_len + g.bs - 1) / g.bs;
-  int32_t* row = a.bt + (int64_t)(a.status[j] == 0 ? s : 0) * g.max_blocks;
-  for (int c = tid; c < g.max_blocks; c += kCutThreads) {
-    const bool gone = c < old_b - new_b;
-    fr[c] = gone ? row[new_b + c] : -1;
-    if (gone) row[new_b + c] = -1;
-  }
-  if (tid == 0) {
-    n_freed[j] = old_b - new_b;
-    if (new_len < len) a.seq_lens[s] = new_len;
-  }
+template <bool STAGED>
+hipError_t launch_move(const EvictArgs& a, int64_t units, size_t lds, hipStream_t stream) {
+  const dim3 grid((unsigned)(units * 3));
+  if (units * 3 <= kMoveWide) hipLaunchKernelGGL((evict_move_kernel<STAGED, 1024>), grid, dim3(1024), lds, stream, a);
+  else hipLaunchKernelGGL((evict_move_kernel<STAGED, 256>), grid, dim3(256), lds, stream, a);
+  return hipGetLastError();
 }
 
 bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && n_layers <= kMaxLayersPerLaunch; }
@@ -528,7 +597,7 @@ kara_status_t kara_evict_workspace_size(const kara_params_t* p, int32_t n, int32
   const kara_status_t st = make_geom(p, n, &g);
   if (st != KARA_OK) return st;
   if (!bytes || !layers_ok(n, n_layers) || keep < 1) return KARA_ERR_INVALID_ARG;
-  *bytes = (size_t)n_layers * n * g.Hkv * keep * sizeof(int32_t);
+  *bytes = align256((size_t)n * sizeof(int32_t)) + (size_t)n_layers * n * g.Hkv * keep * sizeof(int32_t);
   return KARA_OK;
 }
 
@@ -553,9 +622,10 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
       !scales_ok(k_scales, v_scales, n_layers) || !pools_ok((const void* const*)weights, n_layers) ||
       (commit && (!freed || !n_freed)))
     return KARA_ERR_INVALID_ARG;
-  if (!kept && (!workspace || workspace_bytes < need)) return KARA_ERR_WORKSPACE;
+  if (kept) need = (size_t)n * sizeof(int32_t);     // (the lengths alone)
+  if (!workspace || workspace_bytes < need) return KARA_ERR_WORKSPACE;
   const int64_t units = (int64_t)n_layers * n * g.Hkv;
-  if (!grid_ok(units * 3)) return KARA_ERR_UNSUPPORTED;
+  if (!grid_ok(units * 12)) return KARA_ERR_UNSUPPORTED;
   a.n = n;
   a.n_layers = n_layers;
   a.keep = keep;
@@ -565,7 +635,11 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
   a.seqs = seqs;
   a.bt = block_table;
   a.seq_lens = seq_lens;
-  a.kept = kept ? kept : (int32_t*)workspace;
+  a.commit = commit != 0;
+  a.old_len = (int32_t*)workspace;
+  a.kept = kept ? kept : (int32_t*)((char*)workspace + align256((size_t)n * sizeof(int32_t)));
+  a.freed = commit ? freed : nullptr;
+  a.n_freed = commit ? n_freed : nullptr;
   a.status = status;
   a.k = ptrs(k_pools, n_layers);
   a.v = ptrs(v_pools, n_layers);
@@ -578,19 +652,12 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
   hipLaunchKernelGGL(evict_validate_kernel, dim3((unsigned)n), dim3(kValidateThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
-  const size_t pick_lds = (size_t)std::min(max_len, kPickLds) * sizeof(uint32_t);
+  const size_t pick_lds = (size_t)std::min((max_len + 3) / 4 * 4, kPickLds) * sizeof(uint32_t);
   hipLaunchKernelGGL(evict_pick_kernel, dim3((unsigned)units), dim3(kPickThreads), pick_lds, s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
   const int64_t staged = (int64_t)keep + (max_len + g.bs - 1) / g.bs;
-  if (staged <= kMoveStage)
-    hipLaunchKernelGGL((evict_move_kernel<true>), dim3((unsigned)(units * 3)), dim3(kMoveThreads), (size_t)staged * 4, s, a);
-  else
-    hipLaunchKernelGGL((evict_move_kernel<false>), dim3((unsigned)(units * 3)), dim3(kMoveThreads), 0, s, a);
-  e = hipGetLastError();
-  if (e != hipSuccess || !commit) return hip_status(e);
-  hipLaunchKernelGGL(evict_commit_kernel, dim3((unsigned)n), dim3(kCutThreads), 0, s, a, freed, n_freed);
-  return hip_status(hipGetLastError());
+  return hip_status(staged <= kMoveStage ? launch_move<true>(a, units, (size_t)staged * 4, s) : launch_move<false>(a, units, 0, s));
 }
 
 }  // extern "C"

@@ -451,24 +451,29 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum
       }
     }
   }
+  // The 16 lanes of a row of the wave hold parts of the same 8 sums: reduced and dealt
+  // out, lane li ends with sum (t, r) = (li >> 3, (li >> 1) & 3).
+  static_assert(KT == 2, "eight sums to sixteen lanes");
+  float v8[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
 #pragma unroll
-  for (int t = 0; t < KT; ++t)
+  for (int half = 4; half >= 1; half >>= 1)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float v = acc[t][r];
-#pragma unroll
-      for (int y = 1; y < 16; y <<= 1) v += __shfl_xor(v, y, 64);
-      const int pos = wkey0 + t * 16 + 4 * gq + r;
-      if (li != 0 || pos >= x.len) continue;
-      if (a.parts > 1) {
-        a.sums[((int64_t)u * a.parts + part) * a.ld + pos] = v;
-        continue;
-      }
-      const int b = pos / g.bs, page = row_pages[b];
-      if (page < 0 || page >= g.num_pages) continue;
-      float* to = a.w[x.l] + ((int64_t)page * g.Hkv + x.h) * g.bs + (pos - b * g.bs);
-      *to = pos >= x.len - a.n_new ? v : *to + v;
+    for (int i = 0; i < half; ++i) {
+      const bool up = li & (2 * half);
+      const float keep = up ? v8[i + half] : v8[i], give = up ? v8[i] : v8[i + half];
+      v8[i] = keep + __shfl_xor(give, 2 * half, 64);
     }
+  const float v = v8[0] + __shfl_xor(v8[0], 1, 64);
+  const int pos = wkey0 + (li >> 3) * 16 + 4 * gq + ((li >> 1) & 3);
+  if ((li & 1) || pos >= x.len) return;
+  if (a.parts > 1) {
+    a.sums[((int64_t)u * a.parts + part) * a.ld + pos] = v;
+    return;
+  }
+  const int b = pos / g.bs, page = row_pages[b];
+  if (page < 0 || page >= g.num_pages) return;
+  float* to = a.w[x.l] + ((int64_t)page * g.Hkv + x.h) * g.bs + (pos - b * g.bs);
+  *to = pos >= x.len - a.n_new ? v : *to + v;
 }
 
 // The parts' sums, in order, to the accumulators: one workgroup per (unit, 256 keys).

@@ -196,7 +196,7 @@ def run_evict(c, seqs, keep, n_sink, n_recent, max_len, commit=True, given=True)
     freed = torch.full((n, c.max_blocks), 99, dtype=torch.int32, device="cuda")
     n_freed, status = (torch.full((n,), 99, dtype=torch.int32, device="cuda") for _ in range(2))
     k, v, ks, vs = c.lists("k", "v", "ks", "vs")
-    ws = None if given else torch.empty(kara.evict_workspace_size(c.p, n, L, keep), dtype=torch.uint8, device="cuda")
+    ws = torch.full((4 * n if given else kara.evict_workspace_size(c.p, n, L, keep),), 255, dtype=torch.uint8, device="cuda")
     kara.evict_tokens(c.p, cc.gpu(np.asarray(seqs, dtype=np.int32)), keep, n_sink, n_recent, k, v, c.weights, c.bt, c.sl,
                       max_len, commit, status, ws, kept=kept if given else None, freed=freed if commit else None,
                       n_freed=n_freed if commit else None, k_scales=ks, v_scales=vs)
