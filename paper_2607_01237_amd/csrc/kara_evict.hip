@@ -28,17 +28,17 @@ struct WeightPtrs {
 // ---------------------------------------------------------------- attention that counts
 
 constexpr int kFinThreads = 256;
-constexpr int kFinKeys = 4 * kFinThreads;   // keys per workgroup
+constexpr int kFinKeys = 4 * kFinThreads;   // keys per step
 
 // Second half of a counting decoding step: the splits' records joined to the
 // output (a record: maximum and sum, ml_step apart, and o, o_step apart), and every
 // key's weight -- exp2(logit - M) / L over the group's query
 // heads -- added to its accumulator.  One workgroup per (layer, sequence, KV
-// head, 1024 keys); a sequence's workgroups share out its query heads' outputs.
+// head, `steps` runs of 1024 keys); a sequence's workgroups share out its query heads' outputs.
 template <int D>
 __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
     Geom g, int n, const int32_t* __restrict__ seqs, const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens,
-    int n_new, int max_len, int split_keys, int n_splits, int chunks, const float* __restrict__ rec_ml, int ml_step,
+    int n_new, int max_len, int split_keys, int n_splits, int chunks, int steps, const float* __restrict__ rec_ml, int ml_step,
     const float* __restrict__ rec_o, int o_step, const float* __restrict__ logits, int64_t ld, WeightPtrs wp, float* __restrict__ out) {
   __shared__ float red_m[kMaxGroup], red_i[kMaxGroup];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -57,10 +57,10 @@ __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
       for (int i = tid; i < G * D; i += kFinThreads) out[orow * D + i] = 0.f;
     return;
   }
-  const int k0 = chunk * kFinKeys;
+  const int k0 = chunk * steps * kFinKeys;
   if (k0 >= len) return;
   const int ns = (len + split_keys - 1) / split_keys;
-  const int nc = (len + kFinKeys - 1) / kFinKeys;      // this sequence's workgroups
+  const int nc = (len + steps * kFinKeys - 1) / (steps * kFinKeys);      // this sequence's workgroups
   int dup = 0;
   for (int o = tid; o < j; o += kFinThreads) dup |= seqs[o] == s;
   for (int i = wave; i < G; i += kFinThreads / 64) {
@@ -89,37 +89,49 @@ __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
   }
   if (dup) return;        // an earlier listing counts
   const float c = g.scale * kLog2e;
-  const int k = k0 + 4 * tid;
-  if (k >= len) return;
-  float add[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < G; ++i) {
-    const floatx4 x = *(const floatx4*)(logits + (orow + i) * ld + k);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) add[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[e], c, -red_m[i])), red_i[i], add[e]);
-  }
   const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
-  if ((g.bs & 3) == 0) {
-    // the four keys lie in one page, on 16 bytes
-    const int b = k / g.bs;
-    const int page = row_pages[b];
-    if (page < 0 || page >= g.num_pages) return;
-    floatx4* to = (floatx4*)(wp.p[l] + ((int64_t)page * g.Hkv + h) * g.bs + (k - b * g.bs));
-    const floatx4 was = *to;
-    floatx4 now;
+  for (int k = k0 + 4 * tid; k < min(len, k0 + steps * kFinKeys); k += kFinKeys) {
+    // four keys; in one page and on 16 bytes where pages allow it
+    const bool quad = (g.bs & 3) == 0;
+    floatx4* to = nullptr;
+    floatx4 was = {0.f, 0.f, 0.f, 0.f};
+    if (quad) {
+      const int b = k / g.bs;
+      const int page = row_pages[b];
+      if (page < 0 || page >= g.num_pages) continue;
+      to = (floatx4*)(wp.p[l] + ((int64_t)page * g.Hkv + h) * g.bs + (k - b * g.bs));
+      was = *to;
+    }
+    float add[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < G; i0 += 4) {
+      floatx4 x[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) now[e] = k + e >= len ? was[e] : k + e >= len - n_new ? add[e] : was[e] + add[e];
-    *to = now;
-    return;
-  }
+      for (int y = 0; y < 4; ++y) x[y] = *(const floatx4*)(logits + (orow + min(i0 + y, G - 1)) * ld + k);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int pos = k + e;
-    if (pos >= len) break;
-    const int b = pos / g.bs;
-    const int page = row_pages[b];
-    if (page < 0 || page >= g.num_pages) continue;
-    float* to = wp.p[l] + ((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs);
-    *to = pos >= len - n_new ? add[e] : *to + add[e];
+      for (int y = 0; y < 4; ++y) {
+        if (i0 + y >= G) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          add[e] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[y][e], c, -red_m[i0 + y])), red_i[i0 + y], add[e]);
+      }
+    }
+    if (quad) {
+      floatx4 now;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) now[e] = k + e >= len ? was[e] : k + e >= len - n_new ? add[e] : was[e] + add[e];
+      *to = now;
+      continue;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int pos = k + e;
+      if (pos >= len) break;
+      const int b = pos / g.bs;
+      const int page = row_pages[b];
+      if (page < 0 || page >= g.num_pages) continue;
+      float* one = wp.p[l] + ((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs);
+      *one = pos >= len - n_new ? add[e] : *one + add[e];
+    }
   }
 }
 
@@ -355,15 +367,18 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
   }
 }
 
+constexpr int kMoveThreads = 1024;
 constexpr int kMoveUnroll = 8;
 constexpr int kMoveStage = 32768 / 4;     // kept positions and table entries held in LDS, at most
 
 // One workgroup per (layer, sequence, KV head, part): K rows, V rows, and the small
 // arrays (scales, accumulators).  Row i takes row kept[i] >= i, so working up in
 // tiles -- a tile's rows all loaded before any of it is stored -- never overwrites
-// a row still to be read.
-template <bool STAGED, int THREADS>
-__global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a) {
+// a row still to be read.  1024 threads a workgroup: 64 sequences x 4 layers cut from
+// 3.9-8.2K to 3.8K tokens (8.1 GB) 1705 us with 256, 1679 so; 8 sequences of one
+// layer, where a tile's latency is all that the launch spends, 36 us with 256, 24 so.
+template <bool STAGED>
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
   extern __shared__ int32_t stage[];
   const Geom& g = a.g;
   const int tid = threadIdx.x;
@@ -378,9 +393,9 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a) {
   const int32_t* kept = a.kept + (int64_t)u * a.keep;
   const Pages pages(a, j, a.seqs[j]);
   if constexpr (STAGED) {
-    for (int i = tid; i < a.keep; i += THREADS) stage[i] = kept[i];
+    for (int i = tid; i < a.keep; i += kMoveThreads) stage[i] = kept[i];
     const int nb = (len + g.bs - 1) / g.bs;
-    for (int b = tid; b < nb; b += THREADS) stage[a.keep + b] = pages[b];
+    for (int b = tid; b < nb; b += kMoveThreads) stage[a.keep + b] = pages[b];
     __syncthreads();
   }
   auto source = [&](int i) __attribute__((always_inline)) { return STAGED ? stage[i] : kept[i]; };
@@ -391,7 +406,7 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a) {
   };
   if (part < 2) {
     char* base = (char*)(part ? a.v.p[l] : a.k.p[l]);
-    const int cpr = a.row_bytes >> 4, rpp = THREADS / cpr, tile = rpp * kMoveUnroll;
+    const int cpr = a.row_bytes >> 4, rpp = kMoveThreads / cpr, tile = rpp * kMoveUnroll;
     const int c = tid % cpr, r = tid / cpr;
     for (int x0 = 0; x0 < a.keep; x0 += tile) {
       u32x4 v[kMoveUnroll];
@@ -418,13 +433,13 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a) {
     return;
   }
   constexpr int kRows = 4;               // of a thread and tile
-  for (int x0 = 0; x0 < a.keep; x0 += THREADS * kRows) {
+  for (int x0 = 0; x0 < a.keep; x0 += kMoveThreads * kRows) {
     float w[kRows];
     uint32_t sk[kRows], sv[kRows];
     bool moves[kRows];
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
-      const int i = x0 + k * THREADS + tid;
+      const int i = x0 + k * kMoveThreads + tid;
       const int src = i < a.keep ? source(i) : i;
       moves[k] = src != i;
       if (!moves[k]) continue;
@@ -443,7 +458,7 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a) {
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
       if (!moves[k]) continue;
-      const int64_t to = row(x0 + k * THREADS + tid);
+      const int64_t to = row(x0 + k * kMoveThreads + tid);
       a.w.p[l][to] = w[k];
       if (a.scale_bytes == 4) {
         ((uint32_t*)a.ks.p[l])[to] = sk[k];
@@ -454,19 +469,6 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a) {
       }
     }
   }
-}
-
-// Launches of up to this many workgroups take 1024 threads each: a quarter of the
-// tiles, whose latency is all that such a launch spends (8 x 8 units of 1024 rows
-// of 256 bytes: 36 us with 256).
-constexpr int kMoveWide = 512;
-
-template <bool STAGED>
-hipError_t launch_move(const EvictArgs& a, int64_t units, size_t lds, hipStream_t stream) {
-  const dim3 grid((unsigned)(units * 3));
-  if (units * 3 <= kMoveWide) hipLaunchKernelGGL((evict_move_kernel<STAGED, 1024>), grid, dim3(1024), lds, stream, a);
-  else hipLaunchKernelGGL((evict_move_kernel<STAGED, 256>), grid, dim3(256), lds, stream, a);
-  return hipGetLastError();
 }
 
 bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && n_layers <= kMaxLayersPerLaunch; }
@@ -544,7 +546,10 @@ kara_status_t kara_evict_attention(const kara_params_t* p, int32_t n, const int3
   float* records = (float*)workspace;
   float* logits = (float*)((char*)workspace + w.logits);
   const int64_t units = (int64_t)n_layers * n * g.Hkv;
-  const int chunks = (max_len + kFinKeys - 1) / kFinKeys;
+  // (more keys a workgroup where 8 per CU remain)
+  int steps = 1;
+  while (steps < 4 && units * ((max_len + 2 * steps * kFinKeys - 1) / (2 * steps * kFinKeys)) >= 2048) steps *= 2;
+  const int chunks = (max_len + steps * kFinKeys - 1) / (steps * kFinKeys);
   if (!grid_ok(units * ((max_len + KARA_HARNESS_SPLIT_KEYS - 1) / KARA_HARNESS_SPLIT_KEYS))) return KARA_ERR_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   const PoolPtrs kp = ptrs(k_pools, n_layers), vp = ptrs(v_pools, n_layers);
@@ -585,10 +590,10 @@ kara_status_t kara_evict_attention(const kara_params_t* p, int32_t n, const int3
   const dim3 grid((unsigned)(units * chunks)), block(kFinThreads);
   if (g.d == 128)
     hipLaunchKernelGGL((evict_finish_kernel<128>), grid, block, 0, s, g, n, seqs, block_table, seq_lens, n_new, max_len, keys,
-                       n_splits, chunks, rec_ml, ml_step, rec_o, o_step, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
+                       n_splits, chunks, steps, rec_ml, ml_step, rec_o, o_step, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
   else
     hipLaunchKernelGGL((evict_finish_kernel<64>), grid, block, 0, s, g, n, seqs, block_table, seq_lens, n_new, max_len, keys,
-                       n_splits, chunks, rec_ml, ml_step, rec_o, o_step, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
+                       n_splits, chunks, steps, rec_ml, ml_step, rec_o, o_step, (const float*)logits, w.ld, weight_ptrs(weights, n_layers), out);
   return hip_status(hipGetLastError());
 }
 
@@ -657,7 +662,10 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
   e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
   const int64_t staged = (int64_t)keep + (max_len + g.bs - 1) / g.bs;
-  return hip_status(staged <= kMoveStage ? launch_move<true>(a, units, (size_t)staged * 4, s) : launch_move<false>(a, units, 0, s));
+  const dim3 grid((unsigned)(units * 3)), block(kMoveThreads);
+  if (staged <= kMoveStage) hipLaunchKernelGGL((evict_move_kernel<true>), grid, block, (size_t)staged * 4, s, a);
+  else hipLaunchKernelGGL((evict_move_kernel<false>), grid, block, 0, s, a);
+  return hip_status(hipGetLastError());
 }
 
 }  // extern "C"
