@@ -18,6 +18,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxFloor = -3.402823466e38f;
 constexpr int kMaxGroup = KARA_HARNESS_MAX_GROUP;
 
+// a grid of one dimension, of 256 threads a block: HIP counts its threads in 32 bits
 bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 

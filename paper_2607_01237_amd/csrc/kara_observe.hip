@@ -494,6 +494,7 @@ __global__ __launch_bounds__(256) void observe_add_kernel(ObserveArgs a, int blo
   *to = pos >= x.len - a.n_new ? v : *to + v;
 }
 
+// a grid of one dimension, of 256 threads a block: HIP counts its threads in 32 bits
 bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
 
 // 16-row tiles of a wave's rows, and of its keys (four of them, which 168 registers
@@ -602,7 +603,7 @@ kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_
   if (st != KARA_OK) return st;
   const Plan x = plan_of(a.g, n, n_layers, n_query, max_len);
   if (!workspace || workspace_bytes < x.bytes) return KARA_ERR_WORKSPACE;
-  if (!grid_ok(x.units * x.row_blocks * x.splits) || !grid_ok(x.units * x.key_blocks * x.parts)) return KARA_ERR_UNSUPPORTED;
+  if (!grid_ok(2 * x.units * x.row_blocks * x.splits) || !grid_ok(2 * x.units * x.key_blocks * x.parts)) return KARA_ERR_UNSUPPORTED;
   a.n = n;
   a.T = n_query;
   a.n_new = n_new;

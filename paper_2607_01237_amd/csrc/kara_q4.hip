@@ -37,15 +37,75 @@ __global__ __launch_bounds__(kAppendThreads) void q4_commit_kernel(Geom g, int n
 
 constexpr int kQuantUnroll = 4;       // octets per thread
 
-// Eight values to eight codes: a lane holds an octet, four lanes a block.
-// Grid as the append of rows: (sequences x token chunks, layer, K|V).
+template <int DT>
+struct QuantSrc {
+  static constexpr int kBytes = DT == KARA_BF16 ? 16 : 32;   // of eight values
+  u32x4 v[kBytes / 16];
+  __device__ __forceinline__ void load(const char* p) {
+    // (fp32: a lane's two halves of 32 bytes share a line with its neighbours', which
+    // then has to stay until the second load)
+    if constexpr (kBytes == 16) {
+      v[0] = __builtin_nontemporal_load((const u32x4*)p);
+    } else {
+      v[0] = ((const u32x4*)p)[0];
+      v[1] = ((const u32x4*)p)[1];
+    }
+  }
+};
+
+// Eight values to eight codes; four lanes hold a block and find its scale byte
+// together.  odd: a value was not finite.
+template <int DT>
+__device__ __forceinline__ uint32_t q4_encode(const QuantSrc<DT>& src, uint32_t* byte, bool* odd) {
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (DT == KARA_BF16)
+      x[e] = __uint_as_float((e & 1) ? src.v[0][e >> 1] & 0xffff0000u : src.v[0][e >> 1] << 16);
+    else
+      x[e] = __uint_as_float(src.v[e >> 2][e & 3]);
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  if (top >= 0x7f800000u) {
+    *odd = true;
+    top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t m = __float_as_uint(x[e]) & 0x7fffffffu;
+      if (m > 0x7f800000u) x[e] = 0.f;
+      if (m < 0x7f800000u) top = max(top, m);
+    }
+  }
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+  *byte = q4_scale_byte(top);
+  const float scale = q4_scale(*byte);
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], scale, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], scale, 3);
+  return c;
+}
+
+template <int D>
+__device__ __forceinline__ void q4_store(uint8_t* codes, uint8_t* scales, int64_t row, int o, uint32_t code, uint32_t byte) {
+  *(uint32_t*)(codes + row * (D / 2) + o * 4) = code;
+  if ((o & 3) == 0) scales[row * (D / kQ4Block) + (o >> 2)] = (uint8_t)byte;
+}
+
+// The rows after q4_commit_kernel.  Grid as the append of rows: (sequences x token
+// chunks, layer, K|V).  Bound by the bytes: with the reading back of the same rows, 4
+// x 4 layers of 4000 tokens (664 MB) in 120 us, 5.5 TB/s.
 template <int DT, int D>
 __global__ __launch_bounds__(kAppendThreads) void q4_append_kernel(
     Geom g, int n, const int32_t* __restrict__ seqs, int n_new, int toks, int chunks, const char* __restrict__ k_new,
     const char* __restrict__ v_new, PoolPtrs kp, PoolPtrs vp, PoolPtrs ksp, PoolPtrs vsp,
     const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens, int32_t* __restrict__ status) {
   constexpr int kOctets = D / 8;                     // of a row
-  constexpr int kOctetBytes = DT == KARA_BF16 ? 16 : 32;
+  using Src = QuantSrc<DT>;
   const int j = blockIdx.x / chunks;
   const int tok0 = (blockIdx.x - j * chunks) * toks;
   const int l = blockIdx.y;
@@ -57,65 +117,74 @@ __global__ __launch_bounds__(kAppendThreads) void q4_append_kernel(
   const int count = min(toks, n_new - tok0) * per_tok;
   const int pos0 = seq_lens[s] - n_new + tok0;
   const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
-  const char* src = (kv ? v_new : k_new) + (((int64_t)l * n + j) * n_new + tok0) * per_tok * kOctetBytes;
+  const char* src = (kv ? v_new : k_new) + (((int64_t)l * n + j) * n_new + tok0) * per_tok * Src::kBytes;
   uint8_t* codes = (uint8_t*)(kv ? vp.p[l] : kp.p[l]);
   uint8_t* scales = (uint8_t*)(kv ? vsp.p[l] : ksp.p[l]);
   bool odd = false;
   // (count is a multiple of a block's four octets, so the four lanes of a block
   // stay together)
   for (int i0 = threadIdx.x; i0 < count; i0 += kAppendThreads * kQuantUnroll) {
-    u32x4 v[kQuantUnroll][kOctetBytes / 16];
+    Src v[kQuantUnroll];
 #pragma unroll
     for (int k = 0; k < kQuantUnroll; ++k) {
       const int i = i0 + k * kAppendThreads;
-      if (i < count)
-#pragma unroll
-        for (int y = 0; y < kOctetBytes / 16; ++y)
-          v[k][y] = __builtin_nontemporal_load((const u32x4*)(src + (int64_t)i * kOctetBytes) + y);
+      if (i < count) v[k].load(src + (int64_t)i * Src::kBytes);
     }
 #pragma unroll
     for (int k = 0; k < kQuantUnroll; ++k) {
       const int i = i0 + k * kAppendThreads;
       if (i >= count) continue;
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (DT == KARA_BF16)
-          x[e] = __uint_as_float((e & 1) ? v[k][0][e >> 1] & 0xffff0000u : v[k][0][e >> 1] << 16);
-        else
-          x[e] = __uint_as_float(v[k][e >> 2][e & 3]);
-      }
-      uint32_t top = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-      if (top >= 0x7f800000u) {
-        odd = true;
-        top = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t m = __float_as_uint(x[e]) & 0x7fffffffu;
-          if (m > 0x7f800000u) x[e] = 0.f;
-          if (m < 0x7f800000u) top = max(top, m);
-        }
-      }
-      top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
-      const uint32_t byte = q4_scale_byte(top);
-      const float scale = q4_scale(byte);
-      uint32_t c = 0;
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], scale, 0);
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], scale, 1);
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], scale, 2);
-      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], scale, 3);
+      uint32_t byte;
+      const uint32_t code = q4_encode<DT>(v[k], &byte, &odd);
       const int tok = i / per_tok, r = i - tok * per_tok;
       const int h = r / kOctets, o = r - h * kOctets;
       const int pos = pos0 + tok, b = pos / g.bs;
-      const int64_t row = ((int64_t)row_pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs);
-      *(uint32_t*)(codes + row * (D / 2) + o * 4) = c;
-      if ((o & 3) == 0) scales[row * (D / kQ4Block) + (o >> 2)] = (uint8_t)byte;
+      q4_store<D>(codes, scales, ((int64_t)row_pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs), o, code, byte);
     }
   }
   if (__syncthreads_or(odd) && threadIdx.x == 0) atomicOr(&status[j], KARA_SEQ_NONFINITE);
+}
+
+// A few new tokens: one workgroup per listed sequence checks it, quantises all its
+// rows and commits, in one launch (8 sequences, one token, one layer: a pass with the
+// reading back 27.9 us of host time in two launches, 24.5 so).
+constexpr int kFewThreads = 1024;
+constexpr int kFewOctets = 8 * kFewThreads;          // of a sequence, K and V, all layers
+
+template <int DT, int D>
+__global__ __launch_bounds__(kFewThreads) void q4_append_few_kernel(
+    Geom g, int n, const int32_t* __restrict__ seqs, int n_new, int n_layers, const char* __restrict__ k_new,
+    const char* __restrict__ v_new, PoolPtrs kp, PoolPtrs vp, PoolPtrs ksp, PoolPtrs vsp,
+    const int32_t* __restrict__ bt, int32_t* __restrict__ seq_lens, int32_t* __restrict__ status) {
+  constexpr int kOctets = D / 8;
+  using Src = QuantSrc<DT>;
+  const int j = blockIdx.x;
+  int st = append_status(g, n, seqs, n_new, bt, seq_lens, j);
+  if (st == KARA_SEQ_OK) {
+    const int s = seqs[j];
+    const int per_tok = g.Hkv * kOctets, per_layer = n_new * per_tok;
+    const int pos0 = seq_lens[s];
+    const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
+    bool odd = false;
+    for (int i = threadIdx.x; i < 2 * n_layers * per_layer; i += kFewThreads) {
+      const int part = i / per_layer, kv = part & 1, l = part >> 1;
+      const int x = i - part * per_layer, tok = x / per_tok, r = x - tok * per_tok;
+      const int h = r / kOctets, o = r - h * kOctets;
+      Src v;
+      v.load((kv ? v_new : k_new) + (((int64_t)l * n + j) * per_layer + x) * Src::kBytes);
+      uint32_t byte;
+      const uint32_t code = q4_encode<DT>(v, &byte, &odd);
+      const int pos = pos0 + tok, b = pos / g.bs;
+      q4_store<D>((uint8_t*)(kv ? vp.p[l] : kp.p[l]), (uint8_t*)(kv ? vsp.p[l] : ksp.p[l]),
+                  ((int64_t)row_pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs), o, code, byte);
+    }
+    if (__syncthreads_or(odd)) st = KARA_SEQ_NONFINITE;
+  }
+  __syncthreads();                       // every thread has read the length before it changes
+  if (threadIdx.x == 0) {
+    status[j] = st;
+    if ((st & ~KARA_SEQ_NONFINITE) == 0) seq_lens[seqs[j]] += n_new;
+  }
 }
 
 // ---------------------------------------------------------------- read
@@ -176,8 +245,8 @@ __global__ __launch_bounds__(kAppendThreads) void q4_read_kernel(
         const floatx2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 1);
         const floatx2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 2);
         const floatx2 f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 3);
-        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, floatx4{a[0], a[1], b[0], b[1]}), to);
-        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, floatx4{e[0], e[1], f[0], f[1]}), to + 1);
+        to[0] = __builtin_bit_cast(u32x4, floatx4{a[0], a[1], b[0], b[1]});   // (half a line each: gathered in the cache)
+        to[1] = __builtin_bit_cast(u32x4, floatx4{e[0], e[1], f[0], f[1]});
       }
     }
   }
@@ -633,7 +702,7 @@ int split_keys_of(int bs, int64_t units, int max_len) {
 constexpr int kFewRows = 64;
 bool few_rows(const Geom& g, int T) { return (int64_t)g.G * T <= kFewRows; }
 
-// a grid of one dimension: HIP counts its threads in 32 bits
+// a grid of one dimension, of 256 threads a block: HIP counts its threads in 32 bits
 bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
 
 bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && n_layers <= kMaxLayersPerLaunch; }
@@ -692,15 +761,31 @@ kara_status_t kara_q4_append(const kara_params_t* p, int32_t n, const int32_t* s
   const int per_tok = g.Hkv * (g.d / 8);
   const int toks = std::min(n_new, std::max(1, 2 * kAppendThreads * kQuantUnroll / per_tok));
   const int64_t chunks = ((int64_t)n_new + toks - 1) / toks;
-  if (!grid_ok(n * chunks) || (int64_t)toks * per_tok > INT32_MAX / 2) return KARA_ERR_UNSUPPORTED;
+  if (!grid_ok(n * chunks) || !grid_ok(4 * (int64_t)n) || (int64_t)toks * per_tok > INT32_MAX / 2) return KARA_ERR_UNSUPPORTED;
+  const PoolPtrs kp = ptrs(k_pools, n_layers), vp = ptrs(v_pools, n_layers), ksp = ptrs(k_scales, n_layers),
+                 vsp = ptrs(v_scales, n_layers);
+  if ((int64_t)2 * n_layers * n_new * per_tok <= kFewOctets) {
+#define KARA_Q4_FEW(DT, D)                                                                                         \
+  hipLaunchKernelGGL((q4_append_few_kernel<DT, D>), dim3((unsigned)n), dim3(kFewThreads), 0, s, g, n, seqs, n_new, \
+                     n_layers, (const char*)k_new, (const char*)v_new, kp, vp, ksp, vsp, block_table, seq_lens, status)
+    if (g.dtype == KARA_BF16) {
+      if (g.d == 128) KARA_Q4_FEW(KARA_BF16, 128);
+      else KARA_Q4_FEW(KARA_BF16, 64);
+    } else {
+      if (g.d == 128) KARA_Q4_FEW(KARA_F32, 128);
+      else KARA_Q4_FEW(KARA_F32, 64);
+    }
+#undef KARA_Q4_FEW
+    return hip_status(hipGetLastError());
+  }
   const dim3 grid((unsigned)(n * chunks), (unsigned)n_layers, 2), block(kAppendThreads);
   hipLaunchKernelGGL(q4_commit_kernel, dim3((unsigned)n), block, 0, s, g, n, seqs, n_new, block_table, seq_lens, status);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
 #define KARA_Q4_APPEND(DT, D)                                                                                       \
   hipLaunchKernelGGL((q4_append_kernel<DT, D>), grid, block, 0, s, g, n, seqs, n_new, toks, (int)chunks,            \
-                     (const char*)k_new, (const char*)v_new, ptrs(k_pools, n_layers), ptrs(v_pools, n_layers),      \
-                     ptrs(k_scales, n_layers), ptrs(v_scales, n_layers), block_table, (const int32_t*)seq_lens, status)
+                     (const char*)k_new, (const char*)v_new, kp, vp, ksp, vsp, block_table, (const int32_t*)seq_lens, \
+                     status)
   if (g.dtype == KARA_BF16) {
     if (g.d == 128) KARA_Q4_APPEND(KARA_BF16, 128);
     else KARA_Q4_APPEND(KARA_BF16, 64);
@@ -760,7 +845,7 @@ kara_status_t kara_q4_attention_workspace_size(const kara_params_t* p, int32_t n
   } else {
     // (a launch that splits its keys has so many workgroups at most, records and all)
     const Q4ChunkPlan x = q4_chunk_plan(g, n, n_layers, n_query, max_len);
-    *bytes = (size_t)kQ4ChunkWgs * x.rows_wg * rec;
+    *bytes = (size_t)kQ4ChunkWgs * x.qt * 128 * rec;
   }
   return KARA_OK;
 }

@@ -1,0 +1,265 @@
+"""The 4-bit cache and eviction as a program uses them together: prompts, decoding
+steps and cuts in turn, other streams, and a decoding step captured into a graph."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+import cache_check as cc  # noqa: E402
+from oracle import kara_cache as oc  # noqa: E402
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+class Program:
+    """A small serving program: `layers` layers of n sequences over rows or 4-bit
+    codes, pages handed out by the host."""
+
+    def __init__(self, kind, dtype="bf16", n=3, layers=2, Hq=8, Hkv=2, d=64, bs=16, pages=120, max_blocks=24, seed=1):
+        from paper_2607_01237_amd import kara
+        self.k, self.kind, self.n, self.layers, self.Hq, self.Hkv, self.d, self.bs = kara, kind, n, layers, Hq, Hkv, d, bs
+        self.max_blocks, self.max_len, self.dt = max_blocks, max_blocks * bs, cc.DT[dtype]
+        self.g = torch.Generator().manual_seed(seed)
+        self.free = list(np.random.default_rng(seed).permutation(pages))
+        self.p = cc.params(Hq, Hkv, d, bs, pages, max_blocks, n, dtype)
+        shape = (layers, pages, Hkv, bs)
+        if kind == "q4":
+            self.dev = {x: torch.zeros(shape + (d // w,), dtype=torch.uint8, device="cuda")
+                        for x, w in (("k", 2), ("v", 2), ("ks", 32), ("vs", 32))}
+        else:
+            self.dev = {x: torch.zeros(shape + (d,), dtype=self.dt, device="cuda") for x in ("k", "v")}
+        self.w = torch.full(shape, 1e30, device="cuda")              # stale: a page's last owner left it
+        self.table = np.full((n, max_blocks), -1, dtype=np.int32)
+        self.lens = np.zeros(n, dtype=np.int32)
+        self.bt, self.sl = cc.gpu(self.table), cc.gpu(self.lens)
+        self.seqs = torch.arange(n, dtype=torch.int32, device="cuda")
+        self.status = torch.empty(n, dtype=torch.int32, device="cuda")
+        size = max(kara.evict_attention_workspace_size(self.p, n, layers, self.max_len),
+                   kara.evict_observe_workspace_size(self.p, n, layers, 64, self.max_len),
+                   kara.q4_attention_workspace_size(self.p, n, layers, 64, self.max_len),
+                   kara.evict_workspace_size(self.p, n, layers, self.max_len))
+        self.ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")      # one for every call
+
+    def lists(self, *names):
+        return [list(self.dev[x].unbind(0)) if x in self.dev else None for x in names]
+
+    def randn(self, *shape):
+        return torch.randn(shape, generator=self.g).to(self.dt).cuda()
+
+    def append(self, T):
+        for s in range(self.n):
+            for b in range(-(-int(self.lens[s]) // self.bs), -(-int(self.lens[s] + T) // self.bs)):
+                self.table[s, b] = self.free.pop()
+        self.bt.copy_(torch.from_numpy(self.table))
+        k, v = self.randn(self.layers, self.n, T, self.Hkv, self.d), self.randn(self.layers, self.n, T, self.Hkv, self.d)
+        if self.kind == "q4":
+            self.k.q4_append(self.p, self.seqs, k, v, *self.lists("k", "v", "ks", "vs"), self.bt, self.sl, self.status)
+        else:
+            self.k.kv_append(self.p, self.seqs, k, v, *self.lists("k", "v"), self.bt, self.sl, self.status)
+        self.lens += T
+        assert not self.status.any() and self.sl.tolist() == self.lens.tolist()
+        return k, v
+
+    def cache(self, l, s):
+        """fp64 K and V rows of a sequence as the cache holds them."""
+        n = int(self.lens[s])
+        at = np.arange(n)
+        page, slot = self.table[s][at // self.bs], at % self.bs
+        got = {x: t[l].float().cpu().numpy() if t.dtype != torch.uint8 else t[l].cpu().numpy() for x, t in self.dev.items()}
+        take = {x: a[page, :, slot] for x, a in got.items()}
+        if self.kind == "q4":
+            return oc.q4_values(take["k"], take["ks"]), oc.q4_values(take["v"], take["vs"])
+        return take["k"].astype(np.float64), take["v"].astype(np.float64)
+
+    def weights(self, l, s):
+        at = np.arange(int(self.lens[s]))
+        return self.w[l].cpu().numpy()[self.table[s][at // self.bs], :, at % self.bs].T      # [Hkv, n]
+
+
+@pytest.mark.parametrize("kind,dtype", [("q4", "bf16"), ("rows", "bf16"), ("q4", "f32"), ("rows", "f32")])
+def test_prompts_steps_and_cuts(kind, dtype):
+    pr = Program(kind, dtype)
+    k, v, ks, vs = pr.lists("k", "v", "ks", "vs")
+    wl = list(pr.w.unbind(0))
+    scale, terms = 1 / np.sqrt(pr.d), 1 if dtype == "bf16" else 3
+    mass = np.zeros((pr.layers, pr.n))                     # weight given out so far, a head
+    pr.append(50)
+    q = pr.randn(pr.layers, pr.n, 50, pr.Hq, pr.d)
+    pr.k.evict_observe(pr.p, pr.seqs, 50, q, k, wl, pr.bt, pr.sl, 50, pr.max_len, pr.ws, k_scales=ks)
+    if kind == "q4":
+        out = torch.empty_like(q)
+        pr.k.q4_attention(pr.p, pr.seqs, 50, q, k, v, ks, vs, pr.bt, pr.sl, pr.max_len, out, pr.ws)
+    for l in range(pr.layers):
+        for s in range(pr.n):
+            kk, vv = pr.cache(l, s)
+            q64 = q[l, s].double().cpu().numpy()
+            ref, m, w = oc.attend(q64, kk, vv, scale)
+            delta = cc.logit_error(q64, kk, scale, 3 * terms)
+            assert (np.abs(pr.weights(l, s) - w) <= 1.05 * w * (2 * delta + 500 * cc.EPS)).all()
+            if kind == "q4":
+                bound = cc.attention_bound(ref, m, delta, 50, dtype, dtype == "bf16")
+                assert (np.abs(out[l, s].double().cpu().numpy() - ref) <= bound).all()
+    mass[:] = 50
+    for step in range(30):
+        pr.append(1)
+        q = pr.randn(pr.layers, pr.n, pr.Hq, pr.d)
+        out = torch.empty(q.shape, device="cuda")
+        before = {(l, s): pr.weights(l, s) for l in range(pr.layers) for s in range(pr.n)}
+        pr.k.evict_attention(pr.p, pr.seqs, q, k, v, wl, pr.bt, pr.sl, 1, pr.max_len, out, pr.ws, k_scales=ks, v_scales=vs)
+        for (l, s), old in before.items():
+            kk, vv = pr.cache(l, s)
+            q64 = q[l, s][None].double().cpu().numpy()
+            ref, m, w = oc.attend(q64, kk, vv, scale)
+            delta = cc.logit_error(q64, kk, scale, terms)
+            old[:, -1] = 0
+            assert (np.abs(pr.weights(l, s) - old - w) <= 1.05 * w * (2 * delta + 30 * cc.EPS) + 2 * cc.EPS * (old + w)).all()
+            bound = cc.attention_bound(ref, m, delta, len(kk), "f32", False)
+            assert (np.abs(out[l, s].double().cpu().numpy() - ref[0]) <= bound[0]).all()
+        if step % 8 != 7:
+            continue
+        keep, sink, recent = 40, 2, 10
+        held = {(l, s): (*pr.cache(l, s), pr.weights(l, s)) for l in range(pr.layers) for s in range(pr.n)}
+        kept = torch.empty((pr.layers, pr.n, pr.Hkv, keep), dtype=torch.int32, device="cuda")
+        freed = torch.empty((pr.n, pr.max_blocks), dtype=torch.int32, device="cuda")
+        n_freed = torch.empty(pr.n, dtype=torch.int32, device="cuda")
+        pr.k.evict_tokens(pr.p, pr.seqs, keep, sink, recent, k, v, wl, pr.bt, pr.sl, pr.max_len, True, pr.status, pr.ws,
+                          kept=kept, freed=freed, n_freed=n_freed, k_scales=ks, v_scales=vs)
+        assert not pr.status.any()
+        new_b = -(-keep // pr.bs)
+        for s in range(pr.n):
+            old_b = -(-int(pr.lens[s]) // pr.bs)
+            pages = freed[s, :int(n_freed[s])].tolist()
+            assert pages == pr.table[s, new_b:old_b].tolist()
+            pr.free += pages
+            pr.table[s, new_b:old_b] = -1
+        pr.lens[:] = keep
+        assert np.array_equal(pr.bt.cpu().numpy(), pr.table) and pr.sl.tolist() == pr.lens.tolist()
+        for (l, s), (kk, vv, ww) in held.items():
+            k2, v2 = pr.cache(l, s)
+            for h in range(pr.Hkv):
+                pos = oc.kept(ww[h], keep, sink, recent)
+                assert kept[l, s, h].tolist() == pos.tolist()
+                assert np.array_equal(k2[:, h], kk[pos, h]) and np.array_equal(v2[:, h], vv[pos, h])
+                assert np.array_equal(pr.weights(l, s)[h], ww[h][pos])
+
+
+def test_on_another_stream():
+    # everything queued on one side stream, behind work that takes a while; every
+    # tensor lives until the stream is done
+    pr, qr = Program("q4"), Program("q4")
+    side = torch.cuda.Stream()
+    outs = []
+    for p_, stream in ((pr, None), (qr, side)):
+        k, v = p_.randn(2, 3, 90, 2, 64), p_.randn(2, 3, 90, 2, 64)
+        q = p_.randn(2, 3, 90, 8, 64)
+        for s in range(3):
+            for b in range(6):
+                p_.table[s, b] = p_.free.pop()
+        p_.bt.copy_(torch.from_numpy(p_.table))
+        out, back, back_v = torch.empty_like(q), torch.zeros_like(k), torch.zeros_like(k)   # (rows behind a sequence stay)
+        seen, start = q[:, :, 26:].contiguous(), torch.zeros(3, dtype=torch.int32, device="cuda")
+        freed, n_freed = (torch.zeros(x, dtype=torch.int32, device="cuda") for x in ((3, 24), (3,)))
+        cache = p_.lists("k", "v", "ks", "vs")
+        wl = list(p_.w.unbind(0))
+        torch.cuda.synchronize()
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                big = torch.randn(4096, 4096, device="cuda")
+                for _ in range(5):
+                    big = big @ big * 1e-2
+        kw = dict(stream=stream)
+        p_.k.q4_append(p_.p, p_.seqs, k, v, *cache, p_.bt, p_.sl, p_.status, **kw)
+        p_.k.q4_attention(p_.p, p_.seqs, 90, q, *cache, p_.bt, p_.sl, p_.max_len, out, p_.ws, **kw)
+        p_.k.evict_observe(p_.p, p_.seqs, 64, seen, cache[0], wl, p_.bt, p_.sl, 90, p_.max_len, p_.ws,
+                           k_scales=cache[2], **kw)
+        p_.k.evict_tokens(p_.p, p_.seqs, 33, 1, 5, cache[0], cache[1], wl, p_.bt, p_.sl, p_.max_len, True, p_.status, p_.ws,
+                          freed=freed, n_freed=n_freed, k_scales=cache[2], v_scales=cache[3], **kw)
+        p_.k.q4_read(p_.p, p_.seqs, start, 90, *cache, p_.bt, p_.sl, back, back_v, **kw)
+        torch.cuda.synchronize()
+        outs.append((out, back, back_v, freed, n_freed, p_.w, p_.sl, p_.bt, *p_.dev.values()))
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kind", ["q4", "rows"])
+def test_captured_steps(kind):
+    """A decoding step and a cut in a graph, replayed with eager steps of another
+    program, on the same workspace, between: every replay's bits are the eager run's."""
+    def step(p_, st):
+        cache = p_.lists("k", "v", "ks", "vs")
+        wl = list(p_.w.unbind(0))
+        app = p_.k.q4_append if kind == "q4" else p_.k.kv_append
+        app(p_.p, p_.seqs, st["k"], st["v"], *[c for c in cache if c is not None], p_.bt, p_.sl, p_.status)
+        p_.k.evict_attention(p_.p, p_.seqs, st["q"], cache[0], cache[1], wl, p_.bt, p_.sl, 1, p_.max_len, st["out"], p_.ws,
+                             k_scales=cache[2], v_scales=cache[3])
+        p_.k.evict_tokens(p_.p, p_.seqs, st["keep"], 1, 4, cache[0], cache[1], wl, p_.bt, p_.sl, p_.max_len, False,
+                          p_.status, p_.ws, k_scales=cache[2], v_scales=cache[3])
+
+    runs = []
+    for captured in (False, True):
+        pr, other = Program(kind, seed=5), Program(kind, seed=6)
+        other.ws = pr.ws
+        for p_ in (pr, other):
+            p_.append(70)
+            p_.w.fill_(0.5)
+            p_.w[:, :, :, ::3] = 0.25
+            for s in range(3):
+                for b in range(5, 24):
+                    p_.table[s, b] = p_.free.pop()
+            p_.bt.copy_(torch.from_numpy(p_.table))
+        st, so = ({"k": p_.randn(2, 3, 1, 2, 64), "v": p_.randn(2, 3, 1, 2, 64), "q": p_.randn(2, 3, 8, 64),
+                   "out": torch.zeros(2, 3, 8, 64, device="cuda"), "keep": 60} for p_ in (pr, other))
+        graph = None
+        if captured:
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            keep = [t.clone() for t in (pr.w, pr.sl, *pr.dev.values())]
+            with torch.cuda.stream(side):
+                step(pr, st)                               # (once outside: modules are loaded)
+            torch.cuda.current_stream().wait_stream(side)
+            for t, c in zip((pr.w, pr.sl, *pr.dev.values()), keep):
+                t.copy_(c)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step(pr, st)
+        seen = []
+        for i in range(6):
+            st["q"].copy_(torch.randn(st["q"].shape, generator=torch.Generator().manual_seed(i)).to(st["q"].dtype))
+            if graph is not None:
+                graph.replay()
+            else:
+                step(pr, st)
+            seen.append([t.clone() for t in (st["out"], pr.w, pr.sl, *pr.dev.values())])
+            step(other, so)
+            if i % 2:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        runs.append(seen)
+    for i, (a, b) in enumerate(zip(*runs)):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y), i
+
+
+def test_refused_on_the_host():
+    pr = Program("q4")
+    k, v, ks, vs = pr.lists("k", "v", "ks", "vs")
+    q = pr.randn(2, 3, 8, 64)
+    out = torch.empty(2, 3, 8, 64, device="cuda")
+    wl = list(pr.w.unbind(0))
+    good = dict(p=pr.p, seqs=pr.seqs, q=q, k_pools=k, v_pools=v, weights=wl, block_table=pr.bt, seq_lens=pr.sl, n_new=1,
+                max_len=pr.max_len, out=out, workspace=pr.ws, k_scales=ks, v_scales=vs)
+    for bad in (dict(q=q.cpu()), dict(q=q.float()), dict(q=q.transpose(0, 1)), dict(out=out.bfloat16()), dict(out=out[:1]),
+                dict(seqs=pr.seqs.long()), dict(k_scales=None), dict(v_pools=v[:1]), dict(weights=wl[:1]),
+                dict(weights=[w.half() for w in wl]), dict(workspace=pr.ws[:64]), dict(workspace=None), dict(n_new=-1),
+                dict(max_len=pr.max_len + 1), dict(block_table=pr.bt[:2]), dict(workspace=pr.ws.cpu())):
+        with pytest.raises(pr.k.KaraError):
+            pr.k.evict_attention(**dict(good, **bad))
+    pr.k.evict_attention(**good)
+    torch.cuda.synchronize()
+    assert not out.any()                                  # empty sequences
