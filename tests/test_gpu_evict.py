@@ -91,17 +91,13 @@ def check_weights(c, seqs, n_new, max_len, per_key, T):
 KINDS = [("rows", "bf16"), ("rows", "f32"), ("q4", "bf16"), ("q4", "f32")]
 
 
-@pytest.mark.parametrize("kind,dtype", KINDS)
-@pytest.mark.parametrize("Hq,Hkv,d,bs,layers,n_new", [(32, 8, 128, 16, 2, 1), (5, 1, 128, 24, 1, 0), (6, 6, 64, 7, 1, 3),
-                                                      (32, 2, 64, 256, 1, 2000)])
-def test_attention_counts(kind, dtype, Hq, Hkv, d, bs, layers, n_new):
+def count_case(kind, dtype, Hq, Hkv, d, bs, layers, n_new, lens, max_len, seqs):
+    """Runs evict_attention; the worst error over its bound, of outputs and of accumulators."""
     kara = _kara()
-    print(f"\n[case] count {kind} {dtype} Hq={Hq} Hkv={Hkv} d={d} bs={bs}", flush=True)
+    print(f"\n[case] count {kind} {dtype} Hq={Hq} Hkv={Hkv} d={d} bs={bs} n={len(seqs)}", flush=True)
     rng = np.random.default_rng(Hq * 7 + d + bs)
-    lens = [1, 31, 0, 256, 257, 1100, 1300, 90]
     c = Cache(rng, kind, dtype, Hq, Hkv, d, bs, lens, layers)
-    max_len = 1200                                          # the 1300-token sequence is over it
-    seqs = np.array([7, 5, 1, -1, 0, 8, 3, 4, 6, 2, 5], dtype=np.int32)        # 5 is listed twice
+    seqs = np.asarray(seqs, dtype=np.int32)
     n = len(seqs)
     q = torch.from_numpy(rng.standard_normal((layers, n, Hq, d)).astype(np.float32)).to(cc.DT[dtype])
     out = torch.full(q.shape, 7.0, dtype=torch.float32, device="cuda")
@@ -127,7 +123,24 @@ def test_attention_counts(kind, dtype, Hq, Hkv, d, bs, layers, n_new):
             worst = max(worst, float((np.abs(got[l, j] - ref[0]) / bound[0]).max()))
     ww = check_weights(c, seqs, n_new, max_len, per_key, 1)
     print("worst error / bound: out", worst, "weights", ww)
-    assert worst < 1 and ww < 1
+    return worst, ww
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("Hq,Hkv,d,bs,layers,n_new", [(32, 8, 128, 16, 2, 1), (5, 1, 128, 24, 1, 0), (6, 6, 64, 7, 1, 3),
+                                                      (32, 2, 64, 256, 1, 2000)])
+def test_attention_counts(kind, dtype, Hq, Hkv, d, bs, layers, n_new):
+    # the 1300-token sequence is over max_len, 5 is listed twice
+    assert max(count_case(kind, dtype, Hq, Hkv, d, bs, layers, n_new, [1, 31, 0, 256, 257, 1100, 1300, 90], 1200,
+                          [7, 5, 1, -1, 0, 8, 3, 4, 6, 2, 5])) < 1
+
+
+@pytest.mark.parametrize("kind", ["rows", "q4"])
+@pytest.mark.parametrize("layers,long,bs", [(4, 4200, 16), (2, 2500, 7), (4, 8300, 8)])
+def test_attention_counts_in_large_launches(kind, layers, long, bs):
+    # many units: longer splits, and more keys to a workgroup of the counting half
+    lens = [long, 1, 1025, long - 1] + [40] * 60
+    assert max(count_case(kind, "bf16", 8, 8, 64, bs, layers, 1, lens, long, list(range(63, -1, -1)))) < 1
 
 
 def test_attention_over_rows_is_decode_attention():
@@ -146,24 +159,18 @@ def test_attention_over_rows_is_decode_attention():
     assert float((a - b).abs().max()) <= 8 * cc.EPS * float(a.abs().max())     # (the divisions differ by a rounding)
 
 
-@pytest.mark.parametrize("kind,dtype", KINDS)
-@pytest.mark.parametrize("Hq,Hkv,d,bs,layers,T,n_new", [
-    (32, 8, 128, 16, 1, 1, 1), (8, 2, 128, 24, 2, 33, 33), (6, 2, 64, 7, 1, 200, 0), (16, 1, 64, 256, 1, 70, 5),
-    (40, 2, 128, 16, 1, 13, 2000)])
-def test_observe(kind, dtype, Hq, Hkv, d, bs, layers, T, n_new):
+def observe_case(kind, dtype, Hq, Hkv, d, bs, layers, T, n_new, lens, max_len, seqs):
     kara = _kara()
     print(f"\n[case] observe {kind} {dtype} Hq={Hq} Hkv={Hkv} d={d} bs={bs} T={T}", flush=True)
     rng = np.random.default_rng(Hq + d * 3 + T)
-    lens = [1, 63, 0, 64, 65, 700, 900, 129]
     c = Cache(rng, kind, dtype, Hq, Hkv, d, bs, lens, layers)
-    max_len = 800
-    seqs = np.array([7, 5, 1, -1, 0, 8, 3, 4, 6, 2, 5], dtype=np.int32)
+    seqs = np.asarray(seqs, dtype=np.int32)
     n = len(seqs)
     q = torch.from_numpy(rng.standard_normal((layers, n, T, Hq, d)).astype(np.float32)).to(cc.DT[dtype])
     ws = torch.full((kara.evict_observe_workspace_size(c.p, n, layers, T, max_len),), 255, dtype=torch.uint8, device="cuda")
     k, ks = c.lists("k", "ks")
     kara.evict_observe(c.p, cc.gpu(seqs), T, q.cuda(), k, c.weights, c.bt, c.sl, n_new, max_len, ws, k_scales=ks)
-    terms = 1 if kind == "rows" and dtype == "bf16" or kind == "q4" and dtype == "bf16" else 3
+    terms = 1 if dtype == "bf16" else 3
     per_key = [[None] * n for _ in range(layers)]
     for l in range(layers):
         for j, s in enumerate(seqs):
@@ -173,7 +180,25 @@ def test_observe(kind, dtype, Hq, Hkv, d, bs, layers, T, n_new):
             per_key[l][j] = (oc.attend(q64, kk, None, 1 / np.sqrt(d))[2], cc.logit_error(q64, kk, 1 / np.sqrt(d), 3 * terms))
     worst = check_weights(c, seqs, n_new, max_len, per_key, T)
     print("worst error / bound", worst)
-    assert worst < 1
+    return worst
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("Hq,Hkv,d,bs,layers,T,n_new", [
+    (32, 8, 128, 16, 1, 1, 1), (8, 2, 128, 24, 2, 33, 33), (6, 2, 64, 7, 1, 200, 0), (16, 1, 64, 256, 1, 70, 5),
+    (40, 2, 128, 16, 1, 13, 2000)])
+def test_observe(kind, dtype, Hq, Hkv, d, bs, layers, T, n_new):
+    assert observe_case(kind, dtype, Hq, Hkv, d, bs, layers, T, n_new, [1, 63, 0, 64, 65, 700, 900, 129], 800,
+                        [7, 5, 1, -1, 0, 8, 3, 4, 6, 2, 5]) < 1
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("Hq,Hkv,d,bs,T,n_new,lens,seqs", [
+    (10, 2, 128, 16, 300, 300, [2600, 299, 1700], [0, 2, 1]),       # keys split, rows in parts, more queries than tokens
+    (4, 4, 64, 24, 600, 0, [601, 4100], [1, 0, 1]),                 # a sequence twice, its parts added once
+    (3, 1, 64, 16, 5, 1, [9000], [0])])                             # the most splits of few rows
+def test_observe_in_pieces(kind, dtype, Hq, Hkv, d, bs, T, n_new, lens, seqs):
+    assert observe_case(kind, dtype, Hq, Hkv, d, bs, 1, T, n_new, lens, max(lens), seqs) < 1
 
 
 def test_observe_large_logits():
@@ -305,3 +330,15 @@ def test_evict_leaves_flagged_sequences():
     flagged = {1: kara.SEQ_BAD_PAGE, 2: kara.SEQ_BAD_PAGE, 3: kara.SEQ_DUP_PAGE, 4: win, 5: win, 6: dup, 7: dup,
                8: kara.SEQ_BAD_INDEX, 9: kara.SEQ_BAD_INDEX}
     check_evict(c, seqs, flagged, 100, 4, 20, run_evict(c, seqs, 100, 4, 20, 220))
+
+
+def test_evict_from_a_pool_of_many_pages():
+    # more pages than the check of doubled ones keeps bits for
+    kara = _kara()
+    rng = np.random.default_rng(23)
+    c = Cache(rng, "q4", "bf16", 1, 1, 64, 1, [300, 9000, 200, 250], extra=270000)
+    c.table[2, 7] = c.table[2, 150]
+    c.table[3, 249] = c.pages
+    c.bt.copy_(torch.from_numpy(c.table))
+    flagged = {2: kara.SEQ_DUP_PAGE, 0: kara.SEQ_BAD_PAGE}
+    check_evict(c, [3, 0, 2, 1], flagged, 120, 4, 20, run_evict(c, [3, 0, 2, 1], 120, 4, 20, 9000))

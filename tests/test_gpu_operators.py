@@ -246,6 +246,61 @@ def test_captured_steps(kind):
             assert torch.equal(x, y), i
 
 
+def test_captured_prompt():
+    """A prompt's append, attention and observation and a cut in a graph, replayed
+    with eager runs on the same workspace between: the eager bits every time."""
+    def step(p_, st):
+        k, v, ks, vs = p_.lists("k", "v", "ks", "vs")
+        p_.sl.zero_()
+        p_.k.q4_append(p_.p, p_.seqs, st["k"], st["v"], k, v, ks, vs, p_.bt, p_.sl, p_.status)
+        p_.k.q4_attention(p_.p, p_.seqs, 50, st["q"], k, v, ks, vs, p_.bt, p_.sl, p_.max_len, st["out"], p_.ws)
+        p_.k.evict_observe(p_.p, p_.seqs, 50, st["q"], k, list(p_.w.unbind(0)), p_.bt, p_.sl, 300, p_.max_len, p_.ws, k_scales=ks)
+        p_.k.evict_tokens(p_.p, p_.seqs, 200, 1, 4, k, v, list(p_.w.unbind(0)), p_.bt, p_.sl, p_.max_len, False, p_.status,
+                          p_.ws, k_scales=ks, v_scales=vs)
+        p_.k.q4_read(p_.p, p_.seqs, st["start"], 200, k, v, ks, vs, p_.bt, p_.sl, st["k_out"], st["v_out"])
+
+    runs = []
+    for captured in (False, True):
+        pr = Program("q4", seed=7)
+        for s in range(3):
+            for b in range(20):
+                pr.table[s, b] = pr.free.pop()
+        pr.bt.copy_(torch.from_numpy(pr.table))
+        st = {"k": pr.randn(2, 3, 300, 2, 64), "v": pr.randn(2, 3, 300, 2, 64), "q": pr.randn(2, 3, 50, 8, 64),
+              "out": torch.zeros(2, 3, 50, 8, 64, dtype=pr.dt, device="cuda"),
+              "start": torch.zeros(3, dtype=torch.int32, device="cuda")}
+        st["k_out"], st["v_out"] = (torch.zeros(2, 3, 200, 2, 64, dtype=pr.dt, device="cuda") for _ in range(2))
+        graph = None
+        if captured:
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                step(pr, st)
+            torch.cuda.current_stream().wait_stream(side)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step(pr, st)
+        seen = []
+        for i in range(5):
+            g = torch.Generator().manual_seed(i)
+            for x in ("k", "v", "q"):
+                st[x].copy_(torch.randn(st[x].shape, generator=g).to(pr.dt))
+            if graph is not None:
+                step(pr, st)                               # eager, between the replays
+                graph.replay()
+            else:
+                step(pr, st)
+            seen.append([t.clone() for t in (st["out"], st["k_out"], st["v_out"], pr.w, pr.sl, *pr.dev.values())])
+            if i % 2:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        runs.append(seen)
+    for i, (a, b) in enumerate(zip(*runs)):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y), i
+
+
 def test_refused_on_the_host():
     pr = Program("q4")
     k, v, ks, vs = pr.lists("k", "v", "ks", "vs")

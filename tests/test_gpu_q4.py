@@ -259,3 +259,51 @@ def test_far_rows():
         delta = cc.logit_error(q.double().numpy(), val["k"], 1 / np.sqrt(d))
         bound = cc.attention_bound(ref, mass, delta, n, "bf16", True)
         assert (np.abs(o[0, 0].double().cpu().numpy() - ref) < bound).all()
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,bs,T", [
+    ("bf16", 32, 8, 128, 16, 20), ("bf16", 32, 8, 128, 16, 40), ("bf16", 12, 6, 64, 7, 90), ("f32", 32, 8, 128, 16, 20),
+    ("f32", 16, 8, 64, 24, 60), ("bf16", 32, 8, 64, 16, 140), ("f32", 32, 8, 128, 16, 100)])
+def test_attention_of_many_rows_in_larger_launches(dtype, Hq, Hkv, d, bs, T):
+    # enough row blocks that keys are not split: four waves a workgroup, then eight
+    lens = [1, 19, 20, 64, 65, 300, 0, 129, 700, 400, 128, 333, 90, 41, 512, 299]
+    worst, _ = attention_case(dtype, Hq, Hkv, d, bs, T, 1, lens, 650)       # 700 is over max_len
+    print("worst error / bound", worst)
+    assert worst < 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_long_append_reports_and_leaves(dtype):
+    # the reports and refusals of a few tokens, for an append of many
+    kara = _kara()
+    rng = np.random.default_rng(6)
+    d, Hkv, bs, n_new, mb = 64, 3, 16, 500, 36
+    lens = np.array([10, 3, 20, 10, 10, 0], dtype=np.int32)
+    table, pages, _ = cc.table_for(rng, lens + n_new, bs, mb)
+    table[2, 20] = pages
+    lens[3] = mb * bs - n_new + 1                     # one token past the table
+    p = cc.params(Hkv, Hkv, d, bs, pages, mb, len(lens), dtype)
+    seqs = np.array([5, 2, 1, 3, 4, 4, 6, 0], dtype=np.int32)
+    x = rng.standard_normal((1, len(seqs), n_new, Hkv, d)).astype(np.float32)
+    x[0, 2, 499, 2, 63] = np.nan                      # the last element of a sequence
+    x[0, 7, 250, 0, 0] = np.inf
+    x[0, 1, 3, 0, 0] = np.nan                         # (of one that is left)
+    x = torch.from_numpy(x).to(cc.DT[dtype])
+    pools = [torch.full((pages, Hkv, bs, d // w), 3, dtype=torch.uint8, device="cuda") for w in (2, 2, 32, 32)]
+    status = torch.empty(len(seqs), dtype=torch.int32, device="cuda")
+    sl = cc.gpu(lens)
+    kara.q4_append(p, cc.gpu(seqs), torch.zeros_like(x).cuda(), x.cuda(), *[[t] for t in pools], cc.gpu(table), sl, status)
+    dup, odd = kara.SEQ_DUP_TRIGGER, kara.SEQ_NONFINITE
+    assert status.tolist() == [0, kara.SEQ_BAD_PAGE, odd, kara.SEQ_BAD_WINDOW, dup, dup, kara.SEQ_BAD_INDEX, odd]
+    want = lens.copy()
+    want[[5, 1, 0]] += n_new
+    assert sl.tolist() == want.tolist()
+    codes, scales = oc.q4_quantize(x[0].double().numpy())
+    touched = set()
+    for j, s in ((0, 5), (2, 1), (7, 0)):
+        n = int(want[s])
+        touched |= set(table[s][:-(-n // bs)].tolist())
+        assert np.array_equal(cc.rows_of(pools[1].cpu().numpy(), table, s, n, bs)[lens[s]:], codes[j])
+        assert np.array_equal(cc.rows_of(pools[3].cpu().numpy(), table, s, n, bs)[lens[s]:], scales[j])
+    for t in pools:
+        assert (t.cpu().numpy()[sorted(set(range(pages)) - touched)] == 3).all()
