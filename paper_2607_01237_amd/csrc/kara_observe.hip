@@ -23,6 +23,7 @@ enum { kBf16Rows, kF32Rows, kCodeRows };
 struct ObserveArgs {
   Geom g;
   int n, T, n_new, max_len;
+  uint32_t units;                       // (layer, sequence, KV head)
   int row_blocks, splits, split_keys;   // row statistics
   int bs_shift;                         // log2(bs) when bs is a power of two, else -1
   int key_blocks, parts, part_rows;     // column sums: the rows of a unit in parts
@@ -82,17 +83,27 @@ __device__ __forceinline__ int swz(int row) {
   return ((row & 3) << 1) | ((row >> 2) & 1);
 }
 
-// Piece of a block's item, of `pieces` each.  Blocks go round the 8 XCDs, so the
-// pieces of eight items in a row fall to the same ones; the next eight are shifted,
-// or an XCD would get all the long pieces (2 prompts of 2048 queries: half the CUs'
-// time idle).
-__device__ __forceinline__ int spread(uint32_t block, uint32_t pieces) {
-  return (block + block / (8 * pieces)) % pieces;
+// Unit and piece of a block, the pieces of all units in turn and the longest first:
+// the last ones fill what is left.  Where all blocks are placed at once, two to a CU
+// (pairs), the second half runs backwards, so that long ones share a CU with short
+// ones.  Blocks go round the 8 XCDs: with eight KV heads a unit's pieces stay on one XCD, whose L2 then holds its
+// rows, and each XCD has heads of every sequence; with other counts units are shifted
+// from piece to piece, or an XCD might get all the pieces of a long sequence.
+constexpr uint32_t kCUs = 256;
+struct Piece {
+  uint32_t unit, piece;
+};
+__device__ __forceinline__ Piece piece_of(uint32_t units, int Hkv, bool pairs) {
+  uint32_t block = blockIdx.x;
+  if (pairs && gridDim.x <= 2 * kCUs && block >= kCUs) block = gridDim.x - 1 - (block - kCUs);
+  const uint32_t piece = block / units, at = block - piece * units;
+  return {Hkv % 8 == 0 ? at : (at + piece) % units, piece};
 }
 
 constexpr int kObsThreads = 512;
 constexpr int kObsWaves = kObsThreads / 64;
 constexpr int kChunk = 64;                  // rows staged at a time
+constexpr int kMaxSplits = 16;              // of a row's keys, or parts of a key's rows
 
 template <int NT, int D>
 struct ChunkLds {
@@ -160,11 +171,10 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sta
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
-  uint32_t rest = blockIdx.x;
-  const int split = spread(rest, (uint32_t)a.splits);
-  rest /= (uint32_t)a.splits;
-  const int rb = a.row_blocks - 1 - (int)(rest % (uint32_t)a.row_blocks);     // rows that see most keys first
-  const uint32_t u = rest / (uint32_t)a.row_blocks;
+  const Piece pc = piece_of(a.units, g.Hkv, NK * NQ == 1);
+  const uint32_t u = pc.unit;
+  const int split = pc.piece % (uint32_t)a.splits;
+  const int rb = a.row_blocks - 1 - (int)(pc.piece / (uint32_t)a.splits);     // rows that see most keys first
   Unit x;
   if (!unit_of(a, u, &x)) return;
   const int G = g.G, R = G * a.T;
@@ -214,11 +224,14 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sta
       page[i] = row_pages[b];
     }
   };
+  // (a pool has fewer than 2^32 rows)
+  const void *const kbase = a.k.p[x.l], *const sbase = a.ks.p[x.l];
+  const uint32_t page_rows = (uint32_t)g.Hkv * g.bs, head_row = (uint32_t)x.h * g.bs;
   auto fetch = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int p = min(max(page[i], 0), g.num_pages - 1);
-      pre[i].load(a.k.p[x.l], a.ks.p[x.l], (uint64_t)(((int64_t)p * g.Hkv + x.h) * g.bs + slot[i]), soct, D);
+      const uint32_t p = min(max(page[i], 0), g.num_pages - 1);
+      pre[i].load(kbase, sbase, p * page_rows + (head_row + slot[i]), soct, D);
     }
   };
   // two 16-key tiles against the wave's rows
@@ -337,11 +350,10 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
-  uint32_t rest = blockIdx.x;
-  const int part = spread(rest, (uint32_t)a.parts);
-  rest /= (uint32_t)a.parts;
-  const int kb = rest % (uint32_t)a.key_blocks;        // (the first keys are seen by most rows)
-  const uint32_t u = rest / (uint32_t)a.key_blocks;
+  const Piece pc = piece_of(a.units, g.Hkv, NK * NQ == 1);
+  const uint32_t u = pc.unit;
+  const int part = a.parts - 1 - (int)(pc.piece % (uint32_t)a.parts);
+  const int kb = pc.piece / (uint32_t)a.parts;         // the first keys are seen by most rows
   Unit x;
   if (!unit_of(a, u, &x)) return;
   const int key0 = kb * kObsWaves * 16 * KT;
@@ -383,26 +395,28 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum
   const int srow = tid / kOct, soct = tid % kOct;
   Octet<QSRC> pre[kPer];
   floatx2 st = {0.f, 1.f};
-  int qt[kPer], qg[kPer];                              // query and head in group of the next chunk's rows
-  const int step_t = kChunk / G, step_g = kChunk % G;
+  uint32_t qrow[kPer];                                 // row of q, and head in group, of the next chunk's rows
+  int qg[kPer];
+  const int step_g = kChunk % G, step = kChunk / G * g.Hq + step_g;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int r = r_lo + srow + i * (kObsThreads / kOct);
-    qt[i] = r / G;
-    qg[i] = r - qt[i] * G;
+    qg[i] = r % G;
+    qrow[i] = (uint32_t)(r / G) * g.Hq + qg[i];
   }
-  const uint64_t qrow0 = ((uint64_t)x.l * a.n + x.j) * a.T * g.Hq + x.h * G;
+  const char* const qbase = (const char*)a.q + (((uint64_t)x.l * a.n + x.j) * a.T * g.Hq + x.h * G) * (D * (QSRC == kF32Rows ? 4 : 2));
+  const floatx2* const ustats = a.stats + (int64_t)u * R * a.splits;
   auto fetch = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       pre[i].zero();
       if (r0 + srow + i * (kObsThreads / kOct) < r_hi)
-        pre[i].load(a.q, nullptr, qrow0 + (uint64_t)qt[i] * g.Hq + qg[i], soct, D);
-      qt[i] += step_t;
+        pre[i].load(qbase, nullptr, qrow[i], soct, D);
+      qrow[i] += step;
       qg[i] += step_g;
-      if (qg[i] >= G) qg[i] -= G, ++qt[i];
+      if (qg[i] >= G) qg[i] -= G, qrow[i] += g.Hq - G;
     }
-    if (tid < kChunk && r0 + tid < r_hi) st = a.stats[((int64_t)u * R + r0 + tid) * a.splits];
+    if (tid < kChunk && r0 + tid < r_hi) st = ustats[(int64_t)(r0 + tid) * a.splits];
   };
   // one 16-row tile against the wave's keys
   auto tile = [&](int buf, int rt, int r0, auto masked) __attribute__((always_inline)) {
@@ -505,7 +519,6 @@ constexpr int kHeldWg = kObsWaves * 16 * kHeld;         // of a workgroup
 // Launches with fewer workgroups than this split: the row statistics their keys (512
 // a split at least), the column sums their rows (256 a part at least).
 constexpr int kObsWgs = 512;
-constexpr int kMaxParts = 16;
 
 struct Plan {
   int row_blocks, splits, split_keys, key_blocks, parts, part_rows;
@@ -519,11 +532,11 @@ Plan plan_of(const Geom& g, int n, int n_layers, int T, int max_len) {
   const int64_t R = (int64_t)g.G * T;
   x.row_blocks = (int)((R + kHeldWg - 1) / kHeldWg);
   x.splits = 1;
-  while (x.splits < kMaxParts && x.units * x.row_blocks * x.splits < kObsWgs && max_len > x.splits * 2 * 512) x.splits *= 2;
+  while (x.splits < kMaxSplits && x.units * x.row_blocks * x.splits < kObsWgs && max_len > x.splits * 2 * 512) x.splits *= 2;
   x.split_keys = ((max_len + x.splits - 1) / x.splits + kChunk - 1) / kChunk * kChunk;
   x.key_blocks = (max_len + kHeldWg - 1) / kHeldWg;
   x.parts = 1;
-  while (x.parts < kMaxParts && x.units * x.key_blocks * x.parts < kObsWgs && R > x.parts * 2 * 256) x.parts *= 2;
+  while (x.parts < kMaxSplits && x.units * x.key_blocks * x.parts < kObsWgs && R > x.parts * 2 * 256) x.parts *= 2;
   x.part_rows = (int)(((R + x.parts - 1) / x.parts + kChunk - 1) / kChunk * kChunk);
   x.ld = (max_len + 31) / 32 * 32;
   x.stats_bytes = ((size_t)(x.units * R * x.splits) * sizeof(floatx2) + 255) & ~(size_t)255;
@@ -608,6 +621,7 @@ kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_
   a.T = n_query;
   a.n_new = n_new;
   a.max_len = max_len;
+  a.units = (uint32_t)x.units;
   a.row_blocks = x.row_blocks;
   a.splits = x.splits;
   a.split_keys = x.split_keys;
