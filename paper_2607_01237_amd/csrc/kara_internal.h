@@ -122,7 +122,7 @@ struct Q4Split {
   int T;                      // queries per sequence, its last T positions
   int n_rt;                   // tiles of 16 query rows per (layer, sequence, KV head)
   int split_keys, n_splits, max_len;
-  int run;                    // set by the launch
+  int run, bs_shift;          // set by the launches
   const int32_t *seqs, *bt, *seq_lens;
   const void* q;              // [n_layers][n][T][Hq][d]
   PoolPtrs kp, vp, ksp, vsp;  // codes and scales
@@ -151,7 +151,7 @@ struct Q4ChunkPlan {
   int64_t blocks;
 };
 Q4ChunkPlan q4_chunk_plan(const Geom& g, int n, int n_layers, int T, int max_len);
-hipError_t launch_q4_chunk(const Q4Split& a, const Q4ChunkPlan& x, hipStream_t stream);
+hipError_t launch_q4_chunk(Q4Split a, const Q4ChunkPlan& x, hipStream_t stream);
 
 }  // namespace kara
 

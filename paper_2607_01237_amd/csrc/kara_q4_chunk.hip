@@ -166,14 +166,18 @@ __global__ __launch_bounds__(W * 64, 2) void q4_chunk_kernel(Q4Split a) {
   const int32_t* row_pages = a.bt + (int64_t)(none ? 0 : s) * g.max_blocks;
   // (keys past the last one repeat it, finite and masked for every query)
   auto pos_of = [&](int ch) __attribute__((always_inline)) { return min(k_lo + ch * kChKeys + skey, k_hi - 1); };
-  auto page_of = [&](int ch) __attribute__((always_inline)) { return row_pages[pos_of(ch) / g.bs]; };
+  // (a pool has fewer than 2^32 rows; the page of a chunk is read a chunk before its codes)
+  const uint32_t page_rows = (uint32_t)g.Hkv * g.bs, head_row = (uint32_t)h * g.bs;
   uint4 cw[C::kPer];
   uint32_t cscale[C::kPer];
-  int page = 0;
-  auto fetch = [&](int ch) __attribute__((always_inline)) {
-    const int pos = pos_of(ch), b = pos / g.bs;
-    const int pg = min(max(page, 0), g.num_pages - 1);
-    const uint64_t row = (uint64_t)(((int64_t)pg * g.Hkv + h) * g.bs + (pos - b * g.bs));
+  int page = 0, slot = 0;
+  auto look = [&](int ch) __attribute__((always_inline)) {
+    const int pos = pos_of(ch), b = a.bs_shift >= 0 ? pos >> a.bs_shift : pos / g.bs;
+    slot = pos - b * g.bs;
+    page = row_pages[b];
+  };
+  auto fetch = [&]() __attribute__((always_inline)) {
+    const uint64_t row = (uint32_t)min(max(page, 0), g.num_pages - 1) * page_rows + (head_row + slot);
 #pragma unroll
     for (int i = 0; i < C::kPer; ++i) {
       const bool is_v = C::kPer == 2 ? i == 1 : tid >= kHalf;
@@ -301,14 +305,14 @@ __global__ __launch_bounds__(W * 64, 2) void q4_chunk_kernel(Q4Split a) {
 
   if (n_chunks > 0) {
     if (stager) {
-      page = page_of(0);
-      fetch(0);
+      look(0);
+      fetch();
       stage(0);
       if (n_chunks > 1) {
-        page = page_of(1);
-        fetch(1);
+        look(1);
+        fetch();
       }
-      if (n_chunks > 2) page = page_of(2);
+      if (n_chunks > 2) look(2);
     }
     auto step = [&](int ch, auto masked) __attribute__((always_inline)) {
       // every wave has written its part of chunk ch, and is done with chunk ch - 1,
@@ -325,8 +329,8 @@ __global__ __launch_bounds__(W * 64, 2) void q4_chunk_kernel(Q4Split a) {
       }
       if (stager && ch + 1 < n_chunks) {
         stage((ch + 1) & 1);
-        if (ch + 2 < n_chunks) fetch(ch + 2);
-        if (ch + 3 < n_chunks) page = page_of(ch + 3);
+        if (ch + 2 < n_chunks) fetch();
+        if (ch + 3 < n_chunks) look(ch + 3);
       }
       if (work) phase_b(st);
     };
@@ -405,7 +409,8 @@ Q4ChunkPlan q4_chunk_plan(const Geom& g, int n, int n_layers, int T, int max_len
   return x;
 }
 
-hipError_t launch_q4_chunk(const Q4Split& a, const Q4ChunkPlan& x, hipStream_t stream) {
+hipError_t launch_q4_chunk(Q4Split a, const Q4ChunkPlan& x, hipStream_t stream) {
+  a.bs_shift = (a.g.bs & (a.g.bs - 1)) == 0 ? __builtin_ctz((unsigned)a.g.bs) : -1;
   if (a.g.dtype == KARA_F32) return x.waves == 8 ? launch<3, 1, 8>(a, x.blocks, stream) : launch<3, 1, 4>(a, x.blocks, stream);
   if (x.qt == 1) return x.waves == 8 ? launch<1, 1, 8>(a, x.blocks, stream) : launch<1, 1, 4>(a, x.blocks, stream);
   return x.waves == 8 ? launch<1, 2, 8>(a, x.blocks, stream) : launch<1, 2, 4>(a, x.blocks, stream);
