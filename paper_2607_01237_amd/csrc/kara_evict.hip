@@ -33,9 +33,11 @@ constexpr int kFinKeys = 4 * kFinThreads;   // keys per step
 
 // Second half of a counting decoding step: the splits' records joined to the
 // output (a record: maximum and sum, ml_step apart, and o, o_step apart), and every
-// key's weight -- exp2(logit - M) / L over the group's query
-// heads -- added to its accumulator.  One workgroup per (layer, sequence, KV
-// head, `steps` runs of 1024 keys); a sequence's workgroups share out its query heads' outputs.
+// key's weight -- exp2(logit - M) / L over the group's query heads -- added to its
+// accumulator.  One workgroup per (layer, sequence, KV head, `steps` runs of 1024
+// keys); a sequence's workgroups share out its query heads' outputs.  60 sequences of
+// 4-8.2K tokens, 2 layers, 40/8 heads: 49 us for 165 MB, 3.4 TB/s (accumulators come
+// in pieces of a page's 16 tokens).
 template <int D>
 __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
     Geom g, int n, const int32_t* __restrict__ seqs, const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens,
@@ -150,6 +152,7 @@ struct EvictArgs {
   WeightPtrs w;
   int row_bytes;              // of k and v
   int scale_bytes;            // of ks and vs; 0: none
+  int cols;                   // pieces that the move cuts a row into
 };
 
 // Pages of a listed sequence as they were before the cut: those that it released
@@ -372,19 +375,21 @@ constexpr int kMoveThreads = 1024;
 constexpr int kMoveUnroll = 8;
 constexpr int kMoveStage = 32768 / 4;     // kept positions and table entries held in LDS, at most
 
-// One workgroup per (layer, sequence, KV head, part): K rows, V rows, and the small
-// arrays (scales, accumulators).  Row i takes row kept[i] >= i, so working up in
+// One workgroup per (layer, sequence, KV head, part): a piece of the K rows or of the V
+// rows, or the small arrays (scales, accumulators).  Row i takes row kept[i] >= i, so working up in
 // tiles -- a tile's rows all loaded before any of it is stored -- never overwrites
-// a row still to be read.  1024 threads a workgroup: 64 sequences x 4 layers cut from
-// 3.9-8.2K to 3.8K tokens (8.1 GB) 1705 us with 256, 1679 so; 8 sequences of one
-// layer, where a tile's latency is all that the launch spends, 36 us with 256, 24 so.
+// a row still to be read.  Wide rows are cut into pieces, a workgroup each.  Bound by
+// the bytes: 64 sequences x 4 layers cut from 3.9-8.2K to 3.8K tokens (8.1 GB) in
+// 1576 us, 5.1 TB/s.  1024 threads a workgroup: that cut was 2 % slower with 256; 8
+// sequences of one layer, where a tile's latency is all that the launch spends, took
+// 36 us with 256, 24 so.
 template <bool STAGED>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
   extern __shared__ int32_t stage[];
   const Geom& g = a.g;
   const int tid = threadIdx.x;
-  const int part = blockIdx.x % 3;
-  const uint32_t u = blockIdx.x / 3;
+  const int parts = 2 * a.cols + 1, part = blockIdx.x % (uint32_t)parts;
+  const uint32_t u = blockIdx.x / (uint32_t)parts;
   uint32_t rest = u;
   const int h = rest % (uint32_t)g.Hkv;
   rest /= (uint32_t)g.Hkv;
@@ -405,9 +410,10 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
     const int64_t page = STAGED ? stage[a.keep + b] : pages[b];
     return (page * g.Hkv + h) * g.bs + (pos - b * g.bs);
   };
-  if (part < 2) {
-    char* base = (char*)(part ? a.v.p[l] : a.k.p[l]);
-    const int cpr = a.row_bytes >> 4, rpp = kMoveThreads / cpr, tile = rpp * kMoveUnroll;
+  if (part < 2 * a.cols) {
+    const int piece = a.row_bytes / a.cols;
+    char* base = (char*)(part & 1 ? a.v.p[l] : a.k.p[l]) + (part >> 1) * piece;
+    const int cpr = piece >> 4, rpp = kMoveThreads / cpr, tile = rpp * kMoveUnroll;
     const int c = tid % cpr, r = tid / cpr;
     for (int x0 = 0; x0 < a.keep; x0 += tile) {
       u32x4 v[kMoveUnroll];
@@ -631,7 +637,7 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
   if (kept) need = (size_t)n * sizeof(int32_t);     // (the lengths alone)
   if (!workspace || workspace_bytes < need) return KARA_ERR_WORKSPACE;
   const int64_t units = (int64_t)n_layers * n * g.Hkv;
-  if (!grid_ok(units * 12)) return KARA_ERR_UNSUPPORTED;
+  if (!grid_ok(units * 4 * (2 * 4 + 1))) return KARA_ERR_UNSUPPORTED;
   a.n = n;
   a.n_layers = n_layers;
   a.keep = keep;
@@ -663,7 +669,12 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
   e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
   const int64_t staged = (int64_t)keep + (max_len + g.bs - 1) / g.bs;
-  const dim3 grid((unsigned)(units * 3)), block(kMoveThreads);
+  // Rows in pieces of 128 bytes, of 64 while the launch leaves CUs without a workgroup:
+  // half as many tiles one after the other (8 sequences of one layer 24 -> 18.5 us, two
+  // 12.7 -> 7.4; the large cut above 1589 -> 1576).
+  a.cols = std::max(1, a.row_bytes / 128);
+  while (units * 2 * a.cols < 256 && a.row_bytes / a.cols > 64) a.cols *= 2;
+  const dim3 grid((unsigned)(units * (2 * a.cols + 1))), block(kMoveThreads);
   if (staged <= kMoveStage) hipLaunchKernelGGL((evict_move_kernel<true>), grid, block, (size_t)staged * 4, s, a);
   else hipLaunchKernelGGL((evict_move_kernel<false>), grid, block, 0, s, a);
   return hip_status(hipGetLastError());

@@ -4,16 +4,17 @@
 // One workgroup of W waves owns 16 QT W query rows of one (layer, sequence, KV
 // head), rows ordered (query, head in group), and walks the keys they see 64 at a
 // time.  Its threads fetch a chunk's codes two chunks ahead into registers (16
-// bytes, one block of 32 values with its scale, at a time), convert them in hardware to bf16 -- exactly -- and write them to the other of two LDS
-// stages while the products of the present one run: a chunk is converted once for
-// all rows, with one barrier.  From there the products are those of the recompute
+// bytes, one block of 32 values with its scale, at a time), convert them in hardware
+// to bf16 -- exactly -- and write them to the other of two LDS stages while the
+// products of the present one run: a chunk is converted once for all rows, with one
+// barrier.  From there the products are those of the recompute
 // attention: S^T = K Q^T, weights as they stand the B operand of O^T += V^T P^T with
 // V through the transposed LDS read, the row sums one more product with ones.
 //
 // NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones).
 //
-// 16 sequences x 1024 queries over 2.5-8.7K cached, 32/8 heads, bf16: 1336 us, 1023
-// TFLOP/s; fp32, 8 x 512: 876 us, 409 TFLOP/s of three products for each.
+// 16 sequences x 1024 queries over 2.5-8.7K cached, 32/8 heads, bf16: 1320 us, 1035
+// TFLOP/s; fp32, 8 x 512: 853 us, 420 TFLOP/s of three products for each.
 #include <algorithm>
 #include <type_traits>
 
@@ -392,10 +393,11 @@ Q4ChunkPlan q4_chunk_plan(const Geom& g, int n, int n_layers, int T, int max_len
   auto blocks = [&](int waves) { return units * ((R + waves * 16 * x.qt - 1) / (waves * 16 * x.qt)); };
   // Eight waves, a CU's worth of registers, convert a chunk once for 256 rows (bf16)
   // but stand one to a CU: a launch of half to all of the CUs' number ends with its
-  // longest.  There four waves, two to a CU (4 x 512 queries over 2.5-8.7K, 256
-  // blocks: 267 -> 223 us; 16 x 128: 274 -> 224; 5 x 512, 320 blocks: 269 -> 241; 6 x
-  // 512, 384 blocks: 277 against 329; below 128 blocks keys are split, to the same
-  // number of workgroups either way).
+  // longest.  There four waves, two to a CU, lengths of 2.5-8.7K: 4 x 512 queries,
+  // 256 blocks: 268 -> 215 us; 16 x 128: 272 -> 216; 5 x 512, 320 blocks: 270 -> 229;
+  // 6 x 512, 384 blocks: 276 against 316.  (Lengths are not known here: 4 x 512 over
+  // 8.7K each lose, 272 -> 291.  Below 128 blocks keys are split, to the same number
+  // of workgroups either way.)
   x.waves = blocks(8) * 2 > kCUs && blocks(8) <= kCUs * 5 / 4 ? 4 : 8;
   x.rows_wg = x.waves * 16 * x.qt;
   x.n_rb = (int)((R + x.rows_wg - 1) / x.rows_wg);
