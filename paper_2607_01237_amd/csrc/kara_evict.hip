@@ -35,7 +35,7 @@ constexpr int kFinKeys = 4 * kFinThreads;   // keys per step
 // output (a record: maximum and sum, ml_step apart, and o, o_step apart), and every
 // key's weight -- exp2(logit - M) / L over the group's query heads -- added to its
 // accumulator.  One workgroup per (layer, sequence, KV head, `steps` runs of 1024
-// keys); a sequence's workgroups share out its query heads' outputs.  60 sequences of
+// keys); a sequence's workgroups share out its query heads' outputs.  64 sequences of
 // 4-8.2K tokens, 2 layers, 40/8 heads: 49 us for 165 MB, 3.4 TB/s (accumulators come
 // in pieces of a page's 16 tokens).
 template <int D>

@@ -278,9 +278,9 @@ constexpr int kSplitWgTarget = 4096; // workgroups a launch keeps when its split
 // per lane, and the pairs of columns that the conversion gives are put together to
 // pairs of keys by byte permutes.
 //
-// Bound by the bytes of the codes where there are many workgroups: 124 sequences of
+// Bound by the bytes of the codes where there are many workgroups: 96 sequences of
 // 7-8.2K tokens, 2 layers, 40/8 heads, d = 128: 310 us for 1.59 GB, 5.1 TB/s; with
-// logits for the counting attention (60 sequences of 4-8.2K) 4.0 TB/s of codes, its
+// logits for the counting attention (64 sequences of 4-8.2K) 4.0 TB/s of codes, its
 // weights in three terms.
 //
 // NQ: bf16 terms of a query (1: bf16, exact; 3: fp32, 24 bits); NP: bf16 terms of a
