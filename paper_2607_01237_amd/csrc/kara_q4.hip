@@ -36,19 +36,45 @@ __global__ __launch_bounds__(kAppendThreads) void q4_commit_kernel(Geom g, int n
 }
 
 constexpr int kQuantUnroll = 4;       // octets per thread
+constexpr int kMaxOctets = 1 << 28;   // of a token: 32-bit offsets
 
+// Eight values as loaded.  bf16: 16 bytes a lane.  fp32: 32, which lanes load in two
+// pieces of 16, side by side over the wave -- octets 0..31 of its 64 first, then the
+// others -- and pairs of lanes exchange halves: lane 2i ends with octet i, lane 2i + 1
+// with octet 32 + i.
 template <int DT>
-struct QuantSrc {
+struct Octet {
   static constexpr int kBytes = DT == KARA_BF16 ? 16 : 32;   // of eight values
+  static constexpr int kStep = DT == KARA_BF16 ? 1 : 2;      // lanes between a row's octets
   u32x4 v[kBytes / 16];
-  __device__ __forceinline__ void load(const char* p) {
-    // (fp32: a lane's two halves of 32 bytes share a line with its neighbours', which
-    // then has to stay until the second load)
-    if constexpr (kBytes == 16) {
-      v[0] = __builtin_nontemporal_load((const u32x4*)p);
+  static __device__ __forceinline__ int octet(int lane) { return kStep == 1 ? lane : (lane & 1) * 32 + (lane >> 1); }
+  // octets wave0 .. wave0 + 63 of `count` at p; past the last the end is read again, so
+  // that no branch stands between loads
+  __device__ __forceinline__ void load(const char* p, int wave0, int lane, int count) {
+    const int at = wave0 * kStep + lane, last = count * kStep - 1;
+    v[0] = __builtin_nontemporal_load((const u32x4*)p + min(at, last));
+    if constexpr (kStep == 2) v[1] = __builtin_nontemporal_load((const u32x4*)p + min(at + 64, last));
+  }
+  // the exchange: after a load, before a store
+  __device__ __forceinline__ void exchange(int lane) {
+    if constexpr (kStep == 2) {
+      const bool odd = lane & 1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t give = odd ? v[0][e] : v[1][e];
+        const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)give, 0xb1, 0xf, 0xf, true);   // lanes 2i, 2i + 1
+        v[0][e] = odd ? got : v[0][e];
+        v[1][e] = odd ? v[1][e] : got;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char* p, int wave0, int lane, int count) const {
+    if constexpr (kStep == 1) {
+      if (wave0 + lane < count) __builtin_nontemporal_store(v[0], (u32x4*)(p + (int64_t)(wave0 + lane) * 16));
     } else {
-      v[0] = ((const u32x4*)p)[0];
-      v[1] = ((const u32x4*)p)[1];
+      u32x4* at = (u32x4*)(p + (int64_t)wave0 * 32) + lane;
+      if (wave0 + (lane >> 1) < count) __builtin_nontemporal_store(v[0], at);
+      if (wave0 + 32 + (lane >> 1) < count) __builtin_nontemporal_store(v[1], at + 64);
     }
   }
 };
@@ -56,7 +82,7 @@ struct QuantSrc {
 // Eight values to eight codes; four lanes hold a block and find its scale byte
 // together.  odd: a value was not finite.
 template <int DT>
-__device__ __forceinline__ uint32_t q4_encode(const QuantSrc<DT>& src, uint32_t* byte, bool* odd) {
+__device__ __forceinline__ uint32_t q4_encode(const Octet<DT>& src, uint32_t* byte, bool* odd) {
   float x[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -78,8 +104,8 @@ __device__ __forceinline__ uint32_t q4_encode(const QuantSrc<DT>& src, uint32_t*
       if (m < 0x7f800000u) top = max(top, m);
     }
   }
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+  top = max(top, (uint32_t)__shfl_xor((int)top, Octet<DT>::kStep, 64));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2 * Octet<DT>::kStep, 64));
   *byte = q4_scale_byte(top);
   const float scale = q4_scale(*byte);
   uint32_t c = 0;
@@ -97,50 +123,63 @@ __device__ __forceinline__ void q4_store(uint8_t* codes, uint8_t* scales, int64_
 }
 
 // The rows after q4_commit_kernel.  Grid as the append of rows: (sequences x token
-// chunks, layer, K|V).  Bound by the bytes: with the reading back of the same rows, 4
-// x 4 layers of 4000 tokens (664 MB) in 120 us, 5.5 TB/s.
+// chunks, layer, K|V).  Bound by the bytes: 4 x 4 layers of 4000 tokens (332 MB) in 64
+// us, the reading back 51; fp32 (595 MB) 106 and 101 (152 and 153 with each lane's 32
+// bytes loaded as they lie).
 template <int DT, int D>
 __global__ __launch_bounds__(kAppendThreads) void q4_append_kernel(
     Geom g, int n, const int32_t* __restrict__ seqs, int n_new, int toks, int chunks, const char* __restrict__ k_new,
     const char* __restrict__ v_new, PoolPtrs kp, PoolPtrs vp, PoolPtrs ksp, PoolPtrs vsp,
     const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens, int32_t* __restrict__ status) {
   constexpr int kOctets = D / 8;                     // of a row
-  using Src = QuantSrc<DT>;
+  using Src = Octet<DT>;
   const int j = blockIdx.x / chunks;
   const int tok0 = (blockIdx.x - j * chunks) * toks;
   const int l = blockIdx.y;
   const int kv = blockIdx.z;
+  const int per_tok = g.Hkv * kOctets;
+  const int count = min(toks, n_new - tok0) * per_tok;
+  const char* src = (kv ? v_new : k_new) + (((int64_t)l * n + j) * n_new + tok0) * per_tok * Src::kBytes;
+  const int lane = threadIdx.x & 63, wave0 = threadIdx.x & ~63, octet0 = wave0 + Src::octet(lane);
+  Src v[kQuantUnroll];
+  auto load = [&](int from) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < kQuantUnroll; ++k) v[k].load(src, from + k * kAppendThreads + wave0, lane, count);
+  };
+  // the first rows are on their way while status, length and pages are looked up
+  load(0);
   // (other workgroups may have reported a value that is not finite by now)
   if (status[j] & ~KARA_SEQ_NONFINITE) return;
   const int s = seqs[j];
-  const int per_tok = g.Hkv * kOctets;
-  const int count = min(toks, n_new - tok0) * per_tok;
   const int pos0 = seq_lens[s] - n_new + tok0;
   const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
-  const char* src = (kv ? v_new : k_new) + (((int64_t)l * n + j) * n_new + tok0) * per_tok * Src::kBytes;
   uint8_t* codes = (uint8_t*)(kv ? vp.p[l] : kp.p[l]);
   uint8_t* scales = (uint8_t*)(kv ? vsp.p[l] : ksp.p[l]);
   bool odd = false;
-  // (count is a multiple of a block's four octets, so the four lanes of a block
-  // stay together)
-  for (int i0 = threadIdx.x; i0 < count; i0 += kAppendThreads * kQuantUnroll) {
-    Src v[kQuantUnroll];
+  // (count is a multiple of a row's octets, so the lanes of a block stay together)
+  for (int from = 0; from < count; from += kAppendThreads * kQuantUnroll) {
+    // where they go, looked up together: a lookup between stores would wait for those
+    uint32_t row[kQuantUnroll], page[kQuantUnroll];
+    int o[kQuantUnroll];
 #pragma unroll
     for (int k = 0; k < kQuantUnroll; ++k) {
-      const int i = i0 + k * kAppendThreads;
-      if (i < count) v[k].load(src + (int64_t)i * Src::kBytes);
-    }
-#pragma unroll
-    for (int k = 0; k < kQuantUnroll; ++k) {
-      const int i = i0 + k * kAppendThreads;
-      if (i >= count) continue;
-      uint32_t byte;
-      const uint32_t code = q4_encode<DT>(v[k], &byte, &odd);
+      const int i = min(from + k * kAppendThreads + octet0, count - 1);
       const int tok = i / per_tok, r = i - tok * per_tok;
-      const int h = r / kOctets, o = r - h * kOctets;
-      const int pos = pos0 + tok, b = pos / g.bs;
-      q4_store<D>(codes, scales, ((int64_t)row_pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs), o, code, byte);
+      const int h = r / kOctets, pos = pos0 + tok, b = pos / g.bs;
+      o[k] = r - h * kOctets;
+      page[k] = row_pages[b];
+      row[k] = h * g.bs + (pos - b * g.bs);
     }
+#pragma unroll
+    for (int k = 0; k < kQuantUnroll; ++k) {
+      uint32_t byte;
+      v[k].exchange(lane);
+      const uint32_t code = q4_encode<DT>(v[k], &byte, &odd);
+      // (a pool has fewer than 2^32 rows)
+      if (from + k * kAppendThreads + octet0 < count)
+        q4_store<D>(codes, scales, page[k] * (uint32_t)(g.Hkv * g.bs) + row[k], o[k], code, byte);
+    }
+    if (from + kAppendThreads * kQuantUnroll < count) load(from + kAppendThreads * kQuantUnroll);
   }
   if (__syncthreads_or(odd) && threadIdx.x == 0) atomicOr(&status[j], KARA_SEQ_NONFINITE);
 }
@@ -157,7 +196,7 @@ __global__ __launch_bounds__(kFewThreads) void q4_append_few_kernel(
     const char* __restrict__ v_new, PoolPtrs kp, PoolPtrs vp, PoolPtrs ksp, PoolPtrs vsp,
     const int32_t* __restrict__ bt, int32_t* __restrict__ seq_lens, int32_t* __restrict__ status) {
   constexpr int kOctets = D / 8;
-  using Src = QuantSrc<DT>;
+  using Src = Octet<DT>;
   const int j = blockIdx.x;
   int st = append_status(g, n, seqs, n_new, bt, seq_lens, j);
   if (st == KARA_SEQ_OK) {
@@ -166,12 +205,17 @@ __global__ __launch_bounds__(kFewThreads) void q4_append_few_kernel(
     const int pos0 = seq_lens[s];
     const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
     bool odd = false;
-    for (int i = threadIdx.x; i < 2 * n_layers * per_layer; i += kFewThreads) {
-      const int part = i / per_layer, kv = part & 1, l = part >> 1;
-      const int x = i - part * per_layer, tok = x / per_tok, r = x - tok * per_tok;
-      const int h = r / kOctets, o = r - h * kOctets;
+    // (a sequence's rows of one layer, K or V, lie together; the lanes of a block stay so)
+    const int lane = threadIdx.x & 63, octets = (per_layer + 63) & ~63;
+    for (int at = threadIdx.x & ~63; at < 2 * n_layers * octets; at += kFewThreads) {
+      const int part = at / octets, kv = part & 1, l = part >> 1;
+      const int wave0 = at - part * octets, x = wave0 + Src::octet(lane);
       Src v;
-      v.load((kv ? v_new : k_new) + (((int64_t)l * n + j) * per_layer + x) * Src::kBytes);
+      v.load((kv ? v_new : k_new) + ((int64_t)l * n + j) * per_layer * Src::kBytes, wave0, lane, per_layer);
+      v.exchange(lane);
+      if (x >= per_layer) continue;
+      const int tok = x / per_tok, r = x - tok * per_tok;
+      const int h = r / kOctets, o = r - h * kOctets;
       uint32_t byte;
       const uint32_t code = q4_encode<DT>(v, &byte, &odd);
       const int pos = pos0 + tok, b = pos / g.bs;
@@ -196,7 +240,7 @@ __global__ __launch_bounds__(kAppendThreads) void q4_read_kernel(
     PoolPtrs kp, PoolPtrs vp, PoolPtrs ksp, PoolPtrs vsp, const int32_t* __restrict__ bt,
     const int32_t* __restrict__ seq_lens, char* __restrict__ k_out, char* __restrict__ v_out) {
   constexpr int kOctets = D / 8;
-  constexpr int kOctetBytes = DT == KARA_BF16 ? 16 : 32;
+  using Dst = Octet<DT>;
   const int j = blockIdx.x / chunks;
   const int tok0 = (blockIdx.x - j * chunks) * toks;
   const int l = blockIdx.y;
@@ -208,46 +252,52 @@ __global__ __launch_bounds__(kAppendThreads) void q4_read_kernel(
   const int32_t* row_pages = bt + (int64_t)(listed ? s : 0) * g.max_blocks;
   const int per_tok = g.Hkv * kOctets;
   const int count = min(toks, n_rows - tok0) * per_tok;
-  char* dst = (kv ? v_out : k_out) + (((int64_t)l * n + j) * n_rows + tok0) * per_tok * kOctetBytes;
+  char* dst = (kv ? v_out : k_out) + (((int64_t)l * n + j) * n_rows + tok0) * per_tok * Dst::kBytes;
   const uint8_t* codes = (const uint8_t*)(kv ? vp.p[l] : kp.p[l]);
   const uint8_t* scales = (const uint8_t*)(kv ? vsp.p[l] : ksp.p[l]);
-  for (int i0 = threadIdx.x; i0 < count; i0 += kAppendThreads * kQuantUnroll) {
-    uint32_t c[kQuantUnroll], byte[kQuantUnroll];
+  const int lane = threadIdx.x & 63, wave0 = threadIdx.x & ~63, octet0 = wave0 + Dst::octet(lane);
+  for (int from = 0; from < count; from += kAppendThreads * kQuantUnroll) {
+    // rows that are not there read another one of the pool and become zeros
+    uint32_t c[kQuantUnroll], byte[kQuantUnroll], row[kQuantUnroll];
+    int page[kQuantUnroll], o[kQuantUnroll];
+    bool in[kQuantUnroll];
 #pragma unroll
     for (int k = 0; k < kQuantUnroll; ++k) {
-      const int i = i0 + k * kAppendThreads;
-      c[k] = 0, byte[k] = 127;
-      if (i < count) {
-        const int tok = i / per_tok, r = i - tok * per_tok;
-        const int h = r / kOctets, o = r - h * kOctets;
-        const int64_t pos = pos0 + tok;
-        if (pos >= 0 && pos < len) {
-          const int b = (int)pos / g.bs;
-          const int page = row_pages[b];
-          if (page >= 0 && page < g.num_pages) {
-            const int64_t row = ((int64_t)page * g.Hkv + h) * g.bs + ((int)pos - b * g.bs);
-            c[k] = *(const uint32_t*)(codes + row * (D / 2) + o * 4);
-            byte[k] = scales[row * (D / kQ4Block) + (o >> 2)];
-          }
-        }
-      }
+      const int i = min(from + k * kAppendThreads + octet0, count - 1);
+      const int tok = i / per_tok, r = i - tok * per_tok;
+      const int h = r / kOctets;
+      o[k] = r - h * kOctets;
+      in[k] = pos0 + tok >= 0 && pos0 + tok < len;
+      const int pos = in[k] ? (int)(pos0 + tok) : 0, b = pos / g.bs;
+      page[k] = row_pages[b];
+      row[k] = h * g.bs + (pos - b * g.bs);
     }
 #pragma unroll
     for (int k = 0; k < kQuantUnroll; ++k) {
-      const int i = i0 + k * kAppendThreads;
-      if (i >= count) continue;
+      in[k] &= page[k] >= 0 && page[k] < g.num_pages;
+      row[k] += (uint32_t)(in[k] ? page[k] : 0) * (uint32_t)(g.Hkv * g.bs);
+      c[k] = *(const uint32_t*)(codes + (uint64_t)row[k] * (D / 2) + o[k] * 4);
+      byte[k] = scales[(uint64_t)row[k] * (D / kQ4Block) + (o[k] >> 2)];
+    }
+#pragma unroll
+    for (int k = 0; k < kQuantUnroll; ++k)
+      if (!in[k]) c[k] = 0, byte[k] = 127;
+#pragma unroll
+    for (int k = 0; k < kQuantUnroll; ++k) {
       const float scale = q4_scale(byte[k]);
-      u32x4* to = (u32x4*)(dst + (int64_t)i * kOctetBytes);
+      Dst x;
       if constexpr (DT == KARA_BF16) {
-        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, q4_octet(c[k], scale)), to);
+        x.v[0] = __builtin_bit_cast(u32x4, q4_octet(c[k], scale));
       } else {
         const floatx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 0);
         const floatx2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 1);
         const floatx2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 2);
         const floatx2 f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[k], scale, 3);
-        to[0] = __builtin_bit_cast(u32x4, floatx4{a[0], a[1], b[0], b[1]});   // (half a line each: gathered in the cache)
-        to[1] = __builtin_bit_cast(u32x4, floatx4{e[0], e[1], f[0], f[1]});
+        x.v[0] = __builtin_bit_cast(u32x4, floatx4{a[0], a[1], b[0], b[1]});
+        x.v[1] = __builtin_bit_cast(u32x4, floatx4{e[0], e[1], f[0], f[1]});
       }
+      x.exchange(lane);
+      x.store(dst, from + k * kAppendThreads + wave0, lane, count);
     }
   }
 }
@@ -764,10 +814,11 @@ kara_status_t kara_q4_append(const kara_params_t* p, int32_t n, const int32_t* s
       !pools_ok(v_pools, n_layers) || !pools_ok(k_scales, n_layers) || !pools_ok(v_scales, n_layers))
     return KARA_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
+  if ((int64_t)g.Hkv * (g.d / 8) > kMaxOctets) return KARA_ERR_UNSUPPORTED;
   const int per_tok = g.Hkv * (g.d / 8);
   const int toks = std::min(n_new, std::max(1, 2 * kAppendThreads * kQuantUnroll / per_tok));
   const int64_t chunks = ((int64_t)n_new + toks - 1) / toks;
-  if (!grid_ok(n * chunks) || !grid_ok(4 * (int64_t)n) || (int64_t)toks * per_tok > INT32_MAX / 2) return KARA_ERR_UNSUPPORTED;
+  if (!grid_ok(n * chunks) || !grid_ok(4 * (int64_t)n)) return KARA_ERR_UNSUPPORTED;
   const PoolPtrs kp = ptrs(k_pools, n_layers), vp = ptrs(v_pools, n_layers), ksp = ptrs(k_scales, n_layers),
                  vsp = ptrs(v_scales, n_layers);
   if ((int64_t)2 * n_layers * n_new * per_tok <= kFewOctets) {
@@ -815,10 +866,11 @@ kara_status_t kara_q4_read(const kara_params_t* p, int32_t n, const int32_t* seq
   if (!seqs || !start || !k_out || !v_out || !block_table || !seq_lens || !pools_ok(k_pools, n_layers) ||
       !pools_ok(v_pools, n_layers) || !pools_ok(k_scales, n_layers) || !pools_ok(v_scales, n_layers))
     return KARA_ERR_INVALID_ARG;
+  if ((int64_t)g.Hkv * (g.d / 8) > kMaxOctets) return KARA_ERR_UNSUPPORTED;
   const int per_tok = g.Hkv * (g.d / 8);
   const int toks = std::min(n_rows, std::max(1, 2 * kAppendThreads * kQuantUnroll / per_tok));
   const int64_t chunks = ((int64_t)n_rows + toks - 1) / toks;
-  if (!grid_ok(n * chunks) || (int64_t)toks * per_tok > INT32_MAX / 2) return KARA_ERR_UNSUPPORTED;
+  if (!grid_ok(n * chunks)) return KARA_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)(n * chunks), (unsigned)n_layers, 2), block(kAppendThreads);
 #define KARA_Q4_READ(DT, D)                                                                                        \
   hipLaunchKernelGGL((q4_read_kernel<DT, D>), grid, block, 0, (hipStream_t)stream, g, n, seqs, start, n_rows, toks, \
