@@ -373,7 +373,7 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictArgs a) {
 
 constexpr int kMoveThreads = 1024;
 constexpr int kMoveUnroll = 8;
-constexpr int kMoveStage = 32768 / 4;     // kept positions and table entries held in LDS, at most
+constexpr int kMoveStage = 65536 / 4;     // rows held in LDS, at most
 
 // One workgroup per (layer, sequence, KV head, part): a piece of the K rows or of the V
 // rows, or the small arrays (scales, accumulators).  Row i takes row kept[i] >= i, so working up in
@@ -385,7 +385,7 @@ constexpr int kMoveStage = 32768 / 4;     // kept positions and table entries he
 // 36 us with 256, 24 so.
 template <bool STAGED>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
-  extern __shared__ int32_t stage[];
+  extern __shared__ uint32_t stage[];
   const Geom& g = a.g;
   const int tid = threadIdx.x;
   const int parts = 2 * a.cols + 1, part = blockIdx.x % (uint32_t)parts;
@@ -398,18 +398,20 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
   if (len <= a.keep) return;
   const int32_t* kept = a.kept + (int64_t)u * a.keep;
   const Pages pages(a, j, a.seqs[j]);
-  if constexpr (STAGED) {
-    for (int i = tid; i < a.keep; i += kMoveThreads) stage[i] = kept[i];
-    const int nb = (len + g.bs - 1) / g.bs;
-    for (int b = tid; b < nb; b += kMoveThreads) stage[a.keep + b] = pages[b];
-    __syncthreads();
-  }
-  auto source = [&](int i) __attribute__((always_inline)) { return STAGED ? stage[i] : kept[i]; };
   auto row = [&](int pos) __attribute__((always_inline)) {
     const int b = pos / g.bs;
-    const int64_t page = STAGED ? stage[a.keep + b] : pages[b];
-    return (page * g.Hkv + h) * g.bs + (pos - b * g.bs);
+    return ((uint32_t)pages[b] * g.Hkv + h) * g.bs + (pos - b * g.bs);    // (a pool has fewer than 2^32 rows)
   };
+  // pool rows that row i comes from and goes to
+  if constexpr (STAGED) {
+    for (int i = tid; i < a.keep; i += kMoveThreads) {
+      stage[i] = row(kept[i]);
+      stage[a.keep + i] = row(i);
+    }
+    __syncthreads();
+  }
+  auto source = [&](int i) __attribute__((always_inline)) { return STAGED ? stage[i] : row(kept[i]); };
+  auto target = [&](int i) __attribute__((always_inline)) { return STAGED ? stage[a.keep + i] : row(i); };
   if (part < 2 * a.cols) {
     const int piece = a.row_bytes / a.cols;
     char* base = (char*)(part & 1 ? a.v.p[l] : a.k.p[l]) + (part >> 1) * piece;
@@ -417,17 +419,17 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
     const int c = tid % cpr, r = tid / cpr;
     for (int x0 = 0; x0 < a.keep; x0 += tile) {
       u32x4 v[kMoveUnroll];
-      int dst[kMoveUnroll];
+      uint32_t dst[kMoveUnroll];
+      bool moves[kMoveUnroll];
 #pragma unroll
       for (int k = 0; k < kMoveUnroll; ++k) {
         const int i = x0 + k * rpp + r;
-        dst[k] = -1;
+        moves[k] = false;
         if (i < a.keep) {
-          const int src = source(i);
-          if (src != i) {
-            dst[k] = i;
-            v[k] = __builtin_nontemporal_load((const u32x4*)(base + row(src) * a.row_bytes + c * 16));
-          }
+          const uint32_t src = source(i);
+          dst[k] = target(i);
+          moves[k] = src != dst[k];
+          if (moves[k]) v[k] = __builtin_nontemporal_load((const u32x4*)(base + (uint64_t)src * a.row_bytes + c * 16));
         }
       }
       // all of this tile's loads have landed before any thread stores
@@ -435,7 +437,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < kMoveUnroll; ++k)
-        if (dst[k] >= 0) __builtin_nontemporal_store(v[k], (u32x4*)(base + row(dst[k]) * a.row_bytes + c * 16));
+        if (moves[k]) __builtin_nontemporal_store(v[k], (u32x4*)(base + (uint64_t)dst[k] * a.row_bytes + c * 16));
     }
     return;
   }
@@ -443,14 +445,17 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
   for (int x0 = 0; x0 < a.keep; x0 += kMoveThreads * kRows) {
     float w[kRows];
     uint32_t sk[kRows], sv[kRows];
+    uint32_t to[kRows];
     bool moves[kRows];
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
       const int i = x0 + k * kMoveThreads + tid;
-      const int src = i < a.keep ? source(i) : i;
-      moves[k] = src != i;
+      moves[k] = false;
+      if (i >= a.keep) continue;
+      const uint32_t from = source(i);
+      to[k] = target(i);
+      moves[k] = from != to[k];
       if (!moves[k]) continue;
-      const int64_t from = row(src);
       w[k] = a.w.p[l][from];
       if (a.scale_bytes == 4) {
         sk[k] = ((const uint32_t*)a.ks.p[l])[from];
@@ -465,14 +470,13 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
       if (!moves[k]) continue;
-      const int64_t to = row(x0 + k * kMoveThreads + tid);
-      a.w.p[l][to] = w[k];
+      a.w.p[l][to[k]] = w[k];
       if (a.scale_bytes == 4) {
-        ((uint32_t*)a.ks.p[l])[to] = sk[k];
-        ((uint32_t*)a.vs.p[l])[to] = sv[k];
+        ((uint32_t*)a.ks.p[l])[to[k]] = sk[k];
+        ((uint32_t*)a.vs.p[l])[to[k]] = sv[k];
       } else if (a.scale_bytes == 2) {
-        ((uint16_t*)a.ks.p[l])[to] = (uint16_t)sk[k];
-        ((uint16_t*)a.vs.p[l])[to] = (uint16_t)sv[k];
+        ((uint16_t*)a.ks.p[l])[to[k]] = (uint16_t)sk[k];
+        ((uint16_t*)a.vs.p[l])[to[k]] = (uint16_t)sv[k];
       }
     }
   }
@@ -668,7 +672,7 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
   hipLaunchKernelGGL(evict_pick_kernel, dim3((unsigned)units), dim3(kPickThreads), pick_lds, s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
-  const int64_t staged = (int64_t)keep + (max_len + g.bs - 1) / g.bs;
+  const int64_t staged = 2 * (int64_t)keep;
   // Rows in pieces of 128 bytes, of 64 while the launch leaves CUs without a workgroup:
   // half as many tiles one after the other (8 sequences of one layer 24 -> 18.5 us, two
   // 12.7 -> 7.4; the large cut above 1589 -> 1576).
