@@ -342,3 +342,48 @@ def test_evict_from_a_pool_of_many_pages():
     c.bt.copy_(torch.from_numpy(c.table))
     flagged = {2: kara.SEQ_DUP_PAGE, 0: kara.SEQ_BAD_PAGE}
     check_evict(c, [3, 0, 2, 1], flagged, 120, 4, 20, run_evict(c, [3, 0, 2, 1], 120, 4, 20, 9000))
+
+
+def test_far_rows():
+    # rows past 4 GiB of a pool: counted, observed and cut
+    kara = _kara()
+    rng = np.random.default_rng(31)
+    d, Hkv, bs, n, keep = 128, 8, 256, 700, 300
+    pages = (1 << 32) // (2 * d * Hkv * bs) + 40
+    p = cc.params(16, Hkv, d, bs, pages, 3, 1, "bf16")
+    pool = [torch.empty((pages, Hkv, bs, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    w = torch.zeros((pages, Hkv, bs), device="cuda")
+    table = np.array([[pages - 1, pages - 30, pages - 7]], dtype=np.int32)
+    at = np.arange(n)
+    page, slot = table[0][at // bs], at % bs
+    where = torch.from_numpy(table[0]).long().cuda()
+    rows = [torch.from_numpy(rng.standard_normal((3, Hkv, bs, d)).astype(np.float32)).bfloat16() for _ in range(2)]
+    for t, r in zip(pool, rows):
+        t[where] = r.cuda()
+    kk, vv = (r.double().numpy()[at // bs, :, slot] for r in rows)
+    bt, sl, sq = cc.gpu(table), cc.gpu(np.array([n], dtype=np.int32)), cc.gpu(np.zeros(1, dtype=np.int32))
+    size = max(kara.evict_attention_workspace_size(p, 1, 1, n), kara.evict_observe_workspace_size(p, 1, 1, 50, n),
+               kara.evict_workspace_size(p, 1, 1, keep))
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    q = torch.from_numpy(rng.standard_normal((1, 1, 50, 16, d)).astype(np.float32)).bfloat16()
+    kara.evict_observe(p, sq, 50, q.cuda(), [pool[0]], [w], bt, sl, n, n, ws)
+    out = torch.empty((1, 1, 16, d), device="cuda")
+    kara.evict_attention(p, sq, q[:, :, 0].contiguous().cuda(), [pool[0]], [pool[1]], [w], bt, sl, 0, n, out, ws)
+    q64 = q[0, 0].double().numpy()
+    delta = cc.logit_error(q64, kk, 1 / np.sqrt(d), 3)
+    ref, mass, one = oc.attend(q64[:1], kk, vv, 1 / np.sqrt(d))
+    assert (np.abs(out[0, 0].double().cpu().numpy() - ref[0]) <= cc.attention_bound(ref, mass, delta, n, "f32", False)[0]).all()
+    want = oc.attend(q64, kk, None, 1 / np.sqrt(d))[2] + one
+    got = w[where].cpu().numpy()[at // bs, :, slot].T
+    assert (np.abs(got - want) <= 1.05 * want * (2 * delta + (51 * 2 + 16) * cc.EPS) + 2 * cc.EPS * want).all()
+    kept = torch.empty((1, 1, Hkv, keep), dtype=torch.int32, device="cuda")
+    status = torch.empty(1, dtype=torch.int32, device="cuda")
+    kara.evict_tokens(p, sq, keep, 4, 50, [pool[0]], [pool[1]], [w], bt, sl, n, False, status, ws, kept=kept)
+    assert status.item() == 0
+    to = np.arange(keep)
+    for t, r in zip((*pool, w), (*rows, None)):
+        a = t[where].float().cpu().numpy()[to // bs, :, to % bs]
+        for h in range(Hkv):
+            pos = oc.kept(got[h], keep, 4, 50)
+            assert kept[0, 0, h].tolist() == pos.tolist()
+            assert np.array_equal(a[:, h], got[h][pos] if r is None else r.float().numpy()[pos // bs, h, pos % bs])

@@ -186,6 +186,41 @@ def test_on_another_stream():
         assert torch.equal(a, b)
 
 
+def test_two_programs_at_once():
+    # on two streams, each with its own workspace, in turns that overlap: the bits of one alone
+    def step(p_, x, stream):
+        k, v, ks, vs = p_.lists("k", "v", "ks", "vs")
+        wl = list(p_.w.unbind(0))
+        kw = dict(stream=stream)
+        p_.k.q4_append(p_.p, p_.seqs, x["k"], x["v"], k, v, ks, vs, p_.bt, p_.sl, p_.status, **kw)
+        p_.k.evict_observe(p_.p, p_.seqs, 30, x["q"], k, wl, p_.bt, p_.sl, 30, p_.max_len, p_.ws, k_scales=ks, **kw)
+        p_.k.q4_attention(p_.p, p_.seqs, 30, x["q"], k, v, ks, vs, p_.bt, p_.sl, p_.max_len, x["out"], p_.ws, **kw)
+        p_.k.evict_tokens(p_.p, p_.seqs, 100, 2, 20, k, v, wl, p_.bt, p_.sl, p_.max_len, False, p_.status, p_.ws,
+                          k_scales=ks, v_scales=vs, **kw)
+
+    def run(streams):
+        progs = []
+        for seed in (11, 12):
+            p_ = Program("q4", seed=seed, max_blocks=24)
+            for s in range(3):
+                for b in range(24):
+                    p_.table[s, b] = p_.free.pop()
+            p_.bt.copy_(torch.from_numpy(p_.table))
+            x = {a: p_.randn(2, 3, 30, h, 64) for a, h in (("k", 2), ("v", 2), ("q", 8))}
+            x["out"] = torch.empty_like(x["q"])
+            progs.append((p_, x))
+        torch.cuda.synchronize()
+        for _ in range(6):
+            for (p_, x), stream in zip(progs, streams):
+                step(p_, x, stream)
+        torch.cuda.synchronize()
+        assert all(not p_.status.any() and (p_.sl == 180).all() for p_, _ in progs)
+        return [t for p_, x in progs for t in (x["out"], p_.w, *p_.dev.values())]
+
+    for a, b in zip(run((None, None)), run((torch.cuda.Stream(), torch.cuda.Stream()))):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("kind", ["q4", "rows"])
 def test_captured_steps(kind):
     """A decoding step and a cut in a graph, replayed with eager steps of another
