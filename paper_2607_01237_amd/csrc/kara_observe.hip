@@ -26,10 +26,34 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // what a stream of rows is made of
 enum { kBf16Rows, kF32Rows, kCodeRows };
 
+// Unit and piece of a block, the pieces of all units in turn and the longest first: the
+// last ones fill what is left.  Blocks go round the 8 XCDs, and an XCD's round its four
+// shader engines.
+struct Order {
+  // The second half backwards: where all blocks are placed at once, two to a CU, long
+  // ones then share a CU with short ones (2 prompts of 2048 queries over 2048 and 4001
+  // tokens: 260 -> 200 us).
+  int back;
+  // Units moved on by `shift` from piece to piece, or from every second one to the next.
+  // With eight KV heads a unit's pieces stay on one XCD, whose L2 then holds its rows, and
+  // each XCD has heads of every sequence; an even number of sequences is shifted there,
+  // or each engine would keep its own (8 prompts: 787 -> 710 us).  With other counts an
+  // XCD might get all the pieces of a long sequence.
+  uint32_t shift, half;
+};
+constexpr int kCUs = 256;
+Order order_of(const Geom& g, int64_t units, int64_t blocks, bool pairs) {
+  const bool back = pairs && blocks <= 2 * kCUs;
+  if (g.Hkv % 8 != 0) return {back, 1, 0};
+  const int64_t each = units / 8;        // of an XCD
+  return {back, back || each % 2 != 0 ? 0u : 8u, each % 4 != 0};
+}
+
 struct ObserveArgs {
   Geom g;
   int n, T, n_new, max_len;
   uint32_t units;                       // (layer, sequence, KV head)
+  Order order;                          // of the blocks
   int row_blocks, splits, split_keys;   // row statistics
   int bs_shift;                         // log2(bs) when bs is a power of two, else -1
   int key_blocks, parts, part_rows;     // column sums: the rows of a unit in parts
@@ -89,22 +113,14 @@ __device__ __forceinline__ int swz(int row) {
   return ((row & 3) << 1) | ((row >> 2) & 1);
 }
 
-// Unit and piece of a block, the pieces of all units in turn and the longest first:
-// the last ones fill what is left.  Where all blocks are placed at once, two to a CU
-// (pairs), the second half runs backwards, so that long ones share a CU with short
-// ones (2 prompts of 2048 queries over 2048 and 4001 tokens: 260 -> 200 us).  Blocks go
-// round the 8 XCDs: with eight KV heads a unit's pieces stay on one XCD, whose L2 then
-// holds its rows, and each XCD has heads of every sequence; with other counts units are
-// shifted from piece to piece, or an XCD might get all the pieces of a long sequence.
-constexpr uint32_t kCUs = 256;
 struct Piece {
   uint32_t unit, piece;
 };
-__device__ __forceinline__ Piece piece_of(uint32_t units, int Hkv, bool pairs) {
+__device__ __forceinline__ Piece piece_of(uint32_t units, const Order& o) {
   uint32_t block = blockIdx.x;
-  if (pairs && gridDim.x <= 2 * kCUs && block >= kCUs) block = gridDim.x - 1 - (block - kCUs);
+  if (o.back && block >= kCUs) block = gridDim.x - 1 - (block - kCUs);
   const uint32_t piece = block / units, at = block - piece * units;
-  return {Hkv % 8 == 0 ? at : (at + piece) % units, piece};
+  return {o.shift == 0 ? at : (at + o.shift * (piece >> o.half)) % units, piece};
 }
 
 constexpr int kObsThreads = 512;
@@ -178,7 +194,7 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sta
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
-  const Piece pc = piece_of(a.units, g.Hkv, NK * NQ == 1);
+  const Piece pc = piece_of(a.units, a.order);
   const uint32_t u = pc.unit;
   const int split = pc.piece % (uint32_t)a.splits;
   const int rb = a.row_blocks - 1 - (int)(pc.piece / (uint32_t)a.splits);     // rows that see most keys first
@@ -357,7 +373,7 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
-  const Piece pc = piece_of(a.units, g.Hkv, NK * NQ == 1);
+  const Piece pc = piece_of(a.units, a.order);
   const uint32_t u = pc.unit;
   const int part = a.parts - 1 - (int)(pc.piece % (uint32_t)a.parts);
   const int kb = pc.piece / (uint32_t)a.parts;         // the first keys are seen by most rows
@@ -552,9 +568,12 @@ Plan plan_of(const Geom& g, int n, int n_layers, int T, int max_len) {
 }
 
 template <int KSRC, int NK, int QSRC, int NQ, int D>
-hipError_t launch(const ObserveArgs& a, const Plan& x, hipStream_t stream) {
-  hipLaunchKernelGGL((observe_stats_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)(x.units * x.row_blocks * x.splits)),
-                     dim3(kObsThreads), 0, stream, a);
+hipError_t launch(ObserveArgs a, const Plan& x, hipStream_t stream) {
+  constexpr bool kPairs = NK * NQ == 1;                 // two workgroups to a CU
+  const int64_t row_blocks = x.units * x.row_blocks * x.splits, key_blocks = x.units * x.key_blocks * x.parts;
+  a.order = order_of(a.g, x.units, row_blocks, kPairs);
+  hipLaunchKernelGGL((observe_stats_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)row_blocks), dim3(kObsThreads), 0,
+                     stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (x.splits > 1) {
@@ -563,8 +582,9 @@ hipError_t launch(const ObserveArgs& a, const Plan& x, hipStream_t stream) {
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((observe_sum_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)(x.units * x.key_blocks * x.parts)),
-                     dim3(kObsThreads), 0, stream, a);
+  a.order = order_of(a.g, x.units, key_blocks, kPairs);
+  hipLaunchKernelGGL((observe_sum_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)key_blocks), dim3(kObsThreads), 0,
+                     stream, a);
   e = hipGetLastError();
   if (e != hipSuccess || x.parts == 1) return e;
   const int blocks = (a.max_len + 255) / 256;
