@@ -14,7 +14,7 @@
 // NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones).
 //
 // 16 sequences x 1024 queries over 2.5-8.7K cached, 32/8 heads, bf16: 1320 us, 1035
-// TFLOP/s; fp32, 8 x 512: 853 us, 420 TFLOP/s of three products for each.
+// TFLOP/s; fp32, 8 x 512: 894 us, 400 TFLOP/s of three products for each.
 #include <algorithm>
 #include <type_traits>
 
@@ -281,26 +281,58 @@ __global__ __launch_bounds__(W * 64, 2) void q4_chunk_kernel(Q4Split a) {
         for (int y = 0; y < NT; ++y) pb[qt][y][jj] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
       }
     }
+    auto v_operand = [&](int jj, int dt) __attribute__((always_inline)) {
+      const v4i16 lo = read_tr(st + voff[dt] + (32 * jj) * C::kRow);
+      const v4i16 hi = read_tr(st + voff[dt] + (32 * jj + 16) * C::kRow);
+      bf16x8 va;
+      __builtin_memcpy(&va, &lo, 8);
+      __builtin_memcpy((char*)&va + 8, &hi, 8);
+      return va;
+    };
+    if constexpr (NT > 1) {
+      // A chunk's products are summed from zero, smallest terms first, and added once: a
+      // running sum over thousands of keys is rounded once a chunk, not with each of its six
+      // products (4 x 512 queries over 2.5-8.7K tokens: off by 4.3e-7 of the result where six
+      // roundings a chunk leave 2.0e-6, 444 us against 424).
+      static_assert(QT == 1, "one tile of rows");
 #pragma unroll
-    for (int jj = 0; jj < 2; ++jj) {
+      for (int dt = 0; dt < DT; dt += 2) {
+        floatx4 part[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        bf16x8 va[2][2];
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const v4i16 lo = read_tr(st + voff[dt] + (32 * jj) * C::kRow);
-        const v4i16 hi = read_tr(st + voff[dt] + (32 * jj + 16) * C::kRow);
-        bf16x8 va;
-        __builtin_memcpy(&va, &lo, 8);
-        __builtin_memcpy((char*)&va + 8, &hi, 8);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj) va[i][jj] = v_operand(jj, dt + i);
 #pragma unroll
         for (int y = NT - 1; y >= 0; --y)
 #pragma unroll
-          for (int qt = 0; qt < QT; ++qt)
-            o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qt][y][jj], o[qt][dt], 0, 0, 0);
+          for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              part[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[i][jj], pb[0][y][jj], part[i], 0, 0, 0);
+        o[0][dt] += part[0];
+        o[0][dt + 1] += part[1];
       }
+      floatx4 part[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int y = NT - 1; y >= 0; --y)
 #pragma unroll
+        for (int jj = 0; jj < 2; ++jj) part[jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[0][y][jj], part[jj], 0, 0, 0);
+      lsum[0] += part[0] + part[1];
+    } else {
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const bf16x8 va = v_operand(jj, dt);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qt][0][jj], o[qt][dt], 0, 0, 0);
+        }
+#pragma unroll
         for (int qt = 0; qt < QT; ++qt)
-          lsum[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[qt][y][jj], lsum[qt], 0, 0, 0);
+          lsum[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[qt][0][jj], lsum[qt], 0, 0, 0);
+      }
     }
   };
 

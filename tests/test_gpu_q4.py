@@ -307,3 +307,35 @@ def test_long_append_reports_and_leaves(dtype):
         assert np.array_equal(cc.rows_of(pools[3].cpu().numpy(), table, s, n, bs)[lens[s]:], scales[j])
     for t in pools:
         assert (t.cpu().numpy()[sorted(set(range(pages)) - touched)] == 3).all()
+
+
+@pytest.mark.parametrize("d,T", [(128, 80), (64, 300)])
+def test_long_sums_in_fp32(d, T):
+    # fp32, many rows over 8000 keys: 125 chunks of 64 keys are added to the output and to
+    # the sum of weights, each addition off by half a step at most, 2^-24 / sqrt(3) of the
+    # running sum on average: sqrt(2 * 125 / 3) 2^-24 = 5.4e-7 of the result (root mean
+    # square); the logits' own roundings average out over the keys.  1e-6 at most.
+    kara = _kara()
+    rng = np.random.default_rng(d)
+    n, Hq, Hkv, bs = 8000, 2, 1, 16
+    table, pages, _ = cc.table_for(rng, [n], bs, n // bs)
+    p = cc.params(Hq, Hkv, d, bs, pages, n // bs, 1, "f32")
+    host = {x: cc.random_q4(rng, (pages, Hkv, bs), d) for x in "kv"}
+    lists = [[cc.gpu(host[x][i])] for i in (0, 1) for x in "kv"]
+    q = torch.from_numpy(rng.standard_normal((1, 1, T, Hq, d)).astype(np.float32)) / 8
+    out = torch.empty(q.shape, device="cuda")
+    ws = torch.empty(kara.q4_attention_workspace_size(p, 1, 1, T, n), dtype=torch.uint8, device="cuda")
+    seqs = cc.gpu(np.zeros(1, dtype=np.int32))
+    # (one listing a copy: 300 of them are enough that keys are not split)
+    many = 300
+    outs = torch.empty((1, many, T, Hq, d), device="cuda")
+    ws_many = torch.empty(kara.q4_attention_workspace_size(p, many, 1, T, n), dtype=torch.uint8, device="cuda")
+    bt, sl = cc.gpu(table), cc.gpu(np.array([n], dtype=np.int32))
+    kara.q4_attention(p, seqs, T, q.cuda(), *lists, bt, sl, n, out, ws)
+    kara.q4_attention(p, seqs.repeat(many), T, q.cuda().expand(outs.shape).contiguous(), *lists, bt, sl, n, outs, ws_many)
+    k, v = (oc.q4_values(cc.rows_of(host[x][0], table, 0, n, bs), cc.rows_of(host[x][1], table, 0, n, bs)) for x in "kv")
+    ref = oc.attend(q[0, 0].double().numpy(), k, v, 1 / np.sqrt(d))[0]
+    for got in (out[0, 0], outs[0, 0], outs[0, many - 1]):
+        err = np.linalg.norm(got.double().cpu().numpy() - ref) / np.linalg.norm(ref)
+        print("error", err)
+        assert err < 1e-6
