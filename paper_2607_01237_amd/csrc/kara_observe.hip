@@ -182,6 +182,38 @@ __device__ __forceinline__ uint64_t key_row(const Geom& g, const int32_t* row_pa
   return (uint64_t)(((int64_t)page * g.Hkv + h) * g.bs + (pos - b * g.bs));
 }
 
+// A lane's maximum and sum of its rows, over the logits of two 16-key tiles.  The
+// reference is raised only where a logit passes it by more than 2^8.
+template <int QT>
+__device__ __forceinline__ void add_logits(const floatx4 (&sv)[2][QT], float c, float (&m)[QT], float (&sum)[QT]) {
+  float over = kNegInf, mx[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    mx[t] = sv[0][t][0];
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx[t] = fmaxf(mx[t], sv[y][t][r]);
+    over = fmaxf(over, fmaf(mx[t], c, -m[t]));
+  }
+  if (__ballot(over > 8.f) != 0ull) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const float mn = fmaxf(m[t], mx[t] * c);
+      sum[t] *= __builtin_amdgcn_exp2f(m[t] - mn);
+      m[t] = mn;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][0], c, -m[t])), e1 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][1], c, -m[t]));
+      const float e2 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][2], c, -m[t])), e3 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][3], c, -m[t]));
+      sum[t] += (e0 + e1) + (e2 + e3);
+    }
+}
+
 // ---- row statistics: one workgroup per (unit, 128 QT query rows, split of the
 // keys); a wave holds 16 QT rows, the keys pass through LDS 64 at a time.  A lane
 // keeps a maximum and a sum of its own -- of the keys 4gq + r -- and the four of a
@@ -278,33 +310,7 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sta
             if (y * 16 + r >= sees) sv[y][t][r] = kNegInf;
       }
     }
-    // a lane's reference is raised only where a logit passes it by more than 2^8
-    float over = kNegInf, mx[QT];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      mx[t] = sv[0][t][0];
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) mx[t] = fmaxf(mx[t], sv[y][t][r]);
-      over = fmaxf(over, fmaf(mx[t], c, -m[t]));
-    }
-    if (__ballot(over > 8.f) != 0ull) {
-#pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        const float mn = fmaxf(m[t], mx[t] * c);
-        sum[t] *= __builtin_amdgcn_exp2f(m[t] - mn);
-        m[t] = mn;
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < QT; ++t)
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][0], c, -m[t])), e1 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][1], c, -m[t]));
-        const float e2 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][2], c, -m[t])), e3 = __builtin_amdgcn_exp2f(fmaf(sv[y][t][3], c, -m[t]));
-        sum[t] += (e0 + e1) + (e2 + e3);
-      }
+    add_logits(sv, c, m, sum);
   };
   if (k_lo < k_hi) {
     look(k_lo);
@@ -345,6 +351,159 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sta
     L += __shfl_xor(L, 32, 64);
     const int r = wrow0 + t * 16 + li;
     if (gq == 0 && r < R) a.stats[((int64_t)u * R + r) * a.splits + split] = floatx2{M, L};
+  }
+}
+
+// The same for few query rows: a workgroup of four waves per (unit, 32 rows, split of the
+// keys).  The waves take 32 keys each in turn, straight from the pages to registers, the
+// next ones on their way, without barriers: staged, most waves would have no rows.
+constexpr int kFewThreads = 256;
+constexpr int kFewWaves = kFewThreads / 64;
+constexpr int kFewRows = 32;                // of a workgroup
+
+// a lane's part of 16 keys as loaded: values gq * D / 4 .. of key li
+template <int KSRC, int D>
+struct KeyPart {
+  static constexpr int KS = D / 32;
+  uint32_t v[KSRC == kCodeRows ? KS + 1 : 4 * KS];
+  __device__ __forceinline__ void load(const void* base, const void* scales, uint64_t row, int gq) {
+    if constexpr (KSRC == kCodeRows) {
+      __builtin_memcpy(v, (const char*)base + row * (D / 2) + gq * (D / 8), D / 8);
+      v[KS] = ((const uint8_t*)scales)[row * (D / kQ4Block) + gq * KS / 4];
+    } else {
+      __builtin_memcpy(v, (const char*)base + row * (D * 2) + gq * (D / 2), D / 2);
+    }
+  }
+  __device__ __forceinline__ void operand(bf16x8 (&t)[1][KS]) const {
+    if constexpr (KSRC == kCodeRows) {
+      const float scale = q4_scale(v[KS]);
+#pragma unroll
+      for (int x = 0; x < KS; ++x) t[0][x] = q4_octet(v[x], scale);
+    } else {
+      __builtin_memcpy(t, v, sizeof(v));
+    }
+  }
+};
+
+template <int KSRC, int QSRC, int NQ, int D>
+__global__ __launch_bounds__(kFewThreads, 2) void observe_few_kernel(ObserveArgs a) {
+  constexpr int KS = D / 32, QT = kFewRows / 16;
+  __shared__ floatx2 part[kFewWaves][kFewRows];
+  const Geom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int gq = lane >> 4, li = lane & 15;
+  const Piece pc = piece_of(a.units, a.order);
+  const uint32_t u = pc.unit;
+  const int split = pc.piece / (uint32_t)a.row_blocks;
+  const int row0 = (a.row_blocks - 1 - (int)(pc.piece % (uint32_t)a.row_blocks)) * kFewRows;
+  Unit x;
+  if (!unit_of(a, u, &x)) return;
+  const int G = g.G, R = G * a.T;
+  const int first = x.len - a.T;                       // position of query 0
+  const int first_pos = first + row0 / G, last_pos = first + (min(row0 + kFewRows, R) - 1) / G;
+  const int k_lo = split * a.split_keys;
+  const int k_hi = min(min(x.len, last_pos + 1), k_lo + a.split_keys);
+  const int32_t* row_pages = a.bt + (int64_t)x.s * g.max_blocks;
+
+  // this wave's keys k0 .. k0 + 31 (past the end: the last key, masked), their pages
+  // looked up a step before they are read
+  const void *const kbase = a.k.p[x.l], *const sbase = a.ks.p[x.l];
+  const uint32_t page_rows = (uint32_t)g.Hkv * g.bs, head_row = (uint32_t)x.h * g.bs;
+  int page[2], slot[2];
+  auto look = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int pos = min(k0 + y * 16 + li, k_hi - 1);
+      const int b = a.bs_shift >= 0 ? pos >> a.bs_shift : pos / g.bs;
+      slot[y] = pos - b * g.bs;
+      page[y] = row_pages[b];
+    }
+  };
+  KeyPart<KSRC, D> keys[2];
+  auto fetch = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const uint32_t p = min(max(page[y], 0), g.num_pages - 1);
+      keys[y].load(kbase, sbase, p * page_rows + (head_row + slot[y]), gq);
+    }
+  };
+  constexpr int kStep = kFewWaves * 32;
+  const int k_wave = k_lo + wave * 32;
+  if (k_wave < k_hi) look(k_wave);
+
+  bf16x8 qa[QT][NQ][KS];
+  int qpos[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = min(row0 + t * 16 + li, R - 1);
+    const int qt = r / G;
+    qpos[t] = first + qt;
+    const uint64_t row = (((uint64_t)x.l * a.n + x.j) * a.T + qt) * g.Hq + x.h * G + (r - qt * G);
+#pragma unroll
+    for (int y = 0; y < KS; ++y) {
+      Octet<QSRC> o;
+      o.load(a.q, nullptr, row, gq * KS + y, D);
+      bf16x8 tt[NQ];
+      o.terms(tt);
+#pragma unroll
+      for (int z = 0; z < NQ; ++z) qa[t][z][y] = tt[z];
+    }
+  }
+  float m[QT], sum[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) m[t] = kMaxFloor, sum[t] = 0.f;
+  const float c = g.scale * kLog2e;
+  if (k_wave < k_hi) {
+    fetch();
+    look(k_wave + kStep);
+    for (int k0 = k_wave; k0 < k_hi; k0 += kStep) {
+      bf16x8 ka[2][1][KS];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) keys[y].operand(ka[y]);
+      if (k0 + kStep < k_hi) {
+        fetch();
+        look(k0 + 2 * kStep);
+      }
+      floatx4 sv[2][QT];
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) sv[y][t] = dot_tile<1, NQ, KS>(ka[y], qa[t]);
+      // (wait states before the products' results are read past the branch)
+#pragma unroll
+      for (int t = 0; t < QT; ++t) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[0][t]), "+v"(sv[1][t]));
+      if (k0 + 32 > min(k_hi, first_pos + 1)) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          const int sees = min(k_hi, qpos[t] + 1) - (k0 + 4 * gq);
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (y * 16 + r >= sees) sv[y][t][r] = kNegInf;
+        }
+      }
+      add_logits(sv, c, m, sum);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float M = fmaxf(m[t], __shfl_xor(m[t], 16, 64));
+    M = fmaxf(M, __shfl_xor(M, 32, 64));
+    float L = sum[t] * __builtin_amdgcn_exp2f(m[t] - M);
+    L += __shfl_xor(L, 16, 64);
+    L += __shfl_xor(L, 32, 64);
+    if (gq == 0) part[wave][t * 16 + li] = floatx2{M, L};
+  }
+  __syncthreads();
+  if (tid < kFewRows && row0 + tid < R) {
+    float M = kMaxFloor, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) M = fmaxf(M, part[w][tid][0]);
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) L += part[w][tid][1] * __builtin_amdgcn_exp2f(part[w][tid][0] - M);
+    a.stats[((int64_t)u * R + row0 + tid) * a.splits + split] = floatx2{M, L};
   }
 }
 
@@ -542,20 +701,35 @@ constexpr int kHeldWg = kObsWaves * 16 * kHeld;         // of a workgroup
 // Launches with fewer workgroups than this split: the row statistics their keys (512
 // a split at least), the column sums their rows (256 a part at least).
 constexpr int kObsWgs = 512;
+// Row statistics of a few rows a unit by waves that take keys in turn: as long as it pays
+// to read the keys once for 32 rows.  45 sequences of 2.6-3.8K tokens, 32/8 heads, whole
+// calls: codes, 28 rows 148 -> 96 us, 128 rows 172 -> 152 (over 160 tokens, where the four
+// waves have little to share, 61 against 68); fp32 queries 279 -> 171, 64 rows 280 -> 203;
+// bf16 rows, 32 rows 169 -> 159, but 64 rows 171 against 184.
+bool few_rows(const Geom& g, int64_t R, int max_len, bool codes) {
+  if (!codes) return g.dtype == KARA_BF16 && R <= kFewRows;
+  return R <= (g.dtype == KARA_BF16 && max_len > 1024 ? 4 * kFewRows : 2 * kFewRows);
+}
+constexpr int kFewWgs = 2048;
+static_assert(kFewWgs * kFewRows <= kObsWgs * kHeldWg, "their records fit");
 
 struct Plan {
   int row_blocks, splits, split_keys, key_blocks, parts, part_rows;
   int64_t units, ld;
+  bool few;
   size_t stats_bytes, bytes;
 };
 
-Plan plan_of(const Geom& g, int n, int n_layers, int T, int max_len) {
+Plan plan_of(const Geom& g, int n, int n_layers, int T, int max_len, bool codes) {
   Plan x{};
   x.units = (int64_t)n_layers * n * g.Hkv;
   const int64_t R = (int64_t)g.G * T;
-  x.row_blocks = (int)((R + kHeldWg - 1) / kHeldWg);
+  x.few = few_rows(g, R, max_len, codes);
+  const int row_wg = x.few ? kFewRows : kHeldWg;
+  x.row_blocks = (int)((R + row_wg - 1) / row_wg);
   x.splits = 1;
-  while (x.splits < kMaxSplits && x.units * x.row_blocks * x.splits < kObsWgs && max_len > x.splits * 2 * 512) x.splits *= 2;
+  while (x.splits < kMaxSplits && x.units * x.row_blocks * x.splits < (x.few ? kFewWgs : kObsWgs) && max_len > x.splits * 2 * 512)
+    x.splits *= 2;
   x.split_keys = ((max_len + x.splits - 1) / x.splits + kChunk - 1) / kChunk * kChunk;
   x.key_blocks = (max_len + kHeldWg - 1) / kHeldWg;
   x.parts = 1;
@@ -571,9 +745,14 @@ template <int KSRC, int NK, int QSRC, int NQ, int D>
 hipError_t launch(ObserveArgs a, const Plan& x, hipStream_t stream) {
   constexpr bool kPairs = NK * NQ == 1;                 // two workgroups to a CU
   const int64_t row_blocks = x.units * x.row_blocks * x.splits, key_blocks = x.units * x.key_blocks * x.parts;
-  a.order = order_of(a.g, x.units, row_blocks, kPairs);
-  hipLaunchKernelGGL((observe_stats_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)row_blocks), dim3(kObsThreads), 0,
-                     stream, a);
+  a.order = order_of(a.g, x.units, row_blocks, kPairs && !x.few);
+  if constexpr (NK == 1) {
+    if (x.few)
+      hipLaunchKernelGGL((observe_few_kernel<KSRC, QSRC, NQ, D>), dim3((unsigned)row_blocks), dim3(kFewThreads), 0, stream, a);
+  }
+  if (!x.few)
+    hipLaunchKernelGGL((observe_stats_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)row_blocks), dim3(kObsThreads), 0,
+                       stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (x.splits > 1) {
@@ -641,7 +820,7 @@ kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_
   ObserveArgs a{};
   st = make_geom(p, n, &a.g);
   if (st != KARA_OK) return st;
-  const Plan x = plan_of(a.g, n, n_layers, n_query, max_len);
+  const Plan x = plan_of(a.g, n, n_layers, n_query, max_len, k_scales != nullptr);
   if (!workspace || workspace_bytes < x.bytes) return KARA_ERR_WORKSPACE;
   if (!grid_ok(2 * x.units * x.row_blocks * x.splits) || !grid_ok(2 * x.units * x.key_blocks * x.parts)) return KARA_ERR_UNSUPPORTED;
   a.n = n;

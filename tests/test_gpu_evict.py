@@ -196,7 +196,9 @@ def test_observe(kind, dtype, Hq, Hkv, d, bs, layers, T, n_new):
 @pytest.mark.parametrize("Hq,Hkv,d,bs,T,n_new,lens,seqs", [
     (10, 2, 128, 16, 300, 300, [2600, 299, 1700], [0, 2, 1]),       # keys split, rows in parts, more queries than tokens
     (4, 4, 64, 24, 600, 0, [601, 4100], [1, 0, 1]),                 # a sequence twice, its parts added once
-    (3, 1, 64, 16, 5, 1, [9000], [0])])                             # the most splits of few rows
+    (3, 1, 64, 16, 5, 1, [9000], [0]),                              # the most splits of few rows
+    (8, 2, 128, 24, 33, 40, [1500, 30, 1, 32, 1100], [3, 0, 2, 4, 1]),   # few rows in several workgroups, some without keys
+    (4, 4, 64, 7, 7, 7, [2100, 6, 129], [2, 0, 1])])
 def test_observe_in_pieces(kind, dtype, Hq, Hkv, d, bs, T, n_new, lens, seqs):
     assert observe_case(kind, dtype, Hq, Hkv, d, bs, 1, T, n_new, lens, max(lens), seqs) < 1
 
