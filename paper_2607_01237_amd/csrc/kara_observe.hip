@@ -3,7 +3,7 @@
 // weights need the rows' sums first: row statistics (each row's maximum and sum of
 // exponentials), then column sums with K held and the queries streamed.  No V, no
 // atomics: every key's sum is formed by one workgroup, in row order (or in a few parts
-// that a last launch adds in order).
+// that a last launch adds in order).  Few rows have kernels of their own in either sweep.
 //
 // Bound by the vector work on the logits, 3 operations and an exponential for each in
 // either sweep, beside the matrix products: 2 prompts of 2048 queries over 2048 and
@@ -54,7 +54,7 @@ struct ObserveArgs {
   int n, T, n_new, max_len;
   uint32_t units;                       // (layer, sequence, KV head)
   Order order;                          // of the blocks
-  int row_blocks, splits, split_keys;   // row statistics
+  int row_blocks, splits, split_keys;   // row statistics (split_keys: column sums of few rows, too)
   int bs_shift;                         // log2(bs) when bs is a power of two, else -1
   int key_blocks, parts, part_rows;     // column sums: the rows of a unit in parts
   const int32_t *seqs, *bt, *seq_lens;
@@ -507,17 +507,35 @@ __global__ __launch_bounds__(kFewThreads, 2) void observe_few_kernel(ObserveArgs
   }
 }
 
-// A row's splits joined into the first: a thread per row.
-__global__ __launch_bounds__(256) void observe_join_kernel(floatx2* stats, int splits, int64_t rows) {
-  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (r >= rows) return;
-  floatx2* st = stats + r * splits;
+// A row's maximum and sum from its splits'.
+__device__ __forceinline__ floatx2 join_splits(const floatx2* st, int splits) {
   float M = kMaxFloor, L = 0.f;
 #pragma unroll 4
   for (int i = 0; i < splits; ++i) M = fmaxf(M, st[i][0]);
 #pragma unroll 4
   for (int i = 0; i < splits; ++i) L += st[i][1] * __builtin_amdgcn_exp2f(st[i][0] - M);
-  st[0] = floatx2{M, L};
+  return floatx2{M, L};
+}
+
+// A row's splits joined into the first: a thread per row.  (Few rows are joined by the
+// workgroups that read them.)
+__global__ __launch_bounds__(256) void observe_join_kernel(floatx2* stats, int splits, int64_t rows) {
+  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r >= rows) return;
+  stats[r * splits] = join_splits(stats + r * splits, splits);
+}
+
+// The 16 lanes of a row of the wave hold parts of the same 8 sums: reduced and dealt out,
+// lanes li and li ^ 1 end with sum (t, r) = (li >> 3, (li >> 1) & 3).
+__device__ __forceinline__ float deal_sums(const floatx4 (&acc)[2], int li) {
+  auto half = [&](float lo, float hi, int bit) __attribute__((always_inline)) {
+    const bool up = li & bit;
+    return (up ? hi : lo) + __shfl_xor(up ? lo : hi, bit, 64);
+  };
+  const float a0 = half(acc[0][0], acc[1][0], 8), a1 = half(acc[0][1], acc[1][1], 8);
+  const float a2 = half(acc[0][2], acc[1][2], 8), a3 = half(acc[0][3], acc[1][3], 8);
+  const float v = half(half(a0, a2, 4), half(a1, a3, 4), 2);
+  return v + __shfl_xor(v, 1, 64);
 }
 
 // ---- column sums: one workgroup per (unit, 128 KT keys, part of the rows); a wave
@@ -647,19 +665,8 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum
       }
     }
   }
-  // The 16 lanes of a row of the wave hold parts of the same 8 sums: reduced and dealt
-  // out, lane li ends with sum (t, r) = (li >> 3, (li >> 1) & 3).
   static_assert(KT == 2, "eight sums to sixteen lanes");
-  float v8[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
-#pragma unroll
-  for (int half = 4; half >= 1; half >>= 1)
-#pragma unroll
-    for (int i = 0; i < half; ++i) {
-      const bool up = li & (2 * half);
-      const float keep = up ? v8[i + half] : v8[i], give = up ? v8[i] : v8[i + half];
-      v8[i] = keep + __shfl_xor(give, 2 * half, 64);
-    }
-  const float v = v8[0] + __shfl_xor(v8[0], 1, 64);
+  const float v = deal_sums(acc, li);
   const int pos = wkey0 + (li >> 3) * 16 + 4 * gq + ((li >> 1) & 3);
   if ((li & 1) || pos >= x.len) return;
   if (a.parts > 1) {
@@ -670,6 +677,129 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum
   if (page < 0 || page >= g.num_pages) return;
   float* to = a.w[x.l] + ((int64_t)page * g.Hkv + x.h) * g.bs + (pos - b * g.bs);
   *to = pos >= x.len - a.n_new ? v : *to + v;
+}
+
+// The same for few query rows, all in LDS with their statistics: a workgroup of four
+// waves per (unit, split_keys keys), the waves taking 32 keys each in turn as in
+// observe_few_kernel, without the prologue that a workgroup of observe_sum_kernel has for
+// each 256 keys (45 sequences of 2.6-3.8K tokens, 32/8 heads, codes, 28 rows: 96 -> 68 us a
+// call, 128 rows 152 -> 148, fp32 with 64 rows 203 -> 154).
+template <int KSRC, int QSRC, int NQ, int D>
+__global__ __launch_bounds__(kFewThreads, 2) void observe_few_sum_kernel(ObserveArgs a) {
+  constexpr int KS = D / 32, kOct = D / 8, kMost = (NQ == 1 ? 4 : 2) * kFewRows;
+  __shared__ __attribute__((aligned(16))) char rows[NQ][kMost * D * 2];
+  __shared__ floatx2 row_stat[kMost];                  // maximum and reciprocal sum
+  const Geom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int gq = lane >> 4, li = lane & 15;
+  const Piece pc = piece_of(a.units, a.order);
+  const uint32_t u = pc.unit;
+  Unit x;
+  if (!unit_of(a, u, &x)) return;
+  const int k_lo = pc.piece * a.split_keys, k_hi = min(x.len, k_lo + a.split_keys);
+  if (k_lo >= k_hi) return;
+  const int G = g.G, R = G * a.T, R16 = (R + 15) & ~15;
+  const int first = x.len - a.T;                       // position of query 0
+  const int32_t* row_pages = a.bt + (int64_t)x.s * g.max_blocks;
+  const void *const kbase = a.k.p[x.l], *const sbase = a.ks.p[x.l];
+  float* const wbase = a.w[x.l];
+  const uint32_t page_rows = (uint32_t)g.Hkv * g.bs, head_row = (uint32_t)x.h * g.bs;
+
+  // A wave's keys k0 .. k0 + 31 (past the end: the last one, dropped), and the
+  // accumulator that a lane writes, that of key (li >> 3) * 16 + 4 gq + ((li >> 1) & 3); pages are
+  // looked up a step before.
+  const int mine = (li >> 3) * 16 + 4 * gq + ((li >> 1) & 3);
+  int page[3], slot[3];
+  auto look = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int y = 0; y < 3; ++y) {
+      const int pos = min(k0 + (y < 2 ? y * 16 + li : mine), k_hi - 1);
+      const int b = a.bs_shift >= 0 ? pos >> a.bs_shift : pos / g.bs;
+      slot[y] = pos - b * g.bs;
+      page[y] = row_pages[b];
+    }
+  };
+  KeyPart<KSRC, D> keys[2];
+  float was = 0.f;
+  float* to = nullptr;
+  auto fetch = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const uint32_t p = min(max(page[y], 0), g.num_pages - 1);
+      keys[y].load(kbase, sbase, p * page_rows + (head_row + slot[y]), gq);
+    }
+    const bool mapped = page[2] >= 0 && page[2] < g.num_pages;
+    to = mapped ? wbase + (uint64_t)((uint32_t)page[2] * page_rows + (head_row + slot[2])) : nullptr;
+    was = mapped ? *to : 0.f;
+  };
+  constexpr int kStep = kFewWaves * 32;
+  const int k_wave = k_lo + wave * 32;
+  if (k_wave < k_hi) look(k_wave);
+  int dup = 0;
+  for (int o = tid; o < x.j; o += kFewThreads) dup |= a.seqs[o] == x.s;
+
+  const uint64_t qrow0 = ((uint64_t)x.l * a.n + x.j) * a.T * g.Hq + x.h * G;
+  for (int i = tid; i < R16 * kOct; i += kFewThreads) {
+    const int row = i / kOct, o = i % kOct, t = row / G;
+    Octet<QSRC> v;
+    v.zero();
+    if (row < R) v.load(a.q, nullptr, qrow0 + (uint64_t)t * g.Hq + (row - t * G), o, D);
+    bf16x8 tt[NQ];
+    v.terms(tt);
+#pragma unroll
+    for (int y = 0; y < NQ; ++y)
+      __builtin_memcpy(&rows[y][row * D * 2 + ((o ^ swz<D>(row & 15)) * 16)], &tt[y], 16);
+  }
+  if (tid < R) {
+    const floatx2 st = join_splits(a.stats + ((int64_t)u * R + tid) * a.splits, a.splits);
+    row_stat[tid] = floatx2{st[0], 1.f / st[1]};
+  }
+  if (__syncthreads_or(dup)) return;                   // an earlier listing counts
+  const float c = g.scale * kLog2e;
+  if (k_wave >= k_hi) return;
+  fetch();
+  look(k_wave + kStep);
+  for (int k0 = k_wave; k0 < k_hi; k0 += kStep) {
+    bf16x8 ka[2][1][KS];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) keys[y].operand(ka[y]);
+    float* const at = to;
+    const float old = was;
+    if (k0 + kStep < k_hi) {
+      fetch();
+      look(k0 + 2 * kStep);
+    }
+    floatx4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    // rows from the first that sees key k0, in tiles of 16
+    const int r_lo = max(0, k0 - first) * G & ~15;
+    for (int r0 = r_lo; r0 < R16; r0 += 16) {
+      bf16x8 qb[NQ][KS];
+#pragma unroll
+      for (int y = 0; y < NQ; ++y)
+#pragma unroll
+        for (int z = 0; z < KS; ++z)
+          __builtin_memcpy(&qb[y][z], &rows[y][(r0 + li) * D * 2 + (((gq * KS + z) ^ swz<D>(li)) * 16)], 16);
+      const int r = r0 + li;
+      const floatx2 stat = row_stat[min(r, R - 1)];
+      floatx4 sv[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) sv[y] = dot_tile<1, NQ, KS>(ka[y], qb);
+      // the last key that the row sees (a row that sees none may have no sum: its weight is
+      // dropped, not multiplied by 0)
+      const int sees = r < R ? first + r / G - k0 : -1;
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(sv[y][e], c, -stat[0]));
+          acc[y][e] += y * 16 + 4 * gq + e > sees ? 0.f : p * stat[1];
+        }
+    }
+    const float v = deal_sums(acc, li);
+    const int pos = k0 + mine;
+    if (!(li & 1) && pos < k_hi && at) *at = pos >= x.len - a.n_new ? v : old + v;
+  }
 }
 
 // The parts' sums, in order, to the accumulators: one workgroup per (unit, 256 keys).
@@ -701,11 +831,11 @@ constexpr int kHeldWg = kObsWaves * 16 * kHeld;         // of a workgroup
 // Launches with fewer workgroups than this split: the row statistics their keys (512
 // a split at least), the column sums their rows (256 a part at least).
 constexpr int kObsWgs = 512;
-// Row statistics of a few rows a unit by waves that take keys in turn: as long as it pays
-// to read the keys once for 32 rows.  45 sequences of 2.6-3.8K tokens, 32/8 heads, whole
-// calls: codes, 28 rows 148 -> 96 us, 128 rows 172 -> 152 (over 160 tokens, where the four
-// waves have little to share, 61 against 68); fp32 queries 279 -> 171, 64 rows 280 -> 203;
-// bf16 rows, 32 rows 169 -> 159, but 64 rows 171 against 184.
+// Few rows a unit: as long as it pays to read the keys once for 32 rows.  45 sequences of
+// 2.6-3.8K tokens, 32/8 heads, whole calls: codes, 28 rows 148 -> 68 us, 128 rows 172 ->
+// 148 (their statistics over 160 tokens, where the four waves have little to share, 61
+// against 68); fp32 queries 279 -> 97, 64 rows 280 -> 154; bf16 rows, 32 rows 169 -> 129,
+// but 64 rows' statistics 171 against 184.
 bool few_rows(const Geom& g, int64_t R, int max_len, bool codes) {
   if (!codes) return g.dtype == KARA_BF16 && R <= kFewRows;
   return R <= (g.dtype == KARA_BF16 && max_len > 1024 ? 4 * kFewRows : 2 * kFewRows);
@@ -714,7 +844,7 @@ constexpr int kFewWgs = 2048;
 static_assert(kFewWgs * kFewRows <= kObsWgs * kHeldWg, "their records fit");
 
 struct Plan {
-  int row_blocks, splits, split_keys, key_blocks, parts, part_rows;
+  int row_blocks, splits, split_keys, key_blocks, parts, part_rows, few_keys;
   int64_t units, ld;
   bool few;
   size_t stats_bytes, bytes;
@@ -732,8 +862,11 @@ Plan plan_of(const Geom& g, int n, int n_layers, int T, int max_len, bool codes)
     x.splits *= 2;
   x.split_keys = ((max_len + x.splits - 1) / x.splits + kChunk - 1) / kChunk * kChunk;
   x.key_blocks = (max_len + kHeldWg - 1) / kHeldWg;
+  // (few rows: keys for up to 16 steps of the four waves while 8 workgroups a CU remain)
+  x.few_keys = 128;
+  while (x.few_keys < 2048 && x.units * ((max_len + 2 * x.few_keys - 1) / (2 * x.few_keys)) >= kFewWgs) x.few_keys *= 2;
   x.parts = 1;
-  while (x.parts < kMaxSplits && x.units * x.key_blocks * x.parts < kObsWgs && R > x.parts * 2 * 256) x.parts *= 2;
+  while (!x.few && x.parts < kMaxSplits && x.units * x.key_blocks * x.parts < kObsWgs && R > x.parts * 2 * 256) x.parts *= 2;
   x.part_rows = (int)(((R + x.parts - 1) / x.parts + kChunk - 1) / kChunk * kChunk);
   x.ld = (max_len + 31) / 32 * 32;
   x.stats_bytes = ((size_t)(x.units * R * x.splits) * sizeof(floatx2) + 255) & ~(size_t)255;
@@ -755,11 +888,20 @@ hipError_t launch(ObserveArgs a, const Plan& x, hipStream_t stream) {
                        stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (x.splits > 1) {
+  if (x.splits > 1 && !x.few) {
     const int64_t rows = x.units * a.g.G * a.T;
     hipLaunchKernelGGL(observe_join_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, stream, a.stats, x.splits, rows);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
+  }
+  if constexpr (NK == 1) {
+    if (x.few) {
+      a.split_keys = x.few_keys;
+      const int64_t blocks = x.units * ((a.max_len + x.few_keys - 1) / x.few_keys);
+      a.order = order_of(a.g, x.units, blocks, false);
+      hipLaunchKernelGGL((observe_few_sum_kernel<KSRC, QSRC, NQ, D>), dim3((unsigned)blocks), dim3(kFewThreads), 0, stream, a);
+      return hipGetLastError();
+    }
   }
   a.order = order_of(a.g, x.units, key_blocks, kPairs);
   hipLaunchKernelGGL((observe_sum_kernel<KSRC, NK, QSRC, NQ, D, kHeld>), dim3((unsigned)key_blocks), dim3(kObsThreads), 0,
