@@ -71,7 +71,7 @@ kara_status_t kara_q4_read(const kara_params_t* p, int32_t n, const int32_t* seq
 
 /*
  * Bytes of device workspace kara_q4_attention needs for n sequences of at most
- * max_len tokens, n_layers layers and n_query queries each (written to *bytes, a
+ * max_len tokens (2^30 at most), n_layers layers and n_query queries each (written to *bytes, a
  * HOST pointer).
  */
 kara_status_t kara_q4_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers,

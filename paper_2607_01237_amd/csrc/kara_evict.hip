@@ -532,6 +532,7 @@ kara_status_t kara_evict_attention_workspace_size(const kara_params_t* p, int32_
   if (g.G > kMaxGroup) return KARA_ERR_UNSUPPORTED;
   if (!bytes || !layers_ok(n, n_layers) || max_len < 1 || (int64_t)max_len > (int64_t)g.max_blocks * g.bs)
     return KARA_ERR_INVALID_ARG;
+  if (max_len > kMaxLen) return KARA_ERR_UNSUPPORTED;
   *bytes = count_ws(g, n, n_layers, max_len).total;
   return KARA_OK;
 }
@@ -633,6 +634,7 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
   if (n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > keep || max_len < 1 ||
       (int64_t)max_len > (int64_t)g.max_blocks * g.bs)
     return KARA_ERR_INVALID_ARG;
+  if (max_len > kMaxLen) return KARA_ERR_UNSUPPORTED;
   if (n == 0) return KARA_OK;
   if (!seqs || !block_table || !seq_lens || !status || !pools_ok(k_pools, n_layers) || !pools_ok(v_pools, n_layers) ||
       !scales_ok(k_scales, v_scales, n_layers) || !pools_ok((const void* const*)weights, n_layers) ||

@@ -940,6 +940,7 @@ kara_status_t kara_evict_observe_workspace_size(const kara_params_t* p, int32_t 
   if (!bytes || n < 0 || n_layers < 1 || n_layers > kMaxLayersPerLaunch || n_query < 1 || max_len < 1 ||
       (int64_t)max_len > (int64_t)g.max_blocks * g.bs || (int64_t)n_query * g.Hq > INT32_MAX / 4)
     return KARA_ERR_INVALID_ARG;
+  if (max_len > kMaxLen) return KARA_ERR_UNSUPPORTED;
   // (a launch of kObsWgs row blocks or more does not split; a smaller one has fewer
   // than twice as many, records and all; the same for key blocks and their sums)
   const int64_t rows = (int64_t)n_layers * n * g.Hkv * g.G * n_query;

@@ -895,6 +895,7 @@ kara_status_t kara_q4_attention_workspace_size(const kara_params_t* p, int32_t n
   if (!bytes || !layers_ok(n, n_layers) || n_query < 1 || max_len < 1 || (int64_t)max_len > (int64_t)g.max_blocks * g.bs ||
       (int64_t)n_query * g.Hq > INT32_MAX / 4)
     return KARA_ERR_INVALID_ARG;
+  if (max_len > kMaxLen) return KARA_ERR_UNSUPPORTED;
   const size_t rec = (g.d + 2) * sizeof(float);
   const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
   if (few_rows(g, n_query)) {

@@ -174,3 +174,20 @@ def test_binding_checks():
                 (codes, codes, [scales[0][1:], scales[1]], scales, weights)):
         with pytest.raises(kara.KaraError):
             kara._cache_args(torch, cpu, p, 2, *bad)
+
+
+def test_longest_sequences(lib):
+    # max_len up to 2^30, whatever the table could map; sizes there do not wrap
+    out = ctypes.c_size_t(0)
+    p = params(block_size=256, num_pages=1, max_blocks_per_seq=(2 ** 31 - 1) // 256)
+    sizes = {"kara_q4_attention_workspace_size": (1, 1, 1), "kara_evict_attention_workspace_size": (1, 1),
+             "kara_evict_observe_workspace_size": (1, 1, 4)}
+    for name, args in sizes.items():
+        fn = getattr(lib, name)
+        assert fn(ctypes.byref(p), *args, 2 ** 30, ctypes.byref(out)) == OK
+        if "observe" not in name:                      # a record per 256 keys and query head
+            assert out.value >= 2 ** 22 * 32 * 130 * 4, name
+        assert fn(ctypes.byref(p), *args, 2 ** 30 + 1, ctypes.byref(out)) == UNSUPPORTED, name
+    for name in ("kara_q4_attention", "kara_evict_attention", "kara_evict_observe", "kara_evict_tokens"):
+        args = [2 ** 30 + 1 if k == "max_len" else v for k, v in CALLS[name]]
+        assert getattr(lib, name)(ctypes.byref(p), *args) == UNSUPPORTED, name
