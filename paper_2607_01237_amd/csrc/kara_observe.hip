@@ -98,7 +98,7 @@ struct Octet {
       uint32_t w[4][NT];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        bf16_term_pairs(__uint_as_float(v[i >> 1][2 * i & 3]), __uint_as_float(v[i >> 1][(2 * i & 3) + 1]), w[i]);
+        bf16_term_pairs<true>(__uint_as_float(v[i >> 1][2 * i & 3]), __uint_as_float(v[i >> 1][(2 * i & 3) + 1]), w[i]);
 #pragma unroll
       for (int y = 0; y < NT; ++y) t[y] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
     }

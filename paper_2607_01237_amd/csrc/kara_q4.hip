@@ -434,7 +434,7 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float x0 = i < 2 ? u[2 * i] : v[2 * i - 4], x1 = i < 2 ? u[2 * i + 1] : v[2 * i - 3];
-        bf16_term_pairs(there ? x0 : 0.f, there ? x1 : 0.f, w[i]);
+        bf16_term_pairs<true>(there ? x0 : 0.f, there ? x1 : 0.f, w[i]);
       }
 #pragma unroll
       for (int y = 0; y < NQ; ++y) qa[y][x] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
@@ -583,7 +583,7 @@ __global__ __launch_bounds__(kSplitThreads, 2) void q4_split_kernel(Q4Split a) {
         const float p1 = __builtin_amdgcn_exp2f(fmaf(sv[t][r + 1], c, -m));
         if constexpr (NP > 1) lsum += p0 + p1;
         uint32_t w[NP];
-        bf16_term_pairs(p0, p1, w);
+        bf16_term_pairs<false>(p0, p1, w);
 #pragma unroll
         for (int y = 0; y < NP; ++y) pw[y][2 * t + (r >> 1)] = w[y];
       }

@@ -137,7 +137,8 @@ __global__ __launch_bounds__(W * 64, 2) void q4_chunk_kernel(Q4Split a) {
         const floatx4 p = src[0], q = src[1];
         uint32_t w[4][NT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) bf16_term_pairs(i < 2 ? p[2 * i] : q[2 * i - 4], i < 2 ? p[2 * i + 1] : q[2 * i - 3], w[i]);
+        for (int i = 0; i < 4; ++i)
+          bf16_term_pairs<true>(i < 2 ? p[2 * i] : q[2 * i - 4], i < 2 ? p[2 * i + 1] : q[2 * i - 3], w[i]);
 #pragma unroll
         for (int y = 0; y < NT; ++y) qop[qt][y][x] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
       }
@@ -274,8 +275,8 @@ __global__ __launch_bounds__(W * 64, 2) void q4_chunk_kernel(Q4Split a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const floatx4 x = sv[qt][2 * jj + (i >> 1)];
-          bf16_term_pairs(__builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1)], c, -mr)),
-                          __builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1) + 1], c, -mr)), w[i]);
+          bf16_term_pairs<false>(__builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1)], c, -mr)),
+                                 __builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1) + 1], c, -mr)), w[i]);
         }
 #pragma unroll
         for (int y = 0; y < NT; ++y) pb[qt][y][jj] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});

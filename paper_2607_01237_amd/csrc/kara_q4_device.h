@@ -41,22 +41,29 @@ __device__ __forceinline__ bf16x8 q4_octet(uint32_t codes, float scale) {
 // x as the sum of NT bf16 values: each but the last the upper half of what the ones
 // before leave (8 bits of it), the last rounded -- 8, 16 or 24 bits of x.  As fp32
 // whose upper halves are the terms.
-template <int NT>
+//
+// INF (queries and keys; weights are finite or NaN): an infinity is the last term
+// alone.  As the first it would leave inf - inf to the others, and it would meet the
+// other factor's lower terms, zeros where one bf16 holds that; the last term meets
+// only its first.
+template <bool INF, int NT>
 __device__ __forceinline__ void bf16_parts(float x, uint32_t (&t)[NT]) {
+  uint32_t upper = 0xffff0000u;
+  if constexpr (INF && NT > 1) upper = __builtin_isinf(x) ? 0u : upper;
 #pragma unroll
   for (int i = 0; i + 1 < NT; ++i) {
-    t[i] = __float_as_uint(x) & 0xffff0000u;
+    t[i] = __float_as_uint(x) & upper;
     x -= __uint_as_float(t[i]);
   }
   t[NT - 1] = __float_as_uint(x);
 }
 
 // Two values' terms as packed pairs, the first value in the lower halves
-template <int NT>
+template <bool INF, int NT>
 __device__ __forceinline__ void bf16_term_pairs(float x0, float x1, uint32_t (&t)[NT]) {
   uint32_t a[NT], b[NT];
-  bf16_parts(x0, a);
-  bf16_parts(x1, b);
+  bf16_parts<INF>(x0, a);
+  bf16_parts<INF>(x1, b);
 #pragma unroll
   for (int i = 0; i + 1 < NT; ++i) t[i] = __builtin_amdgcn_perm(b[i], a[i], 0x07060302u);
   const bf16x2 last = {(__bf16)__uint_as_float(a[NT - 1]), (__bf16)__uint_as_float(b[NT - 1])};
