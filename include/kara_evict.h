@@ -14,7 +14,13 @@
  * the call that first counts them, so pages need no clearing.
  *
  * The cache is either rows of p->dtype (kara.h; k_scales and v_scales NULL) or
- * held in 4 bits (kara_q4.h; both given, p->dtype the type of q).  Conventions
+ * held in 4 bits (kara_q4.h; both given, p->dtype the type of q).
+ *
+ * Infinite and NaN elements of keys and queries enter the logits as they are: a
+ * logit of -inf is a weight of 0, one of +inf or NaN makes the weights that its
+ * query gives NaN.  A query whose every logit is -inf gives no weights.
+ *
+ * Conventions
  * are those of kara.h and kara_harness.h: device pointers unless stated (pool
  * arrays: host arrays of n_layers device pointers, 1 <= n_layers <= 64), the
  * caller owns all memory, nothing synchronises or allocates, host-checkable
@@ -40,7 +46,8 @@ kara_status_t kara_evict_attention_workspace_size(const kara_params_t* p, int32_
  * kara_harness_decode_attention (one query per layer, sequence and query head
  * over the whole cache, G <= KARA_HARNESS_MAX_GROUP; out fp32) that also adds
  * each key's weight, summed over the group's query heads, to its accumulator:
- * positions below seq_len - n_new are added to, the last n_new are set.  A
+ * positions below seq_len - n_new are added to, the last n_new are set.  The output
+ * row of a query that gives no weights is zero.  A
  * sequence listed more than once is counted once, by its first listing.  Longer
  * sequences than max_len, empty ones and indices outside [0, n_seqs) give zero
  * output rows and leave their accumulators alone.  The block table must map

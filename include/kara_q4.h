@@ -85,8 +85,8 @@ kara_status_t kara_q4_attention_workspace_size(const kara_params_t* p, int32_t n
  *                         scale * q . K_k,  KV head hq / G.
  * n_query = 1 is a decoding step.  q, out: [n_layers][n][n_query][n_q_heads]
  * [head_dim] (p->dtype).  Rows before the sequence's start (n_query > seq_len),
- * sequences longer than max_len and sequence indices outside [0, n_seqs) give
- * zeros.  The block table must map every position below seq_len to a page of the
+ * sequences longer than max_len, sequence indices outside [0, n_seqs) and queries
+ * whose every logit is -inf give zeros; a logit of +inf or NaN gives NaN.  The block table must map every position below seq_len to a page of the
  * pool; where it does not, the sequence's output is unspecified, and nothing
  * outside the pools is read.  Softmax statistics and sums are fp32; bf16 calls
  * round each weight to bf16 before it meets V (the same rounded weights make up

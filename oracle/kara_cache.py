@@ -49,8 +49,9 @@ def q4_values(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
 
 def attend(q, k, v, scale):
     """q [T, Hq, d], k, v [n, Hkv, d] (v may be None), fp64.  Query t sits at
-    position n - T + t and sees the keys up to it.  Returns out [T, Hq, d],
-    the sums of w|v| [T, Hq, d], and the keys' weights [Hkv, n]."""
+    position n - T + t and sees the keys up to it; one whose every logit is -inf
+    gives no key a weight.  Returns out [T, Hq, d], the sums of w|v| [T, Hq, d],
+    and the keys' weights [Hkv, n]."""
     T, Hq, d = q.shape
     n, Hkv = k.shape[:2]
     G = Hq // Hkv
@@ -63,6 +64,8 @@ def attend(q, k, v, scale):
         for hq in range(Hq):
             h = hq // G
             x = scale * (k[:m, h] @ q[t, hq])
+            if x.max() == -np.inf:
+                continue
             w = np.exp(x - x.max())
             w /= w.sum()
             weights[h, :m] += w

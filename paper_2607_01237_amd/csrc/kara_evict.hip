@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kFinThreads) void evict_finish_kernel(
       L += w[(int64_t)sp * ml_step + 1] * __builtin_amdgcn_exp2f(w[(int64_t)sp * ml_step] - M);
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) L += __shfl_xor(L, x, 64);
-    if (lane == 0) red_m[i] = M, red_i[i] = 1.f / L;
+    if (lane == 0) red_m[i] = M, red_i[i] = L == 0.f ? 0.f : 1.f / L;     // (0: every logit is -inf)
   }
   dup = __syncthreads_or(dup);
   for (int i = chunk; i < G; i += nc) {

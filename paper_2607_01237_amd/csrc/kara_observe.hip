@@ -634,7 +634,7 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float p = __builtin_amdgcn_exp2f(fmaf(sv[t][r], c, -rm));
-        // (a row that sees none of these keys may have no sum: its weight is dropped, not multiplied by 0)
+        // (dropped, not multiplied by 0: against the maximum of a row that sees no key it may be infinite)
         if constexpr (decltype(masked)::value) acc[t][r] += wkey0 + t * 16 + 4 * gq + r > pos ? 0.f : p * ri;
         else acc[t][r] = fmaf(p, ri, acc[t][r]);
       }
@@ -652,7 +652,8 @@ __global__ __launch_bounds__(kObsThreads, NK * NQ == 1 ? 4 : 2) void observe_sum
         for (int y = 0; y < NQ; ++y)
           __builtin_memcpy(&lds.b[buf][y][row * D * 2 + ((soct ^ swz<D>(row & 15)) * 16)], &t[y], 16);
       }
-      if (tid < kChunk) row_stat[buf][tid] = floatx2{st[0], 1.f / st[1]};
+      // (a sum of 0: every logit of the row is -inf, or it sees no key)
+      if (tid < kChunk) row_stat[buf][tid] = floatx2{st[0], st[1] == 0.f ? 0.f : 1.f / st[1]};
       if (r0 + kChunk < r_hi) fetch(r0 + kChunk);
       __syncthreads();
       if (wkey0 >= x.len || first + (min(r0 + kChunk, r_hi) - 1) / G < wkey0) continue;     // (uniform in the wave)
@@ -753,7 +754,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void observe_few_sum_kernel(Observe
   }
   if (tid < R) {
     const floatx2 st = join_splits(a.stats + ((int64_t)u * R + tid) * a.splits, a.splits);
-    row_stat[tid] = floatx2{st[0], 1.f / st[1]};
+    row_stat[tid] = floatx2{st[0], st[1] == 0.f ? 0.f : 1.f / st[1]};   // (0: as in observe_sum_kernel)
   }
   if (__syncthreads_or(dup)) return;                   // an earlier listing counts
   const float c = g.scale * kLog2e;
@@ -785,8 +786,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void observe_few_sum_kernel(Observe
       floatx4 sv[2];
 #pragma unroll
       for (int y = 0; y < 2; ++y) sv[y] = dot_tile<1, NQ, KS>(ka[y], qb);
-      // the last key that the row sees (a row that sees none may have no sum: its weight is
-      // dropped, not multiplied by 0)
+      // the last key that the row sees (weights past it are dropped, not multiplied by 0:
+      // against the maximum of a row that sees no key they may be infinite)
       const int sees = r < R ? first + r / G - k0 : -1;
 #pragma unroll
       for (int y = 0; y < 2; ++y)

@@ -126,3 +126,59 @@ def test_nothing_past_the_sequences_enters(fn, T, kind, dtype):
     c = Cache(rng, kind, dtype, 8, 2, 64, 16, lens)
     spoil_the_rest(c)
     assert check(c, fn, [3, 1, 0, 2], queries(rng, c, 4, T), T, 1, 700) < 1
+
+
+@pytest.mark.parametrize("fn,T,kind,dtype", FORMS + [("observe", 300, "rows", "bf16"), ("observe", 300, "q4", "f32"),
+                                                     ("q4", 300, "q4", "bf16"), ("q4", 300, "q4", "f32")])
+def test_a_query_of_no_weights(fn, T, kind, dtype):
+    # one query whose every logit is -inf, the others as ever: it has a zero row and adds nothing
+    print(f"\n[case] no weights {fn} {kind} {dtype} T={T}", flush=True)
+    rng = np.random.default_rng(T)
+    lens = [270, 1, 2700, 33]
+    c = Cache(rng, kind, dtype, 8, 2, 64, 16, lens)
+    if kind == "q4":                                   # element 9 of every key: the code of 1
+        for codes in (c.host["k"], c.dev["k"]):
+            codes[..., 4] = (codes[..., 4] & 15) | (2 << 4)
+    else:
+        c.host["k"][..., 9] = c.dev["k"][..., 9] = 1.0
+    q = queries(rng, c, 4, T)
+    q[0, 1, T // 2, 3, 9] = q[0, 3, T // 2, 5, 9] = q[0, 0, T - 1, 0, 9] = -np.inf
+    seqs = [3, 0, 1, 2]
+    assert check(c, fn, seqs, q, T, 1, 2700) < 1
+    if fn != "observe":
+        c = Cache(np.random.default_rng(1), kind, dtype, 8, 2, 64, 16, [40])
+        assert not run(c, fn, [5], q[:, :1], T, 1, 40).any()               # (no sequence: zeros too)
+
+
+@pytest.mark.parametrize("value", [np.inf, np.nan])
+@pytest.mark.parametrize("fn,T,kind,dtype", FORMS)
+def test_a_query_of_nan(fn, T, kind, dtype, value):
+    # a logit of +inf or NaN: that query's row is NaN and the weights it gives, no others
+    print(f"\n[case] NaN {fn} {kind} {dtype} T={T} {value}", flush=True)
+    lens = [270, 1, 2700, 33]
+    c = Cache(np.random.default_rng(T), kind, dtype, 8, 2, 64, 16, lens)
+    if kind == "q4":
+        for codes in (c.host["k"], c.dev["k"]):
+            codes[..., 4] = (codes[..., 4] & 15) | (2 << 4)
+    else:
+        c.host["k"][..., 9] = c.dev["k"][..., 9] = 1.0
+    q = queries(np.random.default_rng(T + 1), c, 4, T)
+    seqs, at = [3, 0, 1, 2], {0: (T - 1, 0), 1: (T // 2, 3), 3: (T // 2, 5)}
+    for j, (t, hq) in at.items():
+        q[0, j, t, hq, 9] = value
+    got = run(c, fn, seqs, q, T, 1, 2700)
+    w = c.w[0].cpu().numpy()
+    for j, s in enumerate(seqs):
+        t, hq = at.get(j, (0, None))
+        n, seen = lens[s], lens[s] - T + t + 1
+        if got is not None:
+            want = np.zeros(got.shape[2:4], dtype=bool)
+            if hq is not None and seen > 0:
+                want[t, hq] = True
+            assert np.array_equal(np.isnan(got[0, j]), np.broadcast_to(want[..., None], got.shape[2:])), j
+        if fn != "q4":
+            want = np.zeros((n, 2), dtype=bool)
+            if hq is not None:
+                want[:max(seen, 0), hq // 4] = True
+            pos = np.arange(n)
+            assert np.array_equal(np.isnan(w[c.table[s][pos // 16], :, pos % 16]), want), j
