@@ -98,7 +98,8 @@ kara_status_t kara_evict_workspace_size(const kara_params_t* p, int32_t n, int32
  *   kept     [n_layers][n][n_kv_heads][keep] int32, ascending positions, -1 past
  *            the end of a shorter sequence; NULL: held in the workspace
  *   commit   non-zero: seq_lens[s] = keep, and the blocks past it released as in
- *            kara_commit_tables (freed [n][max_blocks_per_seq], n_freed [n]).
+ *            kara_commit_tables (freed [n][max_blocks_per_seq], n_freed [n]), by the
+ *            last launch, with the rows: where a launch fails, lengths and tables stay.
  *            Zero: lengths and tables stay, for a caller that passes its layers in
  *            several calls and commits with the last; freed, n_freed are not used.
  *   status   KARA_SEQ_* bits: BAD_INDEX, DUP_TRIGGER, BAD_WINDOW (seq_len negative,

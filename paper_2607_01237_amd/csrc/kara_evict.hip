@@ -144,8 +144,8 @@ struct EvictArgs {
   Geom g;
   int n, n_layers, keep, n_sink, n_recent, max_len;
   int commit;
-  const int32_t* seqs;
-  int32_t *bt, *seq_lens, *kept, *status;
+  const int32_t *seqs, *bt, *seq_lens;
+  int32_t *kept, *status;
   int32_t *freed, *n_freed;   // commit: pages released (each listing's blocks past the cut)
   int32_t* old_len;           // [n] lengths before the cut, 0 where there is none
   PoolPtrs k, v, ks, vs;      // rows or codes; scales (null: rows)
@@ -155,8 +155,14 @@ struct EvictArgs {
   int cols;                   // pieces that the move cuts a row into
 };
 
-// Pages of a listed sequence as they were before the cut: those that it released
-// are in `freed` by the time rows move.
+// What the last launch writes where the call commits: no earlier one can change a
+// table or a length, so a call that fails between them leaves sequences as they were.
+struct EvictCommit {
+  int32_t *bt, *seq_lens;
+};
+
+// Pages of a listed sequence as they were before the cut: while rows move, one
+// workgroup takes those past it out of the table, and the others read them in `freed`.
 struct Pages {
   const int32_t *row, *tail;
   int first_tail;
@@ -167,9 +173,8 @@ struct Pages {
   __device__ __forceinline__ int operator[](int b) const { return *(b < first_tail ? row + b : tail + (b - first_tail)); }
 };
 
-// One workgroup per listed sequence: its status and, where the call commits, the
-// release of the blocks past the cut and the new length -- first, in one launch;
-// the rows follow by what this leaves in old_len and freed.
+// One workgroup per listed sequence: its status, its length in old_len (0: left
+// alone) and, where the call commits, its pages past the cut in `freed`.
 __global__ __launch_bounds__(kValidateThreads) void evict_validate_kernel(EvictArgs a) {
   __shared__ uint32_t lds[kValidateLds];
   const Geom& g = a.g;
@@ -192,20 +197,11 @@ __global__ __launch_bounds__(kValidateThreads) void evict_validate_kernel(EvictA
     a.old_len[j] = len;
   }
   if (!a.commit) return;
-  __syncthreads();                       // every thread has read the length before it changes
-  const int new_len = min(len, a.keep);
-  const int old_b = (len + g.bs - 1) / g.bs, new_b = (new_len + g.bs - 1) / g.bs;
-  int32_t* row = a.bt + (int64_t)(st == 0 ? s : 0) * g.max_blocks;
+  const int old_b = (len + g.bs - 1) / g.bs, new_b = (min(len, a.keep) + g.bs - 1) / g.bs;
+  const int32_t* row = a.bt + (int64_t)(st == 0 ? s : 0) * g.max_blocks;
   int32_t* fr = a.freed + (int64_t)j * g.max_blocks;
-  for (int c = tid; c < g.max_blocks; c += kValidateThreads) {
-    const bool gone = c < old_b - new_b;
-    fr[c] = gone ? row[new_b + c] : -1;
-    if (gone) row[new_b + c] = -1;
-  }
-  if (tid == 0) {
-    a.n_freed[j] = old_b - new_b;
-    if (new_len < len) a.seq_lens[s] = new_len;
-  }
+  for (int c = tid; c < g.max_blocks; c += kValidateThreads) fr[c] = c < old_b - new_b ? row[new_b + c] : -1;
+  if (tid == 0) a.n_freed[j] = 0;        // (until the pages are released)
 }
 
 constexpr int kPickThreads = 512;
@@ -382,9 +378,9 @@ constexpr int kMoveStage = 65536 / 4;     // rows held in LDS, at most
 // the bytes: 64 sequences x 4 layers cut from 3.9-8.2K to 3.8K tokens (8.1 GB) in
 // 1576 us, 5.1 TB/s.  1024 threads a workgroup: that cut was 2 % slower with 256; 8
 // sequences of one layer, where a tile's latency is all that the launch spends, took
-// 36 us with 256, 24 so.
+// 36 us with 256, 24 so.  The workgroup of a sequence's first small arrays commits.
 template <bool STAGED>
-__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, EvictCommit out) {
   extern __shared__ uint32_t stage[];
   const Geom& g = a.g;
   const int tid = threadIdx.x;
@@ -478,6 +474,16 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
         ((uint16_t*)a.ks.p[l])[to[k]] = (uint16_t)sk[k];
         ((uint16_t*)a.vs.p[l])[to[k]] = (uint16_t)sv[k];
       }
+    }
+  }
+  if (a.commit && l == 0 && h == 0) {
+    // blocks past the cut and the length: no workgroup of this launch reads them here
+    const int s = a.seqs[j];
+    const int old_b = (len + g.bs - 1) / g.bs, new_b = (a.keep + g.bs - 1) / g.bs;
+    for (int b = new_b + tid; b < old_b; b += kMoveThreads) out.bt[(int64_t)s * g.max_blocks + b] = -1;
+    if (tid == 0) {
+      a.n_freed[j] = old_b - new_b;
+      out.seq_lens[s] = a.keep;
     }
   }
 }
@@ -681,8 +687,9 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
   a.cols = std::max(1, a.row_bytes / 128);
   while (units * 2 * a.cols < 256 && a.row_bytes / a.cols > 64) a.cols *= 2;
   const dim3 grid((unsigned)(units * (2 * a.cols + 1))), block(kMoveThreads);
-  if (staged <= kMoveStage) hipLaunchKernelGGL((evict_move_kernel<true>), grid, block, (size_t)staged * 4, s, a);
-  else hipLaunchKernelGGL((evict_move_kernel<false>), grid, block, 0, s, a);
+  const EvictCommit out{block_table, seq_lens};
+  if (staged <= kMoveStage) hipLaunchKernelGGL((evict_move_kernel<true>), grid, block, (size_t)staged * 4, s, a, out);
+  else hipLaunchKernelGGL((evict_move_kernel<false>), grid, block, 0, s, a, out);
   return hip_status(hipGetLastError());
 }
 
