@@ -26,7 +26,7 @@
  * caller owns all memory, nothing synchronises or allocates, host-checkable
  * argument errors come back as KARA_ERR_* with nothing enqueued.  The
  * window-related fields of p must be valid but are not used.  Device arrays are
- * 16-byte aligned; max_len is 2^30 at most.
+ * 16-byte aligned; max_len and keep are 2^30 at most.
  */
 #ifndef KARA_EVICT_H
 #define KARA_EVICT_H

@@ -620,6 +620,7 @@ kara_status_t kara_evict_workspace_size(const kara_params_t* p, int32_t n, int32
   const kara_status_t st = make_geom(p, n, &g);
   if (st != KARA_OK) return st;
   if (!bytes || !layers_ok(n, n_layers) || keep < 1) return KARA_ERR_INVALID_ARG;
+  if (keep > kMaxLen) return KARA_ERR_UNSUPPORTED;      // (positions step in 32 bits)
   *bytes = align256((size_t)n * sizeof(int32_t)) + (size_t)n_layers * n * g.Hkv * keep * sizeof(int32_t);
   return KARA_OK;
 }

@@ -114,8 +114,8 @@ hipError_t launch_rope(const void* qraw, void* q_out, int n_trig, int W, int Hq,
                        const int32_t* trig, const int32_t* rope_pos0, const int32_t* status, hipStream_t stream);
 hipError_t launch_swiglu(void* gate, const void* up, int64_t n, hipStream_t stream);
 
-// Longest sequence that the 4-bit cache's attention and eviction take: round-ups stay
-// in 32 bits (a pool has at most 2^29 rows).
+// Longest sequence that the 4-bit cache's attention and eviction take, and most tokens
+// that a cut keeps: round-ups and steps stay in 32 bits (a pool has at most 2^29 rows).
 constexpr int kMaxLen = 1 << 30;
 
 // Attention of few query rows over the 4-bit cache, keys split over workgroups
