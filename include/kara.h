@@ -89,7 +89,7 @@ typedef enum kara_dtype {
 
 typedef enum kara_status {
   KARA_OK = 0,
-  KARA_ERR_INVALID_ARG = -1, /* a parameter is out of range or a pointer is NULL */
+  KARA_ERR_INVALID_ARG = -1, /* a parameter is out of range, or a pointer is NULL or not aligned */
   KARA_ERR_UNSUPPORTED = -2, /* valid but not built (e.g. head_dim not 64/128) */
   KARA_ERR_WORKSPACE = -3,   /* workspace missing or smaller than kara_workspace_size() */
   KARA_ERR_HIP = -4,         /* the HIP runtime rejected a launch */

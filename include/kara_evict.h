@@ -25,8 +25,9 @@
  * arrays: host arrays of n_layers device pointers, 1 <= n_layers <= 64), the
  * caller owns all memory, nothing synchronises or allocates, host-checkable
  * argument errors come back as KARA_ERR_* with nothing enqueued.  The
- * window-related fields of p must be valid but are not used.  Device arrays are
- * 16-byte aligned; max_len and keep are 2^30 at most.
+ * window-related fields of p must be valid but are not used.  max_len and keep are
+ * 2^30 at most.  Alignment, checked: that of kara_q4.h, rows 16 bytes, accumulators
+ * 16 where block_size is a multiple of 4, else 4.
  */
 #ifndef KARA_EVICT_H
 #define KARA_EVICT_H

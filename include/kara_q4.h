@@ -19,8 +19,10 @@
  *                        uint8, element 2i in the low half of byte i
  *   k_scales, v_scales   scales [num_pages][n_kv_heads][block_size][head_dim / 32]
  *                        uint8
- * 68 bytes a row at head_dim 128 where bf16 takes 256.  Device arrays are
- * 16-byte aligned.
+ * 68 bytes a row at head_dim 128 where bf16 takes 256.
+ *
+ * Alignment, checked: codes, k_new, v_new, q, k_out, v_out, out and workspaces 16
+ * bytes, scales those of a row (head_dim / 32), int32 arrays 4.
  *
  * Conventions are those of kara.h and kara_harness.h: device pointers unless
  * stated (pool arrays: host arrays of n_layers device pointers, 1 <= n_layers

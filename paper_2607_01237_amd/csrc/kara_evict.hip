@@ -560,6 +560,9 @@ kara_status_t kara_evict_attention(const kara_params_t* p, int32_t n, const int3
   Geom g;
   st = make_geom(p, n, &g);
   if (st != KARA_OK) return st;
+  if (!aligned(16, {q, out, workspace}) || !aligned(4, {seqs, block_table, seq_lens}) ||
+      !cache_aligned(g, n_layers, k_pools, v_pools, k_scales, v_scales, (const void* const*)weights))
+    return KARA_ERR_INVALID_ARG;
   const CountWs w = count_ws(g, n, n_layers, max_len);
   float* records = (float*)workspace;
   float* logits = (float*)((char*)workspace + w.logits);
@@ -649,6 +652,9 @@ kara_status_t kara_evict_tokens(const kara_params_t* p, int32_t n, const int32_t
     return KARA_ERR_INVALID_ARG;
   if (kept) need = (size_t)n * sizeof(int32_t);     // (the lengths alone)
   if (!workspace || workspace_bytes < need) return KARA_ERR_WORKSPACE;
+  if (!aligned(16, {workspace}) || !aligned(4, {seqs, block_table, seq_lens, kept, freed, n_freed, status}) ||
+      !cache_aligned(g, n_layers, k_pools, v_pools, k_scales, v_scales, (const void* const*)weights))
+    return KARA_ERR_INVALID_ARG;
   const int64_t units = (int64_t)n_layers * n * g.Hkv;
   if (!grid_ok(units * 4 * (2 * 4 + 1))) return KARA_ERR_UNSUPPORTED;
   a.n = n;

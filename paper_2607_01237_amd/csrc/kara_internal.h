@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "kara.h"
 
 namespace kara {
@@ -39,6 +41,26 @@ struct PoolPtrs {
 kara_status_t make_geom(const kara_params_t* p, int32_t n_trig, Geom* g);
 kara_status_t hip_status(hipError_t e);
 bool pools_ok(const void* const* pools, int n_layers);
+
+// Alignment of arrays and of pools (null ones: none to check).
+inline bool aligned(size_t to, std::initializer_list<const void*> arrays) {
+  for (const void* a : arrays)
+    if ((uintptr_t)a % to) return false;
+  return true;
+}
+inline bool pools_aligned(size_t to, const void* const* pools, int n_layers) {
+  for (int i = 0; pools && i < n_layers; ++i)
+    if ((uintptr_t)pools[i] % to) return false;
+  return true;
+}
+// Pools of a cache and of accumulators as the kernels of 4 bits and of eviction
+// address them: rows and codes by 16 bytes, a row's scales at once, accumulators by
+// four where a page holds a multiple of that.
+inline bool cache_aligned(const Geom& g, int n_layers, const void* const* k, const void* const* v, const void* const* ks,
+                          const void* const* vs, const void* const* w) {
+  return pools_aligned(16, k, n_layers) && pools_aligned(16, v, n_layers) && pools_aligned(g.d / 32, ks, n_layers) &&
+         pools_aligned(g.d / 32, vs, n_layers) && pools_aligned(g.bs % 4 == 0 ? 16 : 4, w, n_layers);
+}
 
 // Validation kernel (kara_pages.hip).  keep_kept: a KARA_SEQ_BAD_KEPT bit
 // already in status survives (staged per-layer compaction and the commit).

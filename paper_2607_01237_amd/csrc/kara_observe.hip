@@ -966,6 +966,9 @@ kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_
   if (st != KARA_OK) return st;
   const Plan x = plan_of(a.g, n, n_layers, n_query, max_len, k_scales != nullptr);
   if (!workspace || workspace_bytes < x.bytes) return KARA_ERR_WORKSPACE;
+  if (!aligned(16, {q, workspace}) || !aligned(4, {seqs, block_table, seq_lens}) ||
+      !cache_aligned(a.g, n_layers, k_pools, nullptr, k_scales, nullptr, (const void* const*)weights))
+    return KARA_ERR_INVALID_ARG;
   if (!grid_ok(2 * x.units * x.row_blocks * x.splits) || !grid_ok(2 * x.units * x.key_blocks * x.parts)) return KARA_ERR_UNSUPPORTED;
   a.n = n;
   a.T = n_query;

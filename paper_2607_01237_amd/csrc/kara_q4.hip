@@ -813,6 +813,9 @@ kara_status_t kara_q4_append(const kara_params_t* p, int32_t n, const int32_t* s
   if (!seqs || !k_new || !v_new || !block_table || !seq_lens || !status || !pools_ok(k_pools, n_layers) ||
       !pools_ok(v_pools, n_layers) || !pools_ok(k_scales, n_layers) || !pools_ok(v_scales, n_layers))
     return KARA_ERR_INVALID_ARG;
+  if (!aligned(16, {k_new, v_new}) || !aligned(4, {seqs, block_table, seq_lens, status}) ||
+      !cache_aligned(g, n_layers, k_pools, v_pools, k_scales, v_scales, nullptr))
+    return KARA_ERR_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
   if ((int64_t)g.Hkv * (g.d / 8) > kMaxOctets) return KARA_ERR_UNSUPPORTED;
   const int per_tok = g.Hkv * (g.d / 8);
@@ -865,6 +868,9 @@ kara_status_t kara_q4_read(const kara_params_t* p, int32_t n, const int32_t* seq
   if (n == 0 || n_rows == 0) return KARA_OK;
   if (!seqs || !start || !k_out || !v_out || !block_table || !seq_lens || !pools_ok(k_pools, n_layers) ||
       !pools_ok(v_pools, n_layers) || !pools_ok(k_scales, n_layers) || !pools_ok(v_scales, n_layers))
+    return KARA_ERR_INVALID_ARG;
+  if (!aligned(16, {k_out, v_out}) || !aligned(4, {seqs, start, block_table, seq_lens}) ||
+      !cache_aligned(g, n_layers, k_pools, v_pools, k_scales, v_scales, nullptr))
     return KARA_ERR_INVALID_ARG;
   if ((int64_t)g.Hkv * (g.d / 8) > kMaxOctets) return KARA_ERR_UNSUPPORTED;
   const int per_tok = g.Hkv * (g.d / 8);
@@ -926,6 +932,9 @@ kara_status_t kara_q4_attention(const kara_params_t* p, int32_t n, const int32_t
   st = make_geom(p, n, &a.g);
   if (st != KARA_OK) return st;
   const Geom& g = a.g;
+  if (!aligned(16, {q, out, need ? workspace : nullptr}) || !aligned(4, {seqs, block_table, seq_lens}) ||
+      !cache_aligned(g, n_layers, k_pools, v_pools, k_scales, v_scales, nullptr))
+    return KARA_ERR_INVALID_ARG;
   a.n = n;
   a.n_layers = n_layers;
   a.T = n_query;

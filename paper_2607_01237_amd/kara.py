@@ -523,7 +523,8 @@ def recompute_queries(p, m: KaraModel, trig, weights, hidden_in, hidden_out, k_p
 
 # ---- the operators of include/kara_q4.h and include/kara_evict.h.  Their calls are
 # made once per layer group and step, from a few microseconds on: each tensor is
-# looked at once, and a call's pool pointers share one array.
+# looked at once, and a call's pool pointers share one array.  (The library looks at
+# the pointers' alignment: here it took 1 to 2 us a call.)
 
 def _launch(stream):
     """(torch, current device, the stream's handle); the stream must be of that

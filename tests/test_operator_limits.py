@@ -1,8 +1,10 @@
 """Limits of the operators of include/kara_q4.h and include/kara_evict.h, without a GPU."""
 import ctypes
 
+import pytest
+
 from paper_2607_01237_amd import kara
-from test_abi_operators import UNSUPPORTED, call, lib, params  # noqa: F401
+from test_abi_operators import CALLS, FAKE, INVALID, UNSUPPORTED, call, lib, params  # noqa: F401
 
 
 def test_most_tokens_that_a_cut_keeps(lib):  # noqa: F811
@@ -12,3 +14,32 @@ def test_most_tokens_that_a_cut_keeps(lib):  # noqa: F811
         assert lib.kara_evict_workspace_size(ctypes.byref(params()), 1, 1, keep, ctypes.byref(out)) == UNSUPPORTED
         assert call(lib, "kara_evict_tokens", keep=keep) == UNSUPPORTED
     assert kara.evict_workspace_size(params(), 1, 1, 2 ** 30) >= 8 * 4 * 2 ** 30
+
+
+WIDE = {"k_new", "v_new", "q", "k_out", "v_out", "out", "workspace"}
+
+
+def pools_at(address):
+    a = (ctypes.c_void_p * 2)(FAKE, address)
+    return a, ctypes.addressof(a)
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_unaligned_arrays_are_refused(lib, name):  # noqa: F811
+    scales = pools_at(FAKE + 4), pools_at(FAKE + 2)      # of rows of 128: 4 bytes each
+    change = {}
+    if "k_scales" in dict(CALLS[name]):
+        change = {x: scales[0][1] for x in ("k_scales", "v_scales") if x in dict(CALLS[name])}
+    for key, good in CALLS[name]:
+        if key in WIDE:
+            assert call(lib, name, **{key: FAKE + 8}, **change) == INVALID, key
+        elif good == FAKE or key == "kept":
+            assert call(lib, name, **{key: FAKE + 2}, **change) == INVALID, key
+        elif key in ("k_pools", "v_pools", "weights"):
+            held, at = pools_at(FAKE + 8)
+            assert call(lib, name, **{key: at}, **change) == INVALID, key
+        elif key.endswith("_scales"):
+            assert call(lib, name, **dict(change, **{key: scales[1][1]})) == INVALID, key
+    if "weights" in dict(CALLS[name]):                   # pages of three tokens: accumulators one at a time
+        held, at = pools_at(FAKE + 2)
+        assert call(lib, name, params(block_size=3, max_blocks_per_seq=400), weights=at) == INVALID
