@@ -575,8 +575,9 @@ def _pool_args(dev, L, pools):
     return ptrs, [None if x is None else base + x for x in at]
 
 
-def _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights=None, values=True):
-    """Pool arguments of a cache of rows (no scales) or of 4-bit codes."""
+def _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights=(), values=True):
+    """Pool arguments of a cache of rows (no scales) or of 4-bit codes, and of
+    accumulators where the call takes them."""
     rows = p.num_pages * p.n_kv_heads * p.block_size
     d = p.head_dim
     if values and (k_scales is None) != (v_scales is None):
@@ -591,7 +592,9 @@ def _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights=
     pools.append(("k_scales", k_scales, rows * d // 32, torch.uint8))
     if values:
         pools.append(("v_scales", v_scales, rows * d // 32, torch.uint8))
-    if weights is not None:
+    if weights is None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "weights: missing")
+    if weights != ():
         pools.append(("weights", weights, rows, torch.float32))
     return _pool_args(dev, L, pools)
 

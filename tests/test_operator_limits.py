@@ -43,3 +43,12 @@ def test_unaligned_arrays_are_refused(lib, name):  # noqa: F811
     if "weights" in dict(CALLS[name]):                   # pages of three tokens: accumulators one at a time
         held, at = pools_at(FAKE + 2)
         assert call(lib, name, params(block_size=3, max_blocks_per_seq=400), weights=at) == INVALID
+
+
+def test_binding_refuses_missing_accumulators():
+    torch = pytest.importorskip("torch")
+    x = [torch.zeros(8 * 16 * 128, dtype=torch.bfloat16)]
+    for values in (True, False):
+        with pytest.raises(kara.KaraError, match="weights: missing"):
+            kara._cache_args(torch, -1, params(num_pages=1), 1, x, x, None, None, None, values=values)
+    assert len(kara._cache_args(torch, -1, params(num_pages=1), 1, x, x, None, None)[1]) == 4
