@@ -575,7 +575,10 @@ def _pool_args(dev, L, pools):
     return ptrs, [None if x is None else base + x for x in at]
 
 
-def _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights=(), values=True):
+_NONE_TAKEN = object()     # for calls without accumulators: None is a missing argument
+
+
+def _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights=_NONE_TAKEN, values=True):
     """Pool arguments of a cache of rows (no scales) or of 4-bit codes, and of
     accumulators where the call takes them."""
     rows = p.num_pages * p.n_kv_heads * p.block_size
@@ -594,7 +597,7 @@ def _cache_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales, weights=
         pools.append(("v_scales", v_scales, rows * d // 32, torch.uint8))
     if weights is None:
         raise KaraError("marshal", ERR_INVALID_ARG, "weights: missing")
-    if weights != ():
+    if weights is not _NONE_TAKEN:
         pools.append(("weights", weights, rows, torch.float32))
     return _pool_args(dev, L, pools)
 

@@ -52,3 +52,10 @@ def test_binding_refuses_missing_accumulators():
         with pytest.raises(kara.KaraError, match="weights: missing"):
             kara._cache_args(torch, -1, params(num_pages=1), 1, x, x, None, None, None, values=values)
     assert len(kara._cache_args(torch, -1, params(num_pages=1), 1, x, x, None, None)[1]) == 4
+
+
+def test_binding_takes_layers_of_one_tensor():
+    torch = pytest.importorskip("torch")
+    rows, w = torch.zeros((2, 8 * 16 * 128), dtype=torch.bfloat16), torch.zeros((2, 8 * 16))
+    held, at = kara._cache_args(torch, -1, params(num_pages=1), 2, rows, rows, None, None, w)
+    assert list(held) == [t.data_ptr() for x in (rows, rows, w) for t in x]
