@@ -13,6 +13,14 @@
  * puts it.  Those of the n_new newest positions of a sequence start from zero in
  * the call that first counts them, so pages need no clearing.
  *
+ * Every page below the seq_len of a sequence that a call lists must be that
+ * sequence's alone among the listed ones (not checked): accumulators are added to
+ * without atomics, in one order, so that results are the same bits every time, and
+ * two sequences at one page would lose weights.  Sequences that share a prefix are
+ * listed in calls of their own, one after the other; their weights then add up in
+ * the shared accumulators, n_new counting each one's own positions.  Before
+ * kara_evict_tokens, which moves rows, a page belongs to one sequence of all.
+ *
  * The cache is either rows of p->dtype (kara.h; k_scales and v_scales NULL) or
  * held in 4 bits (kara_q4.h; both given, p->dtype the type of q).
  *
@@ -52,8 +60,9 @@ kara_status_t kara_evict_attention_workspace_size(const kara_params_t* p, int32_
  * sequence listed more than once is counted once, by its first listing.  Longer
  * sequences than max_len, empty ones and indices outside [0, n_seqs) give zero
  * output rows and leave their accumulators alone.  The block table must map
- * every position below seq_len; where it does not, the sequence's output is
- * unspecified, and nothing outside the pools is read or written.
+ * every position below seq_len, to pages of no other listed sequence; a position on
+ * no page leaves the sequence's output unspecified, and nothing outside the pools is
+ * read or written.
  */
 kara_status_t kara_evict_attention(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,
                                    const void* q, const void* const* k_pools, const void* const* v_pools,
@@ -74,8 +83,8 @@ kara_status_t kara_evict_observe_workspace_size(const kara_params_t* p, int32_t 
  * q: [n_layers][n][n_query][n_q_heads][head_dim] (p->dtype).  The last n_new
  * positions are set, those before are added to (n_new = n_query for a prompt just
  * appended, n_new >= seq_len for all).  Queries before the sequence's start
- * (n_query > seq_len) do not count.  Listings, lengths and pages as in
- * kara_evict_attention.
+ * (n_query > seq_len) do not count.  Listings, lengths and pages, one sequence's
+ * alone, as in kara_evict_attention.
  */
 kara_status_t kara_evict_observe(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,
                                  int32_t n_query, const void* q, const void* const* k_pools,

@@ -49,7 +49,8 @@ extern "C" {
  * one of n_layers layers, quantised: row of token i, KV head h, layer l from
  * k_new / v_new [n_layers][n][n_new][n_kv_heads][head_dim] (p->dtype) to logical
  * position seq_lens[s] + i of sequence s = seqs[j].  Then seq_lens[s] += n_new.
- * The caller maps the blocks covering the new positions beforehand.  status[j]
+ * The caller maps the blocks covering the new positions beforehand, to pages that
+ * no other sequence maps.  status[j]
  * as in kara_harness_kv_append (BAD_INDEX, DUP_TRIGGER, BAD_WINDOW, BAD_PAGE;
  * such sequences are not written), or KARA_SEQ_NONFINITE.
  */

@@ -688,7 +688,8 @@ def evict_attention_workspace_size(p, n, n_layers, max_len) -> int:
 def evict_attention(p, seqs, q, k_pools, v_pools, weights, block_table, seq_lens, n_new, max_len, out, workspace,
                     k_scales=None, v_scales=None, stream=None):
     """decode_attention that adds every key's weight to its accumulator (weights:
-    fp32 [num_pages][Hkv][block_size] per layer); fp32 out of q's shape."""
+    fp32 [num_pages][Hkv][block_size] per layer); fp32 out of q's shape.  Listed
+    sequences share no pages (those of a shared prefix: a call each)."""
     lib = load()
     torch, dev, s = _launch(stream)
     n, L = seqs.numel(), len(k_pools)
@@ -708,7 +709,8 @@ def evict_observe_workspace_size(p, n, n_layers, n_query, max_len) -> int:
 def evict_observe(p, seqs, n_query, q, k_pools, weights, block_table, seq_lens, n_new, max_len, workspace, k_scales=None,
                   stream=None):
     """Adds the weights that each listed sequence's last n_query tokens give
-    (q [n_layers][n][n_query][Hq][d]) to the accumulators."""
+    (q [n_layers][n][n_query][Hq][d]) to the accumulators.  Listed sequences share
+    no pages (those of a shared prefix: a call each)."""
     lib = load()
     torch, dev, s = _launch(stream)
     n, L, n_query = seqs.numel(), len(k_pools), int(n_query)
