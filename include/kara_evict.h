@@ -14,9 +14,9 @@
  * the call that first counts them, so pages need no clearing.
  *
  * Every page below the seq_len of a sequence that a call lists must be that
- * sequence's alone among the listed ones (not checked): accumulators are added to
- * without atomics, in one order, so that results are the same bits every time, and
- * two sequences at one page would lose weights.  Sequences that share a prefix are
+ * sequence's alone among the listed ones, and in its table once (not checked):
+ * accumulators are added to without atomics, in one order, so that results are the
+ * same bits every time, and two sequences at one page would lose weights.  Sequences that share a prefix are
  * listed in calls of their own, one after the other; their weights then add up in
  * the shared accumulators, n_new counting each one's own positions.  Before
  * kara_evict_tokens, which moves rows, a page belongs to one sequence of all.
@@ -28,13 +28,12 @@
  * logit of -inf is a weight of 0, one of +inf or NaN makes the weights that its
  * query gives NaN.  A query whose every logit is -inf gives no weights.
  *
- * Conventions
- * are those of kara.h and kara_harness.h: device pointers unless stated (pool
- * arrays: host arrays of n_layers device pointers, 1 <= n_layers <= 64), the
- * caller owns all memory, nothing synchronises or allocates, host-checkable
- * argument errors come back as KARA_ERR_* with nothing enqueued.  The
- * window-related fields of p must be valid but are not used.  max_len and keep are
- * 2^30 at most.  Alignment, checked: that of kara_q4.h, rows 16 bytes, accumulators
+ * Conventions are those of kara.h and kara_harness.h: device pointers unless
+ * stated (pool arrays: host arrays of n_layers device pointers, 1 <= n_layers <=
+ * 64), the caller owns all memory, nothing synchronises or allocates,
+ * host-checkable argument errors come back as KARA_ERR_* with nothing enqueued.
+ * The window-related fields of p must be valid but are not used.  max_len and keep
+ * are 2^30 at most.  Alignment, checked: that of kara_q4.h, rows 16 bytes, accumulators
  * 16 where block_size is a multiple of 4, else 4.
  */
 #ifndef KARA_EVICT_H
@@ -47,7 +46,11 @@ extern "C" {
 #endif
 
 /* Bytes of device workspace kara_evict_attention needs for n sequences of at most
- * max_len tokens and n_layers layers (written to *bytes, a HOST pointer). */
+ * max_len tokens and n_layers layers (written to *bytes, a HOST pointer); it is
+ * enough for fewer and shorter ones.  Every logit of the call passes through it: 4
+ * bytes a layer, sequence, query head and key, and a record of head_dim + 2 fp32 per
+ * 256 keys (64 sequences of 32K tokens, 40 heads: 0.5 GB a layer).  A program with
+ * many layers passes them in groups of a few, which share one workspace. */
 kara_status_t kara_evict_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers,
                                                   int32_t max_len, size_t* bytes);
 
@@ -56,8 +59,8 @@ kara_status_t kara_evict_attention_workspace_size(const kara_params_t* p, int32_
  * over the whole cache, G <= KARA_HARNESS_MAX_GROUP; out fp32) that also adds
  * each key's weight, summed over the group's query heads, to its accumulator:
  * positions below seq_len - n_new are added to, the last n_new are set.  The output
- * row of a query that gives no weights is zero.  A
- * sequence listed more than once is counted once, by its first listing.  Longer
+ * row of a query that gives no weights is zero.  A sequence listed more than once is
+ * counted once, by its first listing.  Longer
  * sequences than max_len, empty ones and indices outside [0, n_seqs) give zero
  * output rows and leave their accumulators alone.  The block table must map
  * every position below seq_len, to pages of no other listed sequence; a position on

@@ -74,8 +74,12 @@ kara_status_t kara_q4_read(const kara_params_t* p, int32_t n, const int32_t* seq
 
 /*
  * Bytes of device workspace kara_q4_attention needs for n sequences of at most
- * max_len tokens (2^30 at most), n_layers layers and n_query queries each (written to *bytes, a
- * HOST pointer).
+ * max_len tokens (2^30 at most), n_layers layers and n_query queries each (written
+ * to *bytes, a HOST pointer).  It is enough for fewer sequences and layers and for
+ * shorter ones, not for fewer queries: few queries split their keys further, so a
+ * decoding step may need more than a prompt's chunk (100 sequences of 32000 tokens,
+ * 32/8 heads, one layer: 208 MB for one query, 34 for 300).  A workspace for calls
+ * of several n_query is the largest of their sizes.
  */
 kara_status_t kara_q4_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers,
                                                int32_t n_query, int32_t max_len, size_t* bytes);

@@ -659,6 +659,8 @@ def q4_read(p, seqs, start, n_rows, k_pools, v_pools, k_scales, v_scales, block_
 
 
 def q4_attention_workspace_size(p, n, n_layers, n_query, max_len) -> int:
+    """Of calls with this n_query and up to n sequences, n_layers layers and max_len
+    tokens; fewer queries may need more."""
     return _size("kara_q4_attention_workspace_size", ctypes.byref(p), n, n_layers, n_query, max_len)
 
 
@@ -682,6 +684,7 @@ def q4_attention(p, seqs, n_query, q, k_pools, v_pools, k_scales, v_scales, bloc
 # ---- eviction by accumulated attention weight (include/kara_evict.h)
 
 def evict_attention_workspace_size(p, n, n_layers, max_len) -> int:
+    """4 bytes a layer, sequence, query head and key, and a quarter to a half of that for records."""
     return _size("kara_evict_attention_workspace_size", ctypes.byref(p), n, n_layers, max_len)
 
 

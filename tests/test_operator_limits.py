@@ -59,3 +59,15 @@ def test_binding_takes_layers_of_one_tensor():
     rows, w = torch.zeros((2, 8 * 16 * 128), dtype=torch.bfloat16), torch.zeros((2, 8 * 16))
     held, at = kara._cache_args(torch, -1, params(num_pages=1), 2, rows, rows, None, None, w)
     assert list(held) == [t.data_ptr() for x in (rows, rows, w) for t in x]
+
+
+def test_workspace_sizes_the_headers_name(lib):  # noqa: F811
+    # one for each n_query: a decoding step over many sequences needs more than a chunk of a prompt
+    p = params(max_blocks_per_seq=2000)
+    step, chunk = (kara.q4_attention_workspace_size(p, 100, 1, t, 32000) for t in (1, 300))
+    assert step == 100 * 32 * 125 * 130 * 4 and 33e6 < chunk < 35e6
+    args = dict(n=8, n_layers=1, max_len=32000)
+    small = kara.q4_attention_workspace_size(p, 8, 1, 300, 32000) // 4
+    assert call(lib, "kara_q4_attention", p, n_query=1, bytes=small, **args) == kara.ERR_WORKSPACE
+    few = params(max_blocks_per_seq=2048, n_q_heads=40)
+    assert 0.50e9 < kara.evict_attention_workspace_size(few, 64, 1, 32768) < 0.51e9
