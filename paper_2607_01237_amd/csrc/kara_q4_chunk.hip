@@ -11,7 +11,10 @@
 // attention: S^T = K Q^T, weights as they stand the B operand of O^T += V^T P^T with
 // V through the transposed LDS read, the row sums one more product with ones.
 //
-// NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones).
+// NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones).  bf16 calls
+// so round a weight, in the output as in its sum, to bf16: 1.74e-3 of the result against
+// 64 bits (4 x 512 queries over 2.5-8.7K) where whole weights give 1.61e-3, mostly the
+// output's own rounding; a second term would double V's products.
 //
 // 16 sequences x 1024 queries over 2.5-8.7K cached, 32/8 heads, bf16: 1320 us, 1035
 // TFLOP/s; fp32, 8 x 512: 894 us, 400 TFLOP/s of three products for each.
