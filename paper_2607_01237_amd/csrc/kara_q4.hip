@@ -19,20 +19,23 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------- append
 
-// One workgroup per listed sequence: its status and, if it has nothing but
-// KARA_SEQ_OK, its new length.  The rows follow in a second launch, which
-// counts back from that length.
-__global__ __launch_bounds__(kAppendThreads) void q4_commit_kernel(Geom g, int n, const int32_t* __restrict__ seqs,
-                                                                   int n_new, const int32_t* __restrict__ bt,
+// One workgroup per listed sequence: its status.
+__global__ __launch_bounds__(kAppendThreads) void q4_check_kernel(Geom g, int n, const int32_t* __restrict__ seqs,
+                                                                  int n_new, const int32_t* __restrict__ bt,
+                                                                  const int32_t* __restrict__ seq_lens,
+                                                                  int32_t* __restrict__ status) {
+  const int st = append_status(g, n, seqs, n_new, bt, seq_lens, blockIdx.x);
+  if (threadIdx.x == 0) status[blockIdx.x] = st;
+}
+
+// A thread per listed sequence: its new length, once the rows are there (committed
+// first, and counted back from by the rows' launch, a call that could not make that
+// launch left lengths without rows; 3.5 us less).
+__global__ __launch_bounds__(kAppendThreads) void q4_commit_kernel(int n, const int32_t* __restrict__ seqs, int n_new,
                                                                    int32_t* __restrict__ seq_lens,
-                                                                   int32_t* __restrict__ status) {
-  const int j = blockIdx.x;
-  const int st = append_status(g, n, seqs, n_new, bt, seq_lens, j);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    status[j] = st;
-    if (st == KARA_SEQ_OK) seq_lens[seqs[j]] += n_new;
-  }
+                                                                   const int32_t* __restrict__ status) {
+  const int j = blockIdx.x * kAppendThreads + threadIdx.x;
+  if (j < n && (status[j] & ~KARA_SEQ_NONFINITE) == 0) seq_lens[seqs[j]] += n_new;
 }
 
 constexpr int kQuantUnroll = 4;       // octets per thread
@@ -122,7 +125,7 @@ __device__ __forceinline__ void q4_store(uint8_t* codes, uint8_t* scales, int64_
   if ((o & 3) == 0) scales[row * (D / kQ4Block) + (o >> 2)] = (uint8_t)byte;
 }
 
-// The rows after q4_commit_kernel.  Grid as the append of rows: (sequences x token
+// The rows between q4_check_kernel and q4_commit_kernel.  Grid as the append of rows: (sequences x token
 // chunks, layer, K|V).  Bound by the bytes: 4 x 4 layers of 4000 tokens (332 MB) in 64
 // us, the reading back 51; fp32 (595 MB) 106 and 101 (152 and 153 with each lane's 32
 // bytes loaded as they lie).
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(kAppendThreads) void q4_append_kernel(
   // (other workgroups may have reported a value that is not finite by now)
   if (status[j] & ~KARA_SEQ_NONFINITE) return;
   const int s = seqs[j];
-  const int pos0 = seq_lens[s] - n_new + tok0;
+  const int pos0 = seq_lens[s] + tok0;
   const int32_t* row_pages = bt + (int64_t)s * g.max_blocks;
   uint8_t* codes = (uint8_t*)(kv ? vp.p[l] : kp.p[l]);
   uint8_t* scales = (uint8_t*)(kv ? vsp.p[l] : ksp.p[l]);
@@ -845,8 +848,9 @@ kara_status_t kara_q4_append(const kara_params_t* p, int32_t n, const int32_t* s
     return hip_status(hipGetLastError());
   }
   const dim3 grid((unsigned)(n * chunks), (unsigned)n_layers, 2), block(kAppendThreads);
-  hipLaunchKernelGGL(q4_commit_kernel, dim3((unsigned)n), block, 0, s, g, n, seqs, n_new, block_table, seq_lens, status);
-  const hipError_t e = hipGetLastError();
+  hipLaunchKernelGGL(q4_check_kernel, dim3((unsigned)n), block, 0, s, g, n, seqs, n_new, block_table,
+                     (const int32_t*)seq_lens, status);
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
 #define KARA_Q4_APPEND(DT, D)                                                                                       \
   hipLaunchKernelGGL((q4_append_kernel<DT, D>), grid, block, 0, s, g, n, seqs, n_new, toks, (int)chunks,            \
@@ -860,6 +864,10 @@ kara_status_t kara_q4_append(const kara_params_t* p, int32_t n, const int32_t* s
     else KARA_Q4_APPEND(KARA_F32, 64);
   }
 #undef KARA_Q4_APPEND
+  e = hipGetLastError();
+  if (e != hipSuccess) return hip_status(e);
+  hipLaunchKernelGGL(q4_commit_kernel, dim3(((unsigned)n + kAppendThreads - 1) / kAppendThreads), block, 0, s, n, seqs,
+                     n_new, seq_lens, (const int32_t*)status);
   return hip_status(hipGetLastError());
 }
 
