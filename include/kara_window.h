@@ -1,0 +1,63 @@
+/*
+ * kara_window.h -- causal attention within a sliding window, with the first tokens
+ * of a sequence always visible, over paged rows or 8-bit codes.
+ *
+ * Conventions are those of kara.h and kara_q8.h.
+ */
+#ifndef KARA_WINDOW_H
+#define KARA_WINDOW_H
+
+#include "kara_q8.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * Bytes of device workspace kara_window_attention needs (written to *bytes, a HOST
+ * pointer) for n sequences of at most max_len tokens (2^30 at most), n_layers layers and
+ * n_query queries each; as for kara_q8_attention it is enough for fewer sequences and
+ * layers and for a smaller max_len, not for other values of n_query, window and n_sink,
+ * nor of p.
+ */
+kara_status_t kara_window_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers,
+                                                   int32_t n_query, int32_t window, int32_t n_sink,
+                                                   int32_t max_len, size_t* bytes);
+
+/*
+ * Attention of the last n_query tokens of each listed sequence: query t of sequence s
+ * = seqs[j], at position i = seq_lens[s] - n_query + t, sees the keys
+ *   k <= i  with  k > i - window  or  k < n_sink
+ * (itself, the window - 1 before it and the first n_sink; window = 0: all up to i) and
+ * gives out[l][j][t][hq][:] = sum_k w_k V_k, w = softmax over them of scale * q . K_k,
+ * KV head hq / G.  q, out: [n_layers][n][n_query][n_q_heads][head_dim] (p->dtype).
+ *
+ * The cache is rows of p->dtype (kara.h; k_scales and v_scales NULL) or held in 8 bits
+ * (both given).  Keys and values that a query does not see do not reach its result,
+ * whatever they hold.  Blocks of which no query sees a token are not needed: their
+ * entries of the block table may be -1 or name pages that others own by now, so that a
+ * program may take back the pages between the first tokens and the window.  Visible
+ * positions must be mapped to pages of the pool; where they are not, the sequence's
+ * output is unspecified, and nothing outside the pools is read.
+ *
+ * Rows before the sequence's start (n_query > seq_len), sequences longer than max_len,
+ * sequence indices outside [0, n_seqs) and queries whose every visible logit is -inf
+ * give zeros; a visible logit of +inf or NaN gives NaN, and a visible infinite or NaN
+ * value enters the sum as it is.  Softmax statistics and sums are fp32; bf16 calls
+ * round each weight to bf16 before it meets V (the same rounded weights make up its
+ * sum), fp32 calls keep it whole.  Results are the same bits from call to call;
+ * they may differ in the last ones with n, n_layers, n_query and max_len, which decide
+ * how keys are split.
+ */
+kara_status_t kara_window_attention(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,
+                                    int32_t n_query, int32_t window, int32_t n_sink, const void* q,
+                                    const void* const* k_pools, const void* const* v_pools,
+                                    const void* const* k_scales, const void* const* v_scales,
+                                    const int32_t* block_table, const int32_t* seq_lens, int32_t max_len, void* out,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* KARA_WINDOW_H */

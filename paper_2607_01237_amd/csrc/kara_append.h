@@ -1,5 +1,6 @@
 // The check of a listed sequence before tokens are appended to it, shared by
-// the appends of rows (kara_harness.hip) and of 4-bit codes (kara_q4.hip).
+// the appends of rows (kara_harness.hip), of 4-bit codes (kara_q4.hip) and with a
+// rotation or into 8 bits (kara_store.hip).
 #pragma once
 
 #include "kara_internal.h"
@@ -10,14 +11,14 @@ namespace {
 constexpr int kAppendThreads = 256;
 
 // Status of listed sequence j, by all threads of a workgroup; the same value
-// in each.
+// in each.  counted: seq_lens holds the new tokens already.
 __device__ inline int append_status(const Geom& g, int n, const int32_t* __restrict__ seqs, int n_new,
-                             const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens, int j) {
+                             const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens, int j, bool counted = false) {
   const int s = seqs[j];
   if (s < 0 || s >= g.n_seqs) return KARA_SEQ_BAD_INDEX;
   int dup = 0;
   for (int o = threadIdx.x; o < n; o += kAppendThreads) dup |= o != j && seqs[o] == s;
-  const int64_t len = seq_lens[s];
+  const int64_t len = (int64_t)seq_lens[s] - (counted ? n_new : 0);
   const int64_t new_len = len + n_new;
   const bool fits = len >= 0 && new_len <= (int64_t)g.max_blocks * g.bs;
   int bad = 0;

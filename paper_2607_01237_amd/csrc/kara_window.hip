@@ -1,0 +1,741 @@
+// Attention within a sliding window and the first tokens (include/kara_window.h) of few
+// query rows, with the keys split over workgroups, and over rows of fp32; the 8-bit
+// cache's attention (include/kara_q8.h), which is the same without a window.
+#include <algorithm>
+#include <type_traits>
+
+#include "kara_q8_device.h"
+#include "kara_window.h"
+#include "kara_window_call.h"
+
+namespace kara {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegInf = -__builtin_huge_valf();
+// Lower end of a running maximum: finite, so that a logit of -inf weighs 0.
+constexpr float kMaxFloor = -3.402823466e38f;
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kSplitMin = 256;       // keys per split, at least (the workspace's records are sized for that)
+constexpr int kSplitMax = 2048;
+constexpr int kSplitRuns = 1024;     // runs of keys a split's LDS table holds
+constexpr int kWgTarget = 4096;      // workgroups a launch keeps when its splits grow
+constexpr int kTileRows = 16;
+
+enum Cache { kRowsBf16, kRowsF32, kCodes };
+
+template <Cache CT, int D>
+struct WinCfg {
+  static constexpr int kTB = CT == kRowsF32 ? 1 : 2;               // tiles of 16 keys per block
+  static constexpr int kBlock = 16 * kTB;
+  static constexpr int kRow = D * (CT == kRowsF32 ? 4 : CT == kRowsBf16 ? 2 : 1);
+  static constexpr int kKC = kRow / 64;                            // 16-byte pieces of a key in a lane
+  static constexpr int kE = D / 16;                                // columns of a lane
+  static constexpr int kVB = kRow / 16;                            // bytes of a value row in a lane
+  static constexpr int kVW = kVB / 4;
+};
+
+// One workgroup of four waves per (layer, sequence, KV head, tile of 16 query rows, split
+// of split_keys keys of the tile's span): for the tile's rows, the split's maximum m,
+// exponential sum l and unnormalised output o, in log2 units and fp32.  Rows of a (layer,
+// sequence, KV head) run over (query, head in group).
+//
+// The pool rows of the split's keys go to LDS first; the four waves then take its blocks
+// of 32 keys (16 of fp32) in turn, each with the next block on its way into registers
+// while it works on the present one, straight from the pages in the layout of the matrix
+// operands: S^T = K Q^T with a lane's pieces of one key as they lie (the query's pieces
+// are taken the same way), and V as rows, d/16 columns of a key per lane.  A lane so holds
+// four keys of one query per tile, and its weights are the B operand of O^T += V^T P^T as
+// they stand; of 16-bit values, pairs of columns are put together to pairs of keys by
+// byte permutes.
+//
+// Rows of fp32 go through the fp32 matrix instructions.  NT: bf16 terms of a query and of
+// a weight over codes (3 where p->dtype is fp32: 24 bits; codes are exact in one).
+template <Cache CT, int NT, int D>
+__global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a) {
+  using C = WinCfg<CT, D>;
+  constexpr int TB = C::kTB, KC = C::kKC, E = C::kE, VW = C::kVW;
+  constexpr bool F32 = CT == kRowsF32;
+  constexpr bool kOutBf16 = !F32 && NT == 1;
+  constexpr int KS = D / 32;                       // bf16 products per dot product
+  struct Table {
+    uint32_t row[kSplitRuns];                      // pool rows of runs of keys
+    uint32_t scale[CT == kCodes ? kSplitRuns : 1]; // K's scale byte, V's above it
+  };
+  __shared__ __attribute__((aligned(16))) union {
+    Table t;
+    float o[kWaves][16][D];
+  } lds;
+  __shared__ float red_m[kWaves][16], red_l[kWaves][16];
+  Table& tab = lds.t;
+
+  const Geom& g = a.g;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int gq = lane >> 4, li = lane & 15;
+  uint32_t rest = blockIdx.x;
+  // (blocks go round the 8 XCDs: the splits of eight units in a row fall to the same ones,
+  // those of the next eight are shifted, so that no XCD gets all the short last ones)
+  const uint32_t unit8 = rest / ((uint32_t)a.n_splits * 8);
+  const int split = (rest + unit8) % (uint32_t)a.n_splits;
+  rest /= (uint32_t)a.n_splits;
+  const int rt = rest % (uint32_t)a.n_rt;
+  rest /= (uint32_t)a.n_rt;
+  const int h = rest % (uint32_t)g.Hkv;
+  rest /= (uint32_t)g.Hkv;
+  const int j = rest % (uint32_t)a.n;
+  const int l = rest / (uint32_t)a.n;
+  const int s = a.seqs[j];
+  const int G = g.G, T = a.T, R = G * T;
+  const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
+  // row r of the unit: output row orow + (r / G) * Hq + r % G
+  const int64_t orow = ((int64_t)l * a.n + j) * T * g.Hq + h * G;
+  const int row0 = rt * kTileRows;
+  const int rows = min(kTileRows, R - row0);
+  const bool none = len <= 0 || len > a.max_len;
+  const Span sp = span_of(none ? 0 : len, T, G, row0, row0 + rows, a.window, a.sink);
+  const int k0 = split * a.split_keys;
+  if (none || k0 >= sp.n) {
+    // no keys: zero rows where no combine kernel follows
+    if (a.n_splits == 1)
+      for (int i = tid; i < rows * D; i += kThreads) {
+        const int r = row0 + i / D;
+        const int64_t at = (orow + (int64_t)(r / G) * g.Hq + r % G) * D + i % D;
+        if constexpr (kOutBf16) ((__bf16*)a.out)[at] = (__bf16)0.f;
+        else ((float*)a.out)[at] = 0.f;
+      }
+    return;
+  }
+  const int nk = min(sp.n - k0, a.split_keys);                // keys of this split
+  const float c = g.scale * kLog2e;
+  const int nblk = (nk + C::kBlock - 1) / C::kBlock;
+
+  // lane (gq, li): its pieces of query row li, and the row's position
+  const bool there = li < rows;
+  int qpos = -1;
+  uint4 qraw[F32 || NT > 1 ? D / 16 : KS];
+  {
+    const int r = row0 + (there ? li : 0);
+    const int t = T == 1 ? 0 : r / G;
+    if (there) qpos = len - T + t;
+    const char* src = (const char*)a.q + (orow + (int64_t)t * g.Hq + (r - t * G)) * D * (kOutBf16 ? 2 : 4);
+    if constexpr (F32) {
+#pragma unroll
+      for (int x = 0; x < KC; ++x) qraw[x] = *(const uint4*)(src + (gq + 4 * x) * 16);
+    } else if constexpr (CT == kRowsBf16) {
+#pragma unroll
+      for (int x = 0; x < KS; ++x) qraw[x] = *(const uint4*)(src + (gq + 4 * x) * 16);
+    } else {
+      // (octet x lies in 16 codes: those of piece x / 2)
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        const int at = (gq + 4 * (x >> 1)) * 16 + (x & 1) * 8;
+        if constexpr (NT == 1) {
+          qraw[x] = *(const uint4*)(src + at * 2);
+        } else {
+          qraw[2 * x] = *(const uint4*)(src + at * 4);
+          qraw[2 * x + 1] = *(const uint4*)(src + at * 4 + 16);
+        }
+      }
+    }
+  }
+  // Pool rows of the split's keys: runs of 2^run keys lie in one page, an entry each.
+  // (Keys that no row sees may be on no page: any row of the pool stands for them.)
+  const int run = a.run;
+  {
+    const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
+    for (int i = tid; i < (nblk * C::kBlock) >> run; i += kThreads) {
+      const int pos = sp.position(k0 + min(i << run, (nk - 1) >> run << run));
+      const int b = pos / g.bs;
+      const int page = min(max(row_pages[b], 0), g.num_pages - 1);
+      const uint32_t unit = (uint32_t)page * (uint32_t)g.Hkv + (uint32_t)h;
+      tab.row[i] = unit * (uint32_t)g.bs + (uint32_t)(pos - b * g.bs);
+      if constexpr (CT == kCodes)
+        tab.scale[i] = (uint32_t)((const uint8_t*)a.ksp.p[l])[unit] | (uint32_t)((const uint8_t*)a.vsp.p[l])[unit] << 16;
+    }
+  }
+  bf16x8 qa[F32 ? 1 : NT][KS];
+  if constexpr (!F32) {
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      if constexpr (NT == 1) {
+        qa[0][x] = __builtin_bit_cast(bf16x8, there ? qraw[x] : uint4{0, 0, 0, 0});
+      } else {
+        const floatx4 u = __builtin_bit_cast(floatx4, qraw[2 * x]), v = __builtin_bit_cast(floatx4, qraw[2 * x + 1]);
+        uint32_t w[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x0 = i < 2 ? u[2 * i] : v[2 * i - 4], x1 = i < 2 ? u[2 * i + 1] : v[2 * i - 3];
+          bf16_term_pairs<true>(there ? x0 : 0.f, there ? x1 : 0.f, w[i]);
+        }
+#pragma unroll
+        for (int y = 0; y < NT; ++y) qa[y][x] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
+      }
+    }
+  } else {
+#pragma unroll
+    for (int x = 0; x < KC; ++x) qraw[x] = there ? qraw[x] : uint4{0, 0, 0, 0};
+  }
+  __syncthreads();
+
+  const char* kbase = (const char*)a.kp.p[l] + gq * 16;
+  const char* vbase = (const char*)a.vp.p[l] + li * (C::kVB < 16 ? C::kVB : 16);
+  const int run_mask = (1 << run) - 1;
+  // (padding keys past the last one repeat it)
+  auto row_of = [&](int key) __attribute__((always_inline)) {
+    key = min(key, nk - 1);
+    return tab.row[key >> run] + (uint32_t)(key & run_mask);
+  };
+  auto scale_of = [&](int key) __attribute__((always_inline)) { return tab.scale[min(key, nk - 1) >> run]; };
+  uint4 kb[2][TB][KC];
+  uint32_t vb[2][TB][4][VW];
+  auto load = [&](int blk, int b) __attribute__((always_inline)) {
+    uint64_t kat[TB], vat[TB][4];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      kat[t] = (uint64_t)row_of(blk * C::kBlock + t * 16 + li) * C::kRow;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) vat[t][r] = (uint64_t)row_of(blk * C::kBlock + t * 16 + 4 * gq + r) * C::kRow;
+    }
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int x = 0; x < KC; ++x) kb[b][t][x] = *(const uint4*)(kbase + kat[t] + x * 64);
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const char* src = vbase + vat[t][r];
+        if constexpr (VW == 1) {
+          vb[b][t][r][0] = *(const uint32_t*)src;
+        } else if constexpr (VW == 2) {
+          const uint2 v = *(const uint2*)src;
+          vb[b][t][r][0] = v.x, vb[b][t][r][1] = v.y;
+        } else {
+          // (fp32 at d = 128: columns 4li.. and 64 + 4li..)
+#pragma unroll
+          for (int y = 0; y < VW / 4; ++y) {
+            const uint4 v = *(const uint4*)(src + y * 256);
+            vb[b][t][r][4 * y] = v.x, vb[b][t][r][4 * y + 1] = v.y, vb[b][t][r][4 * y + 2] = v.z, vb[b][t][r][4 * y + 3] = v.w;
+          }
+        }
+      }
+  };
+
+  float m = kMaxFloor, lsum = 0.f;   // query li's reference, and this lane's part of its sum
+  floatx4 lones = {0.f, 0.f, 0.f, 0.f};   // bf16: the sum, in every element
+  floatx4 o[E];                      // query li, column e of lanes 4gq + r
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  bf16x8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
+
+  // keys from `all_lo` to `all_hi` are seen by every row of the tile (sinks are not counted)
+  const int all_lo = sp.i1 - a.window < 0 ? 0 : sp.i1 - a.window + 1 - sp.gap;
+  const int all_hi = sp.i0 - sp.gap;
+  auto sees = [&](int p, int i) __attribute__((always_inline)) { return p <= i && (p > i - a.window || p < a.sink); };
+  // seen by some row
+  auto seen = [&](int p) __attribute__((always_inline)) { return p <= sp.i1 && (p > sp.i0 - a.window || p < a.sink); };
+
+  auto work = [&](int blk, int b) __attribute__((always_inline)) {
+    floatx4 sv[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (F32) {
+#pragma unroll
+        for (int x = 0; x < KC; ++x) {
+          const floatx4 ka = __builtin_bit_cast(floatx4, kb[b][t][x]), qx = __builtin_bit_cast(floatx4, qraw[x]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[i], qx[i], acc, 0, 0, 0);
+        }
+      } else {
+        float scale = 0.f;
+        if constexpr (CT == kCodes) scale = q8_scale(scale_of(blk * C::kBlock + t * 16 + li) & 255);
+#pragma unroll
+        for (int x = 0; x < KS; ++x) {
+          bf16x8 ka;
+          if constexpr (CT == kCodes) {
+            const uint4 w = kb[b][t][x >> 1];
+            ka = x & 1 ? q8_octet(w.z, w.w, scale) : q8_octet(w.x, w.y, scale);
+          } else {
+            ka = __builtin_bit_cast(bf16x8, kb[b][t][x]);
+          }
+#pragma unroll
+          for (int y = NT - 1; y >= 0; --y) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qa[y][x], acc, 0, 0, 0);
+        }
+      }
+      sv[t] = acc;
+    }
+    // Wait states between the last product and the first read of its result, which lies
+    // past a branch: the compiler does not count across it.
+#pragma unroll
+    for (int t = 0; t < TB; ++t) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[t]));
+    // values as the second products take them: of 16 bits, pairs of columns
+    constexpr int VP = F32 ? E : E / 2;
+    uint32_t pv[TB * 4][VP];
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (CT == kCodes) {
+          const float scale = q8_scale(scale_of(blk * C::kBlock + t * 16 + 4 * gq + r) >> 16);
+#pragma unroll
+          for (int y = 0; y < VW; ++y) {
+            pv[4 * t + r][2 * y] = q8_pair<false>(vb[b][t][r][y], scale);
+            pv[4 * t + r][2 * y + 1] = q8_pair<true>(vb[b][t][r][y], scale);
+          }
+        } else {
+#pragma unroll
+          for (int y = 0; y < VP; ++y) pv[4 * t + r][y] = vb[b][t][r][y];
+        }
+      }
+    const int v0 = k0 + blk * C::kBlock;
+    bool odd_values = false;
+    const bool masked = v0 < all_lo || v0 + C::kBlock - 1 > all_hi;
+    if (masked) {
+#pragma unroll
+      for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int p = sp.position(v0 + t * 16 + 4 * gq + r);
+          if (!sees(p, qpos)) sv[t][r] = kNegInf;
+          // what no row sees may be anything: its weights are 0, its values must be finite
+          if (!seen(p))
+#pragma unroll
+            for (int y = 0; y < VP; ++y) pv[4 * t + r][y] = 0;
+        }
+      if constexpr (CT != kCodes) {
+        // what some rows see and others do not must not reach those either
+        if (sp.i0 != sp.i1) {
+          uint32_t hit = 0;
+#pragma unroll
+          for (int i = 0; i < TB * 4; ++i)
+#pragma unroll
+            for (int y = 0; y < VP; ++y) {
+              if constexpr (F32) hit |= (pv[i][y] & 0x7fffffffu) >= 0x7f800000u;
+              else hit |= ((pv[i][y] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+            }
+          odd_values = __ballot(hit != 0) != 0ull;
+          if (odd_values) {
+#pragma unroll
+            for (int i = 0; i < TB * 4; ++i)
+#pragma unroll
+              for (int y = 0; y < VP; ++y) {
+                if constexpr (F32) {
+                  if ((pv[i][y] & 0x7fffffffu) >= 0x7f800000u) pv[i][y] = 0;
+                } else {
+                  if ((pv[i][y] & 0x7f80u) == 0x7f80u) pv[i][y] &= 0xffff0000u;
+                  if ((pv[i][y] & 0x7f800000u) == 0x7f800000u) pv[i][y] &= 0xffffu;
+                }
+              }
+          }
+        }
+      }
+    }
+    float mx = sv[0][0];
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sv[t][r]);
+    // The reference m, one for the four lanes of a query, is raised only where a
+    // logit passes it by more than 2^8: no exchange between lanes before that.
+    if (__ballot(mx * c > m + 8.f) != 0ull) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
+      const float mn = fmaxf(m, mx);
+      const float f = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      lsum *= f;
+      lones *= f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= f;
+    }
+    float p[TB][4];
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[t][r] = __builtin_amdgcn_exp2f(fmaf(sv[t][r], c, -m));
+    if constexpr (F32) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        lsum += p[0][r];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(pv[r][e]), p[0][r], o[e], 0, 0, 0);
+      }
+    } else {
+      uint32_t pw[NT][4];                  // terms of the lane's eight weights, in pairs
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) {
+          if constexpr (NT > 1) lsum += p[t][r] + p[t][r + 1];
+          uint32_t w[NT];
+          bf16_term_pairs<false>(p[t][r], p[t][r + 1], w);
+#pragma unroll
+          for (int y = 0; y < NT; ++y) pw[y][2 * t + (r >> 1)] = w[y];
+        }
+      bf16x8 pb[NT];
+#pragma unroll
+      for (int y = 0; y < NT; ++y) pb[y] = __builtin_bit_cast(bf16x8, uint4{pw[y][0], pw[y][1], pw[y][2], pw[y][3]});
+      // (one term: the sum is of the rounded weights, as the output is, and formed as
+      // one more product, with ones)
+      if constexpr (NT == 1) lones = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[0], lones, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+        const uint4 va = {__builtin_amdgcn_perm(pv[1][e >> 1], pv[0][e >> 1], sel),
+                          __builtin_amdgcn_perm(pv[3][e >> 1], pv[2][e >> 1], sel),
+                          __builtin_amdgcn_perm(pv[5][e >> 1], pv[4][e >> 1], sel),
+                          __builtin_amdgcn_perm(pv[7][e >> 1], pv[6][e >> 1], sel)};
+#pragma unroll
+        for (int y = NT - 1; y >= 0; --y)
+          o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[y], o[e], 0, 0, 0);
+      }
+    }
+    if constexpr (CT != kCodes) {
+      if (odd_values) {
+        // infinite and NaN values, taken out above: added where they are seen (a weight
+        // is positive), key by key, the rows read again
+#pragma unroll
+        for (int e = 0; e < E; ++e) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[e]));
+        for (int key = 0; key < C::kBlock; ++key) {
+          const int pos = sp.position(v0 + key);
+          if (!seen(pos)) continue;
+          const char* row = (const char*)a.vp.p[l] + (uint64_t)row_of(blk * C::kBlock + key) * C::kRow;
+          const bool mine = sees(pos, qpos);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const int col = F32 && E == 8 ? (e >> 2) * 64 + 4 * (4 * gq + r) + (e & 3) : E * (4 * gq + r) + e;
+              uint32_t x;
+              if constexpr (F32) x = ((const uint32_t*)row)[col];
+              else x = (uint32_t)((const uint16_t*)row)[col] << 16;
+              if (mine && (x & 0x7fffffffu) >= 0x7f800000u) o[e][r] += __uint_as_float(x);
+            }
+        }
+      }
+    }
+  };
+  if (wave < nblk) {
+    load(wave, 0);
+    int blk = wave;
+    for (;;) {
+      const int n1 = blk + kWaves;
+      if (n1 < nblk) load(n1, 1);
+      work(blk, 0);
+      if (n1 >= nblk) break;
+      blk = n1 + kWaves;
+      if (blk < nblk) load(blk, 0);
+      work(n1, 1);
+      if (blk >= nblk) break;
+    }
+  }
+
+  // ---- the four waves' sums ----
+#pragma unroll
+  for (int e = 0; e < E; ++e) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[e]));   // (as above, past the loop's branch)
+  if constexpr (kOutBf16) {
+    asm volatile("s_nop 7\n\ts_nop 3" : "+v"(lones));
+    lsum = lones[0];
+  } else {
+    lsum += __shfl_xor(lsum, 16, 64);
+    lsum += __shfl_xor(lsum, 32, 64);
+  }
+  if (gq == 0) {
+    red_m[wave][li] = m;
+    red_l[wave][li] = lsum;
+  }
+  __syncthreads();   // the table is no longer read
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      const int col = F32 && E == 8 ? (e >> 2) * 64 + 4 * (4 * gq + r) : E * (4 * gq + r) + e;
+      *(floatx4*)&lds.o[wave][li][col] = floatx4{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]};
+    }
+  __syncthreads();
+  const bool direct = sp.n <= a.split_keys;
+  for (int x = tid; x < rows * D; x += kThreads) {
+    const int i = x / D, e = x - i * D;
+    // (a wave without keys left its start: a maximum below all, sums of 0)
+    float wm[kWaves], M = kMaxFloor, L = 0.f, O = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, wm[w] = red_m[w][i]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(wm[w] - M);
+      L = fmaf(red_l[w][i], f, L);
+      O = fmaf(lds.o[w][i][e], f, O);
+    }
+    const int r = row0 + i, t = T == 1 ? 0 : r / G;
+    const int64_t at = orow + (int64_t)t * g.Hq + (r - t * G);
+    if (direct) {
+      const float v = L == 0.f ? 0.f : O / L;   // (a row that sees no key)
+      if constexpr (kOutBf16) ((__bf16*)a.out)[at * D + e] = (__bf16)v;
+      else ((float*)a.out)[at * D + e] = v;
+    } else {
+      const int64_t rec = at * a.n_splits + split;
+      if (e == 0) a.rec_ml[2 * rec] = M, a.rec_ml[2 * rec + 1] = L;
+      a.rec_o[rec * D + e] = O;
+    }
+  }
+}
+
+// One wave per output row whose tile's span is longer than one split: its splits'
+// records joined.
+template <int D, bool OUT_BF16>
+__global__ __launch_bounds__(256) void window_combine_kernel(WindowCall a, int64_t n_rows) {
+  constexpr int kDPerLane = D / 64;
+  const Geom& g = a.g;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);   // (l, j, t, hq)
+  if (row >= n_rows) return;
+  const int64_t lj = row / ((int64_t)g.Hq * a.T);
+  const int in_seq = (int)(row - lj * ((int64_t)g.Hq * a.T));
+  const int s = a.seqs[lj % a.n];
+  const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
+  const bool none = len <= 0 || len > a.max_len;
+  const int t = in_seq / g.Hq, r = t * g.G + (in_seq - t * g.Hq) % g.G;
+  const int row0 = r / a.rows * a.rows;
+  const Span sp = span_of(none ? 0 : len, a.T, g.G, row0, min(row0 + a.rows, g.G * a.T), a.window, a.sink);
+  float L = 0.f, acc[kDPerLane] = {};
+  if (!none && sp.n > 0) {
+    if (sp.n <= a.split_keys) return;   // the split kernel wrote it
+    const int ns = (sp.n + a.split_keys - 1) / a.split_keys;
+    const float* ml = a.rec_ml + row * a.n_splits * 2;
+    // lane i: split i's maximum and sum, 64 at a time, the first kept
+    const float m0 = lane < ns ? ml[2 * lane] : kMaxFloor, l0 = lane < ns ? ml[2 * lane + 1] : 0.f;
+    float M = m0;
+    for (int x = lane + 64; x < ns; x += 64) M = fmaxf(M, ml[2 * x]);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
+    for (int sp0 = 0; sp0 < ns; sp0 += 64) {
+      const int x = sp0 + lane;
+      const float ms = sp0 == 0 ? m0 : x < ns ? ml[2 * x] : kMaxFloor;
+      const float f = __builtin_amdgcn_exp2f(ms - M);
+      const float lf = (sp0 == 0 ? l0 : x < ns ? ml[2 * x + 1] : 0.f) * f;
+      const int cnt = min(64, ns - sp0);
+      const float* v = a.rec_o + (row * a.n_splits + sp0) * D + lane * kDPerLane;
+      // (four records at once; past the last a record of weight 0 is read again)
+      for (int i = 0; i < cnt; i += 4) {
+        float y4[4][kDPerLane];
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < kDPerLane; ++e) y4[y][e] = v[min(i + y, cnt - 1) * D + e];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          if (i + y >= cnt) break;
+          const float fi = __shfl(f, i + y, 64);
+          L += __shfl(lf, i + y, 64);
+#pragma unroll
+          for (int e = 0; e < kDPerLane; ++e) acc[e] = fmaf(y4[y][e], fi, acc[e]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kDPerLane; ++e) {
+    const float v = L == 0.f ? 0.f : acc[e] / L;   // (a row that sees no key)
+    if constexpr (OUT_BF16) ((__bf16*)a.out)[row * D + lane * kDPerLane + e] = (__bf16)v;
+    else ((float*)a.out)[row * D + lane * kDPerLane + e] = v;
+  }
+}
+
+int run_of(int bs) { return std::min(4, __builtin_ctz((unsigned)bs)); }
+
+// Keys per split: 256 while the launch has few workgroups, up to 2048 (1024 where pages
+// give runs of one key) where 16 workgroups per CU remain: fewer records and prologues.
+int split_most(int bs) { return std::min(kSplitMax, kSplitRuns << run_of(bs)); }
+int split_keys_of(int bs, int64_t tiles, int span) {
+  int keys = kSplitMin;
+  while (keys < split_most(bs) && tiles * ((span + 2 * keys - 1) / (2 * keys)) >= kWgTarget) keys *= 2;
+  return keys;
+}
+
+// Up to this many query rows per (layer, sequence, KV head) go through the split kernel,
+// 16 a workgroup, and all over rows of fp32; more through the chunk kernel.
+constexpr int kFewRows = 64;
+bool splits(const Geom& g, int T, bool q8) { return (int64_t)g.G * T <= kFewRows || (g.dtype == KARA_F32 && !q8); }
+
+// a grid of one dimension, of 256 threads a block: HIP counts its threads in 32 bits
+bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24); }
+
+bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && n_layers <= kMaxLayersPerLaunch; }
+
+PoolPtrs ptrs(const void* const* pools, int n_layers) {
+  PoolPtrs x{};
+  for (int i = 0; pools && i < n_layers; ++i) x.p[i] = const_cast<void*>(pools[i]);
+  return x;
+}
+
+template <Cache CT, int NT>
+void launch_split(const WindowCall& a, int64_t blocks, hipStream_t s) {
+  if (a.g.d == 128) hipLaunchKernelGGL((window_split_kernel<CT, NT, 128>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((window_split_kernel<CT, NT, 64>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+}
+
+// q8: whether the cache is of codes (the size over either is the same where it says nothing)
+kara_status_t workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers, int32_t n_query, int32_t window,
+                             int32_t n_sink, int32_t max_len, bool q8, size_t* bytes) {
+  Geom g;
+  const kara_status_t st = make_geom(p, n, &g);
+  if (st != KARA_OK) return st;
+  if (!bytes || !layers_ok(n, n_layers) || n_query < 1 || window < 0 || n_sink < 0 || max_len < 1 ||
+      (int64_t)max_len > (int64_t)g.max_blocks * g.bs || (int64_t)n_query * g.Hq > INT32_MAX / 4)
+    return KARA_ERR_INVALID_ARG;
+  if (max_len > kMaxLen) return KARA_ERR_UNSUPPORTED;
+  const int w = window == 0 ? kMaxLen : std::min(window, kMaxLen), sink = std::min(n_sink, kMaxLen);
+  const size_t rec = (g.d + 2) * sizeof(float);
+  const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
+  if (splits(g, n_query, q8)) {
+    const int span = span_most(n_query, g.G, kTileRows, w, sink, max_len);
+    const int64_t most = ((int64_t)span + kSplitMin - 1) / kSplitMin;
+    // (a split grows until fewer than kWgTarget workgroups would be left at twice its
+    // length, or to the longest)
+    const int longest = split_most(g.bs);
+    const int64_t grown = std::max((int64_t)2 * kWgTarget * kTileRows, rows * (((int64_t)span + longest - 1) / longest));
+    *bytes = most == 1 ? 0 : (size_t)std::min(rows * most, grown) * rec;
+  } else {
+    // (a launch that splits its keys has so many workgroups at most, records and all)
+    const WindowChunkPlan x = window_chunk_plan(g, n, n_layers, n_query, w, sink, max_len);
+    *bytes = (size_t)kWindowChunkWgs * x.qt * 128 * rec;
+  }
+  return KARA_OK;
+}
+
+kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers, int32_t n_query,
+                     int32_t window, int32_t n_sink, const void* q, const void* const* k_pools,
+                     const void* const* v_pools, const void* const* k_scales, const void* const* v_scales,
+                     const int32_t* block_table, const int32_t* seq_lens, int32_t max_len, void* out, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  if ((k_scales == nullptr) != (v_scales == nullptr)) return KARA_ERR_INVALID_ARG;
+  const bool q8 = k_scales != nullptr;
+  size_t need = 0;
+  kara_status_t st = workspace_size(p, n, n_layers, n_query, window, n_sink, max_len, q8, &need);
+  if (st != KARA_OK) return st;
+  if (n == 0) return KARA_OK;
+  if (!seqs || !q || !block_table || !seq_lens || !out || !pools_ok(k_pools, n_layers) || !pools_ok(v_pools, n_layers) ||
+      (q8 && (!pools_ok(k_scales, n_layers) || !pools_ok(v_scales, n_layers))))
+    return KARA_ERR_INVALID_ARG;
+  if (need && (!workspace || workspace_bytes < need)) return KARA_ERR_WORKSPACE;
+  if (!aligned(16, {q, out, need ? workspace : nullptr}) || !aligned(4, {seqs, block_table, seq_lens}) ||
+      !pools_aligned(16, k_pools, n_layers) || !pools_aligned(16, v_pools, n_layers))
+    return KARA_ERR_INVALID_ARG;
+  WindowCall a{};
+  st = make_geom(p, n, &a.g);
+  if (st != KARA_OK) return st;
+  const Geom& g = a.g;
+  a.n = n;
+  a.n_layers = n_layers;
+  a.T = n_query;
+  a.window = window == 0 ? kMaxLen : std::min(window, kMaxLen);
+  a.sink = std::min(n_sink, kMaxLen);
+  a.run = run_of(g.bs);
+  a.max_len = max_len;
+  const bool few = splits(g, n_query, q8), f32 = g.dtype == KARA_F32;
+  const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
+  WindowChunkPlan plan{};
+  int64_t blocks;
+  if (few) {
+    a.rows = kTileRows;
+    a.n_rt = (int)(((int64_t)g.G * n_query + kTileRows - 1) / kTileRows);
+    const int64_t tiles = (int64_t)n_layers * n * g.Hkv * a.n_rt;
+    const int span = span_most(n_query, g.G, kTileRows, a.window, a.sink, max_len);
+    a.split_keys = split_keys_of(g.bs, tiles, span);
+    a.n_splits = (span + a.split_keys - 1) / a.split_keys;
+    blocks = tiles * a.n_splits;
+  } else {
+    plan = window_chunk_plan(g, n, n_layers, n_query, a.window, a.sink, max_len);
+    a.rows = plan.rows_wg;
+    a.n_rt = plan.n_rb;
+    a.split_keys = plan.split_keys;
+    a.n_splits = plan.splits;
+    blocks = 2 * plan.blocks;
+  }
+  if (!grid_ok(blocks) || !grid_ok((rows + 3) / 4)) return KARA_ERR_UNSUPPORTED;
+  a.seqs = seqs;
+  a.bt = block_table;
+  a.seq_lens = seq_lens;
+  a.q = q;
+  a.kp = ptrs(k_pools, n_layers);
+  a.vp = ptrs(v_pools, n_layers);
+  a.ksp = ptrs(k_scales, n_layers);
+  a.vsp = ptrs(v_scales, n_layers);
+  a.rec_o = (float*)workspace;
+  a.rec_ml = a.rec_o + rows * a.n_splits * g.d;
+  a.out = out;
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t e = hipSuccess;
+  if (few) {
+    if (q8 && f32) launch_split<kCodes, 3>(a, blocks, s);
+    else if (q8) launch_split<kCodes, 1>(a, blocks, s);
+    else if (f32) launch_split<kRowsF32, 1>(a, blocks, s);
+    else launch_split<kRowsBf16, 1>(a, blocks, s);
+    e = hipGetLastError();
+  } else {
+    e = launch_window_chunk(a, plan, q8, s);
+  }
+  if (e != hipSuccess || a.n_splits == 1) return hip_status(e);
+  const dim3 grid((unsigned)((rows + 3) / 4));
+#define KARA_WINDOW_COMBINE(D, B) hipLaunchKernelGGL((window_combine_kernel<D, B>), grid, dim3(256), 0, s, a, rows)
+  if (g.d == 128) {
+    if (f32) KARA_WINDOW_COMBINE(128, false);
+    else KARA_WINDOW_COMBINE(128, true);
+  } else {
+    if (f32) KARA_WINDOW_COMBINE(64, false);
+    else KARA_WINDOW_COMBINE(64, true);
+  }
+#undef KARA_WINDOW_COMBINE
+  return hip_status(hipGetLastError());
+}
+
+}  // namespace
+}  // namespace kara
+
+using namespace kara;
+
+extern "C" {
+
+kara_status_t kara_window_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers, int32_t n_query,
+                                                   int32_t window, int32_t n_sink, int32_t max_len, size_t* bytes) {
+  // (for a cache of either kind: over rows of fp32 all queries take the split kernel)
+  size_t rows = 0, codes = 0;
+  kara_status_t st = workspace_size(p, n, n_layers, n_query, window, n_sink, max_len, false, bytes ? &rows : nullptr);
+  if (st == KARA_OK) st = workspace_size(p, n, n_layers, n_query, window, n_sink, max_len, true, &codes);
+  if (st == KARA_OK) *bytes = std::max(rows, codes);
+  return st;
+}
+
+kara_status_t kara_window_attention(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,
+                                    int32_t n_query, int32_t window, int32_t n_sink, const void* q,
+                                    const void* const* k_pools, const void* const* v_pools, const void* const* k_scales,
+                                    const void* const* v_scales, const int32_t* block_table, const int32_t* seq_lens,
+                                    int32_t max_len, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return attend(p, n, seqs, n_layers, n_query, window, n_sink, q, k_pools, v_pools, k_scales, v_scales, block_table,
+                seq_lens, max_len, out, workspace, workspace_bytes, stream);
+}
+
+kara_status_t kara_q8_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers, int32_t n_query,
+                                               int32_t max_len, size_t* bytes) {
+  return workspace_size(p, n, n_layers, n_query, 0, 0, max_len, true, bytes);
+}
+
+kara_status_t kara_q8_attention(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,
+                                int32_t n_query, const void* q, const void* const* k_pools, const void* const* v_pools,
+                                const void* const* k_scales, const void* const* v_scales, const int32_t* block_table,
+                                const int32_t* seq_lens, int32_t max_len, void* out, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  if (n > 0 && (!k_scales || !v_scales)) return KARA_ERR_INVALID_ARG;
+  return attend(p, n, seqs, n_layers, n_query, 0, 0, q, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens,
+                max_len, out, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,533 @@
+// Attention within a sliding window and the first tokens (include/kara_window.h) of many
+// query rows, a prompt's chunk over what is cached, over 8-bit codes or bf16 rows.  Bound
+// by the matrix products.
+//
+// One workgroup of W waves owns 16 QT W query rows of one (layer, sequence, KV head),
+// rows ordered (query, head in group), and walks the keys of their span 64 at a time.  Its
+// threads fetch a chunk two chunks ahead into registers and write it, codes converted in
+// hardware to bf16 -- exactly --, to the other of two LDS stages while the products of the
+// present one run: a chunk is fetched and converted once for all rows, with one barrier.
+// From there S^T = K Q^T, weights as they stand the B operand of O^T += V^T P^T with V
+// through the transposed LDS read, the row sums one more product with ones.
+//
+// NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones over codes).  bf16
+// calls so round a weight, in the output as in its sum, to bf16.
+#include <algorithm>
+#include <type_traits>
+
+#include "kara_q8_device.h"
+#include "kara_window_call.h"
+
+namespace kara {
+namespace {
+
+constexpr int kChKeys = 64;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kMaxFloor = -3.402823466e38f;
+constexpr float kHeadroom = 8.f;
+
+template <bool Q8, int D, int W>
+struct ChCfg {
+  static constexpr int kThreads = W * 64;
+  static constexpr int kRow = D * 2;                 // bytes of a row in LDS
+  static constexpr int kChunks = kRow / 16;
+  static constexpr int kKS = D / 32;                 // products per dot product
+  static constexpr int kDT = D / 16;                 // 16-row tiles of O^T
+  static constexpr int kTile = kChKeys * kRow;       // a chunk of K, or of V
+  static constexpr int kSrc = Q8 ? D : 2 * D;        // bytes of a row in the pool
+  static constexpr int kPieces = kSrc / 16;          // 16-byte pieces of it, a thread each
+  static constexpr int kStagers = kChKeys * kPieces; // pieces of K's chunk, and of V's
+  static constexpr int kKeys = kStagers > kThreads ? kStagers / kThreads : 1;   // keys of a thread
+  // XOR swizzles of a row's 16-byte chunks
+  static __device__ __forceinline__ int swz_k(int row) {
+    if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    return ((row & 3) << 1) | ((row >> 2) & 1);
+  }
+  static __device__ __forceinline__ int swz_v(int row) { return (2 * (D == 128 ? row : row >> 1)) & (kChunks - 1); }
+};
+
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+__device__ inline v4i16 read_tr(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) v4i16*)(__attribute__((address_space(3))) char*)p);
+}
+
+template <bool Q8, int NT, int D, int QT, int W>
+__global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
+  using C = ChCfg<Q8, D, W>;
+  constexpr int kRowsWg = W * 16 * QT;
+  constexpr int KS = C::kKS, DT = C::kDT, KP = C::kKeys;
+  __shared__ __attribute__((aligned(16))) char smem[2][2 * C::kTile];
+  const Geom& g = a.g;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int gq = lane >> 4, li = lane & 15;
+
+  // All row blocks and splits of a (layer, sequence, KV head) on one XCD, whose L2
+  // then holds its keys once, where the units divide among the 8.
+  uint32_t u, rest = blockIdx.x;
+  const uint32_t per = (uint32_t)a.n_rt * (uint32_t)a.n_splits;
+  const uint32_t units = (uint32_t)(a.n_layers * a.n * g.Hkv);
+  if (units % 8 == 0) {
+    u = rest / (8 * per) * 8 + rest % 8;
+    rest = rest / 8 % per;
+  } else {
+    u = rest / per;
+    rest = rest % per;
+  }
+  const int split = rest % (uint32_t)a.n_splits;
+  const int rb = a.n_rt - 1 - (int)(rest / (uint32_t)a.n_splits);     // the blocks that see most keys first
+  const int h = u % (uint32_t)g.Hkv;
+  u /= (uint32_t)g.Hkv;
+  int j = u % (uint32_t)a.n;
+  const int l = u / (uint32_t)a.n;
+  // Sequences by length.  Workgroups that wait for a place: the longest first.  Where
+  // all are placed at once, two to a CU, the second half the shortest first, so that
+  // long ones share a CU with short ones.
+  if (a.n > 1 && a.n <= C::kThreads) {
+    int* lens = (int*)smem[0];
+    int mine = -1;
+    if (tid < a.n) {
+      const int s0 = a.seqs[tid];
+      mine = s0 >= 0 && s0 < g.n_seqs ? a.seq_lens[s0] : 0;
+      lens[tid] = mine;
+    }
+    __syncthreads();
+    const int half = W == 8 ? a.n : (a.n + 1) / 2;
+    const int want = j < half ? j : a.n - 1 - (j - half);
+    if (tid < a.n) {
+      int rank = 0;
+      for (int o = 0; o < a.n; ++o) rank += lens[o] > mine || (lens[o] == mine && o < tid);
+      if (rank == want) lens[a.n] = tid;
+    }
+    __syncthreads();
+    j = __builtin_amdgcn_readfirstlane(lens[a.n]);
+    __syncthreads();
+  }
+  const int s = a.seqs[j];
+  const int G = g.G, T = a.T, R = G * T;
+  const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
+  const int row0 = rb * kRowsWg;
+  const int64_t orow = ((int64_t)l * a.n + j) * T * g.Hq + h * G;
+  const bool none = len <= 0 || len > a.max_len;
+  const Span sp = span_of(none ? 0 : len, T, G, row0, min(row0 + kRowsWg, R), a.window, a.sink);
+  const int first = len - T;                               // position of query 0
+  const int k_lo = split * a.split_keys;
+  const int k_hi = none ? 0 : min(sp.n, k_lo + a.split_keys);
+  const int n_chunks = k_hi > k_lo ? (k_hi - k_lo + kChKeys - 1) / kChKeys : 0;
+
+  // ---- this wave's queries as B operands (lane: query li of each tile) ----
+  const int wrow0 = row0 + wave * 16 * QT;
+  bf16x8 qop[QT][NT][KS];
+  int qpos[QT];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const int r = min(wrow0 + qt * 16 + li, R - 1);
+    const int t = r / G;
+    qpos[qt] = first + t;
+    const int64_t at = (orow + (int64_t)t * g.Hq + (r - t * G)) * D;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      if constexpr (NT == 1) {
+        qop[qt][0][x] = *(const bf16x8*)((const __bf16*)a.q + at + (gq * KS + x) * 8);
+      } else {
+        const floatx4* src = (const floatx4*)((const float*)a.q + at + (gq * KS + x) * 8);
+        const floatx4 p = src[0], q = src[1];
+        uint32_t w[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          bf16_term_pairs<true>(i < 2 ? p[2 * i] : q[2 * i - 4], i < 2 ? p[2 * i + 1] : q[2 * i - 3], w[i]);
+#pragma unroll
+        for (int y = 0; y < NT; ++y) qop[qt][y][x] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
+      }
+    }
+  }
+  const int wave_i0 = first + min(wrow0, R - 1) / G;
+  const int wave_i1 = first + min(wrow0 + 16 * QT - 1, R - 1) / G;
+
+  floatx4 o[QT][DT], lsum[QT];
+  float m[QT];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    m[qt] = kMaxFloor;
+    lsum[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[qt][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  bf16x8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
+  const float c = g.scale * kLog2e;
+
+  // ---- staging: thread (key, piece) of K and of V, KP keys ----
+  constexpr int kKeyStep = C::kThreads / C::kPieces;
+  const bool stager = tid < C::kStagers;
+  const int skey = tid / C::kPieces, spiece = tid % C::kPieces;
+  const int32_t* row_pages = a.bt + (int64_t)(none ? 0 : s) * g.max_blocks;
+  const char* const kbase = (const char*)a.kp.p[l] + spiece * 16;
+  const char* const vbase = (const char*)a.vp.p[l] + spiece * 16;
+  uint4 kw[KP], vw[KP];
+  uint32_t ks[KP], vs[KP];
+  int page[KP], slot[KP];
+  bool live[KP], next_live[KP];        // whether some row sees the key
+  // (the page of a chunk is read a chunk before its rows; keys past the last one repeat it)
+  auto look = [&](int ch) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      const int v = k_lo + ch * kChKeys + skey + i * kKeyStep;
+      const int pos = sp.position(min(v, k_hi - 1));
+      const int b = pos / g.bs;
+      slot[i] = pos - b * g.bs;
+      page[i] = row_pages[b];
+      next_live[i] = v < k_hi && (pos > sp.i0 - a.window || pos < a.sink);
+    }
+  };
+  auto fetch = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      // (a pool has fewer than 2^32 rows)
+      const uint32_t unit = (uint32_t)min(max(page[i], 0), g.num_pages - 1) * (uint32_t)g.Hkv + (uint32_t)h;
+      const uint64_t row = (uint64_t)(unit * (uint32_t)g.bs + (uint32_t)slot[i]) * C::kSrc;
+      kw[i] = *(const uint4*)(kbase + row);
+      vw[i] = *(const uint4*)(vbase + row);
+      if constexpr (Q8) {
+        ks[i] = ((const uint8_t*)a.ksp.p[l])[unit];
+        vs[i] = ((const uint8_t*)a.vsp.p[l])[unit];
+      }
+      live[i] = next_live[i];
+    }
+  };
+  auto stage = [&](int st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      const int key = skey + i * kKeyStep;
+      char* const kto = &smem[st][key * C::kRow];
+      char* const vto = &smem[st][C::kTile + key * C::kRow];
+      const int kz = C::swz_k(key & 15), vz = C::swz_v(key);
+      // what no row sees may be anything: its weights are 0, its values must be finite
+      const uint4 vv = live[i] ? vw[i] : uint4{0, 0, 0, 0};
+      if constexpr (Q8) {
+        // (a piece is two octets; odd keys write the second first, so that two keys' lanes
+        // write different chunks at a time)
+        const int turn = key & 1;
+        const float kscale = q8_scale(ks[i]), vscale = live[i] ? q8_scale(vs[i]) : 0.f;
+        const uint32_t k0 = turn ? kw[i].z : kw[i].x, k1 = turn ? kw[i].w : kw[i].y;
+        const uint32_t k2 = turn ? kw[i].x : kw[i].z, k3 = turn ? kw[i].y : kw[i].w;
+        const uint32_t v0 = turn ? vv.z : vv.x, v1 = turn ? vv.w : vv.y, v2 = turn ? vv.x : vv.z, v3 = turn ? vv.y : vv.w;
+        *(bf16x8*)(kto + (((2 * spiece + turn) ^ kz) * 16)) = q8_octet(k0, k1, kscale);
+        *(bf16x8*)(kto + (((2 * spiece + 1 - turn) ^ kz) * 16)) = q8_octet(k2, k3, kscale);
+        *(bf16x8*)(vto + (((2 * spiece + turn) ^ vz) * 16)) = q8_octet(v0, v1, vscale);
+        *(bf16x8*)(vto + (((2 * spiece + 1 - turn) ^ vz) * 16)) = q8_octet(v2, v3, vscale);
+      } else {
+        *(uint4*)(kto + ((spiece ^ kz) * 16)) = kw[i];
+        *(uint4*)(vto + ((spiece ^ vz) * 16)) = vv;
+      }
+    }
+  };
+
+  int koff[KS], voff[DT];
+#pragma unroll
+  for (int x = 0; x < KS; ++x) koff[x] = li * C::kRow + (((gq * KS + x) ^ C::swz_k(li)) * 16);
+  {
+    const int vrow = 4 * gq + (li >> 2);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      voff[dt] = C::kTile + vrow * C::kRow + (((dt * 2 + ((li & 3) >> 1)) ^ C::swz_v(vrow)) * 16) + (li & 1) * 8;
+  }
+
+  auto sees = [&](int p, int i) __attribute__((always_inline)) { return p <= i && (p > i - a.window || p < a.sink); };
+  floatx4 sv[QT][4];
+  auto phase_a = [&](const char* st, int k0, auto masked) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) sv[qt][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        const bf16x8 ka = *(const bf16x8*)(st + koff[x] + kt * 16 * C::kRow);
+#pragma unroll
+        for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            sv[qt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qop[qt][y][x], sv[qt][kt], 0, 0, 0);
+      }
+    }
+    if constexpr (decltype(masked)::value) {
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const int v = k0 + kt * 16 + 4 * gq, p = sp.position(v);   // (16 keys lie on one side of the gap)
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (v + r >= k_hi || !sees(p + r, qpos[qt])) sv[qt][kt][r] = kNegInf;
+      }
+    }
+  };
+  auto v_operand = [&](const char* st, int jj, int dt) __attribute__((always_inline)) {
+    const v4i16 lo = read_tr(st + voff[dt] + (32 * jj) * C::kRow);
+    const v4i16 hi = read_tr(st + voff[dt] + (32 * jj + 16) * C::kRow);
+    bf16x8 va;
+    __builtin_memcpy(&va, &lo, 8);
+    __builtin_memcpy((char*)&va + 8, &hi, 8);
+    return va;
+  };
+  // Whether a value of the chunk is infinite or NaN.  Asked in chunks that some rows see
+  // keys of and others do not: it must not reach those.
+  auto odd_values = [&](const char* st) __attribute__((always_inline)) {
+    uint32_t hit = 0;
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint4 w = __builtin_bit_cast(uint4, v_operand(st, jj, dt));
+        hit |= ((w.x & 0x7fff7fffu) + 0x00800080u) | ((w.y & 0x7fff7fffu) + 0x00800080u) |
+               ((w.z & 0x7fff7fffu) + 0x00800080u) | ((w.w & 0x7fff7fffu) + 0x00800080u);
+      }
+    return __ballot((hit & 0x80008000u) != 0) != 0ull;
+  };
+  auto phase_b = [&](const char* st, int k0, auto careful) __attribute__((always_inline)) {
+    bf16x8 pb[QT][NT][2];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      float cmax = kNegInf;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) cmax = fmaxf(cmax, sv[qt][kt][r]);
+      // the reference, one for a query's four lanes, is raised only past a headroom
+      if (__ballot(cmax * c > m[qt] + kHeadroom) != 0ull) {
+        cmax = fmaxf(cmax, __shfl_xor(cmax, 16, 64));
+        cmax = fmaxf(cmax, __shfl_xor(cmax, 32, 64)) * c;
+        const float mn = fmaxf(m[qt], cmax);
+        const float f = __builtin_amdgcn_exp2f(m[qt] - mn);
+        m[qt] = mn;
+        lsum[qt] *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[qt][dt] *= f;
+      }
+      const float mr = m[qt];
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        uint32_t w[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const floatx4 x = sv[qt][2 * jj + (i >> 1)];
+          bf16_term_pairs<false>(__builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1)], c, -mr)),
+                                 __builtin_amdgcn_exp2f(fmaf(x[2 * (i & 1) + 1], c, -mr)), w[i]);
+        }
+#pragma unroll
+        for (int y = 0; y < NT; ++y) pb[qt][y][jj] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
+      }
+    }
+    if constexpr (NT > 1) {
+      // A chunk's products are summed from zero, smallest terms first, and added once: a
+      // running sum over thousands of keys is rounded once a chunk, not with each of its six
+      // products.
+      static_assert(QT == 1, "one tile of rows");
+#pragma unroll
+      for (int dt = 0; dt < DT; dt += 2) {
+        floatx4 part[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        bf16x8 va[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj) va[i][jj] = v_operand(st, jj, dt + i);
+#pragma unroll
+        for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              part[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[i][jj], pb[0][y][jj], part[i], 0, 0, 0);
+        o[0][dt] += part[0];
+        o[0][dt + 1] += part[1];
+      }
+      floatx4 part[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj) part[jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[0][y][jj], part[jj], 0, 0, 0);
+      lsum[0] += part[0] + part[1];
+    } else {
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          bf16x8 va = v_operand(st, jj, dt);
+          if constexpr (decltype(careful)::value) {
+            uint32_t w[4];
+            __builtin_memcpy(w, &va, 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
+              if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
+            }
+            __builtin_memcpy(&va, w, 16);
+          }
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[qt][0][jj], o[qt][dt], 0, 0, 0);
+        }
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+          lsum[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[qt][0][jj], lsum[qt], 0, 0, 0);
+      }
+      if constexpr (decltype(careful)::value) {
+        // the infinite and NaN values that the products left out: added where they are
+        // seen (a weight is positive), key by key
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][dt]));
+        for (int key = 0; key < kChKeys && k0 + key < k_hi; ++key) {
+          const int p = sp.position(k0 + key);
+          const char* row = st + C::kTile + key * C::kRow + (gq & 1) * 8;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const uint2 w = *(const uint2*)(row + (((dt * 2 + (gq >> 1)) ^ C::swz_v(key)) * 16));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const uint32_t x = ((r & 2 ? w.y : w.x) >> (16 * (r & 1))) << 16;
+              if ((x & 0x7f800000u) == 0x7f800000u)
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt)
+                  if (sees(p, qpos[qt])) o[qt][dt][r] += __uint_as_float(x);
+            }
+          }
+        }
+      }
+    }
+  };
+
+  if (n_chunks > 0) {
+    if (stager) {
+      look(0);
+      fetch();
+      stage(0);
+      if (n_chunks > 1) {
+        look(1);
+        fetch();
+      }
+      if (n_chunks > 2) look(2);
+    }
+    // keys from `all_lo` to `all_hi` are seen by every row of the wave (sinks are not counted)
+    const int all_lo = wave_i1 - a.window < 0 ? 0 : wave_i1 - a.window + 1 - sp.gap;
+    const int all_hi = min(wave_i0 - sp.gap, k_hi - 1);
+    for (int ch = 0; ch < n_chunks; ++ch) {
+      // every wave has written its part of chunk ch, and is done with chunk ch - 1,
+      // whose stage takes chunk ch + 1
+      __syncthreads();
+      const int k0 = k_lo + ch * kChKeys;
+      const char* st = smem[ch & 1];
+      // (no row of the wave sees a key past its last position, nor one before its first
+      // window that is no sink)
+      const int p0 = sp.position(k0), p1 = sp.position(min(k0 + kChKeys, k_hi) - 1);
+      const bool work = p0 <= wave_i1 && (p1 > wave_i0 - a.window || p0 < a.sink);
+      const bool masked = k0 < all_lo || k0 + kChKeys - 1 > all_hi;
+      if (work) {
+        if (masked) phase_a(st, k0, std::true_type{});
+        else phase_a(st, k0, std::false_type{});
+        // (wait states before the products' results are read past the branches below)
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[qt][3]));
+      }
+      if (stager && ch + 1 < n_chunks) {
+        stage((ch + 1) & 1);
+        if (ch + 2 < n_chunks) fetch();
+        if (ch + 3 < n_chunks) look(ch + 3);
+      }
+      if (work) {
+        bool careful = false;
+        if constexpr (!Q8) careful = masked && odd_values(st);
+        if constexpr (!Q8) {
+          if (careful) phase_b(st, k0, std::true_type{});
+          else phase_b(st, k0, std::false_type{});
+        } else {
+          phase_b(st, k0, std::false_type{});
+        }
+      }
+    }
+  }
+
+  // ---- lane holds O^T[dt*16 + 4*gq + r][query li] ----
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][DT - 1]), "+v"(lsum[qt]));   // (as above)
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const int r = wrow0 + qt * 16 + li;
+    if (r >= R) continue;
+    const int t = r / G;
+    const int64_t at = orow + (int64_t)t * g.Hq + (r - t * G);
+    if (a.n_splits == 1 || (sp.n > 0 && sp.n <= a.split_keys && split == 0)) {
+      const float inv = lsum[qt][0] == 0.f ? 0.f : 1.f / lsum[qt][0];    // (a row that sees no key)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const floatx4 v = o[qt][dt] * inv;
+        if constexpr (NT == 1) {
+          const bf16x2 x = {(__bf16)v[0], (__bf16)v[1]}, y = {(__bf16)v[2], (__bf16)v[3]};
+          *(uint2*)((__bf16*)a.out + at * D + dt * 16 + 4 * gq) =
+              uint2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
+        } else {
+          *(floatx4*)((float*)a.out + at * D + dt * 16 + 4 * gq) = v;
+        }
+      }
+    } else if (!none && k_lo < sp.n) {
+      const int64_t rec = at * a.n_splits + split;
+      if (gq == 0) *(floatx2*)(a.rec_ml + 2 * rec) = floatx2{m[qt], lsum[qt][0]};
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *(floatx4*)(a.rec_o + rec * D + dt * 16 + 4 * gq) = o[qt][dt];
+    }
+  }
+}
+
+template <bool Q8, int NT, int QT, int W>
+hipError_t launch(const WindowCall& a, int64_t blocks, hipStream_t stream) {
+  if (a.g.d == 128)
+    hipLaunchKernelGGL((window_chunk_kernel<Q8, NT, 128, QT, W>), dim3((unsigned)blocks), dim3(W * 64), 0, stream, a);
+  else
+    hipLaunchKernelGGL((window_chunk_kernel<Q8, NT, 64, QT, W>), dim3((unsigned)blocks), dim3(W * 64), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <bool Q8>
+hipError_t launch_bf16(const WindowCall& a, const WindowChunkPlan& x, hipStream_t s) {
+  if (x.qt == 1) return x.waves == 8 ? launch<Q8, 1, 1, 8>(a, x.blocks, s) : launch<Q8, 1, 1, 4>(a, x.blocks, s);
+  return x.waves == 8 ? launch<Q8, 1, 2, 8>(a, x.blocks, s) : launch<Q8, 1, 2, 4>(a, x.blocks, s);
+}
+
+constexpr int kCUs = 256;
+
+}  // namespace
+
+// Rows per workgroup, key splits and blocks of a call.
+WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int window, int sink, int max_len) {
+  WindowChunkPlan x{};
+  const int64_t units = (int64_t)n_layers * n * g.Hkv, R = (int64_t)g.G * T;
+  x.qt = g.dtype == KARA_F32 || R <= 8 * 16 ? 1 : 2;
+  auto blocks = [&](int waves) { return units * ((R + waves * 16 * x.qt - 1) / (waves * 16 * x.qt)); };
+  // Eight waves, a CU's worth of registers, fetch a chunk once for 256 rows (bf16) but
+  // stand one to a CU: a launch of half to all of the CUs' number ends with its longest.
+  // There four waves, two to a CU.
+  x.waves = blocks(8) * 2 > kCUs && blocks(8) <= kCUs * 5 / 4 ? 4 : 8;
+  x.rows_wg = x.waves * 16 * x.qt;
+  x.n_rb = (int)((R + x.rows_wg - 1) / x.rows_wg);
+  x.splits = 1;
+  const int span = span_most(T, g.G, x.rows_wg, window, sink, max_len);
+  // (fewer workgroups than CUs: their keys are split, down to 512)
+  if (x.waves == 8)
+    while (x.splits < 16 && units * x.n_rb * x.splits * 2 <= kWindowChunkWgs && span > 512 * x.splits) x.splits *= 2;
+  x.split_keys = x.splits == 1 ? span : ((span + x.splits - 1) / x.splits + kChKeys - 1) / kChKeys * kChKeys;
+  x.splits = (span + x.split_keys - 1) / x.split_keys;
+  x.blocks = units * x.n_rb * x.splits;
+  return x;
+}
+
+hipError_t launch_window_chunk(WindowCall a, const WindowChunkPlan& x, bool q8, hipStream_t s) {
+  if (a.g.dtype == KARA_F32)   // (over codes: rows of fp32 go through the split kernel)
+    return x.waves == 8 ? launch<true, 3, 1, 8>(a, x.blocks, s) : launch<true, 3, 1, 4>(a, x.blocks, s);
+  return q8 ? launch_bf16<true>(a, x, s) : launch_bf16<false>(a, x, s);
+}
+
+}  // namespace kara

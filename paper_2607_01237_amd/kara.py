@@ -22,6 +22,8 @@ HEADERS = [os.path.join(os.path.dirname(_PKG), "include", h)
 
 # the operators beside the step: the cache in 4 bits, eviction by accumulated weight
 OPERATOR_HEADERS = [os.path.join(os.path.dirname(_PKG), "include", h) for h in ("kara_q4.h", "kara_evict.h")]
+# and those of serving: the cache in 8 bits, the rotating append, windowed attention
+SERVING_HEADERS = [os.path.join(os.path.dirname(_PKG), "include", h) for h in ("kara_q8.h", "kara_rope.h", "kara_window.h")]
 
 BF16, F32 = 0, 1
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_SCHED_MISMATCH, ERR_SCHED_NOMEM = 0, -1, -2, -3, -4, -5, -6
@@ -29,7 +31,7 @@ ERR_SCRATCH_LIMIT = -7
 NOALLOC_SCRATCH_BYTES = 64 << 20      # KARA_NOALLOC_SCRATCH_BYTES
 SEQ_OK, SEQ_BAD_WINDOW, SEQ_BAD_PAGE, SEQ_DUP_TRIGGER, SEQ_BAD_INDEX, SEQ_BAD_KEPT, SEQ_DUP_PAGE = \
     0, 1, 2, 4, 8, 16, 32
-SEQ_NONFINITE = 64                    # kara_q4_append: a report, the sequence was appended
+SEQ_NONFINITE = 64                    # appends into 4 and 8 bits: a report, the sequence was appended
 MAX_COMPRESSIBLE = 4096
 REQ_WAITING, REQ_RUNNING, REQ_FINISHED = 0, 1, 2
 
@@ -67,6 +69,10 @@ class KaraModel(ctypes.Structure):
 
 class LayerWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w_q", "w_o", "w_gate", "w_up", "w_down", "g_attn", "g_ffn")]
+
+
+class KaraRope(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("theta", ctypes.c_float), ("inv_freq", ctypes.c_void_p)]
 
 
 class SchedConfig(ctypes.Structure):
@@ -159,6 +165,17 @@ _SIGS = {
     "kara_evict_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
     "kara_evict_tokens": (_I32, [_PAR, _I32, _VP, _I32, _I32, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _I32,
                                  _VP, _VP, _VP, _VP, _VP, ctypes.c_size_t, _VP]),
+    "kara_q8_append": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "kara_q8_read": (_I32, [_PAR, _I32, _VP, _VP, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "kara_q8_attention_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]),
+    "kara_q8_attention": (_I32, [_PAR, _I32, _VP, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _VP, _VP,
+                                 ctypes.c_size_t, _VP]),
+    "kara_rope_append": (_I32, [_PAR, ctypes.POINTER(KaraRope), _I32, _VP, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
+                                _VP, _VP, _VP, _VP, _I32, _VP, _VP]),
+    "kara_window_attention_workspace_size": (_I32, [_PAR, _I32, _I32, _I32, _I32, _I32, _I32,
+                                                    ctypes.POINTER(ctypes.c_size_t)]),
+    "kara_window_attention": (_I32, [_PAR, _I32, _VP, _I32, _I32, _I32, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32,
+                                     _VP, _VP, ctypes.c_size_t, _VP]),
     "kara_sched_create": (_I32, [ctypes.POINTER(SchedConfig), _P32, ctypes.POINTER(ctypes.c_void_p)]),
     "kara_sched_destroy": (_I32, [_VP]),
     "kara_sched_submit": (_I32, [_VP, _I32, _I32, _P64]),
@@ -521,7 +538,8 @@ def recompute_queries(p, m: KaraModel, trig, weights, hidden_in, hidden_out, k_p
         workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
-# ---- the operators of include/kara_q4.h and include/kara_evict.h.  Their calls are
+# ---- the operators of include/kara_q4.h, kara_evict.h, kara_q8.h, kara_rope.h and
+# kara_window.h.  Their calls are
 # made once per layer group and step, from a few microseconds on: each tensor is
 # looked at once, and a call's pool pointers share one array.  (The library looks at
 # the pointers' alignment: here it took 1 to 2 us a call.)
@@ -747,6 +765,136 @@ def evict_tokens(p, seqs, keep, n_sink, n_recent, k_pools, v_pools, weights, blo
         None if freed is None else _arg(dev, "freed", freed, n * p.max_blocks_per_seq, i32),
         None if n_freed is None else _arg(dev, "n_freed", n_freed, n, i32), _arg(dev, "status", status, n, i32),
         ws, ws_bytes, s))
+
+
+# ---- the cache held in 8 bits (include/kara_q8.h)
+
+def _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales):
+    """Pool arguments of a cache of rows (no scales) or of 8-bit codes."""
+    if (k_scales is None) != (v_scales is None):
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales and v_scales: both or neither")
+    units = p.num_pages * p.n_kv_heads
+    n, dt = units * p.block_size * p.head_dim, torch.uint8 if k_scales is not None else _dtype(torch, p)
+    return _pool_args(dev, L, [("k_pools", k_pools, n, dt), ("v_pools", v_pools, n, dt),
+                               ("k_scales", k_scales, units, torch.uint8), ("v_scales", v_scales, units, torch.uint8)])
+
+
+def q8_append(p, seqs, k_new, v_new, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, status, stream=None):
+    """Quantises k_new / v_new [n_layers][n][n_new][Hkv][d] and appends them after each listed sequence's tokens
+    (codes: uint8 [num_pages][Hkv][block_size][d] per layer, scales: uint8 [num_pages][Hkv])."""
+    lib = load()
+    torch, dev, s = _launch(stream)
+    n, L, n_new = seqs.numel(), len(k_pools), k_new.shape[2]
+    size, dt = L * n * n_new * p.n_kv_heads * p.head_dim, _dtype(torch, p)
+    if k_scales is None or v_scales is None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
+    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    _check("kara_q8_append", lib.kara_q8_append(
+        ctypes.byref(p), n, sq, n_new, L, _arg(dev, "k_new", k_new, size, dt), _arg(dev, "v_new", v_new, size, dt),
+        k, v, ks, vs, bt, sl, _arg(dev, "status", status, n, torch.int32), s))
+
+
+def q8_read(p, seqs, start, n_rows, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, k_out, v_out,
+            stream=None):
+    """Rows [start[s], start[s] + n_rows) of each listed sequence into k_out / v_out [n_layers][n][n_rows][Hkv][d]."""
+    lib = load()
+    torch, dev, s = _launch(stream)
+    n, L, n_rows = seqs.numel(), len(k_pools), int(n_rows)
+    size, dt = L * n * n_rows * p.n_kv_heads * p.head_dim, _dtype(torch, p)
+    if k_scales is None or v_scales is None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
+    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    _check("kara_q8_read", lib.kara_q8_read(
+        ctypes.byref(p), n, sq, _arg(dev, "start", start, p.n_seqs, torch.int32), n_rows, L, k, v, ks, vs, bt, sl,
+        _arg(dev, "k_out", k_out, size, dt), _arg(dev, "v_out", v_out, size, dt), s))
+
+
+def q8_attention_workspace_size(p, n, n_layers, n_query, max_len) -> int:
+    """Of calls with this n_query and up to n sequences, n_layers layers and max_len
+    tokens; fewer queries may need more."""
+    return _size("kara_q8_attention_workspace_size", ctypes.byref(p), n, n_layers, n_query, max_len)
+
+
+def q8_attention(p, seqs, n_query, q, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, max_len, out,
+                 workspace, stream=None):
+    """Causal attention of each listed sequence's last n_query tokens; q, out [n_layers][n][n_query][Hq][d]."""
+    lib = load()
+    torch, dev, s = _launch(stream)
+    n, L, n_query = seqs.numel(), len(k_pools), int(n_query)
+    size, dt = L * n * n_query * p.n_q_heads * p.head_dim, _dtype(torch, p)
+    if k_scales is None or v_scales is None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
+    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    ws, ws_bytes = _workspace_arg(dev, workspace)
+    _check("kara_q8_attention", lib.kara_q8_attention(
+        ctypes.byref(p), n, sq, L, n_query, _arg(dev, "q", q, size, dt), k, v, ks, vs, bt, sl, int(max_len),
+        _arg(dev, "out", out, size, dt), ws, ws_bytes, s))
+
+
+# ---- appends with the position rotation on the way (include/kara_rope.h)
+
+def make_rope(theta=1e6, dim=0, inv_freq=None) -> KaraRope:
+    """The rotation of a head's first `dim` elements (0: all) with frequencies theta^(-2i/dim),
+    or those of inv_freq (fp32 device tensor of dim / 2)."""
+    r = KaraRope(int(dim), float(theta), None)
+    if inv_freq is not None:
+        import torch
+        r.held = inv_freq                      # as long as the structure is
+        r.inv_freq = _arg(inv_freq.get_device(), "inv_freq", inv_freq, dim // 2 if dim > 0 else 0, torch.float32)
+    return r
+
+
+def rope_append(p, rope: KaraRope, seqs, k_new, v_new, k_pools, v_pools, block_table, seq_lens, status, rope_pos=None,
+                q=None, q_out=None, counted=False, k_scales=None, v_scales=None, stream=None):
+    """Appends k_new (turned by its rotary positions) and v_new [n_layers][n][n_new][Hkv][d] after each listed
+    sequence's tokens, to rows or 8-bit codes (k_scales, v_scales given), and turns q [n_layers][n][n_new][Hq][d] into
+    q_out.  rope_pos [n_seqs]: the next token's rotary position (None: its position in the cache).  counted: the tokens
+    are in seq_lens and rope_pos already, by an earlier layer's call."""
+    lib = load()
+    torch, dev, s = _launch(stream)
+    n, L, n_new = seqs.numel(), len(k_pools), k_new.shape[2]
+    size, dt = L * n * n_new * p.n_kv_heads * p.head_dim, _dtype(torch, p)
+    q_size = L * n * n_new * p.n_q_heads * p.head_dim
+    if (q is None) != (q_out is None):
+        raise KaraError("marshal", ERR_INVALID_ARG, "q and q_out: both or neither")
+    held = getattr(rope, "held", None)
+    if held is not None:
+        _arg(dev, "inv_freq", held, (rope.dim or p.head_dim) // 2, torch.float32)
+    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    _check("kara_rope_append", lib.kara_rope_append(
+        ctypes.byref(p), ctypes.byref(rope), n, sq, n_new, L, None if q is None else _arg(dev, "q", q, q_size, dt),
+        _arg(dev, "k_new", k_new, size, dt), _arg(dev, "v_new", v_new, size, dt),
+        None if q is None else _arg(dev, "q_out", q_out, q_size, dt), k, v, ks, vs, bt, sl,
+        None if rope_pos is None else _arg(dev, "rope_pos", rope_pos, p.n_seqs, torch.int32), int(bool(counted)),
+        _arg(dev, "status", status, n, torch.int32), s))
+
+
+# ---- attention within a sliding window and the first tokens (include/kara_window.h)
+
+def window_attention_workspace_size(p, n, n_layers, n_query, window, n_sink, max_len) -> int:
+    """Of calls with this n_query, window and n_sink and up to n sequences, n_layers layers and max_len tokens."""
+    return _size("kara_window_attention_workspace_size", ctypes.byref(p), n, n_layers, n_query, window, n_sink, max_len)
+
+
+def window_attention(p, seqs, n_query, window, n_sink, q, k_pools, v_pools, block_table, seq_lens, max_len, out,
+                     workspace, k_scales=None, v_scales=None, stream=None):
+    """Causal attention of each listed sequence's last n_query tokens, each over the last `window` tokens up to its own
+    (0: all) and the first n_sink, over rows or 8-bit codes (k_scales, v_scales given); q, out
+    [n_layers][n][n_query][Hq][d]."""
+    lib = load()
+    torch, dev, s = _launch(stream)
+    n, L, n_query = seqs.numel(), len(k_pools), int(n_query)
+    size, dt = L * n * n_query * p.n_q_heads * p.head_dim, _dtype(torch, p)
+    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
+    ws, ws_bytes = _workspace_arg(dev, workspace)
+    _check("kara_window_attention", lib.kara_window_attention(
+        ctypes.byref(p), n, sq, L, n_query, int(window), int(n_sink), _arg(dev, "q", q, size, dt), k, v, ks, vs, bt, sl,
+        int(max_len), _arg(dev, "out", out, size, dt), ws, ws_bytes, s))
 
 
 # ---- periodic compression policy (include/kara_sched.h): host runtime
