@@ -115,12 +115,12 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
 
   // lane (gq, li): its pieces of query row li, and the row's position
   const bool there = li < rows;
-  int qpos = -1;
+  int qhi = -1, qlo = 0;                       // the keys it sees, sinks not counted
   uint4 qraw[F32 || NT > 1 ? D / 16 : KS];
   {
     const int r = row0 + (there ? li : 0);
     const int t = T == 1 ? 0 : r / G;
-    if (there) qpos = len - T + t;
+    if (there) qhi = len - T + t - sp.gap, qlo = qhi - a.window + 1;
     const char* src = (const char*)a.q + (orow + (int64_t)t * g.Hq + (r - t * G)) * D * (kOutBf16 ? 2 : 4);
     if constexpr (F32) {
 #pragma unroll
@@ -234,12 +234,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
 
-  // keys from `all_lo` to `all_hi` are seen by every row of the tile (sinks are not counted)
-  const int all_lo = sp.i1 - a.window < 0 ? 0 : sp.i1 - a.window + 1 - sp.gap;
-  const int all_hi = sp.i0 - sp.gap;
-  auto sees = [&](int p, int i) __attribute__((always_inline)) { return p <= i && (p > i - a.window || p < a.sink); };
-  // seen by some row
-  auto seen = [&](int p) __attribute__((always_inline)) { return p <= sp.i1 && (p > sp.i0 - a.window || p < a.sink); };
+  // keys that some row sees, and that every row sees (sinks not counted)
+  const int any_lo = sp.i0 - a.window + 1 - sp.gap, any_hi = sp.n - 1;
+  const int all_lo = sp.i1 - a.window + 1 - sp.gap, all_hi = sp.i0 - sp.gap;
+  auto in = [&](int v, int lo, int hi) __attribute__((always_inline)) { return v <= hi && (v >= lo || v < a.sink); };
 
   auto work = [&](int blk, int b) __attribute__((always_inline)) {
     floatx4 sv[TB];
@@ -302,10 +300,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
       for (int t = 0; t < TB; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int p = sp.position(v0 + t * 16 + 4 * gq + r);
-          if (!sees(p, qpos)) sv[t][r] = kNegInf;
+          const int v = v0 + t * 16 + 4 * gq + r;
+          if (!in(v, qlo, qhi)) sv[t][r] = kNegInf;
           // what no row sees may be anything: its weights are 0, its values must be finite
-          if (!seen(p))
+          if (!in(v, any_lo, any_hi))
 #pragma unroll
             for (int y = 0; y < VP; ++y) pv[4 * t + r][y] = 0;
         }
@@ -405,10 +403,9 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
 #pragma unroll
         for (int e = 0; e < E; ++e) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[e]));
         for (int key = 0; key < C::kBlock; ++key) {
-          const int pos = sp.position(v0 + key);
-          if (!seen(pos)) continue;
+          if (!in(v0 + key, any_lo, any_hi)) continue;
           const char* row = (const char*)a.vp.p[l] + (uint64_t)row_of(blk * C::kBlock + key) * C::kRow;
-          const bool mine = sees(pos, qpos);
+          const bool mine = in(v0 + key, qlo, qhi);
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -605,7 +602,7 @@ kara_status_t workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers
     *bytes = most == 1 ? 0 : (size_t)std::min(rows * most, grown) * rec;
   } else {
     // (a launch that splits its keys has so many workgroups at most, records and all)
-    const WindowChunkPlan x = window_chunk_plan(g, n, n_layers, n_query, w, sink, max_len);
+    const WindowChunkPlan x = window_chunk_plan(g, n, n_layers, n_query, w, sink, max_len, q8);
     *bytes = (size_t)kWindowChunkWgs * x.qt * 128 * rec;
   }
   return KARA_OK;
@@ -653,7 +650,7 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
     a.n_splits = (span + a.split_keys - 1) / a.split_keys;
     blocks = tiles * a.n_splits;
   } else {
-    plan = window_chunk_plan(g, n, n_layers, n_query, a.window, a.sink, max_len);
+    plan = window_chunk_plan(g, n, n_layers, n_query, a.window, a.sink, max_len, q8);
     a.rows = plan.rows_wg;
     a.n_rt = plan.n_rb;
     a.split_keys = plan.split_keys;

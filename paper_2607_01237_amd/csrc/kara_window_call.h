@@ -28,6 +28,10 @@ struct WindowCall {
 // that no row sees: both parts begin and the first ends at a multiple of 16, so that runs
 // of up to 16 keys from a multiple of their length lie in one page wherever the block
 // size allows it.
+//
+// In these numbers a query at position i sees v where
+//   v <= i - gap  and  (v > i - gap - window  or  v < sink):
+// with a gap, head is sink rounded up and lies below every row's window.
 struct Span {
   int i0, i1;                 // first and last position of the rows
   int head, gap, n;
@@ -64,7 +68,7 @@ struct WindowChunkPlan {
   int64_t blocks;
 };
 constexpr int kWindowChunkWgs = 256;   // most workgroups of a launch that splits its keys
-WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int window, int sink, int max_len);
+WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int window, int sink, int max_len, bool q8);
 hipError_t launch_window_chunk(WindowCall a, const WindowChunkPlan& x, bool q8, hipStream_t stream);
 
 }  // namespace kara

@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "kara_lds.h"
 #include "kara_q8_device.h"
 #include "kara_window_call.h"
 
@@ -26,6 +27,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kMaxFloor = -3.402823466e38f;
 constexpr float kHeadroom = 8.f;
+
+constexpr int kRuns = 1024;             // runs of keys in the LDS table at a time
 
 template <bool Q8, int D, int W>
 struct ChCfg {
@@ -39,6 +42,10 @@ struct ChCfg {
   static constexpr int kPieces = kSrc / 16;          // 16-byte pieces of it, a thread each
   static constexpr int kStagers = kChKeys * kPieces; // pieces of K's chunk, and of V's
   static constexpr int kKeys = kStagers > kThreads ? kStagers / kThreads : 1;   // keys of a thread
+  static constexpr int kKeyStep = kThreads / kPieces;
+  // Rows: a ring of four stages, copied three chunks ahead.  Codes: two, written from registers.
+  static constexpr int kStages = Q8 ? 2 : 4;
+  static constexpr int kCopies = 2 * kKeys;          // of a thread and chunk
   // XOR swizzles of a row's 16-byte chunks
   static __device__ __forceinline__ int swz_k(int row) {
     if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
@@ -46,6 +53,9 @@ struct ChCfg {
   }
   static __device__ __forceinline__ int swz_v(int row) { return (2 * (D == 128 ? row : row >> 1)) & (kChunks - 1); }
 };
+
+// Values of keys that no row sees: read in their place.
+__device__ const uint4 kZeroRow[16] = {};
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 __device__ inline v4i16 read_tr(const char* p) {
@@ -58,7 +68,8 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
   using C = ChCfg<Q8, D, W>;
   constexpr int kRowsWg = W * 16 * QT;
   constexpr int KS = C::kKS, DT = C::kDT, KP = C::kKeys;
-  __shared__ __attribute__((aligned(16))) char smem[2][2 * C::kTile];
+  __shared__ __attribute__((aligned(16))) char smem[C::kStages][2 * C::kTile];
+  __shared__ uint32_t run_row[kRuns], run_scale[Q8 ? kRuns : 1];   // pool rows of runs of keys; K's scale byte, V's above it
   const Geom& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -120,12 +131,12 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
   // ---- this wave's queries as B operands (lane: query li of each tile) ----
   const int wrow0 = row0 + wave * 16 * QT;
   bf16x8 qop[QT][NT][KS];
-  int qpos[QT];
+  int qhi[QT];                           // the last key it sees
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) {
     const int r = min(wrow0 + qt * 16 + li, R - 1);
     const int t = r / G;
-    qpos[qt] = first + t;
+    qhi[qt] = first + t - sp.gap;
     const int64_t at = (orow + (int64_t)t * g.Hq + (r - t * G)) * D;
 #pragma unroll
     for (int x = 0; x < KS; ++x) {
@@ -143,8 +154,16 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
       }
     }
   }
-  const int wave_i0 = first + min(wrow0, R - 1) / G;
-  const int wave_i1 = first + min(wrow0 + 16 * QT - 1, R - 1) / G;
+  // (the query loads are waited for here, not in the loop behind the copies)
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+    for (int y = 0; y < NT; ++y)
+#pragma unroll
+      for (int x = 0; x < KS; ++x) asm volatile("" : "+v"(qop[qt][y][x]));
+  // last keys that the wave's first and last row see
+  const int wave_hi0 = first + min(wrow0, R - 1) / G - sp.gap;
+  const int wave_hi1 = first + min(wrow0 + 16 * QT - 1, R - 1) / G - sp.gap;
 
   floatx4 o[QT][DT], lsum[QT];
   float m[QT];
@@ -161,68 +180,98 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
   const float c = g.scale * kLog2e;
 
   // ---- staging: thread (key, piece) of K and of V, KP keys ----
-  constexpr int kKeyStep = C::kThreads / C::kPieces;
   const bool stager = tid < C::kStagers;
   const int skey = tid / C::kPieces, spiece = tid % C::kPieces;
   const int32_t* row_pages = a.bt + (int64_t)(none ? 0 : s) * g.max_blocks;
-  const char* const kbase = (const char*)a.kp.p[l] + spiece * 16;
-  const char* const vbase = (const char*)a.vp.p[l] + spiece * 16;
-  uint4 kw[KP], vw[KP];
-  uint32_t ks[KP], vs[KP];
-  int page[KP], slot[KP];
-  bool live[KP], next_live[KP];        // whether some row sees the key
-  // (the page of a chunk is read a chunk before its rows; keys past the last one repeat it)
-  auto look = [&](int ch) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < KP; ++i) {
-      const int v = k_lo + ch * kChKeys + skey + i * kKeyStep;
-      const int pos = sp.position(min(v, k_hi - 1));
-      const int b = pos / g.bs;
-      slot[i] = pos - b * g.bs;
-      page[i] = row_pages[b];
-      next_live[i] = v < k_hi && (pos > sp.i0 - a.window || pos < a.sink);
+  // (keys that some row sees, sinks not counted: from any_lo on)
+  const int any_lo = sp.i0 - a.window + 1 - sp.gap;
+  const int run = a.run, run_mask = (1 << run) - 1;
+  // Runs of 2^run keys lie in one page: an entry each, kRuns of them at a time.  (Keys that no
+  // row sees may be on no page: any row of the pool stands for them.)
+  int seg_end = k_lo;                    // keys before it are in the table, or were
+  auto load_segment = [&]() __attribute__((always_inline)) {
+    const int from = seg_end;
+    const int runs = min(kRuns, (k_hi - from + run_mask) >> run);
+    for (int i = tid; i < runs; i += C::kThreads) {
+      const int pos = sp.position(from + (i << run)), b = pos / g.bs;
+      const uint32_t unit = (uint32_t)min(max(row_pages[b], 0), g.num_pages - 1) * (uint32_t)g.Hkv + (uint32_t)h;
+      run_row[i] = unit * (uint32_t)g.bs + (uint32_t)(pos - b * g.bs);     // (a pool has fewer than 2^32 rows)
+      if constexpr (Q8)
+        run_scale[i] = (uint32_t)((const uint8_t*)a.ksp.p[l])[unit] | (uint32_t)((const uint8_t*)a.vsp.p[l])[unit] << 16;
+    }
+    seg_end = from + (kRuns << run);
+  };
+  // before chunk ch is addressed, by all threads
+  auto reach = [&](int ch) __attribute__((always_inline)) {
+    if (k_lo + ch * kChKeys >= seg_end) {
+      // (rare: every earlier copy lands first, as the table's loads are waited for with
+      // the compiler's own count)
+      wait_vm<0>();
+      lds_barrier();
+      load_segment();
+      lds_barrier();
     }
   };
-  auto fetch = [&]() __attribute__((always_inline)) {
+  // entry of key v, which the table holds
+  auto entry_of = [&](int v) __attribute__((always_inline)) { return (v - (seg_end - (kRuns << run))) >> run; };
+  auto seen = [&](int v) __attribute__((always_inline)) { return v < k_hi && (v >= any_lo || v < a.sink); };
+
+  // rows: pieces from the pool to LDS, those of one row by adjacent lanes
+  int kpiece[KP], vpiece[KP];
+#pragma unroll
+  for (int i = 0; i < KP; ++i) {
+    const int key = skey + i * C::kKeyStep;
+    kpiece[i] = (spiece ^ C::swz_k(key & 15)) * 16;
+    vpiece[i] = (spiece ^ C::swz_v(key)) * 16;
+  }
+  const char* const kpool = (const char*)a.kp.p[l];
+  const char* const vpool = (const char*)a.vp.p[l];
+  auto issue = [&](int ch) __attribute__((always_inline)) {
+    char* st = smem[ch % C::kStages];
 #pragma unroll
     for (int i = 0; i < KP; ++i) {
-      // (a pool has fewer than 2^32 rows)
-      const uint32_t unit = (uint32_t)min(max(page[i], 0), g.num_pages - 1) * (uint32_t)g.Hkv + (uint32_t)h;
-      const uint64_t row = (uint64_t)(unit * (uint32_t)g.bs + (uint32_t)slot[i]) * C::kSrc;
-      kw[i] = *(const uint4*)(kbase + row);
-      vw[i] = *(const uint4*)(vbase + row);
-      if constexpr (Q8) {
-        ks[i] = ((const uint8_t*)a.ksp.p[l])[unit];
-        vs[i] = ((const uint8_t*)a.vsp.p[l])[unit];
-      }
-      live[i] = next_live[i];
-    }
-  };
-  auto stage = [&](int st) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < KP; ++i) {
-      const int key = skey + i * kKeyStep;
-      char* const kto = &smem[st][key * C::kRow];
-      char* const vto = &smem[st][C::kTile + key * C::kRow];
-      const int kz = C::swz_k(key & 15), vz = C::swz_v(key);
+      const int v = k_lo + ch * kChKeys + skey + i * C::kKeyStep, there = min(v, k_hi - 1);
+      const uint64_t row = (uint64_t)(run_row[entry_of(there)] + (uint32_t)(there & run_mask)) * C::kSrc;
+      copy16(kpool + row + kpiece[i], st + (i * W + wave) * 1024);
       // what no row sees may be anything: its weights are 0, its values must be finite
-      const uint4 vv = live[i] ? vw[i] : uint4{0, 0, 0, 0};
-      if constexpr (Q8) {
-        // (a piece is two octets; odd keys write the second first, so that two keys' lanes
-        // write different chunks at a time)
-        const int turn = key & 1;
-        const float kscale = q8_scale(ks[i]), vscale = live[i] ? q8_scale(vs[i]) : 0.f;
-        const uint32_t k0 = turn ? kw[i].z : kw[i].x, k1 = turn ? kw[i].w : kw[i].y;
-        const uint32_t k2 = turn ? kw[i].x : kw[i].z, k3 = turn ? kw[i].y : kw[i].w;
-        const uint32_t v0 = turn ? vv.z : vv.x, v1 = turn ? vv.w : vv.y, v2 = turn ? vv.x : vv.z, v3 = turn ? vv.y : vv.w;
-        *(bf16x8*)(kto + (((2 * spiece + turn) ^ kz) * 16)) = q8_octet(k0, k1, kscale);
-        *(bf16x8*)(kto + (((2 * spiece + 1 - turn) ^ kz) * 16)) = q8_octet(k2, k3, kscale);
-        *(bf16x8*)(vto + (((2 * spiece + turn) ^ vz) * 16)) = q8_octet(v0, v1, vscale);
-        *(bf16x8*)(vto + (((2 * spiece + 1 - turn) ^ vz) * 16)) = q8_octet(v2, v3, vscale);
-      } else {
-        *(uint4*)(kto + ((spiece ^ kz) * 16)) = kw[i];
-        *(uint4*)(vto + ((spiece ^ vz) * 16)) = vv;
-      }
+      copy16(seen(v) ? vpool + row + vpiece[i] : (const char*)kZeroRow + vpiece[i], st + C::kTile + (i * W + wave) * 1024);
+    }
+  };
+
+  // codes: through registers
+  uint4 kw[KP], vw[KP];
+  uint32_t scales[KP];
+  auto fetch = [&](int ch) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      const int v = k_lo + ch * kChKeys + skey + i * C::kKeyStep, there = min(v, k_hi - 1);
+      const int e = entry_of(there);
+      const uint64_t row = (uint64_t)(run_row[e] + (uint32_t)(there & run_mask)) * C::kSrc + spiece * 16;
+      kw[i] = *(const uint4*)(kpool + row);
+      vw[i] = *(const uint4*)(vpool + row);
+      scales[i] = run_scale[Q8 ? e : 0];
+    }
+  };
+  auto stage = [&](int ch) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      const int key = skey + i * C::kKeyStep;
+      char* const kto = &smem[ch % C::kStages][key * C::kRow];
+      char* const vto = kto + C::kTile;
+      const int kz = C::swz_k(key & 15), vz = C::swz_v(key);
+      const bool live = seen(k_lo + ch * kChKeys + key);
+      // (a piece is two octets; odd keys write the second first, so that two keys' lanes
+      // write different chunks at a time)
+      const int turn = key & 1;
+      const uint4 vv = live ? vw[i] : uint4{0, 0, 0, 0};
+      const float kscale = q8_scale(scales[i] & 255), vscale = live ? q8_scale(scales[i] >> 16) : 0.f;
+      const uint32_t k0 = turn ? kw[i].z : kw[i].x, k1 = turn ? kw[i].w : kw[i].y;
+      const uint32_t k2 = turn ? kw[i].x : kw[i].z, k3 = turn ? kw[i].y : kw[i].w;
+      const uint32_t v0 = turn ? vv.z : vv.x, v1 = turn ? vv.w : vv.y, v2 = turn ? vv.x : vv.z, v3 = turn ? vv.y : vv.w;
+      *(bf16x8*)(kto + (((2 * spiece + turn) ^ kz) * 16)) = q8_octet(k0, k1, kscale);
+      *(bf16x8*)(kto + (((2 * spiece + 1 - turn) ^ kz) * 16)) = q8_octet(k2, k3, kscale);
+      *(bf16x8*)(vto + (((2 * spiece + turn) ^ vz) * 16)) = q8_octet(v0, v1, vscale);
+      *(bf16x8*)(vto + (((2 * spiece + 1 - turn) ^ vz) * 16)) = q8_octet(v2, v3, vscale);
     }
   };
 
@@ -236,13 +285,12 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
       voff[dt] = C::kTile + vrow * C::kRow + (((dt * 2 + ((li & 3) >> 1)) ^ C::swz_v(vrow)) * 16) + (li & 1) * 8;
   }
 
-  auto sees = [&](int p, int i) __attribute__((always_inline)) { return p <= i && (p > i - a.window || p < a.sink); };
+  // whether key v is seen by the query whose last key is hi
+  auto sees = [&](int v, int hi) __attribute__((always_inline)) { return v <= hi && (v > hi - a.window || v < a.sink); };
   floatx4 sv[QT][4];
   auto phase_a = [&](const char* st, int k0, auto masked) __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) sv[qt][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < KS; ++x) {
         const bf16x8 ka = *(const bf16x8*)(st + koff[x] + kt * 16 * C::kRow);
@@ -250,18 +298,19 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
         for (int y = NT - 1; y >= 0; --y)
 #pragma unroll
           for (int qt = 0; qt < QT; ++qt)
-            sv[qt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qop[qt][y][x], sv[qt][kt], 0, 0, 0);
+            sv[qt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                ka, qop[qt][y][x], x == 0 && y == NT - 1 ? floatx4{0.f, 0.f, 0.f, 0.f} : sv[qt][kt], 0, 0, 0);
       }
     }
     if constexpr (decltype(masked)::value) {
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
-        const int v = k0 + kt * 16 + 4 * gq, p = sp.position(v);   // (16 keys lie on one side of the gap)
+        const int v = k0 + kt * 16 + 4 * gq;
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (v + r >= k_hi || !sees(p + r, qpos[qt])) sv[qt][kt][r] = kNegInf;
+            if (v + r >= k_hi || !sees(v + r, qhi[qt])) sv[qt][kt][r] = kNegInf;
       }
     }
   };
@@ -382,7 +431,6 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][dt]));
         for (int key = 0; key < kChKeys && k0 + key < k_hi; ++key) {
-          const int p = sp.position(k0 + key);
           const char* row = st + C::kTile + key * C::kRow + (gq & 1) * 8;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) {
@@ -393,7 +441,7 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
               if ((x & 0x7f800000u) == 0x7f800000u)
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt)
-                  if (sees(p, qpos[qt])) o[qt][dt][r] += __uint_as_float(x);
+                  if (sees(k0 + key, qhi[qt])) o[qt][dt][r] += __uint_as_float(x);
             }
           }
         }
@@ -402,29 +450,41 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
   };
 
   if (n_chunks > 0) {
-    if (stager) {
-      look(0);
-      fetch();
-      stage(0);
-      if (n_chunks > 1) {
-        look(1);
-        fetch();
+    load_segment();
+    lds_barrier();
+    if constexpr (Q8) {
+      if (stager) {
+        fetch(0);
+        stage(0);
+        if (n_chunks > 1) fetch(1);      // (kRuns keys at least are in the table)
       }
-      if (n_chunks > 2) look(2);
+    } else {
+      for (int ch = 0; ch < C::kStages - 1 && ch < n_chunks; ++ch) issue(ch);
     }
-    // keys from `all_lo` to `all_hi` are seen by every row of the wave (sinks are not counted)
-    const int all_lo = wave_i1 - a.window < 0 ? 0 : wave_i1 - a.window + 1 - sp.gap;
-    const int all_hi = min(wave_i0 - sp.gap, k_hi - 1);
+    // keys that every row of the wave sees (sinks not counted)
+    const int all_lo = wave_hi1 - a.window + 1, all_hi = min(wave_hi0, k_hi - 1);
     for (int ch = 0; ch < n_chunks; ++ch) {
+      if constexpr (!Q8) {
+        // (the copies of up to two newer chunks may be outstanding)
+        const int newer = n_chunks - 1 - ch;
+        if (newer >= 2) wait_vm<2 * C::kCopies>();
+        else if (newer == 1) wait_vm<C::kCopies>();
+        else wait_vm<0>();
+      }
       // every wave has written its part of chunk ch, and is done with chunk ch - 1,
-      // whose stage takes chunk ch + 1
-      __syncthreads();
+      // whose stage is free
+      lds_barrier();
+      if constexpr (!Q8) {
+        if (ch + C::kStages - 1 < n_chunks) {
+          reach(ch + C::kStages - 1);
+          issue(ch + C::kStages - 1);
+        }
+      }
       const int k0 = k_lo + ch * kChKeys;
-      const char* st = smem[ch & 1];
-      // (no row of the wave sees a key past its last position, nor one before its first
-      // window that is no sink)
-      const int p0 = sp.position(k0), p1 = sp.position(min(k0 + kChKeys, k_hi) - 1);
-      const bool work = p0 <= wave_i1 && (p1 > wave_i0 - a.window || p0 < a.sink);
+      const char* st = smem[ch % C::kStages];
+      // (no row of the wave sees a key past its last, nor one before its first window that
+      // is no sink)
+      const bool work = k0 <= wave_hi1 && (k0 + kChKeys > wave_hi0 - a.window + 1 || k0 < a.sink);
       const bool masked = k0 < all_lo || k0 + kChKeys - 1 > all_hi;
       if (work) {
         if (masked) phase_a(st, k0, std::true_type{});
@@ -433,10 +493,14 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[qt][3]));
       }
-      if (stager && ch + 1 < n_chunks) {
-        stage((ch + 1) & 1);
-        if (ch + 2 < n_chunks) fetch();
-        if (ch + 3 < n_chunks) look(ch + 3);
+      if constexpr (Q8) {
+        if (ch + 1 < n_chunks) {
+          if (stager) stage(ch + 1);
+          if (ch + 2 < n_chunks) {
+            reach(ch + 2);
+            if (stager) fetch(ch + 2);
+          }
+        }
       }
       if (work) {
         bool careful = false;
@@ -493,8 +557,9 @@ hipError_t launch(const WindowCall& a, int64_t blocks, hipStream_t stream) {
 
 template <bool Q8>
 hipError_t launch_bf16(const WindowCall& a, const WindowChunkPlan& x, hipStream_t s) {
-  if (x.qt == 1) return x.waves == 8 ? launch<Q8, 1, 1, 8>(a, x.blocks, s) : launch<Q8, 1, 1, 4>(a, x.blocks, s);
-  return x.waves == 8 ? launch<Q8, 1, 2, 8>(a, x.blocks, s) : launch<Q8, 1, 2, 4>(a, x.blocks, s);
+  if constexpr (Q8)
+    if (x.waves == 4) return x.qt == 1 ? launch<Q8, 1, 1, 4>(a, x.blocks, s) : launch<Q8, 1, 2, 4>(a, x.blocks, s);
+  return x.qt == 1 ? launch<Q8, 1, 1, 8>(a, x.blocks, s) : launch<Q8, 1, 2, 8>(a, x.blocks, s);
 }
 
 constexpr int kCUs = 256;
@@ -502,7 +567,7 @@ constexpr int kCUs = 256;
 }  // namespace
 
 // Rows per workgroup, key splits and blocks of a call.
-WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int window, int sink, int max_len) {
+WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int window, int sink, int max_len, bool q8) {
   WindowChunkPlan x{};
   const int64_t units = (int64_t)n_layers * n * g.Hkv, R = (int64_t)g.G * T;
   x.qt = g.dtype == KARA_F32 || R <= 8 * 16 ? 1 : 2;
@@ -510,7 +575,8 @@ WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int
   // Eight waves, a CU's worth of registers, fetch a chunk once for 256 rows (bf16) but
   // stand one to a CU: a launch of half to all of the CUs' number ends with its longest.
   // There four waves, two to a CU.
-  x.waves = blocks(8) * 2 > kCUs && blocks(8) <= kCUs * 5 / 4 ? 4 : 8;
+  // (Rows stand one to a CU either way, by their ring.)
+  x.waves = q8 && blocks(8) * 2 > kCUs && blocks(8) <= kCUs * 5 / 4 ? 4 : 8;
   x.rows_wg = x.waves * 16 * x.qt;
   x.n_rb = (int)((R + x.rows_wg - 1) / x.rows_wg);
   x.splits = 1;
