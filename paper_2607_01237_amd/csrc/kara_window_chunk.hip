@@ -96,11 +96,12 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
   // Sequences by length.  Workgroups that wait for a place: the longest first.  Where
   // all are placed at once, two to a CU, the second half the shortest first, so that
   // long ones share a CU with short ones.
+  int s, len;
   if (a.n > 1 && a.n <= C::kThreads) {
     int* lens = (int*)smem[0];
-    int mine = -1;
+    int s0 = 0, mine = -1;
     if (tid < a.n) {
-      const int s0 = a.seqs[tid];
+      s0 = a.seqs[tid];
       mine = s0 >= 0 && s0 < g.n_seqs ? a.seq_lens[s0] : 0;
       lens[tid] = mine;
     }
@@ -110,15 +111,18 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
     if (tid < a.n) {
       int rank = 0;
       for (int o = 0; o < a.n; ++o) rank += lens[o] > mine || (lens[o] == mine && o < tid);
-      if (rank == want) lens[a.n] = tid;
+      if (rank == want) lens[a.n] = tid, lens[a.n + 1] = s0, lens[a.n + 2] = mine;
     }
     __syncthreads();
     j = __builtin_amdgcn_readfirstlane(lens[a.n]);
+    s = __builtin_amdgcn_readfirstlane(lens[a.n + 1]);
+    len = __builtin_amdgcn_readfirstlane(lens[a.n + 2]);
     __syncthreads();
+  } else {
+    s = a.seqs[j];
+    len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
   }
-  const int s = a.seqs[j];
   const int G = g.G, T = a.T, R = G * T;
-  const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
   const int row0 = rb * kRowsWg;
   const int64_t orow = ((int64_t)l * a.n + j) * T * g.Hq + h * G;
   const bool none = len <= 0 || len > a.max_len;
@@ -154,13 +158,6 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
       }
     }
   }
-  // (the query loads are waited for here, not in the loop behind the copies)
-#pragma unroll
-  for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-    for (int y = 0; y < NT; ++y)
-#pragma unroll
-      for (int x = 0; x < KS; ++x) asm volatile("" : "+v"(qop[qt][y][x]));
   // last keys that the wave's first and last row see
   const int wave_hi0 = first + min(wrow0, R - 1) / G - sp.gap;
   const int wave_hi1 = first + min(wrow0 + 16 * QT - 1, R - 1) / G - sp.gap;
@@ -275,25 +272,26 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
     }
   };
 
-  int koff[KS], voff[DT];
-#pragma unroll
-  for (int x = 0; x < KS; ++x) koff[x] = li * C::kRow + (((gq * KS + x) ^ C::swz_k(li)) * 16);
-  {
-    const int vrow = 4 * gq + (li >> 2);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      voff[dt] = C::kTile + vrow * C::kRow + (((dt * 2 + ((li & 3) >> 1)) ^ C::swz_v(vrow)) * 16) + (li & 1) * 8;
-  }
+  // A lane's reads of a row's chunks: their offsets differ in the chunk's bits alone, so one
+  // is kept and the others are formed where they are used (registers are what the loop is
+  // short of).
+  static_assert((KS & (KS - 1)) == 0, "XOR of the chunk");
+  const int koff = li * C::kRow + (((gq * KS) ^ C::swz_k(li)) * 16);
+  const int vrow = 4 * gq + (li >> 2);
+  const int voff = C::kTile + vrow * C::kRow + ((((li & 3) >> 1) ^ C::swz_v(vrow)) * 16) + (li & 1) * 8;
 
-  // whether key v is seen by the query whose last key is hi
-  auto sees = [&](int v, int hi) __attribute__((always_inline)) { return v <= hi && (v > hi - a.window || v < a.sink); };
+  // whether key v is seen by the query whose last key is hi; the window's part alone
+  auto within = [&](int v, int hi) __attribute__((always_inline)) { return (uint32_t)(hi - v) < (uint32_t)a.window; };
+  auto sees = [&](int v, int hi) __attribute__((always_inline)) { return within(v, hi) || (v <= hi && v < a.sink); };
   floatx4 sv[QT][4];
   auto phase_a = [&](const char* st, int k0, auto masked) __attribute__((always_inline)) {
+    int at = koff;
+    asm volatile("" : "+v"(at));
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
       for (int x = 0; x < KS; ++x) {
-        const bf16x8 ka = *(const bf16x8*)(st + koff[x] + kt * 16 * C::kRow);
+        const bf16x8 ka = *(const bf16x8*)(st + (at ^ (x * 16)) + kt * 16 * C::kRow);
 #pragma unroll
         for (int y = NT - 1; y >= 0; --y)
 #pragma unroll
@@ -302,35 +300,42 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
                 ka, qop[qt][y][x], x == 0 && y == NT - 1 ? floatx4{0.f, 0.f, 0.f, 0.f} : sv[qt][kt], 0, 0, 0);
       }
     }
+    // (no key past k_hi is seen: where a split ends inside a chunk, the span does)
     if constexpr (decltype(masked)::value) {
+      auto mask = [&](auto with_sinks) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        const int v = k0 + kt * 16 + 4 * gq;
+        for (int kt = 0; kt < 4; ++kt) {
+          const int v = k0 + kt * 16 + 4 * gq;
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt)
+          for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (v + r >= k_hi || !sees(v + r, qhi[qt])) sv[qt][kt][r] = kNegInf;
-      }
+            for (int r = 0; r < 4; ++r) {
+              const bool seen = decltype(with_sinks)::value ? sees(v + r, qhi[qt]) : within(v + r, qhi[qt]);
+              if (!seen) sv[qt][kt][r] = kNegInf;
+            }
+        }
+      };
+      if (k0 < a.sink) mask(std::true_type{});
+      else mask(std::false_type{});
     }
   };
-  auto v_operand = [&](const char* st, int jj, int dt) __attribute__((always_inline)) {
-    const v4i16 lo = read_tr(st + voff[dt] + (32 * jj) * C::kRow);
-    const v4i16 hi = read_tr(st + voff[dt] + (32 * jj + 16) * C::kRow);
+  auto v_operand = [&](const char* st, int at, int jj, int dt) __attribute__((always_inline)) {
+    const v4i16 lo = read_tr(st + (at ^ (dt * 32)) + (32 * jj) * C::kRow);
+    const v4i16 hi = read_tr(st + (at ^ (dt * 32)) + (32 * jj + 16) * C::kRow);
     bf16x8 va;
     __builtin_memcpy(&va, &lo, 8);
     __builtin_memcpy((char*)&va + 8, &hi, 8);
     return va;
   };
-  // Whether a value of the chunk is infinite or NaN.  Asked in chunks that some rows see
-  // keys of and others do not: it must not reach those.
+  // Whether a value of the chunk is infinite or NaN.
   auto odd_values = [&](const char* st) __attribute__((always_inline)) {
     uint32_t hit = 0;
+    const int at = voff;
 #pragma unroll
     for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const uint4 w = __builtin_bit_cast(uint4, v_operand(st, jj, dt));
+        const uint4 w = __builtin_bit_cast(uint4, v_operand(st, at, jj, dt));
         hit |= ((w.x & 0x7fff7fffu) + 0x00800080u) | ((w.y & 0x7fff7fffu) + 0x00800080u) |
                ((w.z & 0x7fff7fffu) + 0x00800080u) | ((w.w & 0x7fff7fffu) + 0x00800080u);
       }
@@ -370,6 +375,8 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
         for (int y = 0; y < NT; ++y) pb[qt][y][jj] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
       }
     }
+    int at = voff;
+    asm volatile("" : "+v"(at));
     if constexpr (NT > 1) {
       // A chunk's products are summed from zero, smallest terms first, and added once: a
       // running sum over thousands of keys is rounded once a chunk, not with each of its six
@@ -382,7 +389,7 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int jj = 0; jj < 2; ++jj) va[i][jj] = v_operand(st, jj, dt + i);
+          for (int jj = 0; jj < 2; ++jj) va[i][jj] = v_operand(st, at, jj, dt + i);
 #pragma unroll
         for (int y = NT - 1; y >= 0; --y)
 #pragma unroll
@@ -404,7 +411,7 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
       for (int jj = 0; jj < 2; ++jj) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-          bf16x8 va = v_operand(st, jj, dt);
+          bf16x8 va = v_operand(st, at, jj, dt);
           if constexpr (decltype(careful)::value) {
             uint32_t w[4];
             __builtin_memcpy(w, &va, 16);
@@ -449,8 +456,15 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
     }
   };
 
-  if (n_chunks > 0) {
+  auto walk = [&](auto careful) __attribute__((always_inline)) {
     load_segment();
+    // (the query loads are waited for here, not in the loop behind the copies)
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+      for (int y = 0; y < NT; ++y)
+#pragma unroll
+        for (int x = 0; x < KS; ++x) asm volatile("" : "+v"(qop[qt][y][x]));
     lds_barrier();
     if constexpr (Q8) {
       if (stager) {
@@ -503,14 +517,40 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
         }
       }
       if (work) {
-        bool careful = false;
-        if constexpr (!Q8) careful = masked && odd_values(st);
-        if constexpr (!Q8) {
-          if (careful) phase_b(st, k0, std::true_type{});
-          else phase_b(st, k0, std::false_type{});
-        } else {
-          phase_b(st, k0, std::false_type{});
+        if (decltype(careful)::value && masked && odd_values(st)) phase_b(st, k0, careful);
+        else phase_b(st, k0, std::false_type{});
+      }
+    }
+  };
+  if (n_chunks > 0) {
+    walk(std::false_type{});
+    if constexpr (!Q8) {
+      // An infinite or NaN value that a row does not see has met its weight of 0 in the
+      // products: where a result is not finite (codes are), all over again with such
+      // values apart.  (Asked in every chunk that some rows see keys of and others do not,
+      // it took 12 of 113 us: 4 x 1024 queries in a window of 1024.)
+      bool odd = false;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        float x = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][dt]));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x = fmaf(o[qt][dt][r], 0.f, x);
         }
+        odd |= !(x == 0.f);
+      }
+      if (__syncthreads_or(odd)) {
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          m[qt] = kMaxFloor;
+          lsum[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) o[qt][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+        seg_end = k_lo;
+        walk(std::true_type{});
       }
     }
   }
