@@ -12,7 +12,8 @@ constexpr int kAppendThreads = 256;
 
 // Status of listed sequence j, by all threads of a workgroup; the same value
 // in each.  counted: seq_lens holds the new tokens already.
-__device__ inline int append_status(const Geom& g, int n, const int32_t* __restrict__ seqs, int n_new,
+template <class G>   // Geom, or its fields named here
+__device__ inline int append_status(const G& g, int n, const int32_t* __restrict__ seqs, int n_new,
                              const int32_t* __restrict__ bt, const int32_t* __restrict__ seq_lens, int j, bool counted = false) {
   const int s = seqs[j];
   if (s < 0 || s >= g.n_seqs) return KARA_SEQ_BAD_INDEX;

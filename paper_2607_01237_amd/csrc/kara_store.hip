@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "kara_append.h"
+#include "kara_call.h"
 #include "kara_q8_device.h"
 #include "kara_rope.h"
 
@@ -20,8 +21,8 @@ constexpr int kTile = 32;             // tokens that share a table of angles
 constexpr int kGroupHeads = 16;       // KV heads of a unit
 constexpr int kMaxOctets = 1 << 28;   // of a token: 32-bit offsets
 
-struct Store {
-  Geom g;
+struct StoreHead {
+  Dims g;
   int n, n_new, n_layers, counted;
   int units, groups;                  // per (layer, sequence): runs of tokens, groups of KV heads
   int half;                           // pairs that turn; 0: none
@@ -31,7 +32,10 @@ struct Store {
   int32_t *seq_lens, *rope_pos, *status;
   const char *q, *k_new, *v_new;
   char* q_out;
-  PoolPtrs kp, vp, ksp, vsp;
+};
+template <int NL>
+struct Store : StoreHead {
+  Pools<NL> kp, vp, ksp, vsp;
 };
 
 // Eight values as they lie in memory
@@ -90,7 +94,7 @@ struct Angles {
 
 // cos and sin of `count` tokens from rotary position pos on, by all threads
 template <int D, int THREADS>
-__device__ __forceinline__ void fill_angles(Angles<D>& t, const Store& a, int64_t pos, int count) {
+__device__ __forceinline__ void fill_angles(Angles<D>& t, const StoreHead& a, int64_t pos, int count) {
   for (int x = threadIdx.x; x < count * a.half; x += THREADS) {
     const int tok = x / a.half, i = x - tok * a.half;
     const double rev = (double)(pos + tok) * t.rev[i];
@@ -102,7 +106,7 @@ __device__ __forceinline__ void fill_angles(Angles<D>& t, const Store& a, int64_
 }
 
 template <int D, int THREADS>
-__device__ __forceinline__ void fill_frequencies(Angles<D>& t, const Store& a) {
+__device__ __forceinline__ void fill_frequencies(Angles<D>& t, const StoreHead& a) {
   constexpr double kPerTurn = 0.15915494309189533576888376337251;   // 1 / 2 pi
   for (int i = threadIdx.x; i < a.half; i += THREADS)
     t.rev[i] = (a.inv_freq ? (double)a.inv_freq[i] : exp2(-a.step * i)) * kPerTurn;
@@ -150,14 +154,14 @@ __device__ __forceinline__ uint32_t finite_top(float (&x)[8], bool* odd) {
 // their query heads, by all threads.  8 bits: the tokens that fall into one page, as its
 // scale is formed of all of them; a wave takes a (K|V, head) at a time.  Rows: 32 tokens.
 // Returns whether a value to be quantised was not finite.
-template <int DT, int D, bool Q8, int THREADS>
-__device__ __forceinline__ bool store_unit(const Store& a, Angles<D>& t, uint32_t (&tops)[2 * kGroupHeads], uint32_t (&bytes)[2 * kGroupHeads], int j, int l,
+template <int DT, int D, bool Q8, int THREADS, int NL>
+__device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uint32_t (&tops)[2 * kGroupHeads], uint32_t (&bytes)[2 * kGroupHeads], int j, int l,
                                            int unit, int grp, int s, int pos0, int64_t rot0) {
   constexpr int kItems = D / 16;                 // of a row
   constexpr int kRow = D * (DT == KARA_BF16 ? 2 : 4), kOct = kRow / (D / 8);
   constexpr int kWaves = THREADS / 64;
   constexpr int kHeld = kTile * kItems / 64;     // items of a lane, of one head's tile
-  const Geom& g = a.g;
+  const Dims& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h0 = grp * kGroupHeads, heads = min(kGroupHeads, g.Hkv - h0);
@@ -319,19 +323,19 @@ __device__ __forceinline__ bool store_unit(const Store& a, Angles<D>& t, uint32_
   return odd;
 }
 
-__device__ __forceinline__ void start_of(const Store& a, int s, int* pos0, int64_t* rot0) {
+__device__ __forceinline__ void start_of(const StoreHead& a, int s, int* pos0, int64_t* rot0) {
   const int back = a.counted ? a.n_new : 0;
   *pos0 = a.seq_lens[s] - back;
   *rot0 = a.rope_pos ? (int64_t)a.rope_pos[s] - back : *pos0;
 }
 
-__global__ __launch_bounds__(kAppendThreads) void store_check_kernel(Store a) {
+__global__ __launch_bounds__(kAppendThreads) void store_check_kernel(StoreHead a) {
   const int st = append_status(a.g, a.n, a.seqs, a.n_new, a.bt, a.seq_lens, blockIdx.x, a.counted != 0);
   if (threadIdx.x == 0) a.status[blockIdx.x] = st;
 }
 
 // (after the rows, so that a call that could not make their launch counts nothing)
-__global__ __launch_bounds__(kAppendThreads) void store_commit_kernel(Store a) {
+__global__ __launch_bounds__(kAppendThreads) void store_commit_kernel(StoreHead a) {
   const int j = blockIdx.x * kAppendThreads + threadIdx.x;
   if (j < a.n && (a.status[j] & ~KARA_SEQ_NONFINITE) == 0) {
     a.seq_lens[a.seqs[j]] += a.n_new;
@@ -340,8 +344,8 @@ __global__ __launch_bounds__(kAppendThreads) void store_commit_kernel(Store a) {
 }
 
 // Grid (sequence x unit, layer, group of heads), between the check and the commit.
-template <int DT, int D, bool Q8>
-__global__ __launch_bounds__(kStoreThreads) void store_kernel(Store a) {
+template <int DT, int D, bool Q8, int NL>
+__global__ __launch_bounds__(kStoreThreads) void store_kernel(Store<NL> a) {
   __shared__ __attribute__((aligned(16))) Angles<D> t;
   __shared__ uint32_t tops[2 * kGroupHeads], bytes[2 * kGroupHeads];
   const int j = blockIdx.x / a.units, unit = blockIdx.x - j * a.units;
@@ -359,8 +363,8 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(Store a) {
 
 // A few new tokens: one workgroup per listed sequence checks it, appends all its rows and
 // commits, in one launch.
-template <int DT, int D, bool Q8>
-__global__ __launch_bounds__(kFewThreads) void store_few_kernel(Store a) {
+template <int DT, int D, bool Q8, int NL>
+__global__ __launch_bounds__(kFewThreads) void store_few_kernel(Store<NL> a) {
   __shared__ __attribute__((aligned(16))) Angles<D> t;
   __shared__ uint32_t tops[2 * kGroupHeads], bytes[2 * kGroupHeads];
   const int j = blockIdx.x;
@@ -393,10 +397,10 @@ __global__ __launch_bounds__(kFewThreads) void store_few_kernel(Store a) {
 
 constexpr int kReadUnroll = 4;
 
-template <int DT, int D>
+template <int DT, int D, int NL>
 __global__ __launch_bounds__(kStoreThreads) void q8_read_kernel(
-    Geom g, int n, const int32_t* __restrict__ seqs, const int32_t* __restrict__ start, int n_rows, int toks, int chunks,
-    PoolPtrs kp, PoolPtrs vp, PoolPtrs ksp, PoolPtrs vsp, const int32_t* __restrict__ bt,
+    Dims g, int n, const int32_t* __restrict__ seqs, const int32_t* __restrict__ start, int n_rows, int toks, int chunks,
+    Pools<NL> kp, Pools<NL> vp, Pools<NL> ksp, Pools<NL> vsp, const int32_t* __restrict__ bt,
     const int32_t* __restrict__ seq_lens, char* __restrict__ k_out, char* __restrict__ v_out) {
   constexpr int kOctets = D / 8, kOct = DT == KARA_BF16 ? 16 : 32;
   const int j = blockIdx.x / chunks;
@@ -463,28 +467,22 @@ bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 22);
 
 bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && n_layers <= kMaxLayersPerLaunch; }
 
-PoolPtrs ptrs(const void* const* pools, int n_layers) {
-  PoolPtrs x{};
-  for (int i = 0; pools && i < n_layers; ++i) x.p[i] = const_cast<void*>(pools[i]);
-  return x;
-}
-
-template <int DT, int D, bool Q8>
-kara_status_t launch_store(const Store& a, hipStream_t s) {
+template <int DT, int D, bool Q8, int NL>
+kara_status_t launch_store(const Store<NL>& a, hipStream_t s) {
   // a few units in all: one workgroup a sequence
   if ((int64_t)a.n_layers * a.units * a.groups <= 4) {
-    hipLaunchKernelGGL((store_few_kernel<DT, D, Q8>), dim3((unsigned)a.n), dim3(kFewThreads), 0, s, a);
+    hipLaunchKernelGGL((store_few_kernel<DT, D, Q8, NL>), dim3((unsigned)a.n), dim3(kFewThreads), 0, s, a);
     return hip_status(hipGetLastError());
   }
-  hipLaunchKernelGGL(store_check_kernel, dim3((unsigned)a.n), dim3(kAppendThreads), 0, s, a);
+  hipLaunchKernelGGL(store_check_kernel, dim3((unsigned)a.n), dim3(kAppendThreads), 0, s, (const StoreHead&)a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
-  hipLaunchKernelGGL((store_kernel<DT, D, Q8>), dim3((unsigned)(a.n * a.units), (unsigned)a.n_layers, (unsigned)a.groups),
+  hipLaunchKernelGGL((store_kernel<DT, D, Q8, NL>), dim3((unsigned)(a.n * a.units), (unsigned)a.n_layers, (unsigned)a.groups),
                      dim3(kStoreThreads), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.counted) return hip_status(e);
   hipLaunchKernelGGL(store_commit_kernel, dim3((unsigned)((a.n + kAppendThreads - 1) / kAppendThreads)),
-                     dim3(kAppendThreads), 0, s, a);
+                     dim3(kAppendThreads), 0, s, (const StoreHead&)a);
   return hip_status(hipGetLastError());
 }
 
@@ -494,10 +492,11 @@ kara_status_t store(const kara_params_t* p, const kara_rope_t* rope, int32_t n, 
                     void* const* k_pools, void* const* v_pools, void* const* k_scales, void* const* v_scales,
                     const int32_t* block_table, int32_t* seq_lens, int32_t* rope_pos, int32_t counted, int32_t* status,
                     void* stream) {
-  Store a{};
-  const kara_status_t st = make_geom(p, n, &a.g);
+  Geom g;
+  const kara_status_t st = make_geom(p, n, &g);
   if (st != KARA_OK) return st;
-  const Geom& g = a.g;
+  StoreHead a{};
+  a.g = dims_of(g);
   if (!layers_ok(n, n_layers) || n_new < 0 || counted < 0 || counted > 1) return KARA_ERR_INVALID_ARG;
   if (rope) {
     const int dim = rope->dim == 0 ? g.d : rope->dim;
@@ -536,19 +535,23 @@ kara_status_t store(const kara_params_t* p, const kara_rope_t* rope, int32_t n, 
   a.k_new = (const char*)k_new;
   a.v_new = (const char*)v_new;
   a.q_out = (char*)q_out;
-  a.kp = ptrs(k_pools, n_layers);
-  a.vp = ptrs(v_pools, n_layers);
-  a.ksp = ptrs(k_scales, n_layers);
-  a.vsp = ptrs(v_scales, n_layers);
   hipStream_t s = (hipStream_t)stream;
-#define KARA_STORE(DT, D) return q8 ? launch_store<DT, D, true>(a, s) : launch_store<DT, D, false>(a, s)
-  if (g.dtype == KARA_BF16) {
-    if (g.d == 128) KARA_STORE(KARA_BF16, 128);
-    KARA_STORE(KARA_BF16, 64);
-  }
-  if (g.d == 128) KARA_STORE(KARA_F32, 128);
-  KARA_STORE(KARA_F32, 64);
+  auto launch = [&](auto call) {
+    set_pools(&call.kp, k_pools, n_layers);
+    set_pools(&call.vp, v_pools, n_layers);
+    set_pools(&call.ksp, k_scales, n_layers);
+    set_pools(&call.vsp, v_scales, n_layers);
+#define KARA_STORE(DT, D) return q8 ? launch_store<DT, D, true>(call, s) : launch_store<DT, D, false>(call, s)
+    if (g.dtype == KARA_BF16) {
+      if (g.d == 128) KARA_STORE(KARA_BF16, 128);
+      KARA_STORE(KARA_BF16, 64);
+    }
+    if (g.d == 128) KARA_STORE(KARA_F32, 128);
+    KARA_STORE(KARA_F32, 64);
 #undef KARA_STORE
+  };
+  if (n_layers <= kFewLayers) return launch(Store<kFewLayers>{a, {}, {}, {}, {}});
+  return launch(Store<kMaxLayersPerLaunch>{a, {}, {}, {}, {}});
 }
 
 }  // namespace
@@ -598,18 +601,27 @@ kara_status_t kara_q8_read(const kara_params_t* p, int32_t n, const int32_t* seq
   const int64_t chunks = ((int64_t)n_rows + toks - 1) / toks;
   if (!grid_ok(n * chunks)) return KARA_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)(n * chunks), (unsigned)n_layers, 2), block(kStoreThreads);
-#define KARA_Q8_READ(DT, D)                                                                                        \
-  hipLaunchKernelGGL((q8_read_kernel<DT, D>), grid, block, 0, (hipStream_t)stream, g, n, seqs, start, n_rows, toks, \
-                     (int)chunks, ptrs(k_pools, n_layers), ptrs(v_pools, n_layers), ptrs(k_scales, n_layers),      \
-                     ptrs(v_scales, n_layers), block_table, seq_lens, (char*)k_out, (char*)v_out)
-  if (g.dtype == KARA_BF16) {
-    if (g.d == 128) KARA_Q8_READ(KARA_BF16, 128);
-    else KARA_Q8_READ(KARA_BF16, 64);
-  } else {
-    if (g.d == 128) KARA_Q8_READ(KARA_F32, 128);
-    else KARA_Q8_READ(KARA_F32, 64);
-  }
+  auto launch = [&](auto kp) {
+    auto vp = kp, ksp = kp, vsp = kp;
+    set_pools(&kp, k_pools, n_layers);
+    set_pools(&vp, v_pools, n_layers);
+    set_pools(&ksp, k_scales, n_layers);
+    set_pools(&vsp, v_scales, n_layers);
+    constexpr int NL = sizeof(kp) / sizeof(void*);
+#define KARA_Q8_READ(DT, D)                                                                                             \
+  hipLaunchKernelGGL((q8_read_kernel<DT, D, NL>), grid, block, 0, (hipStream_t)stream, dims_of(g), n, seqs, start, n_rows, \
+                     toks, (int)chunks, kp, vp, ksp, vsp, block_table, seq_lens, (char*)k_out, (char*)v_out)
+    if (g.dtype == KARA_BF16) {
+      if (g.d == 128) KARA_Q8_READ(KARA_BF16, 128);
+      else KARA_Q8_READ(KARA_BF16, 64);
+    } else {
+      if (g.d == 128) KARA_Q8_READ(KARA_F32, 128);
+      else KARA_Q8_READ(KARA_F32, 64);
+    }
 #undef KARA_Q8_READ
+  };
+  if (n_layers <= kFewLayers) launch(Pools<kFewLayers>{});
+  else launch(Pools<kMaxLayersPerLaunch>{});
   return hip_status(hipGetLastError());
 }
 

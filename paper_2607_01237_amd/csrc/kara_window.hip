@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "kara_lds.h"
 #include "kara_q8_device.h"
 #include "kara_window.h"
 #include "kara_window_call.h"
@@ -18,10 +19,10 @@ constexpr float kMaxFloor = -3.402823466e38f;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kSplitMin = 256;       // keys per split, at least (the workspace's records are sized for that)
-constexpr int kSplitMax = 2048;
+constexpr int kSplitMin = 512;       // keys per split, at least (of a span of more)
+constexpr int kSplitMax = 4608;      // at most
 constexpr int kSplitRuns = 1024;     // runs of keys a split's LDS table holds
-constexpr int kWgTarget = 4096;      // workgroups a launch keeps when its splits grow
+constexpr int kWgsAtOnce = 512;      // workgroups that run at once, two to a CU
 constexpr int kTileRows = 16;
 
 enum Cache { kRowsBf16, kRowsF32, kCodes };
@@ -35,6 +36,10 @@ struct WinCfg {
   static constexpr int kE = D / 16;                                // columns of a lane
   static constexpr int kVB = kRow / 16;                            // bytes of a value row in a lane
   static constexpr int kVW = kVB / 4;
+  // Blocks of values held: wide rows would take more registers than there are (spilled, they
+  // cost a quarter of a long decoding step).  Then a block's values are on their way while
+  // its logits are formed, the next block's keys behind them.
+  static constexpr int kVBuf = kRow >= 256 ? 1 : 2;
 };
 
 // One workgroup of four waves per (layer, sequence, KV head, tile of 16 query rows, split
@@ -53,8 +58,8 @@ struct WinCfg {
 //
 // Rows of fp32 go through the fp32 matrix instructions.  NT: bf16 terms of a query and of
 // a weight over codes (3 where p->dtype is fp32: 24 bits; codes are exact in one).
-template <Cache CT, int NT, int D>
-__global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a) {
+template <Cache CT, int NT, int D, int NL>
+__global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<NL> a) {
   using C = WinCfg<CT, D>;
   constexpr int TB = C::kTB, KC = C::kKC, E = C::kE, VW = C::kVW;
   constexpr bool F32 = CT == kRowsF32;
@@ -71,7 +76,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
   __shared__ float red_m[kWaves][16], red_l[kWaves][16];
   Table& tab = lds.t;
 
-  const Geom& g = a.g;
+  const Dims& g = a.g;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -99,14 +104,20 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
   const Span sp = span_of(none ? 0 : len, T, G, row0, row0 + rows, a.window, a.sink);
   const int k0 = split * a.split_keys;
   if (none || k0 >= sp.n) {
-    // no keys: zero rows where no combine kernel follows
-    if (a.n_splits == 1)
-      for (int i = tid; i < rows * D; i += kThreads) {
-        const int r = row0 + i / D;
-        const int64_t at = (orow + (int64_t)(r / G) * g.Hq + r % G) * D + i % D;
-        if constexpr (kOutBf16) ((__bf16*)a.out)[at] = (__bf16)0.f;
-        else ((float*)a.out)[at] = 0.f;
+    // no keys: zero rows, or a record of no weight where the combine kernel follows
+    if (a.n_splits > 1) {
+      if (tid < rows) {
+        const int r = row0 + tid;
+        *(floatx2*)(a.rec_ml + 2 * ((orow + (int64_t)(r / G) * g.Hq + r % G) * a.n_splits + split)) = floatx2{kMaxFloor, 0.f};
       }
+      return;
+    }
+    for (int i = tid; i < rows * D; i += kThreads) {
+      const int r = row0 + i / D;
+      const int64_t at = (orow + (int64_t)(r / G) * g.Hq + r % G) * D + i % D;
+      if constexpr (kOutBf16) ((__bf16*)a.out)[at] = (__bf16)0.f;
+      else ((float*)a.out)[at] = 0.f;
+    }
     return;
   }
   const int nk = min(sp.n - k0, a.split_keys);                // keys of this split
@@ -143,19 +154,86 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
     }
   }
   // Pool rows of the split's keys: runs of 2^run keys lie in one page, an entry each.
-  // (Keys that no row sees may be on no page: any row of the pool stands for them.)
+  // (Keys that no row sees may be on no page: any row of the pool stands for them.)  The
+  // scales go to LDS behind the first block's loads.
   const int run = a.run;
+  const int runs = (nblk * C::kBlock) >> run;
+  constexpr int kEntries = kSplitRuns / kThreads;
+  uint32_t scale_pair[kEntries];
   {
     const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
-    for (int i = tid; i < (nblk * C::kBlock) >> run; i += kThreads) {
-      const int pos = sp.position(k0 + min(i << run, (nk - 1) >> run << run));
-      const int b = pos / g.bs;
-      const int page = min(max(row_pages[b], 0), g.num_pages - 1);
-      const uint32_t unit = (uint32_t)page * (uint32_t)g.Hkv + (uint32_t)h;
-      tab.row[i] = unit * (uint32_t)g.bs + (uint32_t)(pos - b * g.bs);
-      if constexpr (CT == kCodes)
-        tab.scale[i] = (uint32_t)((const uint8_t*)a.ksp.p[l])[unit] | (uint32_t)((const uint8_t*)a.vsp.p[l])[unit] << 16;
+#pragma unroll
+    for (int k = 0; k < kEntries; ++k) {
+      const int i = tid + k * kThreads;
+      if (i < runs) {
+        const int pos = sp.position(k0 + min(i << run, (nk - 1) >> run << run));
+        const int b = pos / g.bs;
+        const int page = min(max(row_pages[b], 0), g.num_pages - 1);
+        const uint32_t unit = (uint32_t)page * (uint32_t)g.Hkv + (uint32_t)h;
+        tab.row[i] = unit * (uint32_t)g.bs + (uint32_t)(pos - b * g.bs);
+        if constexpr (CT == kCodes)
+          scale_pair[k] = (uint32_t)((const uint8_t*)a.ksp.p[l])[unit] | (uint32_t)((const uint8_t*)a.vsp.p[l])[unit] << 16;
+      }
     }
+  }
+  lds_barrier();
+  const char* kbase = (const char*)a.kp.p[l] + gq * 16;
+  const char* vbase = (const char*)a.vp.p[l] + li * (C::kVB < 16 ? C::kVB : 16);
+  const int run_mask = (1 << run) - 1;
+  // (padding keys past the last one repeat it)
+  auto row_of = [&](int key) __attribute__((always_inline)) {
+    key = min(key, nk - 1);
+    return tab.row[key >> run] + (uint32_t)(key & run_mask);
+  };
+  auto scale_of = [&](int key) __attribute__((always_inline)) { return tab.scale[min(key, nk - 1) >> run]; };
+  uint4 kb[2][TB][KC];
+  uint32_t vb[C::kVBuf][TB][4][VW];
+  auto load_k = [&](int blk, int b) __attribute__((always_inline)) {
+    uint64_t kat[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) kat[t] = (uint64_t)row_of(blk * C::kBlock + t * 16 + li) * C::kRow;
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int x = 0; x < KC; ++x) kb[b][t][x] = *(const uint4*)(kbase + kat[t] + x * 64);
+  };
+  auto load_v = [&](int blk, int b) __attribute__((always_inline)) {
+    uint64_t vat[TB][4];
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) vat[t][r] = (uint64_t)row_of(blk * C::kBlock + t * 16 + 4 * gq + r) * C::kRow;
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const char* src = vbase + vat[t][r];
+        if constexpr (VW == 1) {
+          vb[b][t][r][0] = *(const uint32_t*)src;
+        } else if constexpr (VW == 2) {
+          const uint2 v = *(const uint2*)src;
+          vb[b][t][r][0] = v.x, vb[b][t][r][1] = v.y;
+        } else {
+          // (fp32 at d = 128: columns 4li.. and 64 + 4li..)
+#pragma unroll
+          for (int y = 0; y < VW / 4; ++y) {
+            const uint4 v = *(const uint4*)(src + y * 256);
+            vb[b][t][r][4 * y] = v.x, vb[b][t][r][4 * y + 1] = v.y, vb[b][t][r][4 * y + 2] = v.z, vb[b][t][r][4 * y + 3] = v.w;
+          }
+        }
+      }
+  };
+
+  constexpr int V1 = C::kVBuf - 1;
+  if (wave < nblk) {
+    load_k(wave, 0);
+    if constexpr (V1) load_v(wave, 0);
+  }
+  if constexpr (CT == kCodes) {
+#pragma unroll
+    for (int k = 0; k < kEntries; ++k)
+      if (tid + k * kThreads < runs) tab.scale[tid + k * kThreads] = scale_pair[k];
+    lds_barrier();
   }
   bf16x8 qa[F32 ? 1 : NT][KS];
   if constexpr (!F32) {
@@ -179,51 +257,6 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
 #pragma unroll
     for (int x = 0; x < KC; ++x) qraw[x] = there ? qraw[x] : uint4{0, 0, 0, 0};
   }
-  __syncthreads();
-
-  const char* kbase = (const char*)a.kp.p[l] + gq * 16;
-  const char* vbase = (const char*)a.vp.p[l] + li * (C::kVB < 16 ? C::kVB : 16);
-  const int run_mask = (1 << run) - 1;
-  // (padding keys past the last one repeat it)
-  auto row_of = [&](int key) __attribute__((always_inline)) {
-    key = min(key, nk - 1);
-    return tab.row[key >> run] + (uint32_t)(key & run_mask);
-  };
-  auto scale_of = [&](int key) __attribute__((always_inline)) { return tab.scale[min(key, nk - 1) >> run]; };
-  uint4 kb[2][TB][KC];
-  uint32_t vb[2][TB][4][VW];
-  auto load = [&](int blk, int b) __attribute__((always_inline)) {
-    uint64_t kat[TB], vat[TB][4];
-#pragma unroll
-    for (int t = 0; t < TB; ++t) {
-      kat[t] = (uint64_t)row_of(blk * C::kBlock + t * 16 + li) * C::kRow;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) vat[t][r] = (uint64_t)row_of(blk * C::kBlock + t * 16 + 4 * gq + r) * C::kRow;
-    }
-#pragma unroll
-    for (int t = 0; t < TB; ++t)
-#pragma unroll
-      for (int x = 0; x < KC; ++x) kb[b][t][x] = *(const uint4*)(kbase + kat[t] + x * 64);
-#pragma unroll
-    for (int t = 0; t < TB; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const char* src = vbase + vat[t][r];
-        if constexpr (VW == 1) {
-          vb[b][t][r][0] = *(const uint32_t*)src;
-        } else if constexpr (VW == 2) {
-          const uint2 v = *(const uint2*)src;
-          vb[b][t][r][0] = v.x, vb[b][t][r][1] = v.y;
-        } else {
-          // (fp32 at d = 128: columns 4li.. and 64 + 4li..)
-#pragma unroll
-          for (int y = 0; y < VW / 4; ++y) {
-            const uint4 v = *(const uint4*)(src + y * 256);
-            vb[b][t][r][4 * y] = v.x, vb[b][t][r][4 * y + 1] = v.y, vb[b][t][r][4 * y + 2] = v.z, vb[b][t][r][4 * y + 3] = v.w;
-          }
-        }
-      }
-  };
 
   float m = kMaxFloor, lsum = 0.f;   // query li's reference, and this lane's part of its sum
   floatx4 lones = {0.f, 0.f, 0.f, 0.f};   // bf16: the sum, in every element
@@ -239,7 +272,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
   const int all_lo = sp.i1 - a.window + 1 - sp.gap, all_hi = sp.i0 - sp.gap;
   auto in = [&](int v, int lo, int hi) __attribute__((always_inline)) { return v <= hi && (v >= lo || v < a.sink); };
 
-  auto work = [&](int blk, int b) __attribute__((always_inline)) {
+  auto work = [&](int blk, int b, int vbuf) __attribute__((always_inline)) {
     floatx4 sv[TB];
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
@@ -284,12 +317,12 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
           const float scale = q8_scale(scale_of(blk * C::kBlock + t * 16 + 4 * gq + r) >> 16);
 #pragma unroll
           for (int y = 0; y < VW; ++y) {
-            pv[4 * t + r][2 * y] = q8_pair<false>(vb[b][t][r][y], scale);
-            pv[4 * t + r][2 * y + 1] = q8_pair<true>(vb[b][t][r][y], scale);
+            pv[4 * t + r][2 * y] = q8_pair<false>(vb[vbuf][t][r][y], scale);
+            pv[4 * t + r][2 * y + 1] = q8_pair<true>(vb[vbuf][t][r][y], scale);
           }
         } else {
 #pragma unroll
-          for (int y = 0; y < VP; ++y) pv[4 * t + r][y] = vb[b][t][r][y];
+          for (int y = 0; y < VP; ++y) pv[4 * t + r][y] = vb[vbuf][t][r][y];
         }
       }
     const int v0 = k0 + blk * C::kBlock;
@@ -420,22 +453,31 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
       }
     }
   };
+  // the next block's keys after this block's values, so that waiting for the values
+  // leaves the keys on their way
   if (wave < nblk) {
-    load(wave, 0);
     int blk = wave;
     for (;;) {
       const int n1 = blk + kWaves;
-      if (n1 < nblk) load(n1, 1);
-      work(blk, 0);
+      if constexpr (!V1) load_v(blk, 0);
+      if (n1 < nblk) {
+        load_k(n1, 1);
+        if constexpr (V1) load_v(n1, 1);
+      }
+      work(blk, 0, 0);
       if (n1 >= nblk) break;
       blk = n1 + kWaves;
-      if (blk < nblk) load(blk, 0);
-      work(n1, 1);
+      if constexpr (!V1) load_v(n1, 0);
+      if (blk < nblk) {
+        load_k(blk, 0);
+        if constexpr (V1) load_v(blk, 0);
+      }
+      work(n1, 1, V1);
       if (blk >= nblk) break;
     }
   }
 
-  // ---- the four waves' sums ----
+  // ---- the waves' sums ----
 #pragma unroll
   for (int e = 0; e < E; ++e) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[e]));   // (as above, past the loop's branch)
   if constexpr (kOutBf16) {
@@ -458,7 +500,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
       *(floatx4*)&lds.o[wave][li][col] = floatx4{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]};
     }
   __syncthreads();
-  const bool direct = sp.n <= a.split_keys;
+  const bool direct = a.n_splits == 1;
   for (int x = tid; x < rows * D; x += kThreads) {
     const int i = x / D, e = x - i * D;
     // (a wave without keys left its start: a maximum below all, sums of 0)
@@ -485,76 +527,74 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCall a)
   }
 }
 
-// One wave per output row whose tile's span is longer than one split: its splits'
-// records joined.
+// One wave per output row: its splits' records joined, those without keys as weights of 0
+// (their sums were not written).  Nothing is looked up but the records, and those of up to
+// eight splits are all asked for at once: a launch of a few rows takes as long as its loads
+// that wait for others.
 template <int D, bool OUT_BF16>
-__global__ __launch_bounds__(256) void window_combine_kernel(WindowCall a, int64_t n_rows) {
-  constexpr int kDPerLane = D / 64;
-  const Geom& g = a.g;
+__global__ __launch_bounds__(256) void window_combine_kernel(const float* __restrict__ rec_o, const float* __restrict__ rec_ml,
+                                                             void* __restrict__ out, int n_splits, int64_t n_rows) {
+  constexpr int kDPerLane = D / 64, kAtOnce = 8;
+  typedef float floatd __attribute__((ext_vector_type(kDPerLane)));
   const int lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);   // (l, j, t, hq)
   if (row >= n_rows) return;
-  const int64_t lj = row / ((int64_t)g.Hq * a.T);
-  const int in_seq = (int)(row - lj * ((int64_t)g.Hq * a.T));
-  const int s = a.seqs[lj % a.n];
-  const int len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
-  const bool none = len <= 0 || len > a.max_len;
-  const int t = in_seq / g.Hq, r = t * g.G + (in_seq - t * g.Hq) % g.G;
-  const int row0 = r / a.rows * a.rows;
-  const Span sp = span_of(none ? 0 : len, a.T, g.G, row0, min(row0 + a.rows, g.G * a.T), a.window, a.sink);
+  const floatx2* ml = (const floatx2*)rec_ml + row * n_splits;
+  const float* v = rec_o + row * n_splits * D + lane * kDPerLane;
+  auto load = [&](int from, floatd (&x)[kAtOnce]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) __builtin_memcpy(&x[i], v + (int64_t)min(from + i, n_splits - 1) * D, sizeof(x[i]));
+  };
+  floatd x[kAtOnce];
+  load(0, x);
+  // lane i: split i's maximum and sum, 64 at a time, the first kept
+  const floatx2 first = lane < n_splits ? ml[lane] : floatx2{kMaxFloor, 0.f};
+  float M = first[0];
+  for (int i = lane + 64; i < n_splits; i += 64) M = fmaxf(M, ml[i][0]);
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) M = fmaxf(M, __shfl_xor(M, i, 64));
   float L = 0.f, acc[kDPerLane] = {};
-  if (!none && sp.n > 0) {
-    if (sp.n <= a.split_keys) return;   // the split kernel wrote it
-    const int ns = (sp.n + a.split_keys - 1) / a.split_keys;
-    const float* ml = a.rec_ml + row * a.n_splits * 2;
-    // lane i: split i's maximum and sum, 64 at a time, the first kept
-    const float m0 = lane < ns ? ml[2 * lane] : kMaxFloor, l0 = lane < ns ? ml[2 * lane + 1] : 0.f;
-    float M = m0;
-    for (int x = lane + 64; x < ns; x += 64) M = fmaxf(M, ml[2 * x]);
+  for (int s0 = 0; s0 < n_splits; s0 += 64) {
+    const floatx2 mine = s0 == 0 ? first : s0 + lane < n_splits ? ml[s0 + lane] : floatx2{kMaxFloor, 0.f};
+    const float f = __builtin_amdgcn_exp2f(mine[0] - M), lf = mine[1] * f;
+    const int cnt = min(64, n_splits - s0);
+    for (int i0 = 0; i0 < cnt; i0 += kAtOnce) {
+      if (s0 + i0 > 0) load(s0 + i0, x);
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x, 64));
-    for (int sp0 = 0; sp0 < ns; sp0 += 64) {
-      const int x = sp0 + lane;
-      const float ms = sp0 == 0 ? m0 : x < ns ? ml[2 * x] : kMaxFloor;
-      const float f = __builtin_amdgcn_exp2f(ms - M);
-      const float lf = (sp0 == 0 ? l0 : x < ns ? ml[2 * x + 1] : 0.f) * f;
-      const int cnt = min(64, ns - sp0);
-      const float* v = a.rec_o + (row * a.n_splits + sp0) * D + lane * kDPerLane;
-      // (four records at once; past the last a record of weight 0 is read again)
-      for (int i = 0; i < cnt; i += 4) {
-        float y4[4][kDPerLane];
+      for (int i = 0; i < kAtOnce; ++i) {
+        // (a record's sum of weights may be NaN, as its row is then: not 0)
+        const float fi = __shfl(f, i0 + i, 64), li = __shfl(lf, i0 + i, 64);
+        const bool in = i0 + i < cnt && __shfl(mine[1], i0 + i, 64) != 0.f;
+        if (in) {
+          L += li;
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-#pragma unroll
-          for (int e = 0; e < kDPerLane; ++e) y4[y][e] = v[min(i + y, cnt - 1) * D + e];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          if (i + y >= cnt) break;
-          const float fi = __shfl(f, i + y, 64);
-          L += __shfl(lf, i + y, 64);
-#pragma unroll
-          for (int e = 0; e < kDPerLane; ++e) acc[e] = fmaf(y4[y][e], fi, acc[e]);
+          for (int e = 0; e < kDPerLane; ++e) acc[e] = fmaf(x[i][e], fi, acc[e]);
         }
       }
     }
   }
 #pragma unroll
   for (int e = 0; e < kDPerLane; ++e) {
-    const float v = L == 0.f ? 0.f : acc[e] / L;   // (a row that sees no key)
-    if constexpr (OUT_BF16) ((__bf16*)a.out)[row * D + lane * kDPerLane + e] = (__bf16)v;
-    else ((float*)a.out)[row * D + lane * kDPerLane + e] = v;
+    const float y = L == 0.f ? 0.f : acc[e] / L;   // (a row that sees no key)
+    if constexpr (OUT_BF16) ((__bf16*)out)[row * D + lane * kDPerLane + e] = (__bf16)y;
+    else ((float*)out)[row * D + lane * kDPerLane + e] = y;
   }
 }
 
 int run_of(int bs) { return std::min(4, __builtin_ctz((unsigned)bs)); }
 
-// Keys per split: 256 while the launch has few workgroups, up to 2048 (1024 where pages
-// give runs of one key) where 16 workgroups per CU remain: fewer records and prologues.
+// Splits of a span into parts of one length, a multiple of 64: as many as run at once with
+// the other tiles', each of 512 keys at least, or as the longest parts make where there are
+// more tiles than that.  Parts of 256, 512, 1K, 2K keys, us: 8 sequences of 300-4000 tokens,
+// 64 tiles 29.9, 22.7, 22.5, 28.9; 13 x 5 queries of 16 heads, 78 tiles 24.4, 21.4, 23.0,
+// 30.2.  Parts of 1K, 2K, 4.1K, whole: 96 x 2 layers of 8K, 1536 tiles 566, 539, 532, 516; a
+// window of 4096 there 577, 561, 541; of 64 sequences, 512 tiles 138, 132, 124.  (Whole
+// sequences of all lengths would end with the longest.)
 int split_most(int bs) { return std::min(kSplitMax, kSplitRuns << run_of(bs)); }
 int split_keys_of(int bs, int64_t tiles, int span) {
-  int keys = kSplitMin;
-  while (keys < split_most(bs) && tiles * ((span + 2 * keys - 1) / (2 * keys)) >= kWgTarget) keys *= 2;
-  return keys;
+  const int64_t longest = split_most(bs), few = ((int64_t)span + kSplitMin - 1) / kSplitMin;
+  const int64_t n = std::min(few, std::max((span + longest - 1) / longest, (kWgsAtOnce + tiles - 1) / tiles));
+  return (int)(((span + n - 1) / n + 63) / 64 * 64);
 }
 
 // Up to this many query rows per (layer, sequence, KV head) go through the split kernel,
@@ -567,16 +607,27 @@ bool grid_ok(int64_t blocks) { return blocks > 0 && blocks < ((int64_t)1 << 24);
 
 bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && n_layers <= kMaxLayersPerLaunch; }
 
-PoolPtrs ptrs(const void* const* pools, int n_layers) {
-  PoolPtrs x{};
-  for (int i = 0; pools && i < n_layers; ++i) x.p[i] = const_cast<void*>(pools[i]);
-  return x;
+template <int NL>
+void set_pools(WindowCallOf<NL>* a, const void* const* k, const void* const* v, const void* const* ks, const void* const* vs) {
+  set_pools(&a->kp, k, a->n_layers);
+  set_pools(&a->vp, v, a->n_layers);
+  set_pools(&a->ksp, ks, a->n_layers);
+  set_pools(&a->vsp, vs, a->n_layers);
 }
 
-template <Cache CT, int NT>
-void launch_split(const WindowCall& a, int64_t blocks, hipStream_t s) {
-  if (a.g.d == 128) hipLaunchKernelGGL((window_split_kernel<CT, NT, 128>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((window_split_kernel<CT, NT, 64>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+template <Cache CT, int NT, int NL>
+void launch_split(int d, const WindowCallOf<NL>& a, int64_t blocks, hipStream_t s) {
+  if (d == 128) hipLaunchKernelGGL((window_split_kernel<CT, NT, 128, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((window_split_kernel<CT, NT, 64, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+}
+template <int NL>
+hipError_t launch_split(const Geom& g, bool q8, const WindowCallOf<NL>& a, int64_t blocks, hipStream_t s) {
+  const bool f32 = g.dtype == KARA_F32;
+  if (q8 && f32) launch_split<kCodes, 3>(g.d, a, blocks, s);
+  else if (q8) launch_split<kCodes, 1>(g.d, a, blocks, s);
+  else if (f32) launch_split<kRowsF32, 1>(g.d, a, blocks, s);
+  else launch_split<kRowsBf16, 1>(g.d, a, blocks, s);
+  return hipGetLastError();
 }
 
 // q8: whether the cache is of codes (the size over either is the same where it says nothing)
@@ -594,12 +645,12 @@ kara_status_t workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers
   const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
   if (splits(g, n_query, q8)) {
     const int span = span_most(n_query, g.G, kTileRows, w, sink, max_len);
-    const int64_t most = ((int64_t)span + kSplitMin - 1) / kSplitMin;
-    // (a split grows until fewer than kWgTarget workgroups would be left at twice its
-    // length, or to the longest)
-    const int longest = split_most(g.bs);
-    const int64_t grown = std::max((int64_t)2 * kWgTarget * kTileRows, rows * (((int64_t)span + longest - 1) / longest));
-    *bytes = most == 1 ? 0 : (size_t)std::min(rows * most, grown) * rec;
+    // (a tile has no more than `few` splits, and no more than the longest ones make or
+    // kWgsAtOnce over the tiles: either way their records grow with the tiles)
+    const int64_t longest = split_most(g.bs), few = ((int64_t)span + kSplitMin - 1) / kSplitMin;
+    const int64_t tiles = (int64_t)n_layers * n * g.Hkv * (((int64_t)g.G * n_query + kTileRows - 1) / kTileRows);
+    const int64_t many = std::max(rows * (((int64_t)span + longest - 1) / longest), (kWgsAtOnce + tiles) * kTileRows);
+    *bytes = few == 1 ? 0 : (size_t)std::min(rows * few, many) * rec;
   } else {
     // (a launch that splits its keys has so many workgroups at most, records and all)
     const WindowChunkPlan x = window_chunk_plan(g, n, n_layers, n_query, w, sink, max_len, q8);
@@ -626,10 +677,11 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
   if (!aligned(16, {q, out, need ? workspace : nullptr}) || !aligned(4, {seqs, block_table, seq_lens}) ||
       !pools_aligned(16, k_pools, n_layers) || !pools_aligned(16, v_pools, n_layers))
     return KARA_ERR_INVALID_ARG;
-  WindowCall a{};
-  st = make_geom(p, n, &a.g);
+  Geom g;
+  st = make_geom(p, n, &g);
   if (st != KARA_OK) return st;
-  const Geom& g = a.g;
+  WindowHead a{};
+  a.g = dims_of(g);
   a.n = n;
   a.n_layers = n_layers;
   a.T = n_query;
@@ -662,27 +714,25 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
   a.bt = block_table;
   a.seq_lens = seq_lens;
   a.q = q;
-  a.kp = ptrs(k_pools, n_layers);
-  a.vp = ptrs(v_pools, n_layers);
-  a.ksp = ptrs(k_scales, n_layers);
-  a.vsp = ptrs(v_scales, n_layers);
   a.rec_o = (float*)workspace;
   a.rec_ml = a.rec_o + rows * a.n_splits * g.d;
   a.out = out;
   hipStream_t s = (hipStream_t)stream;
   hipError_t e = hipSuccess;
-  if (few) {
-    if (q8 && f32) launch_split<kCodes, 3>(a, blocks, s);
-    else if (q8) launch_split<kCodes, 1>(a, blocks, s);
-    else if (f32) launch_split<kRowsF32, 1>(a, blocks, s);
-    else launch_split<kRowsBf16, 1>(a, blocks, s);
-    e = hipGetLastError();
+  if (few && n_layers <= kFewLayers) {
+    WindowCallOf<kFewLayers> c{a, {}, {}, {}, {}};
+    set_pools(&c, k_pools, v_pools, k_scales, v_scales);
+    e = launch_split(g, q8, c, blocks, s);
   } else {
-    e = launch_window_chunk(a, plan, q8, s);
+    WindowCall c{a, {}, {}, {}, {}};
+    set_pools(&c, k_pools, v_pools, k_scales, v_scales);
+    e = few ? launch_split(g, q8, c, blocks, s) : launch_window_chunk(g, c, plan, q8, s);
   }
   if (e != hipSuccess || a.n_splits == 1) return hip_status(e);
   const dim3 grid((unsigned)((rows + 3) / 4));
-#define KARA_WINDOW_COMBINE(D, B) hipLaunchKernelGGL((window_combine_kernel<D, B>), grid, dim3(256), 0, s, a, rows)
+#define KARA_WINDOW_COMBINE(D, B)                                                                               \
+  hipLaunchKernelGGL((window_combine_kernel<D, B>), grid, dim3(256), 0, s, (const float*)a.rec_o, (const float*)a.rec_ml, \
+                     out, a.n_splits, rows)
   if (g.d == 128) {
     if (f32) KARA_WINDOW_COMBINE(128, false);
     else KARA_WINDOW_COMBINE(128, true);

@@ -3,12 +3,12 @@
 // share.
 #pragma once
 
-#include "kara_internal.h"
+#include "kara_call.h"
 
 namespace kara {
 
-struct WindowCall {
-  Geom g;
+struct WindowHead {
+  Dims g;
   int n, n_layers;
   int T;                      // queries per sequence, its last T positions
   int window, sink;           // at most kMaxLen; no window: kMaxLen
@@ -18,10 +18,15 @@ struct WindowCall {
   int run;                    // log2 of the keys that lie in one page wherever they start
   const int32_t *seqs, *bt, *seq_lens;
   const void* q;              // [n_layers][n][T][Hq][d]
-  PoolPtrs kp, vp, ksp, vsp;  // rows, or codes and scales
   float *rec_o, *rec_ml;      // records [n_layers][n][T][Hq][n_splits]: o[d]; m, l
   void* out;                  // [n_layers][n][T][Hq][d]
 };
+
+template <int NL>
+struct WindowCallOf : WindowHead {
+  Pools<NL> kp, vp, ksp, vsp;   // rows, or codes and scales
+};
+using WindowCall = WindowCallOf<kMaxLayersPerLaunch>;
 
 // Keys that a tile of query rows sees, numbered without the gap: key v is at position
 // v while v < head, else at v + gap.  The numbers 0 .. n - 1 hold all of them, and a few
@@ -69,6 +74,6 @@ struct WindowChunkPlan {
 };
 constexpr int kWindowChunkWgs = 256;   // most workgroups of a launch that splits its keys
 WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int window, int sink, int max_len, bool q8);
-hipError_t launch_window_chunk(WindowCall a, const WindowChunkPlan& x, bool q8, hipStream_t stream);
+hipError_t launch_window_chunk(const Geom& g, const WindowCall& a, const WindowChunkPlan& x, bool q8, hipStream_t stream);
 
 }  // namespace kara

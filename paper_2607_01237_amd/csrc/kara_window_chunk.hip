@@ -70,7 +70,7 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
   constexpr int KS = C::kKS, DT = C::kDT, KP = C::kKeys;
   __shared__ __attribute__((aligned(16))) char smem[C::kStages][2 * C::kTile];
   __shared__ uint32_t run_row[kRuns], run_scale[Q8 ? kRuns : 1];   // pool rows of runs of keys; K's scale byte, V's above it
-  const Geom& g = a.g;
+  const Dims& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
@@ -564,7 +564,7 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
     if (r >= R) continue;
     const int t = r / G;
     const int64_t at = orow + (int64_t)t * g.Hq + (r - t * G);
-    if (a.n_splits == 1 || (sp.n > 0 && sp.n <= a.split_keys && split == 0)) {
+    if (a.n_splits == 1) {
       const float inv = lsum[qt][0] == 0.f ? 0.f : 1.f / lsum[qt][0];    // (a row that sees no key)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
@@ -577,18 +577,20 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
           *(floatx4*)((float*)a.out + at * D + dt * 16 + 4 * gq) = v;
         }
       }
-    } else if (!none && k_lo < sp.n) {
+    } else {
+      // (a split without keys: a record of no weight)
       const int64_t rec = at * a.n_splits + split;
       if (gq == 0) *(floatx2*)(a.rec_ml + 2 * rec) = floatx2{m[qt], lsum[qt][0]};
+      if (n_chunks > 0)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) *(floatx4*)(a.rec_o + rec * D + dt * 16 + 4 * gq) = o[qt][dt];
+        for (int dt = 0; dt < DT; ++dt) *(floatx4*)(a.rec_o + rec * D + dt * 16 + 4 * gq) = o[qt][dt];
     }
   }
 }
 
 template <bool Q8, int NT, int QT, int W>
-hipError_t launch(const WindowCall& a, int64_t blocks, hipStream_t stream) {
-  if (a.g.d == 128)
+hipError_t launch(int d, const WindowCall& a, int64_t blocks, hipStream_t stream) {
+  if (d == 128)
     hipLaunchKernelGGL((window_chunk_kernel<Q8, NT, 128, QT, W>), dim3((unsigned)blocks), dim3(W * 64), 0, stream, a);
   else
     hipLaunchKernelGGL((window_chunk_kernel<Q8, NT, 64, QT, W>), dim3((unsigned)blocks), dim3(W * 64), 0, stream, a);
@@ -596,10 +598,10 @@ hipError_t launch(const WindowCall& a, int64_t blocks, hipStream_t stream) {
 }
 
 template <bool Q8>
-hipError_t launch_bf16(const WindowCall& a, const WindowChunkPlan& x, hipStream_t s) {
+hipError_t launch_bf16(int d, const WindowCall& a, const WindowChunkPlan& x, hipStream_t s) {
   if constexpr (Q8)
-    if (x.waves == 4) return x.qt == 1 ? launch<Q8, 1, 1, 4>(a, x.blocks, s) : launch<Q8, 1, 2, 4>(a, x.blocks, s);
-  return x.qt == 1 ? launch<Q8, 1, 1, 8>(a, x.blocks, s) : launch<Q8, 1, 2, 8>(a, x.blocks, s);
+    if (x.waves == 4) return x.qt == 1 ? launch<Q8, 1, 1, 4>(d, a, x.blocks, s) : launch<Q8, 1, 2, 4>(d, a, x.blocks, s);
+  return x.qt == 1 ? launch<Q8, 1, 1, 8>(d, a, x.blocks, s) : launch<Q8, 1, 2, 8>(d, a, x.blocks, s);
 }
 
 constexpr int kCUs = 256;
@@ -630,10 +632,11 @@ WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int
   return x;
 }
 
-hipError_t launch_window_chunk(WindowCall a, const WindowChunkPlan& x, bool q8, hipStream_t s) {
-  if (a.g.dtype == KARA_F32)   // (over codes: rows of fp32 go through the split kernel)
-    return x.waves == 8 ? launch<true, 3, 1, 8>(a, x.blocks, s) : launch<true, 3, 1, 4>(a, x.blocks, s);
-  return q8 ? launch_bf16<true>(a, x, s) : launch_bf16<false>(a, x, s);
+hipError_t launch_window_chunk(const Geom& g, const WindowCall& a, const WindowChunkPlan& x, bool q8, hipStream_t s) {
+  const int d = g.d;
+  if (g.dtype == KARA_F32)   // (over codes: rows of fp32 go through the split kernel)
+    return x.waves == 8 ? launch<true, 3, 1, 8>(d, a, x.blocks, s) : launch<true, 3, 1, 4>(d, a, x.blocks, s);
+  return q8 ? launch_bf16<true>(d, a, x, s) : launch_bf16<false>(d, a, x, s);
 }
 
 }  // namespace kara

@@ -99,7 +99,7 @@ def check(case, **more):
             delta = cc.logit_error(q[l, j], sane, scale, 1 if dtype == "bf16" else 3)
             bound = cc.attention_bound(ref, mass, delta, n, dtype, dtype == "bf16")
             if fine.any():
-                worst = max(worst, float((np.abs(got[l, j] - ref)[fine] / bound[fine]).max()))
+                worst = max(worst, float((np.abs(got[l, j][fine] - ref[fine]) / bound[fine]).max()))
     print(f"[case] worst error / bound {worst:.3f}", flush=True)
     assert worst <= 1.0
 
