@@ -72,6 +72,7 @@ class LayerWeights(ctypes.Structure):
 
 
 class KaraRope(ctypes.Structure):
+    held = None                            # the tensor behind inv_freq
     _fields_ = [("dim", ctypes.c_int32), ("theta", ctypes.c_float), ("inv_freq", ctypes.c_void_p)]
 
 
@@ -577,7 +578,7 @@ def _pool_args(dev, L, pools):
     """pools: (name, one tensor per layer or None, elements, dtype).  Returns the
     array of their pointers, to be kept until the call is made, and the address
     of each pool's part (None: NULL)."""
-    ptrs, at = array.array("Q"), []
+    ptrs, at = [], []
     for name, ts, n, dtype in pools:
         if ts is None:
             at.append(None)
@@ -589,6 +590,7 @@ def _pool_args(dev, L, pools):
             if t is None or t.dtype is not dtype or t.numel() < n or t.get_device() != dev or not t.is_contiguous():
                 _reject(dev, f"{name}[{i}]", t, n, dtype)
             ptrs.append(t.data_ptr())
+    ptrs = array.array("Q", ptrs)
     base = ptrs.buffer_info()[0]
     return ptrs, [None if x is None else base + x for x in at]
 
@@ -771,12 +773,17 @@ def evict_tokens(p, seqs, keep, n_sink, n_recent, k_pools, v_pools, weights, blo
 
 def _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales):
     """Pool arguments of a cache of rows (no scales) or of 8-bit codes."""
-    if (k_scales is None) != (v_scales is None):
-        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales and v_scales: both or neither")
     units = p.num_pages * p.n_kv_heads
-    n, dt = units * p.block_size * p.head_dim, torch.uint8 if k_scales is not None else _dtype(torch, p)
-    return _pool_args(dev, L, [("k_pools", k_pools, n, dt), ("v_pools", v_pools, n, dt),
-                               ("k_scales", k_scales, units, torch.uint8), ("v_scales", v_scales, units, torch.uint8)])
+    size = units * p.block_size * p.head_dim
+    if k_scales is None and v_scales is None:
+        dt = _dtype(torch, p)
+        keep, (k, v) = _pool_args(dev, L, (("k_pools", k_pools, size, dt), ("v_pools", v_pools, size, dt)))
+        return keep, (k, v, None, None)
+    if k_scales is None or v_scales is None:
+        raise KaraError("marshal", ERR_INVALID_ARG, "k_scales and v_scales: both or neither")
+    u8 = torch.uint8
+    return _pool_args(dev, L, (("k_pools", k_pools, size, u8), ("v_pools", v_pools, size, u8),
+                               ("k_scales", k_scales, units, u8), ("v_scales", v_scales, units, u8)))
 
 
 def q8_append(p, seqs, k_new, v_new, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, status, stream=None):
@@ -842,7 +849,7 @@ def make_rope(theta=1e6, dim=0, inv_freq=None) -> KaraRope:
     r = KaraRope(int(dim), float(theta), None)
     if inv_freq is not None:
         import torch
-        r.held = inv_freq                      # as long as the structure is
+        r.held = inv_freq
         r.inv_freq = _arg(inv_freq.get_device(), "inv_freq", inv_freq, dim // 2 if dim > 0 else 0, torch.float32)
     return r
 
@@ -855,14 +862,13 @@ def rope_append(p, rope: KaraRope, seqs, k_new, v_new, k_pools, v_pools, block_t
     are in seq_lens and rope_pos already, by an earlier layer's call."""
     lib = load()
     torch, dev, s = _launch(stream)
-    n, L, n_new = seqs.numel(), len(k_pools), k_new.shape[2]
-    size, dt = L * n * n_new * p.n_kv_heads * p.head_dim, _dtype(torch, p)
-    q_size = L * n * n_new * p.n_q_heads * p.head_dim
+    n, L, n_new = seqs.numel(), len(k_pools), k_new.size(2)
+    rows, dt = L * n * n_new * p.head_dim, _dtype(torch, p)
+    size, q_size = rows * p.n_kv_heads, rows * p.n_q_heads
     if (q is None) != (q_out is None):
         raise KaraError("marshal", ERR_INVALID_ARG, "q and q_out: both or neither")
-    held = getattr(rope, "held", None)
-    if held is not None:
-        _arg(dev, "inv_freq", held, (rope.dim or p.head_dim) // 2, torch.float32)
+    if rope.held is not None:
+        _arg(dev, "inv_freq", rope.held, (rope.dim or p.head_dim) // 2, torch.float32)
     keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
     sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
     _check("kara_rope_append", lib.kara_rope_append(
