@@ -16,15 +16,17 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStoreThreads = 256;
-constexpr int kFewThreads = 512;
+constexpr int kFewThreads = 1024;
 constexpr int kTile = 32;             // tokens that share a table of angles
-constexpr int kGroupHeads = 16;       // KV heads of a unit
+constexpr int kGroupHeads = 16;       // KV heads of a workgroup, at most
+constexpr int kStoreWgs = 1024;       // workgroups of a launch, where heads can be dealt out
 constexpr int kMaxOctets = 1 << 28;   // of a token: 32-bit offsets
 
 struct StoreHead {
   Dims g;
   int n, n_new, n_layers, counted;
-  int units, groups;                  // per (layer, sequence): runs of tokens, groups of KV heads
+  int units;                          // runs of tokens per (layer, sequence)
+  int group;                          // KV heads of a workgroup
   int half;                           // pairs that turn; 0: none
   double step;                        // frequencies: exp2(-step i) revolutions / 2 pi
   const float* inv_freq;
@@ -150,21 +152,23 @@ __device__ __forceinline__ uint32_t finite_top(float (&x)[8], bool* odd) {
   return top;
 }
 
-// One run of tokens of sequence s = seqs[j] in layer l, KV heads [16 grp, 16 grp + 16) and
+// One run of tokens of sequence s = seqs[j] in layers [l0, l1), `heads` KV heads from h0 on and
 // their query heads, by all threads.  8 bits: the tokens that fall into one page, as its
-// scale is formed of all of them; a wave takes a (K|V, head) at a time.  Rows: 32 tokens.
+// scale is formed of all of them; a wave takes a (layer, K|V, head) at a time, HELD items of
+// a lane.  Rows: 32 tokens.  (More than one layer: of 64 HELD items of a head at most.)
 // Returns whether a value to be quantised was not finite.
-template <int DT, int D, bool Q8, int THREADS, int NL>
-__device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uint32_t (&tops)[2 * kGroupHeads], uint32_t (&bytes)[2 * kGroupHeads], int j, int l,
-                                           int unit, int grp, int s, int pos0, int64_t rot0) {
+template <int DT, int D, bool Q8, int THREADS, int HELD, int NL>
+__device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uint32_t (&tops)[2 * kGroupHeads],
+                                           uint32_t (&bytes)[2 * kGroupHeads], int j, int l0, int l1, int unit, int h0,
+                                           int heads, int s, int pos0, int64_t rot0) {
   constexpr int kItems = D / 16;                 // of a row
   constexpr int kRow = D * (DT == KARA_BF16 ? 2 : 4), kOct = kRow / (D / 8);
   constexpr int kWaves = THREADS / 64;
-  constexpr int kHeld = kTile * kItems / 64;     // items of a lane, of one head's tile
+  constexpr int kTokens = 64 * HELD / kItems;    // whose items a wave's lanes hold
   const Dims& g = a.g;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h0 = grp * kGroupHeads, heads = min(kGroupHeads, g.Hkv - h0);
+  const int layers = l1 - l0;
   int tok0 = unit * kTile, tok1 = min(tok0 + kTile, a.n_new), block = 0;
   if constexpr (Q8) {
     block = pos0 / g.bs + unit;
@@ -174,16 +178,16 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
   }
   if (tok0 >= tok1) return false;
   const int32_t* row_pages = a.bt + (int64_t)s * g.max_blocks;
-  const int64_t src0 = ((int64_t)l * a.n + j) * a.n_new;        // row of token 0
+  auto src0 = [&](int l) __attribute__((always_inline)) { return ((int64_t)l * a.n + j) * a.n_new; };   // row of token 0
   const char* src_of[2] = {a.k_new, a.v_new};
   bool odd = false;
 
   // an item's octets as fp32, turned where they turn
-  auto item = [&](int kv, int tile0, int head, int x, float (&u)[8], float (&v)[8], int& tok, Pair& p)
+  auto item = [&](int l, int kv, int tile0, int head, int x, float (&u)[8], float (&v)[8], int& tok, Pair& p)
                   __attribute__((always_inline)) {
     tok = x / kItems;
     p = pair_of(x - tok * kItems, kv ? 0 : a.half);
-    const char* row = src_of[kv] + ((src0 + tile0 + tok) * g.Hkv + head) * kRow;
+    const char* row = src_of[kv] + ((src0(l) + tile0 + tok) * g.Hkv + head) * kRow;
     Raw<DT> ra, rb;
     ra.load(row + p.a * kOct);
     rb.load(row + p.b * kOct);
@@ -192,12 +196,12 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
     if (p.turns) turn(t, tok, p.a, u, v);
   };
 
-  const bool whole = tok1 - tok0 <= kTile;       // one tile
+  const bool whole = tok1 - tok0 <= kTokens;     // one tile
   if (Q8 && !whole) {
     // the page's largest magnitudes first
     for (int i = tid; i < 2 * kGroupHeads; i += THREADS) tops[i] = 0;
-    for (int tile0 = tok0; tile0 < tok1; tile0 += kTile) {
-      const int count = min(kTile, tok1 - tile0);
+    for (int tile0 = tok0; tile0 < tok1; tile0 += kTokens) {
+      const int count = min(kTokens, tok1 - tile0);
       __syncthreads();
       fill_angles<D, THREADS>(t, a, rot0 + tile0, count);
       __syncthreads();
@@ -208,7 +212,7 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
           float u[8], v[8];
           int tok;
           Pair p;
-          item(kv, tile0, head, x, u, v, tok, p);
+          item(l0, kv, tile0, head, x, u, v, tok, p);
           top = max(top, max(finite_top(u, &odd), finite_top(v, &odd)));
         }
         top = wave_max(top);
@@ -216,25 +220,27 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
       }
     }
   }
-  for (int tile0 = tok0; tile0 < tok1; tile0 += kTile) {
-    const int count = min(kTile, tok1 - tile0);
+  constexpr int kStep = Q8 ? kTokens : kTile;
+  for (int tile0 = tok0; tile0 < tok1; tile0 += kStep) {
+    const int count = min(kStep, tok1 - tile0);
     __syncthreads();
     fill_angles<D, THREADS>(t, a, rot0 + tile0, count);
     __syncthreads();
     if constexpr (Q8) {
       const int page = row_pages[block];
       const int slot0 = pos0 + tok0 - block * g.bs;             // of the page's first new token
-      for (int job = wave; job < 2 * heads; job += kWaves) {
+      for (int x0 = wave; x0 < layers * 2 * heads; x0 += kWaves) {
+        const int l = l0 + x0 / (2 * heads), job = x0 - (l - l0) * 2 * heads;
         const int kv = job >= heads, head = h0 + (kv ? job - heads : job);
-        float u[kHeld][8], v[kHeld][8];
-        int tok[kHeld];
-        Pair p[kHeld];
+        float u[HELD][8], v[HELD][8];
+        int tok[HELD];
+        Pair p[HELD];
         uint32_t top = 0;
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
+        for (int k = 0; k < HELD; ++k) {
           const int x = lane + 64 * k;
           if (x >= count * kItems) continue;
-          item(kv, tile0, head, x, u[k], v[k], tok[k], p[k]);
+          item(l, kv, tile0, head, x, u[k], v[k], tok[k], p[k]);
           top = max(top, max(finite_top(u[k], &odd), finite_top(v[k], &odd)));
         }
         const int64_t unit_at = (int64_t)page * g.Hkv + head;
@@ -255,14 +261,14 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
           }
           if (lane == 0) {
             *scales = (uint8_t)byte;
-            bytes[job] = byte;                                  // for the page's further tiles
+            if (!whole) bytes[job] = byte;                      // for the page's further tiles
           }
         } else {
           byte = bytes[job];
         }
         const float per_unit = q8_per_unit(byte);
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
+        for (int k = 0; k < HELD; ++k) {
           if (lane + 64 * k >= count * kItems) continue;
           uint8_t* row = codes + (int64_t)(slot0 + tile0 - tok0 + tok[k]) * D;
           *(u32x2*)(row + p[k].a * 8) = u32x2{q8_codes(u[k][0], u[k][1], u[k][2], u[k][3], per_unit),
@@ -273,12 +279,14 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
       }
     } else {
       // rows of the tile, (K|V, token, head) in order
-      for (int x = tid; x < 2 * count * heads * kItems; x += THREADS) {
-        const int row = x / kItems, i = x - row * kItems;
+      const int layer_rows = 2 * count * heads;
+      for (int x = tid; x < layers * layer_rows * kItems; x += THREADS) {
+        const int lrow = x / kItems, i = x - lrow * kItems;
+        const int l = l0 + lrow / layer_rows, row = lrow - (l - l0) * layer_rows;
         const int kv = row >= count * heads, r = kv ? row - count * heads : row;
         const int tok = r / heads, head = h0 + r - tok * heads;
         const Pair p = pair_of(i, kv ? 0 : a.half);
-        const char* src = src_of[kv] + ((src0 + tile0 + tok) * g.Hkv + head) * kRow;
+        const char* src = src_of[kv] + ((src0(l) + tile0 + tok) * g.Hkv + head) * kRow;
         Raw<DT> ra, rb;
         ra.load(src + p.a * kOct);
         rb.load(src + p.b * kOct);
@@ -299,11 +307,12 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
     }
     if (a.q) {
       const int qh = heads * g.G;
-      for (int x = tid; x < count * qh * kItems; x += THREADS) {
-        const int row = x / kItems, i = x - row * kItems;
+      for (int x = tid; x < layers * count * qh * kItems; x += THREADS) {
+        const int lrow = x / kItems, i = x - lrow * kItems;
+        const int l = l0 + lrow / (count * qh), row = lrow - (l - l0) * count * qh;
         const int tok = row / qh, head = h0 * g.G + row - tok * qh;
         const Pair p = pair_of(i, a.half);
-        const int64_t at = ((src0 + tile0 + tok) * g.Hq + head) * kRow;
+        const int64_t at = ((src0(l) + tile0 + tok) * g.Hq + head) * kRow;
         Raw<DT> ra, rb;
         ra.load(a.q + at + p.a * kOct);
         rb.load(a.q + at + p.b * kOct);
@@ -357,12 +366,15 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(Store<NL> a) {
   int64_t rot0;
   start_of(a, s, &pos0, &rot0);
   __syncthreads();
-  const bool odd = store_unit<DT, D, Q8, kStoreThreads>(a, t, tops, bytes, j, blockIdx.y, unit, blockIdx.z, s, pos0, rot0);
+  const int l = blockIdx.y, h0 = blockIdx.z * a.group;
+  const bool odd = store_unit<DT, D, Q8, kStoreThreads, kTile * (D / 16) / 64>(
+      a, t, tops, bytes, j, l, l + 1, unit, h0, min(a.group, a.g.Hkv - h0), s, pos0, rot0);
   if (Q8 && __syncthreads_or(odd) && threadIdx.x == 0) atomicOr(&a.status[j], KARA_SEQ_NONFINITE);
 }
 
 // A few new tokens: one workgroup per listed sequence checks it, appends all its rows and
-// commits, in one launch.
+// commits, in one launch.  (The tokens' items of a head are one a lane at most, so that no
+// page has further tiles, and `tops` and `bytes` are not used.)
 template <int DT, int D, bool Q8, int NL>
 __global__ __launch_bounds__(kFewThreads) void store_few_kernel(Store<NL> a) {
   __shared__ __attribute__((aligned(16))) Angles<D> t;
@@ -377,10 +389,8 @@ __global__ __launch_bounds__(kFewThreads) void store_few_kernel(Store<NL> a) {
     int64_t rot0;
     start_of(a, s, &pos0, &rot0);
     bool odd = false;
-    for (int l = 0; l < a.n_layers; ++l)
-      for (int grp = 0; grp < a.groups; ++grp)
-        for (int unit = 0; unit < a.units; ++unit)
-          odd |= store_unit<DT, D, Q8, kFewThreads>(a, t, tops, bytes, j, l, unit, grp, s, pos0, rot0);
+    for (int unit = 0; unit < a.units; ++unit)
+      odd |= store_unit<DT, D, Q8, kFewThreads, 1>(a, t, tops, bytes, j, 0, a.n_layers, unit, 0, a.g.Hkv, s, pos0, rot0);
     if (Q8 && __syncthreads_or(odd)) st = KARA_SEQ_NONFINITE;
   }
   __syncthreads();                       // every thread has read the length before it changes
@@ -469,15 +479,17 @@ bool layers_ok(int32_t n, int32_t n_layers) { return n >= 0 && n_layers >= 1 && 
 
 template <int DT, int D, bool Q8, int NL>
 kara_status_t launch_store(const Store<NL>& a, hipStream_t s) {
-  // a few units in all: one workgroup a sequence
-  if ((int64_t)a.n_layers * a.units * a.groups <= 4) {
+  // a few items in all: one workgroup a sequence
+  const int64_t items = (int64_t)a.n_layers * a.n_new * (2 * a.g.Hkv + (a.q ? a.g.Hq : 0)) * (D / 16);
+  if (a.n_new * (D / 16) <= 64 && items <= 8 * kFewThreads) {
     hipLaunchKernelGGL((store_few_kernel<DT, D, Q8, NL>), dim3((unsigned)a.n), dim3(kFewThreads), 0, s, a);
     return hip_status(hipGetLastError());
   }
   hipLaunchKernelGGL(store_check_kernel, dim3((unsigned)a.n), dim3(kAppendThreads), 0, s, (const StoreHead&)a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_status(e);
-  hipLaunchKernelGGL((store_kernel<DT, D, Q8, NL>), dim3((unsigned)(a.n * a.units), (unsigned)a.n_layers, (unsigned)a.groups),
+  const unsigned groups = (unsigned)((a.g.Hkv + a.group - 1) / a.group);
+  hipLaunchKernelGGL((store_kernel<DT, D, Q8, NL>), dim3((unsigned)(a.n * a.units), (unsigned)a.n_layers, groups),
                      dim3(kStoreThreads), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.counted) return hip_status(e);
@@ -519,8 +531,11 @@ kara_status_t store(const kara_params_t* p, const kara_rope_t* rope, int32_t n, 
   if ((int64_t)g.Hq * (g.d / 8) > kMaxOctets) return KARA_ERR_UNSUPPORTED;
   // (8 bits: a run of n_new tokens enters one page more where it starts late in one)
   const int64_t units = q8 ? ((int64_t)n_new + g.bs - 2) / g.bs + 1 : ((int64_t)n_new + kTile - 1) / kTile;
-  a.groups = (g.Hkv + kGroupHeads - 1) / kGroupHeads;
-  if (!grid_ok(n * units) || a.groups > 65535) return KARA_ERR_UNSUPPORTED;
+  // (a page of many tokens is one workgroup's for a head: fewer heads each where there are
+  // few of them)
+  a.group = std::min(g.Hkv, kGroupHeads);
+  while (a.group > 1 && n * units * n_layers * ((g.Hkv + a.group - 1) / a.group) < kStoreWgs) a.group = (a.group + 1) / 2;
+  if (!grid_ok(n * units) || (g.Hkv + a.group - 1) / a.group > 65535) return KARA_ERR_UNSUPPORTED;
   a.units = (int)units;
   a.n = n;
   a.n_new = n_new;
