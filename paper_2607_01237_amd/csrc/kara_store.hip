@@ -3,6 +3,7 @@
 // (include/kara_rope.h, include/kara_q8.h).
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "kara_append.h"
 #include "kara_call.h"
@@ -48,9 +49,13 @@ struct Raw {
 #pragma unroll
     for (int i = 0; i < (DT == KARA_BF16 ? 1 : 2); ++i) v[i] = __builtin_nontemporal_load((const u32x4*)p + i);
   }
+  template <bool STREAM>
   __device__ __forceinline__ void store(char* p) const {
 #pragma unroll
-    for (int i = 0; i < (DT == KARA_BF16 ? 1 : 2); ++i) *((u32x4*)p + i) = v[i];
+    for (int i = 0; i < (DT == KARA_BF16 ? 1 : 2); ++i) {
+      if constexpr (STREAM) __builtin_nontemporal_store(v[i], (u32x4*)p + i);
+      else *((u32x4*)p + i) = v[i];
+    }
   }
   __device__ __forceinline__ void values(float (&x)[8]) const {
 #pragma unroll
@@ -196,6 +201,42 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
     if (p.turns) turn(t, tok, p.a, u, v);
   };
 
+  // rows turned one by one, `total` items of them: four on their way at a time, where there
+  // are so many (THREADS == kStoreThreads).  stream: they are not read again soon.
+  struct Item {
+    const char* from;
+    char* to;
+    Pair p;
+    int tok;
+  };
+  auto rows_by_item = [&](auto stream, int total, auto where) __attribute__((always_inline)) {
+    constexpr int kAtOnce = THREADS == kStoreThreads ? 4 : 1;
+    for (int x0 = tid; x0 < total; x0 += kAtOnce * THREADS) {
+      Item it[kAtOnce];
+      Raw<DT> ra[kAtOnce], rb[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        it[k] = where(min(x0 + k * THREADS, total - 1));
+        ra[k].load(it[k].from + it[k].p.a * kOct);
+        rb[k].load(it[k].from + it[k].p.b * kOct);
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (x0 + k * THREADS >= total) break;
+        if (it[k].p.turns) {
+          float u[8], v[8];
+          ra[k].values(u);
+          rb[k].values(v);
+          turn(t, it[k].tok, it[k].p.a, u, v);
+          ra[k].set(u);
+          rb[k].set(v);
+        }
+        ra[k].template store<decltype(stream)::value && kAtOnce != 1>(it[k].to + it[k].p.a * kOct);
+        rb[k].template store<decltype(stream)::value && kAtOnce != 1>(it[k].to + it[k].p.b * kOct);
+      }
+    }
+  };
+
   const bool whole = tok1 - tok0 <= kTokens;     // one tile
   if (Q8 && !whole) {
     // the page's largest magnitudes first
@@ -280,53 +321,26 @@ __device__ __forceinline__ bool store_unit(const Store<NL>& a, Angles<D>& t, uin
     } else {
       // rows of the tile, (K|V, token, head) in order
       const int layer_rows = 2 * count * heads;
-      for (int x = tid; x < layers * layer_rows * kItems; x += THREADS) {
-        const int lrow = x / kItems, i = x - lrow * kItems;
+      rows_by_item(std::false_type{}, layers * layer_rows * kItems, [&](int x) __attribute__((always_inline)) {
+        const int lrow = x / kItems;
         const int l = l0 + lrow / layer_rows, row = lrow - (l - l0) * layer_rows;
         const int kv = row >= count * heads, r = kv ? row - count * heads : row;
         const int tok = r / heads, head = h0 + r - tok * heads;
-        const Pair p = pair_of(i, kv ? 0 : a.half);
-        const char* src = src_of[kv] + ((src0(l) + tile0 + tok) * g.Hkv + head) * kRow;
-        Raw<DT> ra, rb;
-        ra.load(src + p.a * kOct);
-        rb.load(src + p.b * kOct);
         const int pos = pos0 + tile0 + tok, b = pos / g.bs;
-        char* dst = (char*)(kv ? a.vp.p[l] : a.kp.p[l]) +
-                    (((int64_t)row_pages[b] * g.Hkv + head) * g.bs + (pos - b * g.bs)) * kRow;
-        if (p.turns) {
-          float u[8], v[8];
-          ra.values(u);
-          rb.values(v);
-          turn(t, tok, p.a, u, v);
-          ra.set(u);
-          rb.set(v);
-        }
-        ra.store(dst + p.a * kOct);
-        rb.store(dst + p.b * kOct);
-      }
+        return Item{src_of[kv] + ((src0(l) + tile0 + tok) * g.Hkv + head) * kRow,
+                    (char*)(kv ? a.vp.p[l] : a.kp.p[l]) + (((int64_t)row_pages[b] * g.Hkv + head) * g.bs + (pos - b * g.bs)) * kRow,
+                    pair_of(x - lrow * kItems, kv ? 0 : a.half), tok};
+      });
     }
     if (a.q) {
       const int qh = heads * g.G;
-      for (int x = tid; x < layers * count * qh * kItems; x += THREADS) {
-        const int lrow = x / kItems, i = x - lrow * kItems;
+      rows_by_item(std::true_type{}, layers * count * qh * kItems, [&](int x) __attribute__((always_inline)) {
+        const int lrow = x / kItems;
         const int l = l0 + lrow / (count * qh), row = lrow - (l - l0) * count * qh;
         const int tok = row / qh, head = h0 * g.G + row - tok * qh;
-        const Pair p = pair_of(i, a.half);
         const int64_t at = ((src0(l) + tile0 + tok) * g.Hq + head) * kRow;
-        Raw<DT> ra, rb;
-        ra.load(a.q + at + p.a * kOct);
-        rb.load(a.q + at + p.b * kOct);
-        if (p.turns) {
-          float u[8], v[8];
-          ra.values(u);
-          rb.values(v);
-          turn(t, tok, p.a, u, v);
-          ra.set(u);
-          rb.set(v);
-        }
-        ra.store(a.q_out + at + p.a * kOct);
-        rb.store(a.q_out + at + p.b * kOct);
-      }
+        return Item{a.q + at, a.q_out + at, pair_of(x - lrow * kItems, a.half), tok};
+      });
     }
   }
   return odd;
