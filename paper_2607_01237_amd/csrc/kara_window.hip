@@ -652,9 +652,7 @@ kara_status_t workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers
     const int64_t many = std::max(rows * (((int64_t)span + longest - 1) / longest), (kWgsAtOnce + tiles) * kTileRows);
     *bytes = few == 1 ? 0 : (size_t)std::min(rows * few, many) * rec;
   } else {
-    // (a launch that splits its keys has so many workgroups at most, records and all)
-    const WindowChunkPlan x = window_chunk_plan(g, n, n_layers, n_query, w, sink, max_len, q8);
-    *bytes = (size_t)kWindowChunkWgs * x.qt * 128 * rec;
+    *bytes = window_chunk_workspace(g, n, n_layers, n_query);
   }
   return KARA_OK;
 }
@@ -694,7 +692,6 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
   WindowChunkPlan plan{};
   int64_t blocks;
   if (few) {
-    a.rows = kTileRows;
     a.n_rt = (int)(((int64_t)g.G * n_query + kTileRows - 1) / kTileRows);
     const int64_t tiles = (int64_t)n_layers * n * g.Hkv * a.n_rt;
     const int span = span_most(n_query, g.G, kTileRows, a.window, a.sink, max_len);
@@ -702,12 +699,10 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
     a.n_splits = (span + a.split_keys - 1) / a.split_keys;
     blocks = tiles * a.n_splits;
   } else {
-    plan = window_chunk_plan(g, n, n_layers, n_query, a.window, a.sink, max_len, q8);
-    a.rows = plan.rows_wg;
+    plan = window_chunk_plan(g, n, n_layers, n_query);
     a.n_rt = plan.n_rb;
-    a.split_keys = plan.split_keys;
-    a.n_splits = plan.splits;
-    blocks = 2 * plan.blocks;
+    a.n_splits = 1;
+    blocks = 2 * plan.blocks;           // (of 512 threads)
   }
   if (!grid_ok(blocks) || !grid_ok((rows + 3) / 4)) return KARA_ERR_UNSUPPORTED;
   a.seqs = seqs;
@@ -726,7 +721,7 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
   } else {
     WindowCall c{a, {}, {}, {}, {}};
     set_pools(&c, k_pools, v_pools, k_scales, v_scales);
-    e = few ? launch_split(g, q8, c, blocks, s) : launch_window_chunk(g, c, plan, q8, s);
+    e = few ? launch_split(g, q8, c, blocks, s) : launch_window_chunk(g, c, plan, q8, workspace, s);
   }
   if (e != hipSuccess || a.n_splits == 1) return hip_status(e);
   const dim3 grid((unsigned)((rows + 3) / 4));

@@ -12,8 +12,7 @@ struct WindowHead {
   int n, n_layers;
   int T;                      // queries per sequence, its last T positions
   int window, sink;           // at most kMaxLen; no window: kMaxLen
-  int rows;                   // query rows of a tile (of one (layer, sequence, KV head))
-  int n_rt;                   // tiles
+  int n_rt;                   // tiles of query rows of a (layer, sequence, KV head)
   int split_keys, n_splits, max_len;
   int run;                    // log2 of the keys that lie in one page wherever they start
   const int32_t *seqs, *bt, *seq_lens;
@@ -67,13 +66,16 @@ inline int span_most(int T, int G, int rows, int window, int sink, int max_len) 
   return most < max_len ? (int)most : max_len;
 }
 
-// Many query rows over 8 bits or bf16 rows; splits records as WindowCall says.
+// Many query rows over 8 bits or bf16 rows (kara_window_chunk.hip): bytes of workspace, and
+// the launches.
 struct WindowChunkPlan {
-  int qt, waves, rows_wg, n_rb, splits, split_keys;
-  int64_t blocks;
+  int qt, rows_wg, n_rb;      // tiles of a wave, rows of a workgroup, row blocks of a unit
+  bool split;                 // whether long sequences' keys may be split
+  int64_t blocks;             // row blocks of the call
 };
-constexpr int kWindowChunkWgs = 256;   // most workgroups of a launch that splits its keys
-WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int window, int sink, int max_len, bool q8);
-hipError_t launch_window_chunk(const Geom& g, const WindowCall& a, const WindowChunkPlan& x, bool q8, hipStream_t stream);
+WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T);
+size_t window_chunk_workspace(const Geom& g, int n, int n_layers, int T);
+hipError_t launch_window_chunk(const Geom& g, const WindowCall& a, const WindowChunkPlan& x, bool q8, void* workspace,
+                               hipStream_t stream);
 
 }  // namespace kara

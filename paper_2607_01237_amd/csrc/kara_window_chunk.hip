@@ -2,7 +2,7 @@
 // query rows, a prompt's chunk over what is cached, over 8-bit codes or bf16 rows.  Bound
 // by the matrix products.
 //
-// One workgroup of W waves owns 16 QT W query rows of one (layer, sequence, KV head),
+// One workgroup of 8 waves owns 128 QT query rows of one (layer, sequence, KV head),
 // rows ordered (query, head in group), and walks the keys of their span 64 at a time.  Its
 // threads fetch a chunk two chunks ahead into registers and write it, codes converted in
 // hardware to bf16 -- exactly --, to the other of two LDS stages while the products of the
@@ -22,7 +22,9 @@
 namespace kara {
 namespace {
 
+constexpr int kCUs = 256;
 constexpr int kChKeys = 64;
+constexpr int kLeastChunks = 8;         // of a split
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kMaxFloor = -3.402823466e38f;
@@ -63,8 +65,20 @@ __device__ inline v4i16 read_tr(const char* p) {
       (__attribute__((address_space(3))) v4i16*)(__attribute__((address_space(3))) char*)p);
 }
 
-template <bool Q8, int NT, int D, int QT, int W>
-__global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
+// Where a call has fewer than two workgroups to a CU, long sequences' keys are split, so
+// that it does not end with them: a row block of a sequence of c chunks (its last block's)
+// becomes ceil(c / P) workgroups, P the chunks of all blocks over the CUs, 512 keys at
+// least.  The others write their rows; these write records, which a second launch joins.
+// 9 x 118 queries x 2 layers over 23-5990 tokens: 223 us unsplit; see window_join_kernel.
+struct ChunkSplit {
+  int most;              // sequences whose keys may be split: the first `most` threads' (0: none)
+  float *o, *ml;         // records [..][rows_wg][D]; [..][rows_wg]: m, l
+  int2* of_seq;          // [n]: splits, and the first record
+};
+
+template <bool Q8, int NT, int D, int QT>
+__global__ __launch_bounds__(512, 2) void window_chunk_kernel(WindowCall a, ChunkSplit x) {
+  constexpr int W = 8;
   using C = ChCfg<Q8, D, W>;
   constexpr int kRowsWg = W * 16 * QT;
   constexpr int KS = C::kKS, DT = C::kDT, KP = C::kKeys;
@@ -75,11 +89,84 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, li = lane & 15;
 
-  // All row blocks and splits of a (layer, sequence, KV head) on one XCD, whose L2
-  // then holds its keys once, where the units divide among the 8.
-  uint32_t u, rest = blockIdx.x;
-  const uint32_t per = (uint32_t)a.n_rt * (uint32_t)a.n_splits;
-  const uint32_t units = (uint32_t)(a.n_layers * a.n * g.Hkv);
+  // Sequences in the order of their workgroups' chunks, the longest first: this workgroup's
+  // is the one whose range of blocks it lies in.
+  const uint32_t units = (uint32_t)(a.n_layers * g.Hkv);         // of a sequence
+  const uint32_t blocks = units * (uint32_t)a.n_rt;
+  int j, s, len, splits = 1, piece_chunks = 0, first_record = 0;
+  uint32_t rest = blockIdx.x;
+  if (a.n <= C::kThreads) {
+    struct Seq {
+      int len, splits, chunks;       // chunks of one workgroup, at most
+    };
+    Seq* seqs = (Seq*)smem[0];
+    int* found = (int*)(seqs + a.n);
+    int s0 = 0;
+    Seq mine{0, 1, 1};
+    if (tid < a.n) {
+      s0 = a.seqs[tid];
+      mine.len = s0 >= 0 && s0 < g.n_seqs ? a.seq_lens[s0] : 0;
+      const bool live = mine.len > 0 && mine.len <= a.max_len;
+      const int R0 = g.G * a.T;
+      mine.chunks = live ? (span_of(mine.len, a.T, g.G, (a.n_rt - 1) * kRowsWg, R0, a.window, a.sink).n + kChKeys - 1) / kChKeys : 1;
+      seqs[tid] = mine;
+    }
+    if (tid == 0) found[0] = -1, found[1] = 1 << 30;
+    __syncthreads();
+    if (x.most > 0) {
+      uint64_t all = 0;
+      for (int o = 0; o < a.n; ++o) all += (uint32_t)seqs[o].chunks;
+      const uint64_t per = (all * blocks + kCUs - 1) / kCUs;
+      int share = (int)(per < (uint64_t)kLeastChunks ? (uint64_t)kLeastChunks : per > (1u << 29) ? (uint64_t)(1u << 29) : per);
+      // Up to 3/8 more chunks each where all of them then run at once (a workgroup too many
+      // would double the time of equal ones): a candidate a thread.  (1 x 300 queries over 8K
+      // tokens, 40 blocks: 6 splits 64 us, 7, one round and a part, 100.)
+      const int candidate = share + tid * max(1, share >> 10);
+      uint32_t wgs = 0;
+      if (candidate <= share + share / 8 * 3)
+        for (int o = 0; o < a.n; ++o) wgs += blocks * (uint32_t)((seqs[o].chunks + candidate - 1) / candidate);
+      if (wgs != 0 && wgs <= kCUs) atomicMin(&found[1], candidate);
+      __syncthreads();
+      if (found[1] < (1 << 30)) share = found[1];
+      mine.splits = (mine.chunks + share - 1) / share;
+      mine.chunks = (mine.chunks + mine.splits - 1) / mine.splits;
+      __syncthreads();
+      if (tid < a.n) seqs[tid] = mine;
+      __syncthreads();
+    }
+    if (tid < a.n) {
+      uint32_t at = 0, record = 0;
+      for (int o = 0; o < a.n; ++o) {
+        const Seq other = seqs[o];
+        if (other.chunks > mine.chunks || (other.chunks == mine.chunks && o < tid)) at += blocks * (uint32_t)other.splits;
+        if (o < tid && other.splits > 1) record += blocks * (uint32_t)other.splits;
+      }
+      if (rest >= at && rest - at < blocks * (uint32_t)mine.splits) {
+        found[0] = tid, found[1] = s0, found[2] = mine.len, found[3] = mine.splits, found[4] = mine.chunks;
+        found[5] = (int)record, found[6] = (int)(rest - at);
+      }
+    }
+    __syncthreads();
+    j = __builtin_amdgcn_readfirstlane(found[0]);
+    s = __builtin_amdgcn_readfirstlane(found[1]);
+    len = __builtin_amdgcn_readfirstlane(found[2]);
+    splits = __builtin_amdgcn_readfirstlane(found[3]);
+    piece_chunks = __builtin_amdgcn_readfirstlane(found[4]);
+    first_record = __builtin_amdgcn_readfirstlane(found[5]);
+    rest = __builtin_amdgcn_readfirstlane(found[6]);
+    __syncthreads();
+    if (j < 0) return;                   // (the launch has room for the most splits)
+    if (x.most > 0 && rest == 0 && tid == 0) x.of_seq[j] = int2{splits, first_record};
+  } else {
+    j = rest / blocks;
+    rest -= (uint32_t)j * blocks;
+    s = a.seqs[j];
+    len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
+  }
+  // All row blocks and splits of a (layer, KV head) on one XCD, whose L2 then holds its keys
+  // once, where the units divide among the 8.
+  uint32_t u;
+  const uint32_t per = (uint32_t)a.n_rt * (uint32_t)splits;
   if (units % 8 == 0) {
     u = rest / (8 * per) * 8 + rest % 8;
     rest = rest / 8 % per;
@@ -87,49 +174,18 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
     u = rest / per;
     rest = rest % per;
   }
-  const int split = rest % (uint32_t)a.n_splits;
-  const int rb = a.n_rt - 1 - (int)(rest / (uint32_t)a.n_splits);     // the blocks that see most keys first
-  const int h = u % (uint32_t)g.Hkv;
-  u /= (uint32_t)g.Hkv;
-  int j = u % (uint32_t)a.n;
-  const int l = u / (uint32_t)a.n;
-  // Sequences by length.  Workgroups that wait for a place: the longest first.  Where
-  // all are placed at once, two to a CU, the second half the shortest first, so that
-  // long ones share a CU with short ones.
-  int s, len;
-  if (a.n > 1 && a.n <= C::kThreads) {
-    int* lens = (int*)smem[0];
-    int s0 = 0, mine = -1;
-    if (tid < a.n) {
-      s0 = a.seqs[tid];
-      mine = s0 >= 0 && s0 < g.n_seqs ? a.seq_lens[s0] : 0;
-      lens[tid] = mine;
-    }
-    __syncthreads();
-    const int half = W == 8 ? a.n : (a.n + 1) / 2;
-    const int want = j < half ? j : a.n - 1 - (j - half);
-    if (tid < a.n) {
-      int rank = 0;
-      for (int o = 0; o < a.n; ++o) rank += lens[o] > mine || (lens[o] == mine && o < tid);
-      if (rank == want) lens[a.n] = tid, lens[a.n + 1] = s0, lens[a.n + 2] = mine;
-    }
-    __syncthreads();
-    j = __builtin_amdgcn_readfirstlane(lens[a.n]);
-    s = __builtin_amdgcn_readfirstlane(lens[a.n + 1]);
-    len = __builtin_amdgcn_readfirstlane(lens[a.n + 2]);
-    __syncthreads();
-  } else {
-    s = a.seqs[j];
-    len = s >= 0 && s < g.n_seqs ? a.seq_lens[s] : 0;
-  }
+  const int split = rest % (uint32_t)splits;
+  const int rb = a.n_rt - 1 - (int)(rest / (uint32_t)splits);     // the blocks that see most keys first
+  const int h = u % (uint32_t)g.Hkv, l = u / (uint32_t)g.Hkv;
   const int G = g.G, T = a.T, R = G * T;
   const int row0 = rb * kRowsWg;
   const int64_t orow = ((int64_t)l * a.n + j) * T * g.Hq + h * G;
   const bool none = len <= 0 || len > a.max_len;
   const Span sp = span_of(none ? 0 : len, T, G, row0, min(row0 + kRowsWg, R), a.window, a.sink);
   const int first = len - T;                               // position of query 0
-  const int k_lo = split * a.split_keys;
-  const int k_hi = none ? 0 : min(sp.n, k_lo + a.split_keys);
+  const int k_lo = split * piece_chunks * kChKeys;
+  // (the last split takes what is left: a block may see a few keys more than the sequence's last)
+  const int k_hi = none ? 0 : split + 1 < splits ? min(sp.n, k_lo + piece_chunks * kChKeys) : sp.n;
   const int n_chunks = k_hi > k_lo ? (k_hi - k_lo + kChKeys - 1) / kChKeys : 0;
 
   // ---- this wave's queries as B operands (lane: query li of each tile) ----
@@ -564,7 +620,7 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
     if (r >= R) continue;
     const int t = r / G;
     const int64_t at = orow + (int64_t)t * g.Hq + (r - t * G);
-    if (a.n_splits == 1) {
+    if (splits == 1) {
       const float inv = lsum[qt][0] == 0.f ? 0.f : 1.f / lsum[qt][0];    // (a row that sees no key)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
@@ -579,64 +635,139 @@ __global__ __launch_bounds__(W * 64, 2) void window_chunk_kernel(WindowCall a) {
       }
     } else {
       // (a split without keys: a record of no weight)
-      const int64_t rec = at * a.n_splits + split;
-      if (gq == 0) *(floatx2*)(a.rec_ml + 2 * rec) = floatx2{m[qt], lsum[qt][0]};
+      const int64_t rec = (first_record + (int64_t)(u * a.n_rt + rb) * splits + split) * kRowsWg + (r - row0);
+      if (gq == 0) *(floatx2*)(x.ml + 2 * rec) = floatx2{m[qt], lsum[qt][0]};
       if (n_chunks > 0)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) *(floatx4*)(a.rec_o + rec * D + dt * 16 + 4 * gq) = o[qt][dt];
+        for (int dt = 0; dt < DT; ++dt) *(floatx4*)(x.o + rec * D + dt * 16 + 4 * gq) = o[qt][dt];
     }
   }
 }
 
-template <bool Q8, int NT, int QT, int W>
-hipError_t launch(int d, const WindowCall& a, int64_t blocks, hipStream_t stream) {
-  if (d == 128)
-    hipLaunchKernelGGL((window_chunk_kernel<Q8, NT, 128, QT, W>), dim3((unsigned)blocks), dim3(W * 64), 0, stream, a);
-  else
-    hipLaunchKernelGGL((window_chunk_kernel<Q8, NT, 64, QT, W>), dim3((unsigned)blocks), dim3(W * 64), 0, stream, a);
+// The records of split row blocks joined: a workgroup per (layer, sequence, KV head, row
+// block) and 64 rows, a wave per 4 rows.
+constexpr int kJoinThreads = 1024, kJoinRows = 64;
+template <int D, bool OUT_BF16>
+__global__ __launch_bounds__(kJoinThreads) void window_join_kernel(WindowHead a, ChunkSplit x, int rows_wg) {
+  constexpr int kDPerLane = D / 64, kRowsWave = kJoinRows / (kJoinThreads / 64);
+  typedef float floatd __attribute__((ext_vector_type(kDPerLane)));
+  const Dims& g = a.g;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t units = (uint32_t)(a.n_layers * g.Hkv);
+  uint32_t rest = blockIdx.x;
+  const int rb = rest % (uint32_t)a.n_rt;
+  rest /= (uint32_t)a.n_rt;
+  const uint32_t u = rest % units;
+  const int j = rest / units;
+  const int2 of = x.of_seq[j];
+  if (of.x <= 1) return;
+  const int ns = of.x, R = g.G * a.T;
+  const int h = u % (uint32_t)g.Hkv, l = u / (uint32_t)g.Hkv;
+  const int row0 = blockIdx.y * kJoinRows + wave * kRowsWave;            // of the block's
+  const int64_t rec0 = (of.y + (int64_t)(u * a.n_rt + rb) * ns) * rows_wg + row0;
+  float M[kRowsWave], L[kRowsWave], acc[kRowsWave][kDPerLane];
+#pragma unroll
+  for (int i = 0; i < kRowsWave; ++i) {
+    M[i] = kMaxFloor, L[i] = 0.f;
+#pragma unroll
+    for (int e = 0; e < kDPerLane; ++e) acc[i][e] = 0.f;
+  }
+  for (int sp = 0; sp < ns; ++sp) {
+    floatx2 ml[kRowsWave];
+    floatd v[kRowsWave];
+#pragma unroll
+    for (int i = 0; i < kRowsWave; ++i) {
+      const int64_t rec = rec0 + (int64_t)sp * rows_wg + i;
+      ml[i] = *(const floatx2*)(x.ml + 2 * rec);
+      __builtin_memcpy(&v[i], x.o + rec * D + lane * kDPerLane, sizeof(v[i]));
+    }
+#pragma unroll
+    for (int i = 0; i < kRowsWave; ++i) {
+      // (sums of no weight were not written; one that is NaN, as its row is then, is)
+      const bool in = ml[i][1] != 0.f;
+      const float mn = in ? fmaxf(M[i], ml[i][0]) : M[i];
+      const float f0 = __builtin_amdgcn_exp2f(M[i] - mn), f1 = in ? __builtin_amdgcn_exp2f(ml[i][0] - mn) : 0.f;
+      M[i] = mn;
+      L[i] = L[i] * f0 + (in ? ml[i][1] * f1 : 0.f);
+#pragma unroll
+      for (int e = 0; e < kDPerLane; ++e) acc[i][e] = acc[i][e] * f0 + (in ? v[i][e] * f1 : 0.f);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRowsWave; ++i) {
+    const int r = rb * rows_wg + row0 + i;
+    if (r >= R) continue;
+    const int t = r / g.G;
+    const int64_t at = (((int64_t)l * a.n + j) * a.T + t) * g.Hq + h * g.G + (r - t * g.G);
+#pragma unroll
+    for (int e = 0; e < kDPerLane; ++e) {
+      const float y = L[i] == 0.f ? 0.f : acc[i][e] / L[i];              // (a row that sees no key)
+      if constexpr (OUT_BF16) ((__bf16*)a.out)[at * D + lane * kDPerLane + e] = (__bf16)y;
+      else ((float*)a.out)[at * D + lane * kDPerLane + e] = y;
+    }
+  }
+}
+
+template <bool Q8, int NT, int QT>
+hipError_t launch(int d, const WindowCall& a, const ChunkSplit& sp, unsigned grid, hipStream_t s) {
+  if (d == 128) hipLaunchKernelGGL((window_chunk_kernel<Q8, NT, 128, QT>), dim3(grid), dim3(512), 0, s, a, sp);
+  else hipLaunchKernelGGL((window_chunk_kernel<Q8, NT, 64, QT>), dim3(grid), dim3(512), 0, s, a, sp);
   return hipGetLastError();
 }
 
-template <bool Q8>
-hipError_t launch_bf16(int d, const WindowCall& a, const WindowChunkPlan& x, hipStream_t s) {
-  if constexpr (Q8)
-    if (x.waves == 4) return x.qt == 1 ? launch<Q8, 1, 1, 4>(d, a, x.blocks, s) : launch<Q8, 1, 2, 4>(d, a, x.blocks, s);
-  return x.qt == 1 ? launch<Q8, 1, 1, 8>(d, a, x.blocks, s) : launch<Q8, 1, 2, 8>(d, a, x.blocks, s);
-}
+// Records that a call's splits write: each split sequence has at most twice the workgroups
+// that its share of the CUs is.
+constexpr int kMostRecords = 2 * kCUs;
 
-constexpr int kCUs = 256;
+size_t records_bytes(const Geom& g, const WindowChunkPlan& x) { return (size_t)kMostRecords * x.rows_wg * (g.d + 2) * sizeof(float); }
 
 }  // namespace
 
-// Rows per workgroup, key splits and blocks of a call.
-WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T, int window, int sink, int max_len, bool q8) {
+WindowChunkPlan window_chunk_plan(const Geom& g, int n, int n_layers, int T) {
   WindowChunkPlan x{};
   const int64_t units = (int64_t)n_layers * n * g.Hkv, R = (int64_t)g.G * T;
   x.qt = g.dtype == KARA_F32 || R <= 8 * 16 ? 1 : 2;
-  auto blocks = [&](int waves) { return units * ((R + waves * 16 * x.qt - 1) / (waves * 16 * x.qt)); };
-  // Eight waves, a CU's worth of registers, fetch a chunk once for 256 rows (bf16) but
-  // stand one to a CU: a launch of half to all of the CUs' number ends with its longest.
-  // There four waves, two to a CU.
-  // (Rows stand one to a CU either way, by their ring.)
-  x.waves = q8 && blocks(8) * 2 > kCUs && blocks(8) <= kCUs * 5 / 4 ? 4 : 8;
-  x.rows_wg = x.waves * 16 * x.qt;
+  x.rows_wg = 8 * 16 * x.qt;
   x.n_rb = (int)((R + x.rows_wg - 1) / x.rows_wg);
-  x.splits = 1;
-  const int span = span_most(T, g.G, x.rows_wg, window, sink, max_len);
-  // (fewer workgroups than CUs: their keys are split, down to 512)
-  if (x.waves == 8)
-    while (x.splits < 16 && units * x.n_rb * x.splits * 2 <= kWindowChunkWgs && span > 512 * x.splits) x.splits *= 2;
-  x.split_keys = x.splits == 1 ? span : ((span + x.splits - 1) / x.splits + kChKeys - 1) / kChKeys * kChKeys;
-  x.splits = (span + x.split_keys - 1) / x.split_keys;
-  x.blocks = units * x.n_rb * x.splits;
+  x.blocks = units * x.n_rb;
+  // (two to a CU and more: dealt out longest first)
+  x.split = x.blocks < 2 * kCUs && n <= 512;
   return x;
 }
 
-hipError_t launch_window_chunk(const Geom& g, const WindowCall& a, const WindowChunkPlan& x, bool q8, hipStream_t s) {
-  const int d = g.d;
-  if (g.dtype == KARA_F32)   // (over codes: rows of fp32 go through the split kernel)
-    return x.waves == 8 ? launch<true, 3, 1, 8>(d, a, x.blocks, s) : launch<true, 3, 1, 4>(d, a, x.blocks, s);
-  return q8 ? launch_bf16<true>(d, a, x, s) : launch_bf16<false>(d, a, x, s);
+// (whether keys may be split goes by the blocks, which a smaller call has fewer of)
+size_t window_chunk_workspace(const Geom& g, int n, int n_layers, int T) {
+  const WindowChunkPlan x = window_chunk_plan(g, n, n_layers, T);
+  return records_bytes(g, x) + (size_t)std::min(n, 512) * sizeof(int2);
+}
+
+hipError_t launch_window_chunk(const Geom& g, const WindowCall& a, const WindowChunkPlan& x, bool q8, void* workspace,
+                               hipStream_t s) {
+  ChunkSplit sp{};
+  if (x.split) {
+    sp.most = a.n;
+    sp.o = (float*)workspace;
+    sp.ml = sp.o + (size_t)kMostRecords * x.rows_wg * g.d;
+    sp.of_seq = (int2*)(sp.ml + (size_t)kMostRecords * x.rows_wg * 2);
+  }
+  const unsigned grid = (unsigned)(x.blocks + (x.split ? kCUs : 0));
+  hipError_t e;
+  if (g.dtype == KARA_F32) e = launch<true, 3, 1>(g.d, a, sp, grid, s);   // (over codes: rows of fp32 are split)
+  else if (q8) e = x.qt == 1 ? launch<true, 1, 1>(g.d, a, sp, grid, s) : launch<true, 1, 2>(g.d, a, sp, grid, s);
+  else e = x.qt == 1 ? launch<false, 1, 1>(g.d, a, sp, grid, s) : launch<false, 1, 2>(g.d, a, sp, grid, s);
+  if (e != hipSuccess || !x.split) return e;
+  const dim3 joins((unsigned)x.blocks, (unsigned)(x.rows_wg / kJoinRows));
+#define KARA_WINDOW_JOIN(D, B) \
+  hipLaunchKernelGGL((window_join_kernel<D, B>), joins, dim3(kJoinThreads), 0, s, (const WindowHead&)a, sp, x.rows_wg)
+  if (g.d == 128) {
+    if (g.dtype == KARA_F32) KARA_WINDOW_JOIN(128, false);
+    else KARA_WINDOW_JOIN(128, true);
+  } else {
+    if (g.dtype == KARA_F32) KARA_WINDOW_JOIN(64, false);
+    else KARA_WINDOW_JOIN(64, true);
+  }
+#undef KARA_WINDOW_JOIN
+  return hipGetLastError();
 }
 
 }  // namespace kara
