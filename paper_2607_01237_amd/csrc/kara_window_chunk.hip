@@ -585,18 +585,22 @@ __global__ __launch_bounds__(512, 2) void window_chunk_kernel(WindowCall a, Chun
       // products: where a result is not finite (codes are), all over again with such
       // values apart.  (Asked in every chunk that some rows see keys of and others do not,
       // it took 12 of 113 us: 4 x 1024 queries in a window of 1024.)
-      bool odd = false;
+      floatx4 zero[QT];
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        float x = 0.f;
+        zero[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][dt]));
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x = fmaf(o[qt][dt][r], 0.f, x);
+          for (int r = 0; r < 4; ++r) zero[qt][r] = fmaf(o[qt][dt][r], 0.f, zero[qt][r]);
         }
-        odd |= !(x == 0.f);
       }
+      bool odd = false;
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) odd |= !(zero[qt][r] == 0.f);
       if (__syncthreads_or(odd)) {
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
@@ -614,26 +618,47 @@ __global__ __launch_bounds__(512, 2) void window_chunk_kernel(WindowCall a, Chun
   // ---- lane holds O^T[dt*16 + 4*gq + r][query li] ----
 #pragma unroll
   for (int qt = 0; qt < QT; ++qt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][DT - 1]), "+v"(lsum[qt]));   // (as above)
+  if (splits == 1) {
+    // Through LDS, whose stages no wave reads any more: rows of a few lanes' 16 bytes each,
+    // where the accumulators would give 8 bytes of 16 rows at a time (16 x 1024 queries in a
+    // window of 1024: 395 us so).
+    constexpr int kOut = D * (NT == 1 ? 2 : 4), kOutChunks = kOut / 16;       // bytes of a row, pieces
+    constexpr int kSwz = (kOutChunks < 16 ? kOutChunks : 16) - 1;
+    static_assert(W * QT * 16 * kOut <= C::kStages * 2 * C::kTile, "the waves' rows fit the stages");
+    lds_barrier();
+    char* const mine = smem[0] + wave * (QT * 16 * kOut);
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) {
-    const int r = wrow0 + qt * 16 + li;
-    if (r >= R) continue;
-    const int t = r / G;
-    const int64_t at = orow + (int64_t)t * g.Hq + (r - t * G);
-    if (splits == 1) {
+    for (int qt = 0; qt < QT; ++qt) {
       const float inv = lsum[qt][0] == 0.f ? 0.f : 1.f / lsum[qt][0];    // (a row that sees no key)
+      char* const row = mine + (qt * 16 + li) * kOut;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const floatx4 v = o[qt][dt] * inv;
         if constexpr (NT == 1) {
-          const bf16x2 x = {(__bf16)v[0], (__bf16)v[1]}, y = {(__bf16)v[2], (__bf16)v[3]};
-          *(uint2*)((__bf16*)a.out + at * D + dt * 16 + 4 * gq) =
-              uint2{__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
+          const bf16x2 p = {(__bf16)v[0], (__bf16)v[1]}, q = {(__bf16)v[2], (__bf16)v[3]};
+          *(uint2*)(row + (((dt * 2 + (gq >> 1)) ^ (li & kSwz)) * 16) + (gq & 1) * 8) =
+              uint2{__builtin_bit_cast(uint32_t, p), __builtin_bit_cast(uint32_t, q)};
         } else {
-          *(floatx4*)((float*)a.out + at * D + dt * 16 + 4 * gq) = v;
+          *(floatx4*)(row + (((dt * 4 + gq) ^ (li & kSwz)) * 16)) = v;
         }
       }
-    } else {
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (a wave reads its own rows alone)
+#pragma unroll
+    for (int k = 0; k < QT * 16 * kOutChunks / 64; ++k) {
+      const int i = (k * 64 + lane) / kOutChunks, piece = (k * 64 + lane) % kOutChunks;
+      const int r = wrow0 + i;
+      const uint4 v = *(const uint4*)(mine + i * kOut + ((piece ^ (i & 15 & kSwz)) * 16));
+      if (r < R) {
+        const int t = r / G;
+        *(uint4*)((char*)a.out + (orow + (int64_t)t * g.Hq + (r - t * G)) * kOut + piece * 16) = v;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      const int r = wrow0 + qt * 16 + li;
+      if (r >= R) continue;
       // (a split without keys: a record of no weight)
       const int64_t rec = (first_record + (int64_t)(u * a.n_rt + rb) * splits + split) * kRowsWg + (r - row0);
       if (gq == 0) *(floatx2*)(x.ml + 2 * rec) = floatx2{m[qt], lsum[qt][0]};
