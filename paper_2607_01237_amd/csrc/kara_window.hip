@@ -56,9 +56,11 @@ struct WinCfg {
 // they stand; of 16-bit values, pairs of columns are put together to pairs of keys by
 // byte permutes.
 //
-// Rows of fp32 go through the fp32 matrix instructions.  NT: bf16 terms of a query and of
-// a weight over codes (3 where p->dtype is fp32: 24 bits; codes are exact in one).
-template <Cache CT, int NT, int D, int NL>
+// Rows of fp32 go through the fp32 matrix instructions.  NT: bf16 terms of a query over codes
+// (3 where p->dtype is fp32: 24 bits; codes are exact in one).  NP: bf16 terms of a weight:
+// 3 for fp32 outputs, 2 for bf16 ones: a weight rounded to bf16 would leave an output of
+// flat weights 2.3e-3 off, two terms 1.66e-3, its own rounding, for half a per cent of the time.
+template <Cache CT, int NT, int NP, int D, int NL>
 __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<NL> a) {
   using C = WinCfg<CT, D>;
   constexpr int TB = C::kTB, KC = C::kKC, E = C::kE, VW = C::kVW;
@@ -400,23 +402,24 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
           o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(pv[r][e]), p[0][r], o[e], 0, 0, 0);
       }
     } else {
-      uint32_t pw[NT][4];                  // terms of the lane's eight weights, in pairs
+      uint32_t pw[NP][4];                  // terms of the lane's eight weights, in pairs
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; r += 2) {
-          if constexpr (NT > 1) lsum += p[t][r] + p[t][r + 1];
-          uint32_t w[NT];
+          if constexpr (!kOutBf16) lsum += p[t][r] + p[t][r + 1];
+          uint32_t w[NP];
           bf16_term_pairs<false>(p[t][r], p[t][r + 1], w);
 #pragma unroll
-          for (int y = 0; y < NT; ++y) pw[y][2 * t + (r >> 1)] = w[y];
+          for (int y = 0; y < NP; ++y) pw[y][2 * t + (r >> 1)] = w[y];
         }
-      bf16x8 pb[NT];
+      bf16x8 pb[NP];
 #pragma unroll
-      for (int y = 0; y < NT; ++y) pb[y] = __builtin_bit_cast(bf16x8, uint4{pw[y][0], pw[y][1], pw[y][2], pw[y][3]});
-      // (one term: the sum is of the rounded weights, as the output is, and formed as
-      // one more product, with ones)
-      if constexpr (NT == 1) lones = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[0], lones, 0, 0, 0);
+      for (int y = 0; y < NP; ++y) pb[y] = __builtin_bit_cast(bf16x8, uint4{pw[y][0], pw[y][1], pw[y][2], pw[y][3]});
+      // (of bf16 calls the sum is one more product, with ones, of the weights as they are held)
+      if constexpr (kOutBf16)
+#pragma unroll
+        for (int y = NP - 1; y >= 0; --y) lones = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[y], lones, 0, 0, 0);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
@@ -425,7 +428,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
                           __builtin_amdgcn_perm(pv[5][e >> 1], pv[4][e >> 1], sel),
                           __builtin_amdgcn_perm(pv[7][e >> 1], pv[6][e >> 1], sel)};
 #pragma unroll
-        for (int y = NT - 1; y >= 0; --y)
+        for (int y = NP - 1; y >= 0; --y)
           o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[y], o[e], 0, 0, 0);
       }
     }
@@ -615,18 +618,18 @@ void set_pools(WindowCallOf<NL>* a, const void* const* k, const void* const* v, 
   set_pools(&a->vsp, vs, a->n_layers);
 }
 
-template <Cache CT, int NT, int NL>
+template <Cache CT, int NT, int NP, int NL>
 void launch_split(int d, const WindowCallOf<NL>& a, int64_t blocks, hipStream_t s) {
-  if (d == 128) hipLaunchKernelGGL((window_split_kernel<CT, NT, 128, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((window_split_kernel<CT, NT, 64, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+  if (d == 128) hipLaunchKernelGGL((window_split_kernel<CT, NT, NP, 128, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((window_split_kernel<CT, NT, NP, 64, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
 }
 template <int NL>
 hipError_t launch_split(const Geom& g, bool q8, const WindowCallOf<NL>& a, int64_t blocks, hipStream_t s) {
   const bool f32 = g.dtype == KARA_F32;
-  if (q8 && f32) launch_split<kCodes, 3>(g.d, a, blocks, s);
-  else if (q8) launch_split<kCodes, 1>(g.d, a, blocks, s);
-  else if (f32) launch_split<kRowsF32, 1>(g.d, a, blocks, s);
-  else launch_split<kRowsBf16, 1>(g.d, a, blocks, s);
+  if (q8 && f32) launch_split<kCodes, 3, 3>(g.d, a, blocks, s);
+  else if (q8) launch_split<kCodes, 1, 2>(g.d, a, blocks, s);
+  else if (f32) launch_split<kRowsF32, 1, 1>(g.d, a, blocks, s);
+  else launch_split<kRowsBf16, 1, 2>(g.d, a, blocks, s);
   return hipGetLastError();
 }
 
