@@ -23,11 +23,10 @@ constexpr int kSplitMin = 512;       // keys per split, at least (of a span of m
 constexpr int kSplitMax = 4608;      // at most
 constexpr int kSplitRuns = 1024;     // runs of keys a split's LDS table holds
 constexpr int kWgsAtOnce = 512;      // workgroups that run at once, two to a CU
-constexpr int kTileRows = 16;
 
 enum Cache { kRowsBf16, kRowsF32, kCodes };
 
-template <Cache CT, int D>
+template <Cache CT, int D, int QT>
 struct WinCfg {
   static constexpr int kTB = CT == kRowsF32 ? 1 : 2;               // tiles of 16 keys per block
   static constexpr int kBlock = 16 * kTB;
@@ -40,10 +39,12 @@ struct WinCfg {
   // cost a quarter of a long decoding step).  Then a block's values are on their way while
   // its logits are formed, the next block's keys behind them.
   static constexpr int kVBuf = kRow >= 256 ? 1 : 2;
+  // With two tiles of rows its keys too are asked for behind the products of the present ones.
+  static constexpr int kKBuf = kRow >= 256 && QT == 2 ? 1 : 2;
 };
 
-// One workgroup of four waves per (layer, sequence, KV head, tile of 16 query rows, split
-// of split_keys keys of the tile's span): for the tile's rows, the split's maximum m,
+// One workgroup of four waves per (layer, sequence, KV head, tile of 16 QT query rows,
+// split of split_keys keys of the tile's span): for the tile's rows, the split's maximum m,
 // exponential sum l and unnormalised output o, in log2 units and fp32.  Rows of a (layer,
 // sequence, KV head) run over (query, head in group).
 //
@@ -60,9 +61,10 @@ struct WinCfg {
 // (3 where p->dtype is fp32: 24 bits; codes are exact in one).  NP: bf16 terms of a weight:
 // 3 for fp32 outputs, 2 for bf16 ones: a weight rounded to bf16 would leave an output of
 // flat weights 2.3e-3 off, two terms 1.66e-3, its own rounding, for half a per cent of the time.
-template <Cache CT, int NT, int NP, int D, int NL>
+template <Cache CT, int NT, int NP, int D, int QT, int NL>
 __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<NL> a) {
-  using C = WinCfg<CT, D>;
+  using C = WinCfg<CT, D, QT>;
+  constexpr int kTileRows = 16 * QT;
   constexpr int TB = C::kTB, KC = C::kKC, E = C::kE, VW = C::kVW;
   constexpr bool F32 = CT == kRowsF32;
   constexpr bool kOutBf16 = !F32 && NT == 1;
@@ -73,9 +75,9 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
   };
   __shared__ __attribute__((aligned(16))) union {
     Table t;
-    float o[kWaves][16][D];
+    float o[kWaves][kTileRows][D];
   } lds;
-  __shared__ float red_m[kWaves][16], red_l[kWaves][16];
+  __shared__ float red_m[kWaves][kTileRows], red_l[kWaves][kTileRows];
   Table& tab = lds.t;
 
   const Dims& g = a.g;
@@ -126,31 +128,33 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
   const float c = g.scale * kLog2e;
   const int nblk = (nk + C::kBlock - 1) / C::kBlock;
 
-  // lane (gq, li): its pieces of query row li, and the row's position
-  const bool there = li < rows;
-  int qhi = -1, qlo = 0;                       // the keys it sees, sinks not counted
-  uint4 qraw[F32 || NT > 1 ? D / 16 : KS];
-  {
-    const int r = row0 + (there ? li : 0);
+  // lane (gq, li): its pieces of query row li of each tile, and the keys that the row sees
+  int qhi[QT], qlo[QT];                        // (sinks not counted; none: of a row that is not there)
+  uint4 qraw[QT][F32 || NT > 1 ? D / 16 : KS];
+#pragma unroll
+  for (int qt = 0; qt < QT; ++qt) {
+    const bool there = qt * 16 + li < rows;
+    const int r = row0 + (there ? qt * 16 + li : 0);
     const int t = T == 1 ? 0 : r / G;
-    if (there) qhi = len - T + t - sp.gap, qlo = qhi - a.window + 1;
+    qhi[qt] = there ? len - T + t - sp.gap : -1;
+    qlo[qt] = there ? qhi[qt] - a.window + 1 : 0;
     const char* src = (const char*)a.q + (orow + (int64_t)t * g.Hq + (r - t * G)) * D * (kOutBf16 ? 2 : 4);
     if constexpr (F32) {
 #pragma unroll
-      for (int x = 0; x < KC; ++x) qraw[x] = *(const uint4*)(src + (gq + 4 * x) * 16);
+      for (int x = 0; x < KC; ++x) qraw[qt][x] = *(const uint4*)(src + (gq + 4 * x) * 16);
     } else if constexpr (CT == kRowsBf16) {
 #pragma unroll
-      for (int x = 0; x < KS; ++x) qraw[x] = *(const uint4*)(src + (gq + 4 * x) * 16);
+      for (int x = 0; x < KS; ++x) qraw[qt][x] = *(const uint4*)(src + (gq + 4 * x) * 16);
     } else {
       // (octet x lies in 16 codes: those of piece x / 2)
 #pragma unroll
       for (int x = 0; x < KS; ++x) {
         const int at = (gq + 4 * (x >> 1)) * 16 + (x & 1) * 8;
         if constexpr (NT == 1) {
-          qraw[x] = *(const uint4*)(src + at * 2);
+          qraw[qt][x] = *(const uint4*)(src + at * 2);
         } else {
-          qraw[2 * x] = *(const uint4*)(src + at * 4);
-          qraw[2 * x + 1] = *(const uint4*)(src + at * 4 + 16);
+          qraw[qt][2 * x] = *(const uint4*)(src + at * 4);
+          qraw[qt][2 * x + 1] = *(const uint4*)(src + at * 4 + 16);
         }
       }
     }
@@ -188,7 +192,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
     return tab.row[key >> run] + (uint32_t)(key & run_mask);
   };
   auto scale_of = [&](int key) __attribute__((always_inline)) { return tab.scale[min(key, nk - 1) >> run]; };
-  uint4 kb[2][TB][KC];
+  uint4 kb[C::kKBuf][TB][KC];
   uint32_t vb[C::kVBuf][TB][4][VW];
   auto load_k = [&](int blk, int b) __attribute__((always_inline)) {
     uint64_t kat[TB];
@@ -237,34 +241,43 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
       if (tid + k * kThreads < runs) tab.scale[tid + k * kThreads] = scale_pair[k];
     lds_barrier();
   }
-  bf16x8 qa[F32 ? 1 : NT][KS];
-  if constexpr (!F32) {
+  bf16x8 qa[QT][F32 ? 1 : NT][KS];
 #pragma unroll
-    for (int x = 0; x < KS; ++x) {
-      if constexpr (NT == 1) {
-        qa[0][x] = __builtin_bit_cast(bf16x8, there ? qraw[x] : uint4{0, 0, 0, 0});
-      } else {
-        const floatx4 u = __builtin_bit_cast(floatx4, qraw[2 * x]), v = __builtin_bit_cast(floatx4, qraw[2 * x + 1]);
-        uint32_t w[4][NT];
+  for (int qt = 0; qt < QT; ++qt) {
+    const bool there = qt * 16 + li < rows;
+    if constexpr (!F32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x0 = i < 2 ? u[2 * i] : v[2 * i - 4], x1 = i < 2 ? u[2 * i + 1] : v[2 * i - 3];
-          bf16_term_pairs<true>(there ? x0 : 0.f, there ? x1 : 0.f, w[i]);
+      for (int x = 0; x < KS; ++x) {
+        if constexpr (NT == 1) {
+          qa[qt][0][x] = __builtin_bit_cast(bf16x8, there ? qraw[qt][x] : uint4{0, 0, 0, 0});
+        } else {
+          const floatx4 u = __builtin_bit_cast(floatx4, qraw[qt][2 * x]);
+          const floatx4 v = __builtin_bit_cast(floatx4, qraw[qt][2 * x + 1]);
+          uint32_t w[4][NT];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x0 = i < 2 ? u[2 * i] : v[2 * i - 4], x1 = i < 2 ? u[2 * i + 1] : v[2 * i - 3];
+            bf16_term_pairs<true>(there ? x0 : 0.f, there ? x1 : 0.f, w[i]);
+          }
+#pragma unroll
+          for (int y = 0; y < NT; ++y) qa[qt][y][x] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
         }
-#pragma unroll
-        for (int y = 0; y < NT; ++y) qa[y][x] = __builtin_bit_cast(bf16x8, uint4{w[0][y], w[1][y], w[2][y], w[3][y]});
       }
+    } else {
+#pragma unroll
+      for (int x = 0; x < KC; ++x) qraw[qt][x] = there ? qraw[qt][x] : uint4{0, 0, 0, 0};
     }
-  } else {
-#pragma unroll
-    for (int x = 0; x < KC; ++x) qraw[x] = there ? qraw[x] : uint4{0, 0, 0, 0};
   }
-
-  float m = kMaxFloor, lsum = 0.f;   // query li's reference, and this lane's part of its sum
-  floatx4 lones = {0.f, 0.f, 0.f, 0.f};   // bf16: the sum, in every element
-  floatx4 o[E];                      // query li, column e of lanes 4gq + r
+  float m[QT], lsum[QT];             // query li's reference, and this lane's part of its sum
+  floatx4 lones[QT];                 // bf16: the sum, in every element
+  floatx4 o[QT][E];                  // query li, column e of lanes 4gq + r
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int qt = 0; qt < QT; ++qt) {
+    m[qt] = kMaxFloor, lsum[qt] = 0.f;
+    lones[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[qt][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
   bf16x8 ones;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
@@ -274,17 +287,24 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
   const int all_lo = sp.i1 - a.window + 1 - sp.gap, all_hi = sp.i0 - sp.gap;
   auto in = [&](int v, int lo, int hi) __attribute__((always_inline)) { return v <= hi && (v >= lo || v < a.sink); };
 
-  auto work = [&](int blk, int b, int vbuf) __attribute__((always_inline)) {
-    floatx4 sv[TB];
+  bool careful = false;              // (rows) whether infinite and NaN values are taken apart
+  // block blk, its keys in buffer b and values in vbuf; next: the block whose keys follow
+  // into one buffer
+  auto work = [&](int blk, int b, int vbuf, int next) __attribute__((always_inline)) {
+    floatx4 sv[QT][TB];
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
-      floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) sv[qt][t] = floatx4{0.f, 0.f, 0.f, 0.f};
       if constexpr (F32) {
 #pragma unroll
         for (int x = 0; x < KC; ++x) {
-          const floatx4 ka = __builtin_bit_cast(floatx4, kb[b][t][x]), qx = __builtin_bit_cast(floatx4, qraw[x]);
+          const floatx4 ka = __builtin_bit_cast(floatx4, kb[b][t][x]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[i], qx[i], acc, 0, 0, 0);
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt)
+              sv[qt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[i], __builtin_bit_cast(floatx4, qraw[qt][x])[i], sv[qt][t], 0, 0, 0);
         }
       } else {
         float scale = 0.f;
@@ -299,15 +319,20 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
             ka = __builtin_bit_cast(bf16x8, kb[b][t][x]);
           }
 #pragma unroll
-          for (int y = NT - 1; y >= 0; --y) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qa[y][x], acc, 0, 0, 0);
+          for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) sv[qt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qa[qt][y][x], sv[qt][t], 0, 0, 0);
         }
       }
-      sv[t] = acc;
     }
     // Wait states between the last product and the first read of its result, which lies
     // past a branch: the compiler does not count across it.
 #pragma unroll
-    for (int t = 0; t < TB; ++t) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[t]));
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(sv[qt][t]));
+    if constexpr (C::kKBuf == 1)
+      if (next < nblk) load_k(next, 0);
     // values as the second products take them: of 16 bits, pairs of columns
     constexpr int VP = F32 ? E : E / 2;
     uint32_t pv[TB * 4][VP];
@@ -336,90 +361,98 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int v = v0 + t * 16 + 4 * gq + r;
-          if (!in(v, qlo, qhi)) sv[t][r] = kNegInf;
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            if (!in(v, qlo[qt], qhi[qt])) sv[qt][t][r] = kNegInf;
           // what no row sees may be anything: its weights are 0, its values must be finite
           if (!in(v, any_lo, any_hi))
 #pragma unroll
             for (int y = 0; y < VP; ++y) pv[4 * t + r][y] = 0;
         }
-      if constexpr (CT != kCodes) {
-        // what some rows see and others do not must not reach those either
-        if (sp.i0 != sp.i1) {
-          uint32_t hit = 0;
+    }
+    if (CT != kCodes && careful) {
+      uint32_t hit = 0;
 #pragma unroll
-          for (int i = 0; i < TB * 4; ++i)
+      for (int i = 0; i < TB * 4; ++i)
 #pragma unroll
-            for (int y = 0; y < VP; ++y) {
-              if constexpr (F32) hit |= (pv[i][y] & 0x7fffffffu) >= 0x7f800000u;
-              else hit |= ((pv[i][y] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
-            }
-          odd_values = __ballot(hit != 0) != 0ull;
-          if (odd_values) {
-#pragma unroll
-            for (int i = 0; i < TB * 4; ++i)
-#pragma unroll
-              for (int y = 0; y < VP; ++y) {
-                if constexpr (F32) {
-                  if ((pv[i][y] & 0x7fffffffu) >= 0x7f800000u) pv[i][y] = 0;
-                } else {
-                  if ((pv[i][y] & 0x7f80u) == 0x7f80u) pv[i][y] &= 0xffff0000u;
-                  if ((pv[i][y] & 0x7f800000u) == 0x7f800000u) pv[i][y] &= 0xffffu;
-                }
-              }
-          }
+        for (int y = 0; y < VP; ++y) {
+          if constexpr (F32) hit |= (pv[i][y] & 0x7fffffffu) >= 0x7f800000u;
+          else hit |= ((pv[i][y] & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
         }
+      odd_values = __ballot(hit != 0) != 0ull;
+      if (odd_values) {
+#pragma unroll
+        for (int i = 0; i < TB * 4; ++i)
+#pragma unroll
+          for (int y = 0; y < VP; ++y) {
+            if constexpr (F32) {
+              if ((pv[i][y] & 0x7fffffffu) >= 0x7f800000u) pv[i][y] = 0;
+            } else {
+              if ((pv[i][y] & 0x7f80u) == 0x7f80u) pv[i][y] &= 0xffff0000u;
+              if ((pv[i][y] & 0x7f800000u) == 0x7f800000u) pv[i][y] &= 0xffffu;
+            }
+          }
       }
     }
-    float mx = sv[0][0];
+    bf16x8 pb[QT][F32 ? 1 : NP];           // terms of the lane's eight weights
+    float p[QT][TB][4];
 #pragma unroll
-    for (int t = 0; t < TB; ++t)
+    for (int qt = 0; qt < QT; ++qt) {
+      float mx = sv[qt][0][0];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sv[t][r]);
-    // The reference m, one for the four lanes of a query, is raised only where a
-    // logit passes it by more than 2^8: no exchange between lanes before that.
-    if (__ballot(mx * c > m + 8.f) != 0ull) {
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
-      const float mn = fmaxf(m, mx);
-      const float f = __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      lsum *= f;
-      lones *= f;
+      for (int t = 0; t < TB; ++t)
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] *= f;
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sv[qt][t][r]);
+      // The reference m, one for the four lanes of a query, is raised only where a
+      // logit passes it by more than 2^8: no exchange between lanes before that.
+      if (__ballot(mx * c > m[qt] + 8.f) != 0ull) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
+        const float mn = fmaxf(m[qt], mx);
+        const float f = __builtin_amdgcn_exp2f(m[qt] - mn);
+        m[qt] = mn;
+        lsum[qt] *= f;
+        lones[qt] *= f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[qt][e] *= f;
+      }
+#pragma unroll
+      for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[qt][t][r] = __builtin_amdgcn_exp2f(fmaf(sv[qt][t][r], c, -m[qt]));
+      if constexpr (F32) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) lsum[qt] += p[qt][0][r];
+      } else {
+        uint32_t pw[NP][4];                  // in pairs
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; r += 2) {
+            if constexpr (!kOutBf16) lsum[qt] += p[qt][t][r] + p[qt][t][r + 1];
+            uint32_t w[NP];
+            bf16_term_pairs<false>(p[qt][t][r], p[qt][t][r + 1], w);
+#pragma unroll
+            for (int y = 0; y < NP; ++y) pw[y][2 * t + (r >> 1)] = w[y];
+          }
+#pragma unroll
+        for (int y = 0; y < NP; ++y) pb[qt][y] = __builtin_bit_cast(bf16x8, uint4{pw[y][0], pw[y][1], pw[y][2], pw[y][3]});
+        // (of bf16 calls the sum is one more product, with ones, of the weights as they are held)
+        if constexpr (kOutBf16)
+#pragma unroll
+          for (int y = NP - 1; y >= 0; --y)
+            lones[qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[qt][y], lones[qt], 0, 0, 0);
+      }
     }
-    float p[TB][4];
-#pragma unroll
-    for (int t = 0; t < TB; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) p[t][r] = __builtin_amdgcn_exp2f(fmaf(sv[t][r], c, -m));
     if constexpr (F32) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        lsum += p[0][r];
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(pv[r][e]), p[0][r], o[e], 0, 0, 0);
-      }
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            o[qt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(pv[r][e]), p[qt][0][r], o[qt][e], 0, 0, 0);
     } else {
-      uint32_t pw[NP][4];                  // terms of the lane's eight weights, in pairs
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; r += 2) {
-          if constexpr (!kOutBf16) lsum += p[t][r] + p[t][r + 1];
-          uint32_t w[NP];
-          bf16_term_pairs<false>(p[t][r], p[t][r + 1], w);
-#pragma unroll
-          for (int y = 0; y < NP; ++y) pw[y][2 * t + (r >> 1)] = w[y];
-        }
-      bf16x8 pb[NP];
-#pragma unroll
-      for (int y = 0; y < NP; ++y) pb[y] = __builtin_bit_cast(bf16x8, uint4{pw[y][0], pw[y][1], pw[y][2], pw[y][3]});
-      // (of bf16 calls the sum is one more product, with ones, of the weights as they are held)
-      if constexpr (kOutBf16)
-#pragma unroll
-        for (int y = NP - 1; y >= 0; --y) lones = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[y], lones, 0, 0, 0);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
@@ -429,7 +462,9 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
                           __builtin_amdgcn_perm(pv[7][e >> 1], pv[6][e >> 1], sel)};
 #pragma unroll
         for (int y = NP - 1; y >= 0; --y)
-          o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[y], o[e], 0, 0, 0);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+            o[qt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[qt][y], o[qt][e], 0, 0, 0);
       }
     }
     if constexpr (CT != kCodes) {
@@ -437,11 +472,12 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
         // infinite and NaN values, taken out above: added where they are seen (a weight
         // is positive), key by key, the rows read again
 #pragma unroll
-        for (int e = 0; e < E; ++e) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[e]));
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+          for (int e = 0; e < E; ++e) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][e]));
         for (int key = 0; key < C::kBlock; ++key) {
           if (!in(v0 + key, any_lo, any_hi)) continue;
           const char* row = (const char*)a.vp.p[l] + (uint64_t)row_of(blk * C::kBlock + key) * C::kRow;
-          const bool mine = in(v0 + key, qlo, qhi);
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -450,7 +486,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
               uint32_t x;
               if constexpr (F32) x = ((const uint32_t*)row)[col];
               else x = (uint32_t)((const uint16_t*)row)[col] << 16;
-              if (mine && (x & 0x7fffffffu) >= 0x7f800000u) o[e][r] += __uint_as_float(x);
+              if ((x & 0x7fffffffu) >= 0x7f800000u)
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt)
+                  if (in(v0 + key, qlo[qt], qhi[qt])) o[qt][e][r] += __uint_as_float(x);
             }
         }
       }
@@ -458,50 +497,87 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
   };
   // the next block's keys after this block's values, so that waiting for the values
   // leaves the keys on their way
-  if (wave < nblk) {
-    int blk = wave;
-    for (;;) {
-      const int n1 = blk + kWaves;
-      if constexpr (!V1) load_v(blk, 0);
-      if (n1 < nblk) {
-        load_k(n1, 1);
-        if constexpr (V1) load_v(n1, 1);
+  // the wave's blocks, the first one's loads made
+  for (;;) {
+    if constexpr (C::kKBuf == 1) {
+      for (int blk = wave; blk < nblk; blk += kWaves) {
+        load_v(blk, 0);
+        work(blk, 0, 0, blk + kWaves);
       }
-      work(blk, 0, 0);
-      if (n1 >= nblk) break;
-      blk = n1 + kWaves;
-      if constexpr (!V1) load_v(n1, 0);
-      if (blk < nblk) {
-        load_k(blk, 0);
-        if constexpr (V1) load_v(blk, 0);
+    } else if (wave < nblk) {
+      int blk = wave;
+      for (;;) {
+        const int n1 = blk + kWaves;
+        if constexpr (!V1) load_v(blk, 0);
+        if (n1 < nblk) {
+          load_k(n1, 1);
+          if constexpr (V1) load_v(n1, 1);
+        }
+        work(blk, 0, 0, 0);
+        if (n1 >= nblk) break;
+        blk = n1 + kWaves;
+        if constexpr (!V1) load_v(n1, 0);
+        if (blk < nblk) {
+          load_k(blk, 0);
+          if constexpr (V1) load_v(blk, 0);
+        }
+        work(n1, 1, V1, 0);
+        if (blk >= nblk) break;
       }
-      work(n1, 1, V1);
-      if (blk >= nblk) break;
     }
+    // An infinite or NaN value that a row does not see has met its weight of 0 in the
+    // products, and one that it sees the second term of its weight, which may be 0: where a
+    // result is not finite (codes are), the wave's blocks again with such values apart.
+    if (CT == kCodes || careful) break;
+    floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][e]));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) zero[r] = fmaf(o[qt][e][r], 0.f, zero[r]);
+      }
+    if (__ballot(!(zero[0] + zero[1] + zero[2] + zero[3] == 0.f)) == 0ull) break;
+    careful = true;
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      m[qt] = kMaxFloor, lsum[qt] = 0.f;
+      lones[qt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[qt][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    load_k(wave, 0);                 // (a wave without blocks has sums of 0)
+    if constexpr (V1) load_v(wave, 0);
   }
 
   // ---- the waves' sums ----
 #pragma unroll
-  for (int e = 0; e < E; ++e) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[e]));   // (as above, past the loop's branch)
-  if constexpr (kOutBf16) {
-    asm volatile("s_nop 7\n\ts_nop 3" : "+v"(lones));
-    lsum = lones[0];
-  } else {
-    lsum += __shfl_xor(lsum, 16, 64);
-    lsum += __shfl_xor(lsum, 32, 64);
-  }
-  if (gq == 0) {
-    red_m[wave][li] = m;
-    red_l[wave][li] = lsum;
+  for (int qt = 0; qt < QT; ++qt) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) asm volatile("s_nop 7\n\ts_nop 3" : "+v"(o[qt][e]));   // (as above, past the loop's branch)
+    if constexpr (kOutBf16) {
+      asm volatile("s_nop 7\n\ts_nop 3" : "+v"(lones[qt]));
+      lsum[qt] = lones[qt][0];
+    } else {
+      lsum[qt] += __shfl_xor(lsum[qt], 16, 64);
+      lsum[qt] += __shfl_xor(lsum[qt], 32, 64);
+    }
+    if (gq == 0) {
+      red_m[wave][qt * 16 + li] = m[qt];
+      red_l[wave][qt * 16 + li] = lsum[qt];
+    }
   }
   __syncthreads();   // the table is no longer read
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+  for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-    for (int e = 0; e < E; e += 4) {
-      const int col = F32 && E == 8 ? (e >> 2) * 64 + 4 * (4 * gq + r) : E * (4 * gq + r) + e;
-      *(floatx4*)&lds.o[wave][li][col] = floatx4{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]};
-    }
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const int col = F32 && E == 8 ? (e >> 2) * 64 + 4 * (4 * gq + r) : E * (4 * gq + r) + e;
+        *(floatx4*)&lds.o[wave][qt * 16 + li][col] = floatx4{o[qt][e][r], o[qt][e + 1][r], o[qt][e + 2][r], o[qt][e + 3][r]};
+      }
   __syncthreads();
   const bool direct = a.n_splits == 1;
   for (int x = tid; x < rows * D; x += kThreads) {
@@ -618,19 +694,34 @@ void set_pools(WindowCallOf<NL>* a, const void* const* k, const void* const* v, 
   set_pools(&a->vsp, vs, a->n_layers);
 }
 
-template <Cache CT, int NT, int NP, int NL>
+template <Cache CT, int NT, int NP, int QT, int NL>
 void launch_split(int d, const WindowCallOf<NL>& a, int64_t blocks, hipStream_t s) {
-  if (d == 128) hipLaunchKernelGGL((window_split_kernel<CT, NT, NP, 128, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((window_split_kernel<CT, NT, NP, 64, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+  if (d == 128) hipLaunchKernelGGL((window_split_kernel<CT, NT, NP, 128, QT, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((window_split_kernel<CT, NT, NP, 64, QT, NL>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
 }
 template <int NL>
-hipError_t launch_split(const Geom& g, bool q8, const WindowCallOf<NL>& a, int64_t blocks, hipStream_t s) {
-  const bool f32 = g.dtype == KARA_F32;
-  if (q8 && f32) launch_split<kCodes, 3, 3>(g.d, a, blocks, s);
-  else if (q8) launch_split<kCodes, 1, 2>(g.d, a, blocks, s);
-  else if (f32) launch_split<kRowsF32, 1, 1>(g.d, a, blocks, s);
-  else launch_split<kRowsBf16, 1, 2>(g.d, a, blocks, s);
+hipError_t launch_split(const Geom& g, bool q8, int rows, const WindowCallOf<NL>& a, int64_t blocks, hipStream_t s) {
+  if (g.dtype == KARA_F32) {
+    if (q8) launch_split<kCodes, 3, 3, 1>(g.d, a, blocks, s);
+    else launch_split<kRowsF32, 1, 1, 1>(g.d, a, blocks, s);
+  } else if (rows == 16) {
+    if (q8) launch_split<kCodes, 1, 2, 1>(g.d, a, blocks, s);
+    else launch_split<kRowsBf16, 1, 2, 1>(g.d, a, blocks, s);
+  } else {
+    if (q8) launch_split<kCodes, 1, 2, 2>(g.d, a, blocks, s);
+    else launch_split<kRowsBf16, 1, 2, 2>(g.d, a, blocks, s);
+  }
   return hipGetLastError();
+}
+
+// Query rows of a workgroup.  bf16: 32 where there are more than 16, so that the keys pass
+// once, but in small launches: 96 x 5 queries x 2 layers of 8K, 25 rows a KV head: rows 1667
+// -> 1088 us, codes 858 -> 623; 8 x 5 over 300-4000 tokens, 128 tiles of 16: 28.1, 29.9 so; 8
+// x 16, 256 tiles 41.7, 39.0 so.  fp32 is bound by its products, and workgroups of 32 rows are
+// fewer: 6 x 101 queries of 16 heads 32 us, 44 so.
+int tile_rows(const Geom& g, int n, int n_layers, int T) {
+  const int64_t tiles = (int64_t)n_layers * n * g.Hkv * (((int64_t)g.G * T + 15) / 16);
+  return (int64_t)g.G * T <= 16 || g.dtype == KARA_F32 || tiles < 256 ? 16 : 32;
 }
 
 // q8: whether the cache is of codes (the size over either is the same where it says nothing)
@@ -647,12 +738,13 @@ kara_status_t workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers
   const size_t rec = (g.d + 2) * sizeof(float);
   const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
   if (splits(g, n_query, q8)) {
-    const int span = span_most(n_query, g.G, kTileRows, w, sink, max_len);
+    const int tile = tile_rows(g, n, n_layers, n_query);
+    const int span = span_most(n_query, g.G, tile, w, sink, max_len);
     // (a tile has no more than `few` splits, and no more than the longest ones make or
     // kWgsAtOnce over the tiles: either way their records grow with the tiles)
     const int64_t longest = split_most(g.bs), few = ((int64_t)span + kSplitMin - 1) / kSplitMin;
-    const int64_t tiles = (int64_t)n_layers * n * g.Hkv * (((int64_t)g.G * n_query + kTileRows - 1) / kTileRows);
-    const int64_t many = std::max(rows * (((int64_t)span + longest - 1) / longest), (kWgsAtOnce + tiles) * kTileRows);
+    const int64_t tiles = (int64_t)n_layers * n * g.Hkv * (((int64_t)g.G * n_query + tile - 1) / tile);
+    const int64_t many = std::max(rows * (((int64_t)span + longest - 1) / longest), (kWgsAtOnce + tiles) * tile);
     *bytes = few == 1 ? 0 : (size_t)std::min(rows * few, many) * rec;
   } else {
     *bytes = window_chunk_workspace(g, n, n_layers, n_query);
@@ -691,13 +783,14 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
   a.run = run_of(g.bs);
   a.max_len = max_len;
   const bool few = splits(g, n_query, q8), f32 = g.dtype == KARA_F32;
+  const int tile = tile_rows(g, n, n_layers, n_query);
   const int64_t rows = (int64_t)n_layers * n * n_query * g.Hq;
   WindowChunkPlan plan{};
   int64_t blocks;
   if (few) {
-    a.n_rt = (int)(((int64_t)g.G * n_query + kTileRows - 1) / kTileRows);
+    a.n_rt = (int)(((int64_t)g.G * n_query + tile - 1) / tile);
     const int64_t tiles = (int64_t)n_layers * n * g.Hkv * a.n_rt;
-    const int span = span_most(n_query, g.G, kTileRows, a.window, a.sink, max_len);
+    const int span = span_most(n_query, g.G, tile, a.window, a.sink, max_len);
     a.split_keys = split_keys_of(g.bs, tiles, span);
     a.n_splits = (span + a.split_keys - 1) / a.split_keys;
     blocks = tiles * a.n_splits;
@@ -720,11 +813,11 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
   if (few && n_layers <= kFewLayers) {
     WindowCallOf<kFewLayers> c{a, {}, {}, {}, {}};
     set_pools(&c, k_pools, v_pools, k_scales, v_scales);
-    e = launch_split(g, q8, c, blocks, s);
+    e = launch_split(g, q8, tile, c, blocks, s);
   } else {
     WindowCall c{a, {}, {}, {}, {}};
     set_pools(&c, k_pools, v_pools, k_scales, v_scales);
-    e = few ? launch_split(g, q8, c, blocks, s) : launch_window_chunk(g, c, plan, q8, workspace, s);
+    e = few ? launch_split(g, q8, tile, c, blocks, s) : launch_window_chunk(g, c, plan, q8, workspace, s);
   }
   if (e != hipSuccess || a.n_splits == 1) return hip_status(e);
   const dim3 grid((unsigned)((rows + 3) / 4));
