@@ -118,6 +118,9 @@ CASES = [
     ("f32", "q8", 8, 2, 128, 16, 2, 1, 256, 0), ("bf16", "q8", 8, 2, 128, 7, 150, 1, 100, 4),
     ("f32", "q8", 4, 2, 64, 16, 200, 1, 90, 33), ("bf16", "q8", 16, 8, 64, 256, 200, 1, 1, 1),
     ("bf16", "rows", 2, 1, 128, 16, 33, 1, 40, 2), ("bf16", "rows", 8, 1, 64, 48, 70, 2, 2**31 - 1, 2**31 - 1),
+    # many units of more than 16 rows: 32 a workgroup
+    ("bf16", "rows", 64, 16, 128, 16, 7, 1, 100, 4), ("bf16", "q8", 64, 16, 128, 24, 5, 1, 40, 20),
+    ("bf16", "rows", 32, 16, 64, 7, 13, 1, 0, 0), ("bf16", "q8", 32, 16, 64, 16, 30, 1, 77, 3),
 ]
 
 
@@ -155,7 +158,8 @@ def _odd(kind):
 @pytest.mark.parametrize("case", [
     ("bf16", "rows", 8, 2, 128, 16, 1, 1, 100, 4), ("bf16", "rows", 8, 2, 64, 16, 9, 1, 40, 4),
     ("f32", "rows", 8, 2, 128, 16, 9, 1, 40, 4), ("f32", "rows", 8, 2, 64, 24, 60, 1, 40, 4),
-    ("bf16", "rows", 8, 2, 128, 16, 150, 1, 100, 4), ("bf16", "rows", 4, 2, 64, 24, 120, 1, 0, 0)],
+    ("bf16", "rows", 8, 2, 128, 16, 150, 1, 100, 4), ("bf16", "rows", 4, 2, 64, 24, 120, 1, 0, 0),
+    ("bf16", "rows", 64, 16, 128, 16, 7, 1, 40, 4), ("bf16", "rows", 64, 16, 64, 16, 5, 1, 0, 0)],
     ids=lambda c: "-".join(map(str, c)))
 def test_values_that_are_not_finite_reach_those_who_see_them(case, kind):
     check(case, spoil=_odd(kind))
