@@ -12,6 +12,7 @@ import array
 import ctypes
 import os
 import re
+import struct
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 # the in-tree library; KARA_LIBRARY names another build of the same sources
@@ -771,19 +772,33 @@ def evict_tokens(p, seqs, keep, n_sink, n_recent, k_pools, v_pools, weights, blo
 
 # ---- the cache held in 8 bits (include/kara_q8.h)
 
+_pack_pointer = struct.Struct("Q").pack
+
+
+def _pool_arg(dev, L, name, ts, n, dtype):
+    """One pool's host array of device pointers, a tensor per layer, as the bytes that ctypes passes the address of."""
+    if len(ts) != L:
+        raise KaraError("marshal", ERR_INVALID_ARG, f"{name}: {len(ts)} layers, expected {L}")
+    ptrs = []
+    for t in ts:
+        if t is None or t.dtype is not dtype or t.numel() < n or t.get_device() != dev or not t.is_contiguous():
+            _reject(dev, f"{name}[{len(ptrs)}]", t, n, dtype)
+        ptrs.append(t.data_ptr())
+    return _pack_pointer(ptrs[0]) if L == 1 else array.array("Q", ptrs).tobytes()
+
+
 def _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales):
     """Pool arguments of a cache of rows (no scales) or of 8-bit codes."""
     units = p.num_pages * p.n_kv_heads
     size = units * p.block_size * p.head_dim
     if k_scales is None and v_scales is None:
         dt = _dtype(torch, p)
-        keep, (k, v) = _pool_args(dev, L, (("k_pools", k_pools, size, dt), ("v_pools", v_pools, size, dt)))
-        return keep, (k, v, None, None)
+        return _pool_arg(dev, L, "k_pools", k_pools, size, dt), _pool_arg(dev, L, "v_pools", v_pools, size, dt), None, None
     if k_scales is None or v_scales is None:
         raise KaraError("marshal", ERR_INVALID_ARG, "k_scales and v_scales: both or neither")
     u8 = torch.uint8
-    return _pool_args(dev, L, (("k_pools", k_pools, size, u8), ("v_pools", v_pools, size, u8),
-                               ("k_scales", k_scales, units, u8), ("v_scales", v_scales, units, u8)))
+    return (_pool_arg(dev, L, "k_pools", k_pools, size, u8), _pool_arg(dev, L, "v_pools", v_pools, size, u8),
+            _pool_arg(dev, L, "k_scales", k_scales, units, u8), _pool_arg(dev, L, "v_scales", v_scales, units, u8))
 
 
 def q8_append(p, seqs, k_new, v_new, k_pools, v_pools, k_scales, v_scales, block_table, seq_lens, status, stream=None):
@@ -795,7 +810,7 @@ def q8_append(p, seqs, k_new, v_new, k_pools, v_pools, k_scales, v_scales, block
     size, dt = L * n * n_new * p.n_kv_heads * p.head_dim, _dtype(torch, p)
     if k_scales is None or v_scales is None:
         raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
-    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    k, v, ks, vs = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
     sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
     _check("kara_q8_append", lib.kara_q8_append(
         ctypes.byref(p), n, sq, n_new, L, _arg(dev, "k_new", k_new, size, dt), _arg(dev, "v_new", v_new, size, dt),
@@ -811,7 +826,7 @@ def q8_read(p, seqs, start, n_rows, k_pools, v_pools, k_scales, v_scales, block_
     size, dt = L * n * n_rows * p.n_kv_heads * p.head_dim, _dtype(torch, p)
     if k_scales is None or v_scales is None:
         raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
-    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    k, v, ks, vs = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
     sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
     _check("kara_q8_read", lib.kara_q8_read(
         ctypes.byref(p), n, sq, _arg(dev, "start", start, p.n_seqs, torch.int32), n_rows, L, k, v, ks, vs, bt, sl,
@@ -833,7 +848,7 @@ def q8_attention(p, seqs, n_query, q, k_pools, v_pools, k_scales, v_scales, bloc
     size, dt = L * n * n_query * p.n_q_heads * p.head_dim, _dtype(torch, p)
     if k_scales is None or v_scales is None:
         raise KaraError("marshal", ERR_INVALID_ARG, "k_scales, v_scales: missing")
-    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    k, v, ks, vs = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
     sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
     ws, ws_bytes = _workspace_arg(dev, workspace)
     _check("kara_q8_attention", lib.kara_q8_attention(
@@ -869,7 +884,7 @@ def rope_append(p, rope: KaraRope, seqs, k_new, v_new, k_pools, v_pools, block_t
         raise KaraError("marshal", ERR_INVALID_ARG, "q and q_out: both or neither")
     if rope.held is not None:
         _arg(dev, "inv_freq", rope.held, (rope.dim or p.head_dim) // 2, torch.float32)
-    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    k, v, ks, vs = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
     sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
     _check("kara_rope_append", lib.kara_rope_append(
         ctypes.byref(p), ctypes.byref(rope), n, sq, n_new, L, None if q is None else _arg(dev, "q", q, q_size, dt),
@@ -895,7 +910,7 @@ def window_attention(p, seqs, n_query, window, n_sink, q, k_pools, v_pools, bloc
     torch, dev, s = _launch(stream)
     n, L, n_query = seqs.numel(), len(k_pools), int(n_query)
     size, dt = L * n * n_query * p.n_q_heads * p.head_dim, _dtype(torch, p)
-    keep, (k, v, ks, vs) = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
+    k, v, ks, vs = _rows_or_q8_args(torch, dev, p, L, k_pools, v_pools, k_scales, v_scales)
     sq, bt, sl = _table_args(torch, dev, p, seqs, block_table, seq_lens)
     ws, ws_bytes = _workspace_arg(dev, workspace)
     _check("kara_window_attention", lib.kara_window_attention(

@@ -171,10 +171,12 @@ def test_binding_checks():
     codes = [torch.zeros(units * 16 * 128, dtype=torch.uint8) for _ in range(2)]
     scales = [torch.zeros(units, dtype=torch.uint8) for _ in range(2)]
     rows = [torch.zeros(units * 16 * 128, dtype=torch.bfloat16) for _ in range(2)]
-    held, at = kara._rows_or_q8_args(torch, cpu, p, 2, codes, codes, scales, scales)
-    assert len(held) == 8 and [ctypes.c_void_p.from_address(at[3] + 8 * i).value for i in range(2)] == [t.data_ptr() for t in scales]
-    held, at = kara._rows_or_q8_args(torch, cpu, p, 2, rows, rows, None, None)
-    assert len(held) == 4 and at[2] is None and at[3] is None
+    addresses = lambda b: list(memoryview(b).cast("Q"))  # noqa: E731
+    at = kara._rows_or_q8_args(torch, cpu, p, 2, codes, codes, scales, scales)
+    assert [addresses(b) for b in at] == [[t.data_ptr() for t in ts] for ts in (codes, codes, scales, scales)]
+    at = kara._rows_or_q8_args(torch, cpu, p, 1, rows[:1], rows[1:], None, None)
+    assert [addresses(b) for b in at[:2]] == [[t.data_ptr()] for t in rows] and at[2] is None and at[3] is None
+    assert ctypes.cast(ctypes.c_char_p(at[0]), ctypes.POINTER(ctypes.c_void_p))[0] == rows[0].data_ptr()
     for bad in ((codes, codes, None, None), (rows, rows, scales, scales), (codes, codes, scales, None),
                 (codes, codes[:1], scales, scales), (codes, codes, [scales[0][1:], scales[1]], scales)):
         with pytest.raises(kara.KaraError):
