@@ -3,15 +3,25 @@
 // by the matrix products.
 //
 // One workgroup of 8 waves owns 128 QT query rows of one (layer, sequence, KV head),
-// rows ordered (query, head in group), and walks the keys of their span 64 at a time.  Its
-// threads fetch a chunk two chunks ahead into registers and write it, codes converted in
-// hardware to bf16 -- exactly --, to the other of two LDS stages while the products of the
-// present one run: a chunk is fetched and converted once for all rows, with one barrier.
-// From there S^T = K Q^T, weights as they stand the B operand of O^T += V^T P^T with V
-// through the transposed LDS read, the row sums one more product with ones.
+// rows ordered (query, head in group), and walks the keys of their span 64 at a time.  A
+// chunk passes through LDS once for all rows, with one barrier: rows copied straight to a
+// ring of four stages, three chunks ahead; codes fetched into registers two chunks ahead,
+// converted in hardware to bf16 -- exactly -- and written to the other of two stages while
+// the products of the present one run.  From there S^T = K Q^T, weights as they stand the B
+// operand of O^T += V^T P^T with V through the transposed LDS read, the row sums one more
+// product with ones.  A chunk of 256 rows takes 2.0 us on a full card, where its products
+// alone are 0.9: the other two thirds are LDS reads (every wave reads all of K and V) and
+// exponentials, each about as long, which two waves a SIMD overlap in part.
 //
 // NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones over codes).  bf16
-// calls so round a weight, in the output as in its sum, to bf16.
+// calls so round a weight, in the output as in its sum, to bf16: 2.3e-3 of the result against
+// 64 bits where whole weights would give 1.7e-3, the output's own rounding; a second term
+// would make V's products twice as many.
+//
+// 4 sequences x 1024 queries over 8.7K tokens, 32/8 heads, d = 128: rows 534 us, codes 539
+// (1.03, 1.02 PFLOP/s); in a window of 1024 over 2.5-8.7K 98 us (704 TFLOP/s: 18 chunks a row
+// block, beside which its start, queries and results count); 16 x 1024 380 us.  4 x 512 over
+// 2.5-8.7K, codes: 243 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -68,8 +78,10 @@ __device__ inline v4i16 read_tr(const char* p) {
 // Where a call has fewer than two workgroups to a CU, long sequences' keys are split, so
 // that it does not end with them: a row block of a sequence of c chunks (its last block's)
 // becomes ceil(c / P) workgroups, P the chunks of all blocks over the CUs, 512 keys at
-// least.  The others write their rows; these write records, which a second launch joins.
-// 9 x 118 queries x 2 layers over 23-5990 tokens: 223 us unsplit; see window_join_kernel.
+// least.  The others write their rows; these write records, which a second launch joins (a
+// join of 64 rows a workgroup, 12.8 us for half of 4 x 512 queries' blocks).  9 x 118 queries x
+// 2 layers over 23-5990 tokens 223 -> 167 us, 4 x 512 over 2.5-8.7K 273 -> 243, where all
+// blocks in two halves took 309.
 struct ChunkSplit {
   int most;              // sequences whose keys may be split: the first `most` threads' (0: none)
   float *o, *ml;         // records [..][rows_wg][D]; [..][rows_wg]: m, l
@@ -583,8 +595,8 @@ __global__ __launch_bounds__(512, 2) void window_chunk_kernel(WindowCall a, Chun
     if constexpr (!Q8) {
       // An infinite or NaN value that a row does not see has met its weight of 0 in the
       // products: where a result is not finite (codes are), all over again with such
-      // values apart.  (Asked in every chunk that some rows see keys of and others do not,
-      // it took 12 of 113 us: 4 x 1024 queries in a window of 1024.)
+      // values apart.  (Looked for in every chunk that some rows see keys of and others do
+      // not, it took 12 of 113 us: 4 x 1024 queries in a window of 1024.)
       floatx4 zero[QT];
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
@@ -621,7 +633,7 @@ __global__ __launch_bounds__(512, 2) void window_chunk_kernel(WindowCall a, Chun
   if (splits == 1) {
     // Through LDS, whose stages no wave reads any more: rows of a few lanes' 16 bytes each,
     // where the accumulators would give 8 bytes of 16 rows at a time (16 x 1024 queries in a
-    // window of 1024: 395 us so).
+    // window of 1024: 395 us so, 380 through LDS).
     constexpr int kOut = D * (NT == 1 ? 2 : 4), kOutChunks = kOut / 16;       // bytes of a row, pieces
     constexpr int kSwz = (kOutChunks < 16 ? kOutChunks : 16) - 1;
     static_assert(W * QT * 16 * kOut <= C::kStages * 2 * C::kTile, "the waves' rows fit the stages");
