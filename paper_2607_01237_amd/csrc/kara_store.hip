@@ -21,7 +21,7 @@ constexpr int kFewThreads = 1024;
 constexpr int kTile = 32;             // tokens that share a table of angles
 constexpr int kGroupHeads = 16;       // KV heads of a workgroup, at most
 constexpr int kStoreWgs = 1024;       // workgroups of a launch, where heads can be dealt out
-constexpr int kMaxOctets = 1 << 28;   // of a token: 32-bit offsets
+constexpr int kMaxOctets = 1 << 22;   // of a token's heads: 32 tokens' items stay in 32 bits
 
 struct StoreHead {
   Dims g;

@@ -117,6 +117,8 @@ def test_refusals_of_their_own(lib):
     for name in ("kara_q8_append", "kara_rope_append"):
         assert call(lib, name, n_new=2**30, n=64) == UNSUPPORTED
     assert call(lib, "kara_q8_read", n_rows=2**30, n=64) == UNSUPPORTED
+    for name in ("kara_q8_append", "kara_rope_append"):                 # heads whose items leave 32 bits
+        assert call(lib, name, params(n_q_heads=2**19, n_kv_heads=2**19, num_pages=1)) == UNSUPPORTED
 
 
 def test_workspaces_cover_smaller_launches(lib):

@@ -118,6 +118,8 @@ CASES = [
     ("f32", "q8", 8, 2, 128, 16, 2, 1, 256, 0), ("bf16", "q8", 8, 2, 128, 7, 150, 1, 100, 4),
     ("f32", "q8", 4, 2, 64, 16, 200, 1, 90, 33), ("bf16", "q8", 16, 8, 64, 256, 200, 1, 1, 1),
     ("bf16", "rows", 2, 1, 128, 16, 33, 1, 40, 2), ("bf16", "rows", 8, 1, 64, 48, 70, 2, 2**31 - 1, 2**31 - 1),
+    # many heads of one KV head: a decoding step among the many rows
+    ("bf16", "rows", 70, 1, 64, 16, 1, 1, 50, 4), ("bf16", "q8", 136, 1, 128, 16, 1, 1, 0, 0),
     # many units of more than 16 rows: 32 a workgroup
     ("bf16", "rows", 64, 16, 128, 16, 7, 1, 100, 4), ("bf16", "q8", 64, 16, 128, 24, 5, 1, 40, 20),
     ("bf16", "rows", 32, 16, 64, 7, 13, 1, 0, 0), ("bf16", "q8", 32, 16, 64, 16, 30, 1, 77, 3),
