@@ -43,7 +43,8 @@ kara_status_t kara_window_attention_workspace_size(const kara_params_t* p, int32
  * Rows before the sequence's start (n_query > seq_len), sequences longer than max_len,
  * sequence indices outside [0, n_seqs) and queries whose every visible logit is -inf
  * give zeros; a visible logit of +inf or NaN gives NaN, and a visible infinite or NaN
- * value enters the sum as it is.  Softmax statistics and sums are fp32.  bf16 calls hold
+ * value enters the sum as it is (an infinite one of a weight that is 0 in 32 bits: itself or
+ * NaN).  Softmax statistics and sums are fp32.  bf16 calls hold
  * each weight in 16 bits (two bf16 terms) where a KV head has few query rows (G * n_query
  * at most 64) and round it to bf16 where it has more; the same held weights make up its
  * sum.  fp32 calls keep 24 bits.  Results are the same bits from call to call;

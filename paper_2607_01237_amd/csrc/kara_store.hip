@@ -395,8 +395,9 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(Store<NL> a) {
 }
 
 // A few new tokens: one workgroup per listed sequence checks it, appends all its rows and
-// commits, in one launch (8 sequences, one token, one layer: 6.5 us; 64 into codes 10.4).  (The tokens' items of a head are one a lane at most, so that no
-// page has further tiles, and `tops` and `bytes` are not used.)
+// commits, in one launch (8 sequences, one token, one layer: 6.5 us; 64 into codes 10.4).  (The
+// tokens' items of a head are one a lane at most, so that no page has further tiles, and `tops`
+// and `bytes` are not used.)
 template <int DT, int D, bool Q8, int NL>
 __global__ __launch_bounds__(kFewThreads) void store_few_kernel(Store<NL> a) {
   __shared__ __attribute__((aligned(16))) Angles<D> t;

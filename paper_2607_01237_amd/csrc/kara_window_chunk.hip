@@ -641,11 +641,12 @@ __global__ __launch_bounds__(512, 2) void window_chunk_kernel(WindowCall a, Chun
     char* const mine = smem[0] + wave * (QT * 16 * kOut);
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-      const float inv = lsum[qt][0] == 0.f ? 0.f : 1.f / lsum[qt][0];    // (a row that sees no key)
+      const bool some = lsum[qt][0] != 0.f;                   // (no weight: zeros, whatever the values)
+      const float inv = 1.f / lsum[qt][0];
       char* const row = mine + (qt * 16 + li) * kOut;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const floatx4 v = o[qt][dt] * inv;
+        const floatx4 v = some ? o[qt][dt] * inv : floatx4{0.f, 0.f, 0.f, 0.f};
         if constexpr (NT == 1) {
           const bf16x2 p = {(__bf16)v[0], (__bf16)v[1]}, q = {(__bf16)v[2], (__bf16)v[3]};
           *(uint2*)(row + (((dt * 2 + (gq >> 1)) ^ (li & kSwz)) * 16) + (gq & 1) * 8) =

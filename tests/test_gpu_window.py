@@ -197,6 +197,26 @@ def test_rows_without_a_finite_logit(dtype, T):
     assert (np.abs(got - ref) <= bound).all()
 
 
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("dtype,T,window", [("bf16", 1, 20), ("bf16", 8, 0), ("bf16", 200, 20), ("bf16", 200, 0), ("f32", 40, 20)])
+def test_a_row_of_no_weight_is_zero_whatever_its_values(dtype, T, window, value):
+    kara = _kara()
+    Hq, Hkv, d, bs, n = 4, 2, 64, 16, 300
+    rng = np.random.default_rng(3)
+    table, pages, _ = cc.table_for(rng, [n], bs, 20)
+    p = cc.params(Hq, Hkv, d, bs, pages, 20, 1, dtype)
+    k, v = (torch.from_numpy(rng.standard_normal((pages, Hkv, bs, d)).astype(np.float32)).to(cc.DT[dtype]).cuda() for _ in range(2))
+    k[:, 0, :, 0] = float("-inf")                         # of one head: all its rows' logits are -inf
+    v[:, 0, :, ::3] = value
+    q = torch.from_numpy(rng.standard_normal((1, 1, T, Hq, d)).astype(np.float32)).abs().to(cc.DT[dtype])
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    ws = torch.empty(max(1, kara.window_attention_workspace_size(p, 1, 1, T, window, 0, n)), dtype=torch.uint8, device="cuda")
+    kara.window_attention(p, cc.gpu(np.zeros(1, np.int32)), T, window, 0, q.cuda(), [k], [v], cc.gpu(table),
+                          cc.gpu(np.array([n], np.int32)), n, out, ws)
+    got = out[0, 0].float().cpu()
+    assert not got[:, :2].any() and torch.isfinite(got).all() and got[:, 2:].abs().amin() > 0
+
+
 def test_no_window_is_the_attention_of_all():
     """window = 0, a window past the sequence, and sinks past it: the same bits where keys are split alike."""
     kara = _kara()
