@@ -104,7 +104,7 @@ def visible(T, n, window, sink):
 def attend(q, k, v, scale, window=0, sink=0):
     """q [T][Hq][d], k, v [n][Hkv][d], fp64: out [T][Hq][d] and the sums of w |v|.  A query
     that sees no key, or only logits of -inf, gives zeros; values that it does not see
-    do not enter."""
+    do not enter, those of a weight of 0 do (0 times an infinity or a NaN is NaN)."""
     T, Hq, d = q.shape
     n, Hkv = k.shape[:2]
     sees = visible(T, n, window, sink)
@@ -124,7 +124,6 @@ def attend(q, k, v, scale, window=0, sink=0):
                     continue
                 w = np.exp(x - x.max())
                 w /= w.sum()
-                use = w > 0
-                out[t, hq] = w[use] @ v[at[use], h]
-                mass[t, hq] = w[use] @ np.abs(v[at[use], h])
+                out[t, hq] = w @ v[at, h]
+                mass[t, hq] = w @ np.abs(v[at, h])
     return out, mass

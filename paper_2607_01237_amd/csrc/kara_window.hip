@@ -115,11 +115,11 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
   const Span sp = span_of(none ? 0 : len, T, G, row0, row0 + rows, a.window, a.sink);
   const int k0 = split * a.split_keys;
   if (none || k0 >= sp.n) {
-    // no keys: zero rows, or a record of no weight where the combine kernel follows
+    // no keys: zero rows, or a record marked so where the combine kernel follows
     if (a.n_splits > 1) {
       if (tid < rows) {
         const int r = row0 + tid;
-        *(floatx2*)(a.rec_ml + 2 * ((orow + (int64_t)(r / G) * g.Hq + r % G) * a.n_splits + split)) = floatx2{kMaxFloor, 0.f};
+        *(floatx2*)(a.rec_ml + 2 * ((orow + (int64_t)(r / G) * g.Hq + r % G) * a.n_splits + split)) = floatx2{kNegInf, 0.f};
       }
       return;
     }
@@ -613,8 +613,9 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
   }
 }
 
-// One wave per output row: its splits' records joined, those without keys as weights of 0
-// (their sums were not written).  Nothing is looked up but the records, and those of up to
+// One wave per output row: its splits' records joined, but those without keys (a maximum of
+// -inf; their sums were not written).  A record of weights that are all 0 is joined: its
+// values may not be finite, which a row of one split would show.  Nothing is looked up but the records, and those of up to
 // eight splits are all asked for at once: a launch of a few rows takes as long as its loads
 // that wait for others.
 template <int D, bool OUT_BF16>
@@ -634,23 +635,22 @@ __global__ __launch_bounds__(256) void window_combine_kernel(const float* __rest
   floatd x[kAtOnce];
   load(0, x);
   // lane i: split i's maximum and sum, 64 at a time, the first kept
-  const floatx2 first = lane < n_splits ? ml[lane] : floatx2{kMaxFloor, 0.f};
+  const floatx2 first = lane < n_splits ? ml[lane] : floatx2{kNegInf, 0.f};
   float M = first[0];
   for (int i = lane + 64; i < n_splits; i += 64) M = fmaxf(M, ml[i][0]);
 #pragma unroll
   for (int i = 1; i < 64; i <<= 1) M = fmaxf(M, __shfl_xor(M, i, 64));
   float L = 0.f, acc[kDPerLane] = {};
   for (int s0 = 0; s0 < n_splits; s0 += 64) {
-    const floatx2 mine = s0 == 0 ? first : s0 + lane < n_splits ? ml[s0 + lane] : floatx2{kMaxFloor, 0.f};
+    const floatx2 mine = s0 == 0 ? first : s0 + lane < n_splits ? ml[s0 + lane] : floatx2{kNegInf, 0.f};
     const float f = __builtin_amdgcn_exp2f(mine[0] - M), lf = mine[1] * f;
     const int cnt = min(64, n_splits - s0);
     for (int i0 = 0; i0 < cnt; i0 += kAtOnce) {
       if (s0 + i0 > 0) load(s0 + i0, x);
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
-        // (a record's sum of weights may be NaN, as its row is then: not 0)
         const float fi = __shfl(f, i0 + i, 64), li = __shfl(lf, i0 + i, 64);
-        const bool in = i0 + i < cnt && __shfl(mine[1], i0 + i, 64) != 0.f;
+        const bool in = i0 + i < cnt && __shfl(mine[0], i0 + i, 64) != kNegInf;
         if (in) {
           L += li;
 #pragma unroll

@@ -672,9 +672,9 @@ __global__ __launch_bounds__(512, 2) void window_chunk_kernel(WindowCall a, Chun
     for (int qt = 0; qt < QT; ++qt) {
       const int r = wrow0 + qt * 16 + li;
       if (r >= R) continue;
-      // (a split without keys: a record of no weight)
+      // (a split without keys is marked so: its sums are not written)
       const int64_t rec = (first_record + (int64_t)(u * a.n_rt + rb) * splits + split) * kRowsWg + (r - row0);
-      if (gq == 0) *(floatx2*)(x.ml + 2 * rec) = floatx2{m[qt], lsum[qt][0]};
+      if (gq == 0) *(floatx2*)(x.ml + 2 * rec) = floatx2{n_chunks > 0 ? m[qt] : kNegInf, lsum[qt][0]};
       if (n_chunks > 0)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) *(floatx4*)(x.o + rec * D + dt * 16 + 4 * gq) = o[qt][dt];
@@ -721,8 +721,9 @@ __global__ __launch_bounds__(kJoinThreads) void window_join_kernel(WindowHead a,
     }
 #pragma unroll
     for (int i = 0; i < kRowsWave; ++i) {
-      // (sums of no weight were not written; one that is NaN, as its row is then, is)
-      const bool in = ml[i][1] != 0.f;
+      // (a split without keys wrote no sums; one whose weights are all 0 did, and its values may
+      // not be finite, which an unsplit row would show)
+      const bool in = ml[i][0] != kNegInf;
       const float mn = in ? fmaxf(M[i], ml[i][0]) : M[i];
       const float f0 = __builtin_amdgcn_exp2f(M[i] - mn), f1 = in ? __builtin_amdgcn_exp2f(ml[i][0] - mn) : 0.f;
       M[i] = mn;
