@@ -44,11 +44,11 @@ kara_status_t kara_window_attention_workspace_size(const kara_params_t* p, int32
  * sequence indices outside [0, n_seqs) and queries whose every visible logit is -inf
  * give zeros; a visible logit of +inf or NaN gives NaN, and a visible infinite or NaN
  * value enters the sum as it is (an infinite one of a weight that is 0 in 32 bits: itself or
- * NaN).  Softmax statistics and sums are fp32.  bf16 calls hold
- * each weight in 16 bits (two bf16 terms) where a KV head has few query rows (G * n_query
- * at most 64) and round it to bf16 where it has more; the same held weights make up its
- * sum.  fp32 calls keep 24 bits.  Results are the same bits from call to call;
- * they may differ in the last ones with n, n_layers, n_query and max_len, which decide
+ * NaN).  Softmax statistics and sums are fp32.  fp32 calls, and bf16 ones over rows where a
+ * KV head has few query rows (G * n_query at most 64), keep all 24 bits of a weight; bf16
+ * calls of few rows over 8 bits hold it in 16 (two bf16 terms), and those of more rows round
+ * it to bf16; the same held weights make up its sum.  Results are the same bits from call to
+ * call; they may differ in the last ones with n, n_layers, n_query and max_len, which decide
  * how keys are split.
  */
 kara_status_t kara_window_attention(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,

@@ -65,9 +65,12 @@ struct WinCfg {
 // Rows of fp32 go through the fp32 matrix instructions, and are bound by those where queries
 // are many: 6 x 101 queries of 16 heads, d = 64, in a window of 777, 28-32 us, 1.5 GFLOP (the
 // card's fp32 rate in a large library product is 154 TFLOP/s).  NT: bf16 terms of a query over codes
-// (3 where p->dtype is fp32: 24 bits; codes are exact in one).  NP: bf16 terms of a weight:
-// 3 for fp32 outputs, 2 for bf16 ones: a weight rounded to bf16 would leave an output of
-// flat weights 2.3e-3 off, two terms 1.66e-3, its own rounding, for half a per cent of the time.
+// (3 where p->dtype is fp32: 24 bits; codes are exact in one).  NP: bf16 terms of a weight: 3,
+// all its bits, but for bf16 calls over codes, where the third would cost what it does not over
+// rows: 2.  In us with 2 and 3: over rows, a step of 8 sequences 16.1, 16.3; 96 x 2 layers of 8K
+// in a window of 4096 543, 542; 5 queries there, no window, 1090, 1089.  Over codes, in the same
+// order, no window, 19.4, 20.1; 528, 531; 617, 650.  (A weight rounded to bf16 would leave an
+// output of flat weights 2.3e-3 off, two terms 1.66e-3, which is its own rounding.)
 template <Cache CT, int NT, int NP, int D, int QT, int NL>
 __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<NL> a) {
   using C = WinCfg<CT, D, QT>;
@@ -533,7 +536,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_split_kernel(WindowCallOf<
       }
     }
     // An infinite or NaN value that a row does not see has met its weight of 0 in the
-    // products, and one that it sees the second term of its weight, which may be 0: where a
+    // products, and one that it sees a later term of its weight, which may be 0: where a
     // result is not finite (codes are), the wave's blocks again with such values apart.
     if (CT == kCodes || careful) break;
     floatx4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -713,10 +716,10 @@ hipError_t launch_split(const Geom& g, bool q8, int rows, const WindowCallOf<NL>
     else launch_split<kRowsF32, 1, 1, 1>(g.d, a, blocks, s);
   } else if (rows == 16) {
     if (q8) launch_split<kCodes, 1, 2, 1>(g.d, a, blocks, s);
-    else launch_split<kRowsBf16, 1, 2, 1>(g.d, a, blocks, s);
+    else launch_split<kRowsBf16, 1, 3, 1>(g.d, a, blocks, s);
   } else {
     if (q8) launch_split<kCodes, 1, 2, 2>(g.d, a, blocks, s);
-    else launch_split<kRowsBf16, 1, 2, 2>(g.d, a, blocks, s);
+    else launch_split<kRowsBf16, 1, 3, 2>(g.d, a, blocks, s);
   }
   return hipGetLastError();
 }

@@ -16,7 +16,9 @@
 // NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones over codes).  bf16
 // calls so round a weight, in the output as in its sum, to bf16: 2.3e-3 of the result against
 // 64 bits where whole weights would give 1.7e-3, the output's own rounding; a second term
-// would make V's products twice as many.
+// makes V's products twice as many, and calls a quarter to a third longer (us with one and
+// with two: 4 x 1024 queries in a window of 1024 96, 119; over 8.7K tokens 538, 716, codes 541,
+// 702; 4 x 512 over 2.5-8.7K, codes 243, 304).
 //
 // 4 sequences x 1024 queries over 8.7K tokens, 32/8 heads, d = 128: rows 534 us, codes 539
 // (1.03, 1.02 PFLOP/s); in a window of 1024 over 2.5-8.7K 98 us (704 TFLOP/s: 18 chunks a row
