@@ -50,6 +50,12 @@ kara_status_t kara_window_attention_workspace_size(const kara_params_t* p, int32
  * it to bf16; the same held weights make up its sum.  Results are the same bits from call to
  * call; they may differ in the last ones with n, n_layers, n_query and max_len, which decide
  * how keys are split.
+ *
+ * KARA_ERR_UNSUPPORTED past what one launch holds, also where the workspace's size is given.
+ * With U = n_layers * n * n_kv_heads and R = G * n_query it holds, of few rows (R at most 64,
+ * and all fp32 calls over rows), U * ceil(R / 16) times the parts of the keys up to 2^24, and
+ * 2^26 rows of output where there is more than one part; of more rows U * ceil(R / 128) up to
+ * 2^23.
  */
 kara_status_t kara_window_attention(const kara_params_t* p, int32_t n, const int32_t* seqs, int32_t n_layers,
                                     int32_t n_query, int32_t window, int32_t n_sink, const void* q,

@@ -687,7 +687,7 @@ int split_keys_of(int bs, int64_t tiles, int span) {
 }
 
 // Up to this many query rows per (layer, sequence, KV head) go through the split kernel,
-// 16 a workgroup, and all over rows of fp32; more through the chunk kernel.
+// 16 or 32 a workgroup, and all over rows of fp32; more through the chunk kernel.
 constexpr int kFewRows = 64;
 bool splits(const Geom& g, int T, bool q8) { return (int64_t)g.G * T <= kFewRows || (g.dtype == KARA_F32 && !q8); }
 
@@ -810,7 +810,8 @@ kara_status_t attend(const kara_params_t* p, int32_t n, const int32_t* seqs, int
     a.n_splits = 1;
     blocks = 2 * plan.blocks;           // (of 512 threads)
   }
-  if (!grid_ok(blocks) || !grid_ok((rows + 3) / 4)) return KARA_ERR_UNSUPPORTED;
+  // (the launch that joins records takes four output rows a workgroup)
+  if (!grid_ok(blocks) || (a.n_splits > 1 && !grid_ok((rows + 3) / 4))) return KARA_ERR_UNSUPPORTED;
   a.seqs = seqs;
   a.bt = block_table;
   a.seq_lens = seq_lens;
