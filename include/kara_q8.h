@@ -19,6 +19,9 @@
  * exactly, down to 2^-6 of the new scale; smaller ones lose bits.  The first token of a
  * page (a position that is a multiple of block_size) starts its scale anew.
  *
+ * The calls of this header, kara_rope_append and kara_window_attention are all that take
+ * this cache: compression, eviction and the helpers of kara_harness.h do not.
+ *
  * Pools, per layer (PAGES of kara.h, the same block table and lengths):
  *   k_pools, v_pools     codes  [num_pages][n_kv_heads][block_size][head_dim] uint8
  *   k_scales, v_scales   scales [num_pages][n_kv_heads] uint8

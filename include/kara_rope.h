@@ -44,7 +44,7 @@ typedef struct kara_rope {
  *               with 0 and the others with 1.
  *   rope_pos [n_seqs] rotary position of each sequence's next token; NULL: its position
  *            in the cache.  (After compression or eviction a token's position counts
- *            what was cut; the cache's does not.)
+ *            what was cut; the cache's does not.  A cache in 8 bits is neither compressed nor evicted from.)
  *   status   as in kara_q8_append, KARA_SEQ_NONFINITE from 8-bit caches alone;
  *            BAD_WINDOW too where counted tokens are more than the sequence's.
  *            Flagged sequences' cache, lengths and q_out rows are left as they were.

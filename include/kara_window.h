@@ -19,6 +19,13 @@ extern "C" {
  * n_query queries each; as for kara_q8_attention it is enough for fewer sequences and
  * layers and for a smaller max_len, not for other values of n_query, window and n_sink,
  * nor of p.
+ *
+ * It covers a cache of either kind.  fp32 calls over rows keep a record (head_dim + 2
+ * floats) for each row of output and part of the keys, of 4608 keys at most: 4.4 GB for
+ * one prompt of 32K queries of 32 heads of 128 and one layer, 136 MB for 4 x 1024 queries
+ * over 8.7K tokens.  fp32 calls over 8 bits and bf16 ones of many queries need 34 to 68 MB
+ * (d = 128), so that an fp32 program whose cache is in 8 bits is told more than it needs
+ * here; without a window kara_q8_attention_workspace_size is exact for it.
  */
 kara_status_t kara_window_attention_workspace_size(const kara_params_t* p, int32_t n, int32_t n_layers,
                                                    int32_t n_query, int32_t window, int32_t n_sink,

@@ -167,8 +167,11 @@ __device__ __forceinline__ uint32_t finite_top(float (&x)[8], bool* odd) {
 // fp32, with what the fraction's rounding to fp32 leaves.
 //
 // Bound by the bytes where tokens are many: 4 x 4000 tokens x 4 layers, 32/8 heads, d = 128:
-// into rows 313 us for 1.57 GB, 5.0 TB/s, a large copy's rate; into codes and read back 342
-// for 1.84.
+// into rows 314 us for 1.57 GB, into codes 291 for 1.44, both 5.0 TB/s, a large copy's rate, and
+// what the counters of memory traffic hold; codes read back too 344.  Pages of more tokens than a
+// wave's lanes hold read K and V twice, with a table of angles for every 32 tokens in both sweeps:
+// 14 x 1476 tokens x 4 layers, pages of 256, read back 623 us (1.34 GB fetched for 1.02), pages
+// of 16 432.
 //
 // One run of tokens of sequence s = seqs[j] in layers [l0, l1), `heads` KV heads from h0 on and
 // their query heads, by all threads.  8 bits: the tokens that fall into one page, as its
@@ -400,7 +403,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kernel(Store<NL> a) {
 }
 
 // A few new tokens: one workgroup per listed sequence checks it, appends all its rows and
-// commits, in one launch (8 sequences, one token, one layer: 6.5 us; 64 into codes 10.4).  (The
+// commits, in one launch (8 sequences, one token, one layer: 6.6 us; 64 into codes 10.7).  (The
 // tokens' items of a head are one a lane at most, so that no page has further tiles, and `tops`
 // and `bytes` are not used.)
 template <int DT, int D, bool Q8, int NL>

@@ -58,9 +58,10 @@ struct WinCfg {
 // byte permutes.
 //
 // Bound by the bytes where there are many: 96 sequences of 7-8.2K tokens, 2 layers, 40/8
-// heads, d = 128: over codes 525 us for 2.99 GB, 5.7 TB/s; in a window of 4096 over rows 541
-// us for 3.23 GB, 6.0 TB/s.  A small batch is bound by the loads that wait for one another
-// (list, length, table, keys): 8 sequences of 300-4000 tokens 15.7 us and the join 3.9.
+// heads, d = 128: over codes 525 us for 2.99 GB, 5.7 TB/s; in a window of 4096 over rows 543
+// us for 3.23 GB, 6.0 TB/s (the counters hold 3.05 and 3.24 GB).  A small batch is bound by the
+// loads that wait for one another (list, length, table, keys): 8 sequences of 300-4000 tokens
+// 15.8 us and the join 4.4.
 //
 // Rows of fp32 go through the fp32 matrix instructions, and are bound by those where queries
 // are many: 6 x 101 queries of 16 heads, d = 64, in a window of 777, 28-32 us, 1.5 GFLOP (the
@@ -687,7 +688,12 @@ int split_keys_of(int bs, int64_t tiles, int span) {
 }
 
 // Up to this many query rows per (layer, sequence, KV head) go through the split kernel,
-// 16 or 32 a workgroup, and all over rows of fp32; more through the chunk kernel.
+// 16 or 32 a workgroup, and all over rows of fp32; more through the chunk kernel.  From 33 to
+// 64 rows a tile of the two passes the keys on its own, where the chunk kernel would pass them
+// once but hold a weight in one bf16 term: 96 x 2 layers of 8K, 40 and 60 rows, rows 1670 and
+// 1695 us, there 1300; codes 1030 and 1080, there 1030; 16 of 300-4000 tokens, one layer, rows 69
+// and 71, there 52, codes 55 and 56, there 53; in a window of 1024 of 96 x 2 rows 255 and 263,
+// there 263.  The weights' bits decided.
 constexpr int kFewRows = 64;
 bool splits(const Geom& g, int T, bool q8) { return (int64_t)g.G * T <= kFewRows || (g.dtype == KARA_F32 && !q8); }
 

@@ -9,9 +9,10 @@
 // converted in hardware to bf16 -- exactly -- and written to the other of two stages while
 // the products of the present one run.  From there S^T = K Q^T, weights as they stand the B
 // operand of O^T += V^T P^T with V through the transposed LDS read, the row sums one more
-// product with ones.  A chunk of 256 rows takes 2.0 us on a full card, where its products
-// alone are 0.9: the other two thirds are LDS reads (every wave reads all of K and V) and
-// exponentials, each about as long, which two waves a SIMD overlap in part.
+// product with ones.  A chunk of 256 rows of 128 takes 4550 cycles of a CU, 2.0 us on a full card:
+// its products 2180 (counted), its LDS reads 2050 (every wave reads all of K and V, 256 KB at 128
+// bytes a cycle) and its vector instructions some 2100 (331 of a SIMD counted, 64 of them
+// exponentials, of 16 cycles, the others of 4), which two waves a SIMD overlap in part.
 //
 // NT: bf16 terms of a query and of a weight (1: bf16 calls; 3: fp32 ones over codes).  bf16
 // calls so round a weight, in the output as in its sum, to bf16: 2.3e-3 of the result against
